@@ -1,4 +1,4 @@
-"""ctypes binding of libkvlinc.so.  Same names and argument order as include/kvlinc.h."""
+"""ctypes binding of libkvlinc.so.  Same names and argument order as include/kvlinc.h and include/kvlinc_context.h."""
 import ctypes
 import os
 
@@ -9,6 +9,7 @@ KVLINC_OK, KVLINC_EINVAL, KVLINC_EWORKSPACE, KVLINC_EHIP, KVLINC_ESCRATCH = 0, -
 KVLINC_STATIC_SCRATCH_BYTES = 16 << 20
 KVLINC_FLAG_ALG1_LITERAL = 1
 KVLINC_FLAG_SLIDING_VALUES = 2
+KVLINC_F16, KVLINC_BF16, KVLINC_F32 = 0, 1, 2
 KVLINC_ST_CAPACITY, KVLINC_ST_NONFINITE, KVLINC_ST_STATIC, KVLINC_ST_STATE_RANGE = 1, 2, 4, 8
 
 
@@ -62,6 +63,17 @@ def _load():
                                                 ctypes.c_int32, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p]
     L.kvlinc_decode_attention_noalloc.restype = ctypes.c_int
     L.kvlinc_decode_attention_noalloc.argtypes = [P, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int32, ctypes.c_void_p]
+    i32, ptr = ctypes.c_int32, ctypes.c_void_p
+    L.kvlinc_prompt_workspace_bytes.restype = ctypes.c_size_t
+    L.kvlinc_prompt_workspace_bytes.argtypes = [P, i32, i32, i32, i32]
+    L.kvlinc_prompt_attention.restype = ctypes.c_int
+    L.kvlinc_prompt_attention.argtypes = [P, ptr, ptr, ptr, ptr, i32, i32, i32, ptr, ptr, ctypes.c_size_t, i32, ptr]
+    L.kvlinc_decode_windowed_workspace_bytes.restype = ctypes.c_size_t
+    L.kvlinc_decode_windowed_workspace_bytes.argtypes = [P, i32, i32, i32]
+    L.kvlinc_decode_attention_windowed.restype = ctypes.c_int
+    L.kvlinc_decode_attention_windowed.argtypes = [P, ptr, i32, i32, ptr, ptr, ctypes.c_size_t, i32, ptr]
+    L.kvlinc_cache_read.restype = ctypes.c_int
+    L.kvlinc_cache_read.argtypes = [P, ptr, i32, ptr, ptr, i32, i32, ptr]
     return L
 
 
@@ -139,6 +151,40 @@ def kvlinc_decode_attention_noalloc(cache, q, out, max_context=0, stream=None):
                                                _stream(stream))
 
 
+def _bytes_of(workspace, workspace_bytes):
+    if workspace_bytes is not None:
+        return int(workspace_bytes)
+    return 0 if workspace is None else workspace.numel() * workspace.element_size()
+
+
+def kvlinc_prompt_workspace_bytes(cache, T, window=0, sinks=0, max_context=0):
+    return lib.kvlinc_prompt_workspace_bytes(ctypes.byref(_struct(cache)), int(T), int(window), int(sinks), int(max_context))
+
+
+def kvlinc_prompt_attention(cache, q, k_new, v_new, n_new, T, window, sinks, out, workspace, workspace_bytes=None, max_context=0,
+                            stream=None):
+    """q, out: [B, H_q, T, 128]; k_new, v_new: [B, H_kv, T, 128]; fp16 device tensors (contiguous); n_new: [B] int32 or None."""
+    return lib.kvlinc_prompt_attention(ctypes.byref(_struct(cache)), _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(n_new), int(T), int(window),
+                                       int(sinks), _ptr(out), _ptr(workspace), _bytes_of(workspace, workspace_bytes), int(max_context),
+                                       _stream(stream))
+
+
+def kvlinc_decode_windowed_workspace_bytes(cache, window, sinks=0, max_context=0):
+    return lib.kvlinc_decode_windowed_workspace_bytes(ctypes.byref(_struct(cache)), int(window), int(sinks), int(max_context))
+
+
+def kvlinc_decode_attention_windowed(cache, q, window, sinks, out, workspace, workspace_bytes=None, max_context=0, stream=None):
+    """q, out: [B, H_q, 128] fp16 device tensors (contiguous)."""
+    return lib.kvlinc_decode_attention_windowed(ctypes.byref(_struct(cache)), _ptr(q), int(window), int(sinks), _ptr(out), _ptr(workspace),
+                                                _bytes_of(workspace, workspace_bytes), int(max_context), _stream(stream))
+
+
+def kvlinc_cache_read(cache, first, T, k_out, v_out, dtype=KVLINC_F16, rotated=0, stream=None):
+    """k_out, v_out: [B, H_kv, T, 128] device tensors of the type dtype (KVLINC_F16, ...), either may be None; first: [B] int32 or None."""
+    return lib.kvlinc_cache_read(ctypes.byref(_struct(cache)), _ptr(first), int(T), _ptr(k_out), _ptr(v_out), int(dtype), int(rotated),
+                                 _stream(stream))
+
+
 class KVLincCache:
     """Device buffers of one layer's cache plus the descriptor that points at them (allocation only)."""
 
@@ -181,6 +227,7 @@ class KVLincCache:
             Wq=None if Wq is None else Wq.data_ptr(), Wk=None if Wk is None else Wk.data_ptr(),
             status=self.status.data_ptr(), split_done=self.split_done.data_ptr(), flags=int(flags))
         self._ws = None
+        self._context_ws = []  # scratch of prompt_attention and decode_windowed, the largest last
 
     def bytes(self):
         ts = [self.groups, self.k_res, self.v_res]
@@ -213,3 +260,118 @@ class KVLincCache:
         if rc != KVLINC_OK:
             raise KVLincError("kvlinc_decode_attention: " + kvlinc_strerror(rc))
         return out
+
+    # The calls below check their tensors: what the C entry points take is an address.
+    def _tensor(self, t, name, shape, dtypes):
+        import torch
+        if not torch.is_tensor(t) or t.dtype not in dtypes or tuple(t.shape) != tuple(shape):
+            raise KVLincError("%s has to be a %s tensor of shape %s" % (name, " or ".join(str(d) for d in dtypes), tuple(shape)))
+        if t.device != self.groups.device:
+            raise KVLincError("%s is on %s, the cache on %s" % (name, t.device, self.groups.device))
+        if not t.is_contiguous():
+            raise KVLincError("%s has to be contiguous" % name)
+        return t
+
+    def _on(self, stream):
+        """The cache's device current, and `stream`, if one is given: what is allocated inside belongs to the stream that uses it."""
+        import contextlib
+        import torch
+        dev = self.groups.device
+        if dev.type != "cuda":
+            raise KVLincError("the cache is on %s: the kernels need a GPU" % dev)
+        scope = contextlib.ExitStack()
+        if torch.cuda.current_device() != dev.index:
+            scope.enter_context(torch.cuda.device(dev))
+        if stream is not None:
+            scope.enter_context(torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream), device=dev)))
+        return scope
+
+    @staticmethod
+    def _limits(window, sinks):
+        if window < 0 or sinks < 0:
+            raise KVLincError("window and sinks have to be 0 or more, not %s and %s" % (window, sinks))
+
+    def _context_workspace(self, need):
+        """Scratch of at least `need` bytes.  One that has become too small is kept: a captured graph may still use it."""
+        import torch
+        if need == 0:
+            return None
+        if not self._context_ws or self._context_ws[-1].numel() * 4 < need:
+            self._context_ws.append(torch.empty((need + 3) // 4, dtype=torch.float32, device=self.groups.device))
+        return self._context_ws[-1]
+
+    def prompt_attention(self, q, k_new, v_new, n_new=None, window=0, sinks=0, out=None, max_context=0, stream=None):
+        """Attention of T new tokens of every sequence over the cache and, causally, their own rows; append them afterwards.
+
+        q: [B, H_q, T, 128], k_new, v_new: [B, H_kv, T, 128] fp16; n_new: [B] int32 on the device or None (all T).  Returns out, [B, H_q, T,
+        128] fp16; rows beyond n_new are left as they are (zero in an `out` made here).  window, sinks, max_context: kvlinc_context.h."""
+        import torch
+        if not torch.is_tensor(q) or q.dim() != 4:
+            raise KVLincError("q has to be a tensor of shape [B, H_q, T, 128]")
+        T, half = q.shape[2], (torch.float16,)
+        self._limits(window, sinks)
+        if T < 1:
+            raise KVLincError("q has no rows")
+        self._tensor(q, "q", (self.B, self.H_q, T, 128), half)
+        self._tensor(k_new, "k_new", (self.B, self.H_kv, T, 128), half)
+        self._tensor(v_new, "v_new", (self.B, self.H_kv, T, 128), half)
+        if n_new is not None:
+            self._tensor(n_new, "n_new", (self.B,), (torch.int32,))
+        if out is not None:
+            self._tensor(out, "out", q.shape, half)
+        with self._on(stream):
+            if out is None:
+                out = torch.empty_like(q) if n_new is None else torch.zeros_like(q)
+            ws = self._context_workspace(kvlinc_prompt_workspace_bytes(self, T, window, sinks, max_context))
+            rc = kvlinc_prompt_attention(self, q, k_new, v_new, n_new, T, window, sinks, out, ws, None, max_context, stream)
+        if rc != KVLINC_OK:
+            raise KVLincError("kvlinc_prompt_attention: " + kvlinc_strerror(rc))
+        return out
+
+    def decode_windowed(self, q, window, sinks=0, out=None, max_context=0, stream=None):
+        """decode() over the newest `window` tokens and the first `sinks` ones (window = 0: all).  q: [B, H_q, 128] fp16."""
+        import torch
+        half = (torch.float16,)
+        self._limits(window, sinks)
+        self._tensor(q, "q", (self.B, self.H_q, 128), half)
+        if out is not None:
+            self._tensor(out, "out", q.shape, half)
+        with self._on(stream):
+            if out is None:
+                out = torch.empty_like(q)
+            ws = self._context_workspace(kvlinc_decode_windowed_workspace_bytes(self, window, sinks, max_context))
+            rc = kvlinc_decode_attention_windowed(self, q, window, sinks, out, ws, None, max_context, stream)
+        if rc != KVLINC_OK:
+            raise KVLincError("kvlinc_decode_attention_windowed: " + kvlinc_strerror(rc))
+        return out
+
+    def read(self, first=None, T=None, dtype=None, rotated=False, k_out=None, v_out=None, stream=None):
+        """Keys and values of tokens first[b] .. first[b] + T - 1 (first: [B] int32 on the device, None: 0), dequantized: (k_out, v_out), [B,
+        H_kv, T, 128].  With one of the two given, only that one is read; with none, both are made here, in `dtype` (fp16), and zero where a
+        sequence has no such token.  rotated: values in the basis they are stored in."""
+        import torch
+        types = {torch.float16: KVLINC_F16, torch.bfloat16: KVLINC_BF16, torch.float32: KVLINC_F32}
+        given = [t for t in (k_out, v_out) if t is not None]
+        if T is None:
+            if not given or not torch.is_tensor(given[0]) or given[0].dim() != 4:
+                raise KVLincError("T is needed where neither k_out nor v_out, [B, H_kv, T, 128], gives it")
+            T = given[0].shape[2]
+        if T < 1:
+            raise KVLincError("T has to be 1 or more, not %s" % T)
+        if dtype is None:
+            dtype = given[0].dtype if given and torch.is_tensor(given[0]) else torch.float16
+        if dtype not in types:
+            raise KVLincError("dtype has to be one of %s" % ", ".join(str(t) for t in types))
+        shape = (self.B, self.H_kv, int(T), 128)
+        for t, name in ((k_out, "k_out"), (v_out, "v_out")):
+            if t is not None:
+                self._tensor(t, name, shape, (dtype,))
+        if first is not None:
+            self._tensor(first, "first", (self.B,), (torch.int32,))
+        with self._on(stream):
+            if not given:
+                k_out, v_out = (torch.zeros(shape, dtype=dtype, device=self.groups.device) for _ in range(2))
+            rc = kvlinc_cache_read(self, first, T, k_out, v_out, types[dtype], int(bool(rotated)), stream)
+        if rc != KVLINC_OK:
+            raise KVLincError("kvlinc_cache_read: " + kvlinc_strerror(rc))
+        return k_out, v_out

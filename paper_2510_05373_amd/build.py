@@ -22,11 +22,16 @@ OBJECTS = {
     "kvlinc_api": ("kvlinc_api.hip", []),
     "kvlinc_append": ("kvlinc_append.hip", ["-ffp-contract=off"]),
     "kvlinc_decode": ("kvlinc_decode.hip", []),
+    "kvlinc_context_api": ("kvlinc_context_api.hip", []),
+    "kvlinc_rows": ("kvlinc_rows.hip", []),
+    "kvlinc_prompt_correction": ("kvlinc_prompt_correction.hip", []),
+    "kvlinc_read": ("kvlinc_read.hip", []),
     "kvlinc_decode_nolooks": ("kvlinc_decode.hip", ["-DKVLINC_LOOKS=0"]),
 }
+CONTEXT = ["kvlinc_context_api", "kvlinc_rows", "kvlinc_prompt_correction", "kvlinc_read"]
 LIBRARIES = {
-    LIB_PATH: ["kvlinc_api", "kvlinc_append", "kvlinc_decode"],
-    NOLOOKS_PATH: ["kvlinc_api", "kvlinc_append", "kvlinc_decode_nolooks"],
+    LIB_PATH: ["kvlinc_api", "kvlinc_append", "kvlinc_decode", *CONTEXT],
+    NOLOOKS_PATH: ["kvlinc_api", "kvlinc_append", "kvlinc_decode_nolooks", *CONTEXT],
 }
 PROBE_SOURCE = "kvlinc_readprobe.hip"
 

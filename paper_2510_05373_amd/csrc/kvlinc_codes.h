@@ -1,0 +1,86 @@
+// Packed codes as binary16 numbers, and small pieces shared by the kernels that read the cache with them (not part of the C ABI).
+#pragma once
+
+#include "kvlinc_internal.h"
+#include "kvlinc_mfma.h"
+
+namespace kvlinc {
+namespace {
+
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+typedef _Float16 half8_t __attribute__((ext_vector_type(8)));
+typedef float float2v_t __attribute__((ext_vector_type(2)));
+
+constexpr float kInvSqrtD = 0.08838834764831845f;              // 1 / sqrt(128)
+constexpr float kLog2eSqrtD = 1.4426950408889634f * kInvSqrtD;  // scores in the log2 domain: x = q.k log2(e) / sqrt(d)
+
+__device__ __forceinline__ float bits_f32(uint32_t v) { return __builtin_bit_cast(float, v); }
+__device__ __forceinline__ half2_t pack_h2(float a, float b) { return __builtin_convertvector((float2v_t{a, b}), half2_t); }
+__device__ __forceinline__ half8_t as_h8(uint4 v) { return __builtin_bit_cast(half8_t, v); }
+__device__ __forceinline__ half8_t as_h8(half2_t a, half2_t b, half2_t c, half2_t d) {
+  return as_h8(make_uint4(as_u32(a), as_u32(b), as_u32(c), as_u32(d)));
+}
+
+// A packed word holds the bit pairs of two codes in every nibble, so that the bits of one of them, with the nibble's other two bits
+// set to 0 and 1, are the FP4 (E2M1) number code - 1.5: `first` takes the codes p = 0, 2, ..., 14 of the word, `second` the odd ones.
+struct Nibbles {
+  uint32_t first, second;
+};
+__device__ __forceinline__ Nibbles nibbles_of(uint32_t w) {
+  return Nibbles{(w & 0xAAAAAAAAu) | 0x11111111u, ((w << 1) & 0xAAAAAAAAu) | 0x11111111u};
+}
+// Byte SEL of such nibbles, two codes, as binary16: (code - 1.5) scale, scale a power of two.  One instruction, exact.
+template <int SEL>
+__device__ __forceinline__ half2_t nibble_pair(uint32_t nibbles, float scale) {
+  return __builtin_bit_cast(half2_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(nibbles, scale, SEL));
+}
+// The same for codes of BITS bits, code - Rec<BITS>::kCentre: of 4 bits, the high digit's pair times 4 plus the low digit's (exact).
+template <int BITS, int SEL>
+__device__ __forceinline__ half2_t code_pair(const uint32_t (&plane)[BITS / 2], float scale) {
+  if constexpr (BITS == 2) return nibble_pair<SEL>(plane[0], scale);
+  else return nibble_pair<SEL>(plane[0], 4.0f * scale) + nibble_pair<SEL>(plane[1], scale);
+}
+
+// Butterflies between the 16 lanes of a DPP row, strides 1, 2, 4, 8, NV vectors at once.
+template <int NV>
+__device__ __forceinline__ void row16_butterflies(float (&v)[NV], int lane) {
+  auto sign = [&](int bit) { return (lane & bit) != 0 ? -1.0f : 1.0f; };
+  const float s1 = sign(1), s2 = sign(2), s4 = sign(4), s8 = sign(8);
+#pragma unroll
+  for (int u = 0; u < NV; ++u) v[u] = __builtin_fmaf(v[u], s1, dpp_f<kQuadSwap1>(v[u]));
+#pragma unroll
+  for (int u = 0; u < NV; ++u) v[u] = __builtin_fmaf(v[u], s2, dpp_f<kQuadSwap2>(v[u]));
+#pragma unroll
+  for (int u = 0; u < NV; ++u) v[u] = __builtin_fmaf(v[u], s4, dpp_f<kQuadMirror>(dpp_f<kRowHalfMirror>(v[u])));
+#pragma unroll
+  for (int u = 0; u < NV; ++u) v[u] = __builtin_fmaf(v[u], s8, dpp_f<kRowRor8>(v[u]));
+}
+// Three butterfly stages over 8 neighbouring channels of a lane.
+__device__ __forceinline__ void lane8_butterflies(float (&v)[8]) {
+#pragma unroll
+  for (int h = 1; h < 8; h *= 2)
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if ((i & h) == 0) {
+        const float a = v[i], b = v[i + h];
+        v[i] = a + b;
+        v[i + h] = a - b;
+      }
+}
+
+// What a query sees: its position p, the window's first token, the sinks.  Token t <= p is seen if t >= low or t < sinks.
+__device__ __forceinline__ int window_low(int p, int window) { return window > 0 ? max(p - window + 1, 0) : 0; }
+
+// Counters of a sequence, kept inside the cache's storage.
+struct Lengths {
+  int nq, nr;
+  __device__ __forceinline__ int total() const { return nq + nr; }
+  __device__ __forceinline__ int groups() const { return (nq + kGroup - 1) / kGroup; }
+};
+__device__ __forceinline__ Lengths lengths_of(const kvlinc_cache& c, int b) {
+  const long long cap = c.max_groups * kGroup;
+  return Lengths{(int)min((long long)max(c.n_quant[b], 0), cap), min(max(c.n_res[b], 0), c.R)};
+}
+
+}  // namespace
+}  // namespace kvlinc

@@ -1,0 +1,131 @@
+// Host side of kvlinc_context.h: argument validation, workspaces and launch set-up.  Nothing here touches device memory.
+#include <hip/hip_runtime.h>
+
+#include "kvlinc_context_internal.h"
+
+namespace kvlinc {
+namespace {
+
+inline bool bad_address(const void* p, uintptr_t a) { return p == nullptr || (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
+
+// What a call makes of its sizes: splits of a context, scratch.
+struct ContextPlan {
+  int splits;
+  size_t corr_floats, part_floats;
+  size_t bytes() const { return (corr_floats + part_floats) * sizeof(float); }
+};
+
+// Groups a row of queries meets in a context of the bound.
+long long groups_met(const kvlinc_cache& c, int T, int window, int sinks, int max_context) {
+  const long long cap = (long long)c.max_groups * kGroup + c.R;
+  const long long ctx = max_context > 0 && max_context < cap ? max_context : cap;
+  const long long all = (ctx + kGroup - 1) / kGroup;
+  if (window == 0) return all;
+  const long long near = ((long long)window + T + kGroup - 1) / kGroup + 1 + ((long long)sinks + kGroup - 1) / kGroup;
+  return near < all ? near : all;
+}
+
+constexpr int kMaxContextSplits = 32;
+ContextPlan plan_call(const kvlinc_cache& c, int T, int window, int sinks, int max_context) {
+  const long long gq = c.H_q / c.H_kv, units = (long long)c.B * c.H_kv * ((T * gq + 15) / 16);
+  const long long groups = groups_met(c, T, window, sinks, max_context);
+  long long s = 512 / units, most = (groups + 3) / 4;
+  if (s > most) s = most;
+  if (s > kMaxContextSplits) s = kMaxContextSplits;
+  if (s < 1) s = 1;
+  const size_t places = (size_t)c.B * c.H_q * T;
+  return ContextPlan{(int)s, c.S16 != nullptr ? places * kPartStride : 0, s > 1 ? places * s * kPartStride : 0};
+}
+
+// The grids of a call stay below 2^32 threads (rows beyond that would not fit any card's memory).
+bool too_many(const kvlinc_cache& c, int T) {
+  const long long gq = c.H_q / c.H_kv;
+  return (long long)c.B * c.H_kv >= (1ll << 24) || (long long)c.B * c.H_kv * ((T * gq + 15) / 16) >= (1ll << 24);
+}
+
+int check_prompt(const kvlinc_cache* c, int T, int window, int sinks) {
+  const int rc = kvlinc_cache_validate(c);
+  if (rc != KVLINC_OK) return rc;
+  if (T < 1 || T > (1 << 24) || window < 0 || sinks < 0 || too_many(*c, T)) return KVLINC_EINVAL;
+  // the states stand for all quantized tokens; the literal form needs the maximum over the whole context at one place
+  if (c->S16 != nullptr && (window != 0 || (c->flags & KVLINC_FLAG_ALG1_LITERAL) != 0)) return KVLINC_EINVAL;
+  return KVLINC_OK;
+}
+int check_windowed(const kvlinc_cache* c, int window, int sinks) {
+  const int rc = kvlinc_cache_validate(c);
+  if (rc != KVLINC_OK) return rc;
+  return window < 0 || sinks < 0 || c->S16 != nullptr || too_many(*c, 1) ? KVLINC_EINVAL : KVLINC_OK;
+}
+
+ContextCall make_call(const kvlinc_cache& c, const kvlinc_half* q, int T, int window, int sinks, kvlinc_half* out, void* workspace, const ContextPlan& p) {
+  ContextCall a{};
+  a.cache = c;
+  a.q = reinterpret_cast<const _Float16*>(q);
+  a.T = T; a.window = window; a.sinks = window != 0 ? sinks : 0;
+  a.gq = c.H_q / c.H_kv;
+  a.splits = p.splits;
+  a.corr = p.corr_floats != 0 ? static_cast<float*>(workspace) : nullptr;
+  a.part = p.part_floats != 0 ? static_cast<float*>(workspace) + p.corr_floats : nullptr;
+  a.out = reinterpret_cast<_Float16*>(out);
+  return a;
+}
+bool bad_workspace(const void* workspace, size_t bytes, size_t need) { return need != 0 && (bad_address(workspace, 16) || bytes < need); }
+
+}  // namespace
+}  // namespace kvlinc
+
+using namespace kvlinc;
+
+extern "C" {
+
+size_t kvlinc_prompt_workspace_bytes(const kvlinc_cache* cache, int32_t T, int32_t window, int32_t sinks, int32_t max_context) {
+  return check_prompt(cache, T, window, sinks) == KVLINC_OK ? plan_call(*cache, T, window, sinks, max_context).bytes() : 0;
+}
+
+int kvlinc_prompt_attention(const kvlinc_cache* cache, const kvlinc_half* q, const kvlinc_half* k_new, const kvlinc_half* v_new,
+                            const int32_t* n_new, int32_t T, int32_t window, int32_t sinks, kvlinc_half* out, void* workspace,
+                            size_t workspace_bytes, int32_t max_context, void* stream) {
+  const int rc = check_prompt(cache, T, window, sinks);
+  if (rc != KVLINC_OK) return rc;
+  if (bad_address(q, 16) || bad_address(k_new, 16) || bad_address(v_new, 16) || bad_address(out, 16)) return KVLINC_EINVAL;
+  if (n_new != nullptr && bad_address(n_new, 4)) return KVLINC_EINVAL;
+  const ContextPlan p = plan_call(*cache, T, window, sinks, max_context);
+  if (bad_workspace(workspace, workspace_bytes, p.bytes())) return KVLINC_EWORKSPACE;
+  ContextCall a = make_call(*cache, q, T, window, sinks, out, workspace, p);
+  a.k_new = reinterpret_cast<const _Float16*>(k_new);
+  a.v_new = reinterpret_cast<const _Float16*>(v_new);
+  a.n_new = n_new;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  if (a.corr != nullptr) {
+    const int rl = launch_prompt_correction(a, s);
+    if (rl != KVLINC_OK) return rl;
+  }
+  return launch_rows(a, true, s);
+}
+
+size_t kvlinc_decode_windowed_workspace_bytes(const kvlinc_cache* cache, int32_t window, int32_t sinks, int32_t max_context) {
+  return check_windowed(cache, window, sinks) == KVLINC_OK ? plan_call(*cache, 1, window, sinks, max_context).bytes() : 0;
+}
+
+int kvlinc_decode_attention_windowed(const kvlinc_cache* cache, const kvlinc_half* q, int32_t window, int32_t sinks, kvlinc_half* out,
+                                     void* workspace, size_t workspace_bytes, int32_t max_context, void* stream) {
+  const int rc = check_windowed(cache, window, sinks);
+  if (rc != KVLINC_OK) return rc;
+  if (bad_address(q, 16) || bad_address(out, 16)) return KVLINC_EINVAL;
+  const ContextPlan p = plan_call(*cache, 1, window, sinks, max_context);
+  if (bad_workspace(workspace, workspace_bytes, p.bytes())) return KVLINC_EWORKSPACE;
+  return launch_rows(make_call(*cache, q, 1, window, sinks, out, workspace, p), false, static_cast<hipStream_t>(stream));
+}
+
+int kvlinc_cache_read(const kvlinc_cache* cache, const int32_t* first, int32_t T, void* k_out, void* v_out, int32_t dtype,
+                      int32_t rotated, void* stream) {
+  const int rc = kvlinc_cache_validate(cache);
+  if (rc != KVLINC_OK) return rc;
+  if (T < 1 || T > (1 << 30) || dtype < KVLINC_F16 || dtype > KVLINC_F32 || rotated < 0 || rotated > 1) return KVLINC_EINVAL;
+  if (k_out == nullptr && v_out == nullptr) return KVLINC_EINVAL;
+  if ((k_out != nullptr && bad_address(k_out, 16)) || (v_out != nullptr && bad_address(v_out, 16))) return KVLINC_EINVAL;
+  if (first != nullptr && bad_address(first, 4)) return KVLINC_EINVAL;
+  return launch_read(*cache, first, T, k_out, v_out, dtype, rotated != 0, static_cast<hipStream_t>(stream));
+}
+
+}  // extern "C"

@@ -1,0 +1,265 @@
+// Reading the cache back: keys and values of a range of tokens, dequantized.
+//
+// A workgroup takes the tokens of one aligned block of 128 positions of a (sequence, KV head), keys or values: packed ones from the block's
+// record, raw ones from the window (a cache with a partial last group has both in one block).
+// Values are rotated back by butterflies on the codes themselves: H (s c + z) = s (H c) + z H 1, and the sums of 128 centred
+// codes, multiples of 1/2 below 1024, are exact in binary16, two tokens an instruction.  H 1 = sqrt(128) e_0 leaves the zero-point to channel 0.
+// So a number is rounded once in binary32 and once to its type.  Bound: bytes written (256 to 512 a token and tensor against 32 to 64
+// read); rows go through LDS so that a wave stores whole lines.
+#include <hip/hip_runtime.h>
+
+#include <type_traits>
+
+#include "kvlinc_codes.h"
+#include "kvlinc_context_internal.h"
+
+namespace kvlinc {
+namespace {
+
+struct BF16 { uint16_t bits; };
+template <typename OUT>
+__device__ __forceinline__ OUT rounded(float v);
+template <>
+__device__ __forceinline__ float rounded<float>(float v) { return v; }
+template <>
+__device__ __forceinline__ half_t rounded<half_t>(float v) { return (half_t)fminf(fmaxf(v, -65504.0f), 65504.0f); }
+template <>
+__device__ __forceinline__ BF16 rounded<BF16>(float v) {  // to nearest even (finite numbers)
+  const uint32_t u = __builtin_bit_cast(uint32_t, v);
+  return BF16{(uint16_t)((u + 0x7fffu + ((u >> 16) & 1u)) >> 16)};
+}
+
+// 32 rows of a wave in LDS, 16 bytes more than a row apart
+template <typename OUT>
+struct WaveRows {
+  static constexpr int kStride = kHeadDim + 16 / sizeof(OUT);
+  OUT x[32][kStride];
+};
+// token_of(r): position of row r; written if from <= position < to
+template <typename OUT, typename F>
+__device__ __forceinline__ void store_rows(const WaveRows<OUT>& rows, OUT* out, long long first, int from, int to, int lane, F token_of) {
+  constexpr int kLanes = kHeadDim * sizeof(OUT) / 16;  // lanes a row takes, 16 bytes each
+#pragma unroll
+  for (int r0 = 0; r0 < 32; r0 += 64 / kLanes) {
+    const int r = r0 + lane / kLanes, t = token_of(r);
+    if (t >= from && t < to)
+      reinterpret_cast<uint4*>(out + (t - first) * kHeadDim)[lane % kLanes] = reinterpret_cast<const uint4*>(&rows.x[r][0])[lane % kLanes];
+  }
+}
+
+template <int BITS, int SEL>
+__device__ __forceinline__ void key_pairs(const uint32_t (&e)[BITS / 2], const uint32_t (&s)[16], const uint32_t (&z)[16], int at, float (&v)[8]) {
+  const half2_t c = code_pair<BITS, SEL>(e, 1.0f), ss = as_h2(s[at + SEL]), zz = as_h2(z[at + SEL]);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) v[2 * SEL + i] = fmaf((float)ss[i], (float)c[i] + Rec<BITS>::kCentre, (float)zz[i]);
+}
+
+// Keys: wave w has tokens 32 w .. 32 w + 31; a lane two of them, 32 channels each.
+template <int BITS, typename OUT>
+__device__ __forceinline__ void read_keys(const uint32_t* rec, WaveRows<OUT>& rows, int wave, int lane) {
+  const int j = lane & 15, g = lane >> 4;
+  uint32_t s[16], z[16];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint4 a = reinterpret_cast<const uint4*>(rec + Rec<BITS>::kKeyScale)[4 * g + i], b = reinterpret_cast<const uint4*>(rec + Rec<BITS>::kKeyZero)[4 * g + i];
+    s[4 * i] = a.x; s[4 * i + 1] = a.y; s[4 * i + 2] = a.z; s[4 * i + 3] = a.w;
+    z[4 * i] = b.x; z[4 * i + 1] = b.y; z[4 * i + 2] = b.z; z[4 * i + 3] = b.w;
+  }
+  uint4 w[BITS / 2];
+#pragma unroll
+  for (int pl = 0; pl < BITS / 2; ++pl) w[pl] = reinterpret_cast<const uint4*>(rec + Rec<BITS>::kKeyTile + 1024 * pl)[64 * wave + lane];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {  // token 16 (q / 2) + j of the wave's, channels 32 g + 16 (q % 2) + 0..15
+    uint32_t e[BITS / 2], o[BITS / 2];
+#pragma unroll
+    for (int pl = 0; pl < BITS / 2; ++pl) {
+      const Nibbles n = nibbles_of(q == 0 ? w[pl].x : q == 1 ? w[pl].y : q == 2 ? w[pl].z : w[pl].w);
+      e[pl] = n.first; o[pl] = n.second;
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      float v[8];
+      const int at = 8 * (q % 2) + 4 * u;
+      if (u == 0) { key_pairs<BITS, 0>(e, s, z, at, v); key_pairs<BITS, 1>(e, s, z, at, v); key_pairs<BITS, 2>(e, s, z, at, v); key_pairs<BITS, 3>(e, s, z, at, v); }
+      else { key_pairs<BITS, 0>(o, s, z, at, v); key_pairs<BITS, 1>(o, s, z, at, v); key_pairs<BITS, 2>(o, s, z, at, v); key_pairs<BITS, 3>(o, s, z, at, v); }
+      OUT* dst = &rows.x[16 * (q / 2) + j][32 * g + 16 * (q % 2) + 8 * u];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) dst[i] = rounded<OUT>(v[i]);
+    }
+  }
+}
+
+__device__ __forceinline__ half2_t dpp_h2_swap(half2_t v, int stage) {
+  const uint32_t u = as_u32(v);
+  return as_h2(stage == 0 ? dpp_u<kQuadSwap1>(u) : stage == 1 ? dpp_u<kQuadSwap2>(u) : stage == 2 ? dpp_u<kQuadMirror>(dpp_u<kRowHalfMirror>(u)) : dpp_u<kRowRor8>(u));
+}
+// Butterflies over the channels 32 u + 16 n + j (u = lane / 16, n = 0, 1, j = lane % 16) of two tokens.
+__device__ __forceinline__ void rotate_codes(half2_t (&v)[2], int lane) {
+#pragma unroll
+  for (int st = 0; st < 4; ++st) {
+    const half_t one = (half_t)((lane >> st) & 1 ? -1.0f : 1.0f);
+#pragma unroll
+    for (int n = 0; n < 2; ++n) v[n] = __builtin_elementwise_fma(v[n], half2_t{one, one}, dpp_h2_swap(v[n], st));
+  }
+  const half2_t a = v[0] + v[1], b = v[0] - v[1];
+  v[0] = a; v[1] = b;
+  const half_t s16 = (half_t)((lane & 16) ? -1.0f : 1.0f), s32 = (half_t)((lane & 32) ? -1.0f : 1.0f);
+#pragma unroll
+  for (int n = 0; n < 2; ++n) {
+    const auto x = __builtin_amdgcn_permlane16_swap(as_u32(v[n]), as_u32(v[n]), false, false);
+    v[n] = __builtin_elementwise_fma(as_h2(x[1]), half2_t{s16, s16}, as_h2(x[0]));
+    const auto y = __builtin_amdgcn_permlane32_swap(as_u32(v[n]), as_u32(v[n]), false, false);
+    v[n] = __builtin_elementwise_fma(as_h2(y[1]), half2_t{s32, s32}, as_h2(y[0]));
+  }
+}
+
+// Values: wave w has tokens 16 i + 4 w + 0..3 (i = 0..7), row 4 i + t of its rows; a lane channels 32 u + 16 n + j of all of them.
+template <int BITS, typename OUT, bool ROTATED, int SEL>
+__device__ __forceinline__ void value_pairs(const uint32_t (&e)[2][BITS / 2], const uint32_t* sz, int t, WaveRows<OUT>& rows, int lane) {
+  const int j = lane & 15, u = lane >> 4;
+  half2_t c[2] = {code_pair<BITS, SEL>(e[0], 1.0f), code_pair<BITS, SEL>(e[1], 1.0f)};
+  if constexpr (!ROTATED) rotate_codes(c, lane);
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {  // token 16 i + 4 w + t, i = 2 SEL + k
+    const half2_t p = as_h2(sz[2 * SEL + k]);
+    const float s = (float)p[0], mid = fmaf(s, Rec<BITS>::kCentre, (float)p[1]);
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      const float x = (float)c[n][k];
+      float v;
+      if constexpr (ROTATED) v = fmaf(s, x + Rec<BITS>::kCentre, (float)p[1]);
+      else v = fmaf(s, x, n == 0 && lane == 0 ? 128.0f * mid : 0.0f) * kInvSqrtD;
+      rows.x[4 * (2 * SEL + k) + t][32 * u + 16 * n + j] = rounded<OUT>(v);
+    }
+  }
+}
+template <int BITS, typename OUT, bool ROTATED>
+__device__ __forceinline__ void read_values(const uint32_t* rec, WaveRows<OUT>& rows, int wave, int lane) {
+  const int j = lane & 15, u = lane >> 4;
+#pragma unroll
+  for (int hg = 0; hg < 2; ++hg) {
+    const int g = (wave >> 1) + 2 * hg, w = wave & 1;
+    uint32_t words[2][BITS / 2];
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+      for (int pl = 0; pl < BITS / 2; ++pl) words[n][pl] = rec[Rec<BITS>::kValueTile + 1024 * pl + (64 * u + j + 16 * g) * 4 + 2 * n + w];
+#pragma unroll
+    for (int odd = 0; odd < 2; ++odd) {
+      uint32_t e[2][BITS / 2];
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int pl = 0; pl < BITS / 2; ++pl) {
+          const Nibbles nb = nibbles_of(words[n][pl]);
+          e[n][pl] = odd ? nb.second : nb.first;
+        }
+      const int t = 2 * hg + odd;
+      const uint4* src = reinterpret_cast<const uint4*>(rec + Rec<BITS>::kValueSZ) + 2 * (4 * wave + t);
+      const uint4 a = src[0], b = src[1];
+      const uint32_t sz[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+      value_pairs<BITS, OUT, ROTATED, 0>(e, sz, t, rows, lane);
+      value_pairs<BITS, OUT, ROTATED, 1>(e, sz, t, rows, lane);
+      value_pairs<BITS, OUT, ROTATED, 2>(e, sz, t, rows, lane);
+      value_pairs<BITS, OUT, ROTATED, 3>(e, sz, t, rows, lane);
+    }
+  }
+}
+
+// Grid, one-dimensional: block of 128 positions fastest, then (sequence, KV head); keys in the first half, values in the second (one
+// half where one of the two is not asked for).
+template <int BITS, typename OUT, bool ROTATED>
+__global__ __launch_bounds__(256) void read_kernel(kvlinc_cache c, const int32_t* first_of, int T, OUT* k_out, OUT* v_out, int blocks, int per_tensor) {
+  __shared__ __align__(16) WaveRows<OUT> all[4];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const bool values = k_out == nullptr || (int)blockIdx.x >= per_tensor;
+  const int id = (int)blockIdx.x >= per_tensor ? blockIdx.x - per_tensor : blockIdx.x;
+  const int bh = id / blocks, b = bh / c.H_kv;
+  const Lengths len = lengths_of(c, b);
+  const long long first = first_of != nullptr ? max(first_of[b], 0) : 0;
+  const long long block = first / kGroup + (id - bh * blocks), at = block * kGroup;
+  const long long end = min(first + T, (long long)len.total());
+  if (at >= end) return;
+  OUT* out = (values ? v_out : k_out) + (long long)bh * T * kHeadDim;
+  const int from = (int)max(first, at), to = (int)min(end, at + kGroup);  // positions this workgroup writes
+  // with sliding values, the newest 128 tokens' values are the window's: token t in slot t % 128
+  const bool sliding = (c.flags & KVLINC_FLAG_SLIDING_VALUES) != 0 && values && len.nq % kGroup == 0;
+  const int packed = sliding ? min(len.nq, max(len.total() - kGroup, 0)) : len.nq;
+  if (from < packed) {
+    const uint32_t* rec = c.groups + ((long long)bh * c.max_groups + block) * Rec<BITS>::kWords;
+    if (values) {
+      read_values<BITS, OUT, ROTATED>(rec, all[wave], wave, lane);
+      __builtin_amdgcn_wave_barrier();
+      store_rows<OUT>(all[wave], out, first, from, min(to, packed), lane, [&](int r) { return (int)at + 16 * (r >> 2) + 4 * wave + (r & 3); });
+    } else {
+      read_keys<BITS, OUT>(rec, all[wave], wave, lane);
+      __builtin_amdgcn_wave_barrier();
+      store_rows<OUT>(all[wave], out, first, from, min(to, packed), lane, [&](int r) { return (int)at + 32 * wave + r; });
+    }
+  }
+  const int raw = max(from, packed);
+  if (raw >= to) return;
+  const int slot0 = sliding ? 0 : len.nq;  // slot of position t: t - nq, or t % 128 where values slide (nq is a multiple of 128 there)
+  auto slot_of = [&](int t) { return sliding ? t & (kGroup - 1) : t - slot0; };
+  if (!values) {
+    const half_t* keys = reinterpret_cast<const half_t*>(c.k_res) + (long long)bh * c.R * kHeadDim;
+    for (int t = raw + wave; t < to; t += 4) {
+      const half2_t k = *reinterpret_cast<const half2_t*>(keys + slot_of(t) * kHeadDim + 2 * lane);
+      OUT* dst = out + (t - first) * kHeadDim + 2 * lane;
+      dst[0] = rounded<OUT>((float)k[0]);
+      dst[1] = rounded<OUT>((float)k[1]);
+    }
+    return;
+  }
+  const half_t* vals = reinterpret_cast<const half_t*>(c.v_res) + (long long)bh * c.R * kHeadDim;
+  const int s_first = slot_of(raw), s_last = slot_of(to - 1);  // (a block's slots are consecutive)
+  for (int quad = s_first / 4 + wave; quad <= s_last / 4; quad += 4) {
+    const uint4 w = reinterpret_cast<const uint4*>(vals + (long long)quad * kHeadDim * 4)[lane];  // channels 2 lane, 2 lane + 1, four slots each
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = (float)as_h2(u[i >> 1])[i & 1];  // [channel][slot]
+    if constexpr (!ROTATED) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float a = v[i], d = v[4 + i];
+        v[i] = a + d;
+        v[4 + i] = a - d;
+      }
+      lane_butterflies<8>(v, lane);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] *= kInvSqrtD;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int slot = 4 * quad + i;
+      if (slot < s_first || slot > s_last) continue;
+      OUT* dst = out + (raw + slot - s_first - first) * kHeadDim + 2 * lane;
+      dst[0] = rounded<OUT>(v[i]);
+      dst[1] = rounded<OUT>(v[4 + i]);
+    }
+  }
+}
+
+template <int BITS, typename OUT>
+int launch_read_of(const kvlinc_cache& c, const int32_t* first, int T, void* k_out, void* v_out, bool rotated, hipStream_t stream) {
+  const int blocks = (int)(((long long)T + kGroup - 1) / kGroup) + (first != nullptr ? 1 : 0);
+  const long long per_tensor = (long long)blocks * c.B * c.H_kv, grid = per_tensor * ((k_out != nullptr) + (v_out != nullptr));
+  if (grid >= (1ll << 24)) return KVLINC_EINVAL;  // 2^32 threads: more than the outputs of any card
+  OUT *k = static_cast<OUT*>(k_out), *v = static_cast<OUT*>(v_out);
+  if (rotated) hipLaunchKernelGGL((read_kernel<BITS, OUT, true>), dim3((unsigned)grid), dim3(256), 0, stream, c, first, T, k, v, blocks, (int)per_tensor);
+  else hipLaunchKernelGGL((read_kernel<BITS, OUT, false>), dim3((unsigned)grid), dim3(256), 0, stream, c, first, T, k, v, blocks, (int)per_tensor);
+  return hipGetLastError() == hipSuccess ? KVLINC_OK : KVLINC_EHIP;
+}
+
+}  // namespace
+
+int launch_read(const kvlinc_cache& c, const int32_t* first, int T, void* k_out, void* v_out, int dtype, bool rotated, hipStream_t stream) {
+  switch (dtype) {
+    case KVLINC_F16: return c.bits == 2 ? launch_read_of<2, half_t>(c, first, T, k_out, v_out, rotated, stream) : launch_read_of<4, half_t>(c, first, T, k_out, v_out, rotated, stream);
+    case KVLINC_BF16: return c.bits == 2 ? launch_read_of<2, BF16>(c, first, T, k_out, v_out, rotated, stream) : launch_read_of<4, BF16>(c, first, T, k_out, v_out, rotated, stream);
+    default: return c.bits == 2 ? launch_read_of<2, float>(c, first, T, k_out, v_out, rotated, stream) : launch_read_of<4, float>(c, first, T, k_out, v_out, rotated, stream);
+  }
+}
+
+}  // namespace kvlinc

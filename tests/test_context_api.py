@@ -1,0 +1,154 @@
+"""Host side of kvlinc_context.h: exported names, what is refused before any launch, workspace sizes, and the checks of KVLincCache.
+No compute call is made here."""
+import ctypes
+import os
+import re
+
+import pytest
+import torch
+
+import paper_2510_05373_amd as kv
+from paper_2510_05373_amd import binding as kb
+from tests.test_library_abi import fake_struct
+
+HEADER = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "kvlinc_context.h")
+NONE = dict(S=0, S16=0, P=0, Wq=0, Wk=0)
+
+
+def plain(**over):
+    return fake_struct(**{**NONE, **over})
+
+
+def test_header_functions_are_exported():
+    text = re.sub(r"/\*.*?\*/", "", open(HEADER).read(), flags=re.S)
+    names = sorted(set(re.findall(r"\b(kvlinc_[a-z_]+)\s*\(", text)))
+    assert names == ["kvlinc_cache_read", "kvlinc_decode_attention_windowed", "kvlinc_decode_windowed_workspace_bytes",
+                     "kvlinc_prompt_attention", "kvlinc_prompt_workspace_bytes"]
+    lib = ctypes.CDLL(kb.lib_path)
+    for n in names:
+        assert hasattr(lib, n) and callable(getattr(kv, n))
+    for name, value in re.findall(r"(KVLINC_\w+) = (\d+)", text):
+        assert getattr(kv, name) == int(value)
+
+
+def prompt(c, q=0x20000, k=0x20000, v=0x20000, n=None, T=4, window=0, sinks=0, out=0x40000, ws=0x80000, size=1 << 40, bound=0):
+    p = lambda a: None if a is None else ctypes.c_void_p(a)
+    return kb.lib.kvlinc_prompt_attention(ctypes.byref(c), p(q), p(k), p(v), p(n), T, window, sinks, p(out), p(ws), size, bound, None)
+
+
+@pytest.mark.parametrize("over", [dict(q=None), dict(q=0x20008), dict(k=None), dict(k=0x20002), dict(v=None), dict(v=0x20004), dict(n=0x20002),
+                                  dict(T=0), dict(T=-1), dict(T=(1 << 24) + 1), dict(window=-1), dict(sinks=-1), dict(window=8, sinks=-1),
+                                  dict(out=None), dict(out=0x40002)])
+def test_prompt_attention_refuses(over):
+    assert prompt(plain(), **over) == kb.KVLINC_EINVAL
+
+
+def test_prompt_attention_refuses_what_the_states_do_not_cover():
+    full = fake_struct()
+    assert prompt(full, window=16) == kb.KVLINC_EINVAL
+    assert prompt(fake_struct(flags=kb.KVLINC_FLAG_ALG1_LITERAL)) == kb.KVLINC_EINVAL
+    assert prompt(fake_struct(d=64)) == kb.KVLINC_EINVAL
+    assert kb.lib.kvlinc_prompt_attention(None, *[ctypes.c_void_p(0x20000)] * 4, 1, 0, 0, ctypes.c_void_p(0x20000), None, 0, 0, None) == kb.KVLINC_EINVAL
+    for bad in (dict(window=16), dict(T=0), dict(sinks=-1)):
+        assert kb.kvlinc_prompt_workspace_bytes(full, **{"T": 4, **bad}) == 0
+
+
+def test_prompt_attention_needs_its_workspace():
+    full = fake_struct()
+    need = kb.kvlinc_prompt_workspace_bytes(full, 4)
+    assert need >= 2 * 8 * 4 * 132 * 4  # the correction of every row
+    for over in (dict(ws=None), dict(ws=0x80008), dict(size=need - 1), dict(size=0)):
+        assert prompt(full, **over) == kb.KVLINC_EWORKSPACE
+    # more rows or a longer bound never need less than what they share with fewer
+    assert kb.kvlinc_prompt_workspace_bytes(full, 8) >= need
+
+
+def test_a_bound_beyond_the_capacity_is_the_capacity():
+    c = plain(max_groups=64)
+    sizes = [kb.kvlinc_decode_windowed_workspace_bytes(c, 0, 0, n) for n in (0, -5, 64 * 128 + 128, 1 << 30)]
+    assert len(set(sizes)) == 1 and sizes[0] > 0
+
+
+def windowed(c, q=0x20000, window=16, sinks=0, out=0x40000, ws=0x80000, size=1 << 40):
+    p = lambda a: None if a is None else ctypes.c_void_p(a)
+    return kb.lib.kvlinc_decode_attention_windowed(ctypes.byref(c), p(q), window, sinks, p(out), p(ws), size, 0, None)
+
+
+@pytest.mark.parametrize("over", [dict(q=None), dict(q=0x20004), dict(window=-1), dict(sinks=-2), dict(out=None), dict(out=0x40008)])
+def test_windowed_decode_refuses(over):
+    assert windowed(plain(), **over) == kb.KVLINC_EINVAL
+
+
+def test_windowed_decode_refuses_a_cache_with_adapters():
+    assert windowed(fake_struct()) == kb.KVLINC_EINVAL
+    assert windowed(fake_struct(), window=0) == kb.KVLINC_EINVAL
+    assert kb.kvlinc_decode_windowed_workspace_bytes(fake_struct(), 16) == 0
+
+
+def test_windowed_decode_needs_its_workspace():
+    c = plain(max_groups=256)
+    need = kb.kvlinc_decode_windowed_workspace_bytes(c, 4096, 4)
+    assert need > 0
+    assert windowed(c, window=4096, sinks=4, size=need - 1) == kb.KVLINC_EWORKSPACE
+    assert windowed(c, window=4096, sinks=4, ws=None) == kb.KVLINC_EWORKSPACE
+
+
+def read(c, first=None, T=4, k=0x20000, v=0x40000, dtype=0, rotated=0):
+    p = lambda a: None if a is None else ctypes.c_void_p(a)
+    return kb.lib.kvlinc_cache_read(ctypes.byref(c), p(first), T, p(k), p(v), dtype, rotated, None)
+
+
+@pytest.mark.parametrize("over", [dict(first=0x20002), dict(T=0), dict(T=-3), dict(T=(1 << 30) + 1), dict(k=None, v=None), dict(k=0x20008),
+                                  dict(v=0x40004), dict(dtype=-1), dict(dtype=3), dict(rotated=2), dict(rotated=-1)])
+def test_read_refuses(over):
+    assert read(plain(), **over) == kb.KVLINC_EINVAL
+    assert read(fake_struct(bits=3)) == kb.KVLINC_EINVAL
+
+
+def test_more_rows_than_a_grid_holds_are_refused():
+    assert prompt(plain(B=1 << 20, H_q=32, H_kv=8), T=1 << 20) == kb.KVLINC_EINVAL
+    assert read(plain(B=1 << 16), T=1 << 30) == kb.KVLINC_EINVAL
+
+
+# ---- KVLincCache: what it looks at before it hands out an address ----------------------------------------------------------------
+
+@pytest.fixture(scope="module")
+def cache():
+    return kv.KVLincCache(2, 8, 2, 256, device="cpu")
+
+
+def half(*s):
+    return torch.zeros(*s, dtype=torch.float16)
+
+
+def prompt_args(**over):
+    a = dict(q=half(2, 8, 3, 128), k_new=half(2, 2, 3, 128), v_new=half(2, 2, 3, 128))
+    a.update(over)
+    return a
+
+
+@pytest.mark.parametrize("over", [
+    dict(q=half(2, 8, 128)), dict(q=half(2, 4, 3, 128)), dict(q=half(2, 8, 3, 64)), dict(q=half(2, 8, 3, 128).float()), dict(q=None),
+    dict(q=half(2, 3, 8, 128).transpose(1, 2)), dict(k_new=half(2, 2, 4, 128)), dict(k_new=half(2, 8, 3, 128)),
+    dict(v_new=half(2, 2, 3, 128).bfloat16()), dict(v_new=half(2, 2, 3, 256)[..., ::2]), dict(n_new=torch.zeros(2, dtype=torch.int64)),
+    dict(n_new=torch.zeros(3, dtype=torch.int32)), dict(n_new=[3, 3]), dict(out=half(2, 8, 4, 128)), dict(out=half(2, 8, 3, 128).float()),
+    dict(q=half(2, 8, 0, 128), k_new=half(2, 2, 0, 128), v_new=half(2, 2, 0, 128)), dict(window=-1), dict(sinks=-1)])
+def test_prompt_attention_checks_its_tensors(cache, over):
+    with pytest.raises(kv.KVLincError):
+        cache.prompt_attention(**prompt_args(**over), stream=None)
+
+
+@pytest.mark.parametrize("over", [dict(q=half(2, 8, 1, 128)), dict(q=half(2, 8, 256)[..., ::2]), dict(q=half(2, 2, 128)), dict(window=-4),
+                                  dict(sinks=-1), dict(out=half(2, 2, 128))])
+def test_decode_windowed_checks_its_tensors(cache, over):
+    with pytest.raises(kv.KVLincError):
+        cache.decode_windowed(**{"q": half(2, 8, 128), "window": 16, **over})
+
+
+@pytest.mark.parametrize("over", [dict(), dict(T=0), dict(T=-1), dict(T=4, dtype=torch.float64), dict(k_out=half(2, 2, 4, 64)), dict(T=5, k_out=half(2, 2, 4, 128)),
+                                  dict(k_out=half(2, 2, 4, 128), v_out=half(2, 2, 4, 128).float()), dict(k_out=half(2, 2, 4, 128), dtype=torch.float32),
+                                  dict(T=4, first=torch.zeros(2)), dict(T=4, first=torch.zeros(1, dtype=torch.int32)),
+                                  dict(v_out=half(2, 4, 2, 128).transpose(1, 2))])
+def test_read_checks_its_tensors(cache, over):
+    with pytest.raises(kv.KVLincError):
+        cache.read(**over)
