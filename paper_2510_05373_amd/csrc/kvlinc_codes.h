@@ -16,6 +16,7 @@ constexpr float kLog2eSqrtD = 1.4426950408889634f * kInvSqrtD;  // scores in the
 
 __device__ __forceinline__ float bits_f32(uint32_t v) { return __builtin_bit_cast(float, v); }
 __device__ __forceinline__ half2_t pack_h2(float a, float b) { return __builtin_convertvector((float2v_t{a, b}), half2_t); }
+__device__ __forceinline__ half8_t as_h8(u32x4_t v) { return __builtin_bit_cast(half8_t, v); }
 __device__ __forceinline__ half8_t as_h8(uint4 v) { return __builtin_bit_cast(half8_t, v); }
 __device__ __forceinline__ half8_t as_h8(half2_t a, half2_t b, half2_t c, half2_t d) {
   return as_h8(make_uint4(as_u32(a), as_u32(b), as_u32(c), as_u32(d)));

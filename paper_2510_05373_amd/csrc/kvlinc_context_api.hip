@@ -10,6 +10,7 @@ inline bool bad_address(const void* p, uintptr_t a) { return p == nullptr || (re
 
 // What a call makes of its sizes: splits of a context, scratch.
 struct ContextPlan {
+  bool tiles;  // blocks of 256 rows over shared tiles (kvlinc_prompt.hip), else 16 rows a wave (kvlinc_rows.hip)
   int splits;
   size_t corr_floats, part_floats;
   size_t bytes() const { return (corr_floats + part_floats) * sizeof(float); }
@@ -26,15 +27,24 @@ long long groups_met(const kvlinc_cache& c, int T, int window, int sinks, int ma
 }
 
 constexpr int kMaxContextSplits = 32;
+constexpr long long kFewRows = 64;
 ContextPlan plan_call(const kvlinc_cache& c, int T, int window, int sinks, int max_context) {
-  const long long gq = c.H_q / c.H_kv, units = (long long)c.B * c.H_kv * ((T * gq + 15) / 16);
+  const long long rows = (long long)T * (c.H_q / c.H_kv), pairs = (long long)c.B * c.H_kv;
   const long long groups = groups_met(c, T, window, sinks, max_context);
-  long long s = 512 / units, most = (groups + 3) / 4;
+  const bool tiles = rows > kFewRows;
+  long long s, most;
+  if (tiles) {
+    s = 256 / (pairs * ((rows + 255) / 256));
+    most = (groups + 1) / 2;
+  } else {
+    s = 512 / (pairs * ((rows + 15) / 16));
+    most = (groups + 3) / 4;
+  }
   if (s > most) s = most;
   if (s > kMaxContextSplits) s = kMaxContextSplits;
   if (s < 1) s = 1;
   const size_t places = (size_t)c.B * c.H_q * T;
-  return ContextPlan{(int)s, c.S16 != nullptr ? places * kPartStride : 0, s > 1 ? places * s * kPartStride : 0};
+  return ContextPlan{tiles, (int)s, c.S16 != nullptr ? places * kPartStride : 0, s > 1 ? places * s * kPartStride : 0};
 }
 
 // The grids of a call stay below 2^32 threads (rows beyond that would not fit any card's memory).
@@ -100,7 +110,7 @@ int kvlinc_prompt_attention(const kvlinc_cache* cache, const kvlinc_half* q, con
     const int rl = launch_prompt_correction(a, s);
     if (rl != KVLINC_OK) return rl;
   }
-  return launch_rows(a, true, s);
+  return p.tiles ? launch_tiles(a, s) : launch_rows(a, true, s);
 }
 
 size_t kvlinc_decode_windowed_workspace_bytes(const kvlinc_cache* cache, int32_t window, int32_t sinks, int32_t max_context) {

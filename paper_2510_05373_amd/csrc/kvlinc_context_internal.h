@@ -20,6 +20,7 @@ struct ContextCall {
 };
 
 int launch_rows(const ContextCall& a, bool prompt, hipStream_t stream);
+int launch_tiles(const ContextCall& a, hipStream_t stream);
 int launch_join(const ContextCall& a, bool prompt, hipStream_t stream);
 int launch_prompt_correction(const ContextCall& a, hipStream_t stream);
 int launch_read(const kvlinc_cache& c, const int32_t* first, int T, void* k_out, void* v_out, int dtype, bool rotated, hipStream_t stream);
