@@ -10,10 +10,13 @@ inline bool bad_address(const void* p, uintptr_t a) { return p == nullptr || (re
 
 // What a call makes of its sizes: splits of a context, scratch.
 struct ContextPlan {
-  bool tiles;  // blocks of 256 rows over shared tiles (kvlinc_prompt.hip), else 16 rows a wave (kvlinc_rows.hip)
+  // 16 rows a wave (kvlinc_rows.hip); blocks of 256 rows over tiles of codes (kvlinc_prompt.hip), or of rows dequantized first (kvlinc_dense.hip)
+  enum Kind { kRows, kTiles, kDense } kind;
   int splits;
-  size_t corr_floats, part_floats;
-  size_t bytes() const { return (corr_floats + part_floats) * sizeof(float); }
+  long long cached_rows, sink_rows;      // dequantized rows of a (sequence, KV head)
+  int row_window;                        // see ContextCall
+  size_t corr_floats, part_floats, row_halfs;  // row_halfs: of keys, and as many of values
+  size_t bytes() const { return (corr_floats + part_floats) * sizeof(float) + 2 * row_halfs * sizeof(_Float16); }
 };
 
 // Groups a row of queries meets in a context of the bound.
@@ -27,24 +30,41 @@ long long groups_met(const kvlinc_cache& c, int T, int window, int sinks, int ma
 }
 
 constexpr int kMaxContextSplits = 32;
-constexpr long long kFewRows = 64;
+constexpr long long kFewRows = 64, kDenseRows = 1024;
 ContextPlan plan_call(const kvlinc_cache& c, int T, int window, int sinks, int max_context) {
   const long long rows = (long long)T * (c.H_q / c.H_kv), pairs = (long long)c.B * c.H_kv;
   const long long groups = groups_met(c, T, window, sinks, max_context);
-  const bool tiles = rows > kFewRows;
+  ContextPlan p{};
+  p.kind = rows <= kFewRows ? ContextPlan::kRows : rows < kDenseRows ? ContextPlan::kTiles : ContextPlan::kDense;
   long long s, most;
-  if (tiles) {
-    s = 256 / (pairs * ((rows + 255) / 256));
-    most = (groups + 1) / 2;
-  } else {
+  if (p.kind == ContextPlan::kRows) {
     s = 512 / (pairs * ((rows + 15) / 16));
     most = (groups + 3) / 4;
+  } else {
+    s = 256 / (pairs * ((rows + 255) / 256));
+    most = (groups + 1) / 2;
   }
   if (s > most) s = most;
   if (s > kMaxContextSplits) s = kMaxContextSplits;
   if (s < 1) s = 1;
+  p.splits = (int)s;
   const size_t places = (size_t)c.B * c.H_q * T;
-  return ContextPlan{tiles, (int)s, c.S16 != nullptr ? places * kPartStride : 0, s > 1 ? places * s * kPartStride : 0};
+  p.corr_floats = c.S16 != nullptr ? places * kPartStride : 0;
+  p.part_floats = s > 1 ? places * s * kPartStride : 0;
+  if (p.kind == ContextPlan::kDense) {
+    // all cached tokens; or those near the first row, and the sinks ahead of them where there can be such
+    const long long cap = (long long)c.max_groups * kGroup + c.R, ctx = max_context > 0 && max_context < cap ? max_context : cap;
+    const auto up = [](long long n) { return (n + kTileTokens - 1) / kTileTokens * kTileTokens; };
+    const long long near = up(window + (long long)kTileTokens);
+    p.cached_rows = up(ctx);
+    if (window > 0 && near + up(sinks) < p.cached_rows) {
+      p.sink_rows = up(sinks);
+      p.cached_rows = near + p.sink_rows;
+      p.row_window = window;
+    }
+    p.row_halfs = (size_t)(pairs * p.cached_rows * kHeadDim);
+  }
+  return p;
 }
 
 // The grids of a call stay below 2^32 threads (rows beyond that would not fit any card's memory).
@@ -76,6 +96,13 @@ ContextCall make_call(const kvlinc_cache& c, const kvlinc_half* q, int T, int wi
   a.splits = p.splits;
   a.corr = p.corr_floats != 0 ? static_cast<float*>(workspace) : nullptr;
   a.part = p.part_floats != 0 ? static_cast<float*>(workspace) + p.corr_floats : nullptr;
+  if (p.row_halfs != 0) {  // (the parts before are multiples of 16 bytes)
+    a.k_rows = reinterpret_cast<_Float16*>(static_cast<float*>(workspace) + p.corr_floats + p.part_floats);
+    a.v_rows = a.k_rows + p.row_halfs;
+  }
+  a.cached_rows = (int)p.cached_rows;
+  a.sink_rows = (int)p.sink_rows;
+  a.row_window = p.row_window;
   a.out = reinterpret_cast<_Float16*>(out);
   return a;
 }
@@ -110,7 +137,7 @@ int kvlinc_prompt_attention(const kvlinc_cache* cache, const kvlinc_half* q, con
     const int rl = launch_prompt_correction(a, s);
     if (rl != KVLINC_OK) return rl;
   }
-  return p.tiles ? launch_tiles(a, s) : launch_rows(a, true, s);
+  return p.kind == ContextPlan::kRows ? launch_rows(a, true, s) : p.kind == ContextPlan::kTiles ? launch_tiles(a, s) : launch_dense(a, s);
 }
 
 size_t kvlinc_decode_windowed_workspace_bytes(const kvlinc_cache* cache, int32_t window, int32_t sinks, int32_t max_context) {

@@ -17,12 +17,29 @@ struct ContextCall {
   float* corr;  // [places][kPartStride] {C_d, -, -, -, C_n[128] in the rotated basis}, or NULL: no correction
   float* part;  // [places][splits][kPartStride] as the partial results of the decode kernel, rotated basis; splits > 1 only
   _Float16* out;
+  // dequantized tokens [B H_kv][cached_rows][128], values in the rotated basis (launch_dense only): sink_rows rows of the first tokens, then
+  // those from window_base on
+  const _Float16* k_rows;
+  const _Float16* v_rows;
+  int cached_rows, sink_rows, row_window;  // row_window: the window that window_base takes, 0 where the rows are all cached tokens
 };
+
+// First token that the call's first row sees through its window, down to a multiple of 64: where the dequantized rows start.
+constexpr int kTileTokens = 64;
+__host__ __device__ inline int window_base(int total, int window) {
+  const int low = window > 0 && total - window + 1 > 0 ? total - window + 1 : 0;
+  return low & ~(kTileTokens - 1);
+}
 
 int launch_rows(const ContextCall& a, bool prompt, hipStream_t stream);
 int launch_tiles(const ContextCall& a, hipStream_t stream);
+int launch_dense(const ContextCall& a, hipStream_t stream);
 int launch_join(const ContextCall& a, bool prompt, hipStream_t stream);
 int launch_prompt_correction(const ContextCall& a, hipStream_t stream);
 int launch_read(const kvlinc_cache& c, const int32_t* first, int T, void* k_out, void* v_out, int dtype, bool rotated, hipStream_t stream);
+
+// Tokens window_base(total, window) .. + T - 1 of every sequence as binary16 rows, values in the rotated basis, to rows from_row .. of
+// [B H_kv][rows][128].
+int launch_read_rows(const kvlinc_cache& c, int window, int from_row, int T, int rows, _Float16* k_rows, _Float16* v_rows, hipStream_t stream);
 
 }  // namespace kvlinc

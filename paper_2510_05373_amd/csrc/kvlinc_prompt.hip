@@ -1,8 +1,8 @@
 // Prompt attention of many rows: blocks of 256 query rows over tiles of 64 tokens that the whole workgroup shares through LDS.
 //
 // Rows of a (sequence, KV head) are (token i, head h) pairs, row = i gq + h, so that a block covers few tokens and all heads share the
-// tiles and the causal border.  Eight waves have 32 rows each; a tile is fetched into registers while the one before is worked on, turned
-// into binary16 (packed codes: once for the 256 rows) and put into the other half of the LDS, one barrier a tile.
+// tiles and the causal border.  Eight waves have 32 rows each; a tile is fetched into registers, turned into binary16 (packed codes: once
+// for the 256 rows) and put into LDS.
 //
 // Both products run on v_mfma_f32_32x32x16_f16, transposed: S^T = K Q^T (rows = tokens, columns = query rows) and O^T = V^T P^T (rows =
 // channels), so that a lane holds one query row throughout, and its weights are the operand of the second product as they come: lane
@@ -11,160 +11,159 @@
 // exponential, half a maximum, half a sum and half a conversion a score.  Roundings to binary16: keys and values that are dequantized
 // (codes times scales; a second term would double the products) and the weights; scores, sums and numerators stay binary32.
 // The new rows come first, in their own basis; then the accumulators are rotated, and the cache's tiles follow.
+//
+// Schedule.  A wave's tile is a matrix phase (P V of the tile, K Q of the next) and a vector phase (softmax, its share of a later tile into
+// LDS), about as long as each other.  The two waves of a SIMD take them in turn: waves 4..7 run one phase behind waves 0..3, with a barrier
+// at every change.
 #include <hip/hip_runtime.h>
 
-#include "kvlinc_codes.h"
-#include "kvlinc_context_internal.h"
+#include "kvlinc_tiles.h"
 
 namespace kvlinc {
 namespace {
 
-constexpr int kTileWaves = 8, kTileThreads = 64 * kTileWaves, kTileRows = 32 * kTileWaves;
-constexpr int kTileTokens = 64;
-constexpr float kHeadroom = 8.0f, kLag = 5.0f;
-constexpr float kFusedBound = 0x1p20f;  // references beyond it: the exponent is rounded as the reference is (see scores_to_weights)
-
-typedef float float16_t __attribute__((ext_vector_type(16)));
-
 // LDS tiles, 16-byte chunks permuted within a row so that neighbouring rows' reads, and the writers' pieces, fall on different banks.
 // Keys: [64 tokens][16 chunks of 8 channels]; values: [128 channels][8 chunks of 8 tokens].
+// A value tile is read one phase longer than a key tile: three of them.  Scales and zero-points of a group, 1 KB: one copy for each wave.
 struct Tiles {
-  u32x4_t k[kTileTokens][16];
-  u32x4_t v[kHeadDim][8];
+  u32x4_t k[2][kTileTokens][16];
+  u32x4_t v[3][kHeadDim][8];
+  u32x4_t meta[kTileWaves][64];
 };
+typedef u32x4_t (*KeyTile)[16];
+typedef u32x4_t (*ValueTile)[8];
 __device__ __forceinline__ int key_chunk(int t, int chunk) { return chunk ^ (t & 15); }
 __device__ __forceinline__ int value_chunk(int ch, int chunk) { return chunk ^ (((ch >> 1) ^ (ch >> 4)) & 7); }
-__device__ __forceinline__ void put_value_quad(Tiles& t, int ch, int quad, uint32_t a, uint32_t b) {  // tokens 4 quad .. 4 quad + 3
+__device__ __forceinline__ void put_value_quad(ValueTile v, int ch, int quad, uint32_t a, uint32_t b) {  // tokens 4 quad .. 4 quad + 3
   const int chunk = 2 * (quad >> 2) + (quad & 1);
-  reinterpret_cast<uint2*>(&t.v[ch][value_chunk(ch, chunk)])[(quad >> 1) & 1] = make_uint2(a, b);
+  reinterpret_cast<uint2*>(&v[ch][value_chunk(ch, chunk)])[(quad >> 1) & 1] = make_uint2(a, b);
 }
 __device__ __forceinline__ uint32_t low_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
 __device__ __forceinline__ uint32_t high_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
 
-__device__ __forceinline__ void barrier_lds() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+// A thread's share of a tile on its way from memory to LDS.
+//   raw rows [token][128] (new rows; keys of the window): x[0], x[1] = 8 channels of two tokens; values x[2], x[3] = 4 channels of 4 tokens,
+//     or 4 tokens of a channel four times (the window's values, [slot / 4][channel][slot % 4]);
+//   half a group of packed codes: x[0] 16 bytes of the record's scales and zero-points, which go through the wave's copy in LDS (held by the
+//     threads that need them they take 32 registers); x[1], x[2] the key word (token 32 np + 16 nb + j of the half, channels 32 g + 16 w ..)
+//     and the value words of channel 16 wave + j and the tokens 16 i + 4 q4 + 2 hg + 0, 1 of each plane.
+template <int BITS>
+struct Share {
+  u32x4_t x[4];
+};
 
-// ---- tiles of raw rows [token][128] (new rows; keys of the window) -------------------------------------------------------------------
-struct RawKeys {
-  u32x4_t x[2];
-};
-__device__ __forceinline__ void load_raw_keys(RawKeys& r, const half_t* rows, int count, int tid) {
+template <int BITS>
+__device__ __forceinline__ void load_raw_keys(Share<BITS>& s, const half_t* rows, int count, int tid) {
 #pragma unroll
-  for (int u = 0; u < 2; ++u) r.x[u] = reinterpret_cast<const u32x4_t*>(rows + (long long)min((tid >> 4) + 32 * u, count - 1) * kHeadDim)[tid & 15];
+  for (int u = 0; u < 2; ++u) s.x[u] = reinterpret_cast<const u32x4_t*>(rows + (long long)min((tid >> 4) + 32 * u, count - 1) * kHeadDim)[tid & 15];
 }
-__device__ __forceinline__ void store_raw_keys(const RawKeys& r, Tiles& t, int tid) {
+template <int BITS>
+__device__ __forceinline__ void store_raw_keys(const Share<BITS>& s, KeyTile t, int tid) {
 #pragma unroll
-  for (int u = 0; u < 2; ++u) t.k[(tid >> 4) + 32 * u][key_chunk((tid >> 4) + 32 * u, tid & 15)] = r.x[u];
+  for (int u = 0; u < 2; ++u) t[(tid >> 4) + 32 * u][key_chunk((tid >> 4) + 32 * u, tid & 15)] = s.x[u];
 }
-struct RawValues {
-  u32x2_t x[4];  // 4 tokens (new rows) or 4 quads (window)
-};
-__device__ __forceinline__ void load_raw_values(RawValues& r, const half_t* rows, int count, int tid) {
+template <int BITS>
+__device__ __forceinline__ void load_raw_values(Share<BITS>& s, const half_t* rows, int count, int tid) {
 #pragma unroll
-  for (int u = 0; u < 4; ++u) r.x[u] = reinterpret_cast<const u32x2_t*>(rows + (long long)min(4 * (tid >> 5) + u, count - 1) * kHeadDim)[tid & 31];
+  for (int u = 0; u < 4; ++u) {
+    const u32x2_t w = reinterpret_cast<const u32x2_t*>(rows + (long long)min(4 * (tid >> 5) + u, count - 1) * kHeadDim)[tid & 31];
+    s.x[2 + (u >> 1)][2 * (u & 1)] = w[0];
+    s.x[2 + (u >> 1)][2 * (u & 1) + 1] = w[1];
+  }
 }
-__device__ __forceinline__ void store_raw_values(const RawValues& r, Tiles& t, int tid) {  // 4 tokens x 4 channels, turned over
+template <int BITS>
+__device__ __forceinline__ void store_raw_values(const Share<BITS>& s, ValueTile t, int tid) {  // 4 tokens x 4 channels, turned over
   const int quad = tid >> 5, ch = 4 * (tid & 31);
-  put_value_quad(t, ch, quad, low_halves(r.x[0].x, r.x[1].x), low_halves(r.x[2].x, r.x[3].x));
-  put_value_quad(t, ch + 1, quad, high_halves(r.x[0].x, r.x[1].x), high_halves(r.x[2].x, r.x[3].x));
-  put_value_quad(t, ch + 2, quad, low_halves(r.x[0].y, r.x[1].y), low_halves(r.x[2].y, r.x[3].y));
-  put_value_quad(t, ch + 3, quad, high_halves(r.x[0].y, r.x[1].y), high_halves(r.x[2].y, r.x[3].y));
+  put_value_quad(t, ch, quad, low_halves(s.x[2][0], s.x[2][2]), low_halves(s.x[3][0], s.x[3][2]));
+  put_value_quad(t, ch + 1, quad, high_halves(s.x[2][0], s.x[2][2]), high_halves(s.x[3][0], s.x[3][2]));
+  put_value_quad(t, ch + 2, quad, low_halves(s.x[2][1], s.x[2][3]), low_halves(s.x[3][1], s.x[3][3]));
+  put_value_quad(t, ch + 3, quad, high_halves(s.x[2][1], s.x[2][3]), high_halves(s.x[3][1], s.x[3][3]));
 }
-// the window's values, [slot / 4][channel][slot % 4]
-__device__ __forceinline__ void load_window_values(RawValues& r, const half_t* v_win, int quad0, int quads, int tid) {
+template <int BITS>
+__device__ __forceinline__ void load_window_values(Share<BITS>& s, const half_t* v_win, int quad0, int quads, int tid) {
 #pragma unroll
-  for (int u = 0; u < 4; ++u)
-    r.x[u] = reinterpret_cast<const u32x2_t*>(v_win)[min(quad0 + 4 * u + (tid >> 7), quads - 1) * kHeadDim + (tid & 127)];
+  for (int u = 0; u < 4; ++u) {
+    const u32x2_t w = reinterpret_cast<const u32x2_t*>(v_win)[min(quad0 + 4 * u + (tid >> 7), quads - 1) * kHeadDim + (tid & 127)];
+    s.x[2 + (u >> 1)][2 * (u & 1)] = w[0];
+    s.x[2 + (u >> 1)][2 * (u & 1) + 1] = w[1];
+  }
 }
-__device__ __forceinline__ void store_window_values(const RawValues& r, Tiles& t, int tid) {
+template <int BITS>
+__device__ __forceinline__ void store_window_values(const Share<BITS>& s, ValueTile t, int tid) {
 #pragma unroll
-  for (int u = 0; u < 4; ++u) put_value_quad(t, tid & 127, 4 * u + (tid >> 7), r.x[u].x, r.x[u].y);
+  for (int u = 0; u < 4; ++u) put_value_quad(t, tid & 127, 4 * u + (tid >> 7), s.x[2 + (u >> 1)][2 * (u & 1)], s.x[2 + (u >> 1)][2 * (u & 1) + 1]);
 }
 
-// ---- tiles of packed codes: one half (64 tokens) of a group -----------------------------------------------------------------------
 template <int BITS>
-struct Packed {
-  uint32_t k[BITS / 2], v[2][BITS / 2];
-  u32x4_t ks[2], kz[2];  // key scale and zero-point of the 16 channels of the key word
-  u32x4_t sz[2][2];      // value (scale, zero-point) of tokens 16 i + 4 q4 + 2 hg + e, i = 4 half + 0..3: [hg][e]
-};
-// Thread: a key word (token 32 np + 16 nb + j of the half, channels 32 g + 16 w ..), and the two value words of channel 16 wave + j and the
-// tokens 16 i + 4 q4 + 0..3.
-template <int BITS>
-__device__ __forceinline__ void load_packed(Packed<BITS>& p, const uint32_t* rec, int half, int tid) {
-#pragma unroll
-  for (int pl = 0; pl < BITS / 2; ++pl) p.k[pl] = rec[Rec<BITS>::kKeyTile + 1024 * pl + 512 * half + tid];
-  const int at = 4 * ((tid >> 6) & 3) + 2 * (tid & 1);  // uint4 of the 16 channels' pairs
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    p.ks[i] = reinterpret_cast<const u32x4_t*>(rec + Rec<BITS>::kKeyScale)[at + i];
-    p.kz[i] = reinterpret_cast<const u32x4_t*>(rec + Rec<BITS>::kKeyZero)[at + i];
-  }
+__device__ __forceinline__ void load_packed(Share<BITS>& s, const uint32_t* rec, int half, int tid) {
   const int n = tid >> 6, j = tid & 15, q4 = (tid >> 4) & 3;
+  s.x[0] = reinterpret_cast<const u32x4_t*>(rec + Rec<BITS>::kKeyScale)[tid & 63];
 #pragma unroll
-  for (int hg = 0; hg < 2; ++hg) {
+  for (int pl = 0; pl < BITS / 2; ++pl) {
+    s.x[1 + pl][0] = rec[Rec<BITS>::kKeyTile + 1024 * pl + 512 * half + tid];
 #pragma unroll
-    for (int pl = 0; pl < BITS / 2; ++pl)
-      p.v[hg][pl] = rec[Rec<BITS>::kValueTile + 1024 * pl + ((n >> 1) * 64 + j + 16 * ((q4 >> 1) + 2 * hg)) * 4 + 2 * (n & 1) + (q4 & 1)];
-#pragma unroll
-    for (int e = 0; e < 2; ++e) p.sz[hg][e] = reinterpret_cast<const u32x4_t*>(rec + Rec<BITS>::kValueSZ)[2 * (4 * q4 + 2 * hg + e) + half];
+    for (int hg = 0; hg < 2; ++hg)
+      s.x[1 + pl][1 + hg] = rec[Rec<BITS>::kValueTile + 1024 * pl + ((n >> 1) * 64 + j + 16 * ((q4 >> 1) + 2 * hg)) * 4 + 2 * (n & 1) + (q4 & 1)];
   }
 }
-// (code) s + z of two codes given as code - centre: one rounding; a sum beyond the largest binary16 number is that number.
+static_assert(Rec<2>::kKeyZero == Rec<2>::kKeyScale + 64 && Rec<2>::kValueSZ == Rec<2>::kKeyScale + 128 && Rec<2>::kWords == Rec<2>::kKeyScale + 256, "256 words");
+// (code) s + z of two codes given as code - centre, one rounding; a sum beyond the largest binary16 number (the quantizer's scale was rounded
+// up) is that number.
 template <int BITS>
 __device__ __forceinline__ uint32_t dequantized(half2_t centred, uint32_t s, uint32_t z) {
   const half_t c = (half_t)Rec<BITS>::kCentre, top = (half_t)65504.0f;
-  const half2_t v = __builtin_elementwise_fma(centred + half2_t{c, c}, as_h2(s), as_h2(z));
-  return as_u32(__builtin_elementwise_min(v, half2_t{top, top}));
+  return as_u32(__builtin_elementwise_min(__builtin_elementwise_fma(centred + half2_t{c, c}, as_h2(s), as_h2(z)), half2_t{top, top}));
 }
 template <int BITS, int SEL>
 __device__ __forceinline__ uint32_t key_pair(const uint32_t (&e)[BITS / 2], u32x4_t s, u32x4_t z) {
   return dequantized<BITS>(code_pair<BITS, SEL>(e, 1.0f), s[SEL], z[SEL]);
 }
-template <int BITS, int SEL>  // byte SEL of the value words: i = 2 SEL, 2 SEL + 1, at quads 4 i' + q4
-__device__ __forceinline__ void value_quads(const Packed<BITS>& p, Tiles& t, int ch, int q4) {
+// Tokens i' = 2 SEL, 2 SEL + 1 of a half (quads 4 i' + q4) from byte SEL of the value words.
+template <int BITS, int SEL>
+__device__ __forceinline__ void value_quads(const uint32_t (&e)[2][BITS / 2], const uint32_t (&o)[2][BITS / 2], const u32x4_t (&sz)[4], ValueTile t, int ch, int q4) {
   uint32_t lo[2], hi[2];
 #pragma unroll
   for (int hg = 0; hg < 2; ++hg) {
+    const uint32_t a = as_u32(code_pair<BITS, SEL>(e[hg], 1.0f)), b = as_u32(code_pair<BITS, SEL>(o[hg], 1.0f));
+    const u32x4_t x = sz[2 * hg], y = sz[2 * hg + 1];
+    lo[hg] = dequantized<BITS>(as_h2(low_halves(a, b)), low_halves(x[2 * SEL], y[2 * SEL]), high_halves(x[2 * SEL], y[2 * SEL]));
+    hi[hg] = dequantized<BITS>(as_h2(high_halves(a, b)), low_halves(x[2 * SEL + 1], y[2 * SEL + 1]), high_halves(x[2 * SEL + 1], y[2 * SEL + 1]));
+  }
+  put_value_quad(t, ch, 8 * SEL + q4, lo[0], lo[1]);
+  put_value_quad(t, ch, 8 * SEL + 4 + q4, hi[0], hi[1]);
+}
+template <int BITS>
+__device__ __forceinline__ void store_packed(const Share<BITS>& s, u32x4_t* meta, KeyTile kt, ValueTile vt, int half, int tid) {
+  meta[tid & 63] = s.x[0];
+  __builtin_amdgcn_wave_barrier();  // (a wave's LDS instructions stay in order)
+  {
+    const int u = tid >> 2, token = 32 * (u >> 6) + 16 * ((tid >> 1) & 1) + (u & 15), chunk = 4 * ((u >> 4) & 3) + 2 * (tid & 1);
     uint32_t e[BITS / 2], o[BITS / 2];
 #pragma unroll
     for (int pl = 0; pl < BITS / 2; ++pl) {
-      const Nibbles n = nibbles_of(p.v[hg][pl]);
+      const Nibbles n = nibbles_of(s.x[1 + pl][0]);
       e[pl] = n.first; o[pl] = n.second;
     }
-    const uint32_t a = as_u32(code_pair<BITS, SEL>(e, 1.0f)), b = as_u32(code_pair<BITS, SEL>(o, 1.0f));
-    const u32x4_t x = p.sz[hg][0], y = p.sz[hg][1];
-    const uint32_t x0 = x[2 * (SEL & 1)], x1 = x[2 * (SEL & 1) + 1], y0 = y[2 * (SEL & 1)], y1 = y[2 * (SEL & 1) + 1];
-    lo[hg] = dequantized<BITS>(as_h2(low_halves(a, b)), low_halves(x0, y0), high_halves(x0, y0));
-    hi[hg] = dequantized<BITS>(as_h2(high_halves(a, b)), low_halves(x1, y1), high_halves(x1, y1));
+    const u32x4_t s0 = meta[chunk], s1 = meta[chunk + 1], z0 = meta[16 + chunk], z1 = meta[17 + chunk];  // a chunk of 8 channels is 16 bytes here, too
+    kt[token][key_chunk(token, chunk)] = u32x4_t{key_pair<BITS, 0>(e, s0, z0), key_pair<BITS, 1>(e, s0, z0), key_pair<BITS, 2>(e, s0, z0), key_pair<BITS, 3>(e, s0, z0)};
+    kt[token][key_chunk(token, chunk + 1)] = u32x4_t{key_pair<BITS, 0>(o, s1, z1), key_pair<BITS, 1>(o, s1, z1), key_pair<BITS, 2>(o, s1, z1), key_pair<BITS, 3>(o, s1, z1)};
   }
-  const int i = 2 * (SEL & 1);
-  put_value_quad(t, ch, 4 * i + q4, lo[0], lo[1]);
-  put_value_quad(t, ch, 4 * (i + 1) + q4, hi[0], hi[1]);
-}
-template <int BITS>
-__device__ __forceinline__ void store_packed(const Packed<BITS>& p, Tiles& t, int half, int tid) {
-  const int u = tid >> 2, token = 32 * (u >> 6) + 16 * ((tid >> 1) & 1) + (u & 15), chunk = 4 * ((u >> 4) & 3) + 2 * (tid & 1);
-  uint32_t e[BITS / 2], o[BITS / 2];
-#pragma unroll
-  for (int pl = 0; pl < BITS / 2; ++pl) {
-    const Nibbles n = nibbles_of(p.k[pl]);
-    e[pl] = n.first; o[pl] = n.second;
-  }
-  t.k[token][key_chunk(token, chunk)] = u32x4_t{key_pair<BITS, 0>(e, p.ks[0], p.kz[0]), key_pair<BITS, 1>(e, p.ks[0], p.kz[0]),
-                                                   key_pair<BITS, 2>(e, p.ks[0], p.kz[0]), key_pair<BITS, 3>(e, p.ks[0], p.kz[0])};
-  t.k[token][key_chunk(token, chunk + 1)] = u32x4_t{key_pair<BITS, 0>(o, p.ks[1], p.kz[1]), key_pair<BITS, 1>(o, p.ks[1], p.kz[1]),
-                                                       key_pair<BITS, 2>(o, p.ks[1], p.kz[1]), key_pair<BITS, 3>(o, p.ks[1], p.kz[1])};
   const int ch = 16 * (tid >> 6) + (tid & 15), q4 = (tid >> 4) & 3;
-  if (half == 0) {
-    value_quads<BITS, 0>(p, t, ch, q4);
-    value_quads<BITS, 1>(p, t, ch, q4);
-  } else {
-    value_quads<BITS, 2>(p, t, ch, q4);
-    value_quads<BITS, 3>(p, t, ch, q4);
-  }
+  // word 8 t + n of the value pairs is token 16 n + t: tokens 16 i + 4 q4 + 2 hg + e, i = 4 half + 0..3, in 16 bytes
+  const u32x4_t sz[4] = {meta[32 + 2 * (4 * q4) + half], meta[32 + 2 * (4 * q4 + 1) + half], meta[32 + 2 * (4 * q4 + 2) + half], meta[32 + 2 * (4 * q4 + 3) + half]};
+  uint32_t e[2][BITS / 2], o[2][BITS / 2];
+#pragma unroll
+  for (int hg = 0; hg < 2; ++hg)
+#pragma unroll
+    for (int pl = 0; pl < BITS / 2; ++pl) {
+      const Nibbles n = nibbles_of(s.x[1 + pl][1 + hg] >> (16 * half));  // (bytes 2 half, 2 half + 1 of a value word are these tokens)
+      e[hg][pl] = n.first; o[hg][pl] = n.second;
+    }
+  value_quads<BITS, 0>(e, o, sz, vt, ch, q4);
+  value_quads<BITS, 1>(e, o, sz, vt, ch, q4);
 }
 // Sliding values: the tokens of this half from slot `from` on take the window's values (written over the codes' by the thread that wrote them).
-__device__ __forceinline__ void slide_values(Tiles& t, const half_t* v_win, int half, int from, int tid) {
+__device__ __forceinline__ void slide_values(ValueTile t, const half_t* v_win, int half, int from, int tid) {
   const int ch = 16 * (tid >> 6) + (tid & 15), q4 = (tid >> 4) & 3;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -172,7 +171,7 @@ __device__ __forceinline__ void slide_values(Tiles& t, const half_t* v_win, int 
     if (slot + 3 < from) continue;
     const uint2 w = reinterpret_cast<const uint2*>(v_win)[(slot >> 2) * kHeadDim + ch];
     const int chunk = 2 * (quad >> 2) + (quad & 1);
-    uint2* dst = reinterpret_cast<uint2*>(&t.v[ch][value_chunk(ch, chunk)]) + ((quad >> 1) & 1);
+    uint2* dst = reinterpret_cast<uint2*>(&t[ch][value_chunk(ch, chunk)]) + ((quad >> 1) & 1);
     const uint2 old = *dst;
     const uint32_t m0 = (slot >= from ? 0xffffu : 0u) | (slot + 1 >= from ? 0xffff0000u : 0u);
     const uint32_t m1 = (slot + 2 >= from ? 0xffffu : 0u) | (slot + 3 >= from ? 0xffff0000u : 0u);
@@ -180,173 +179,45 @@ __device__ __forceinline__ void slide_values(Tiles& t, const half_t* v_win, int 
   }
 }
 
-// ---- a wave's rows ----------------------------------------------------------------------------------------------------------------
-struct TileRows {
-  half8_t q[8];      // channels 16 s + 8 h + 0..7 of this lane's row
-  float m, l;        // reference (log2 domain), per-lane sum of the weights
-  float16_t acc[4];  // numerator of channels 32 cb + 8 (r / 4) + 4 h + r % 4
-};
-
-__device__ __forceinline__ void raise_reference(TileRows& st, float largest) {  // largest score of this lane, log2 domain
-  if (__builtin_amdgcn_ballot_w64(largest > st.m + (kHeadroom + kLag)) == 0) return;
-  float x, y;
-  pair_across<32>(largest, x, y);
-  const float mx = fmaxf(x, y);
-  const float to = mx > st.m + (kHeadroom + kLag) ? mx - kHeadroom : st.m;
-  const float f = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(st.m - to);
-  st.m = to;
-  st.l *= f;
-#pragma unroll
-  for (int cb = 0; cb < 4; ++cb) st.acc[cb] *= f;
-}
-
-// One tile: 64 tokens, the first at position `at`.  masked: not every row sees all of them (p, low: of this lane's row).
-__device__ __forceinline__ void attend_tile(TileRows& st, const Tiles& t, int at, int count, bool masked, int p, int low, int sinks, int lane) {
-  const int i = lane & 31, h = lane >> 5;
-  float16_t s[2];
+// S^T = K Q^T of a tile.  A lane's chunks 2 k + h of rows i and 32 + i: key_chunk only flips address bits, so they are one address with
+// k in bits 5..7 flipped (chunk and i & 15 are four bits).
+__device__ __forceinline__ void tile_scores(TileRows& st, KeyTile t, int lane) {
+  const int i = lane & 31, base = i * 256 + 16 * key_chunk(i, lane >> 5);
 #pragma unroll
   for (int tb = 0; tb < 2; ++tb)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) s[tb][r] = 0.0f;
+    for (int r = 0; r < 16; ++r) st.s[tb][r] = 0.0f;
 #pragma unroll
   for (int k = 0; k < 8; ++k)
 #pragma unroll
-    for (int tb = 0; tb < 2; ++tb)
-      s[tb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(as_h8(t.k[32 * tb + i][key_chunk(i, 2 * k + h)]), st.q[k], s[tb], 0, 0, 0);
-  if (masked) {
-#pragma unroll
-    for (int tb = 0; tb < 2; ++tb)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int tok = 32 * tb + 8 * (r >> 2) + 4 * h + (r & 3), pos = at + tok;
-        if (!(tok < count && pos <= p && (pos >= low || pos < sinks))) s[tb][r] = -INFINITY;
-      }
-  }
-  float mx = s[0][0];
-#pragma unroll
-  for (int tb = 0; tb < 2; ++tb)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[tb][r]);
-  raise_reference(st, mx * kLog2eSqrtD);
-  const float m = st.m == -INFINITY ? 0.0f : st.m;
-  if (__builtin_amdgcn_ballot_w64(fabsf(m) > kFusedBound) != 0) {
-#pragma clang fp contract(off)
-#pragma unroll
-    for (int tb = 0; tb < 2; ++tb)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) s[tb][r] = __builtin_amdgcn_exp2f(s[tb][r] * kLog2eSqrtD - m);
-  } else {
-#pragma unroll
-    for (int tb = 0; tb < 2; ++tb)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) s[tb][r] = __builtin_amdgcn_exp2f(fmaf(s[tb][r], kLog2eSqrtD, -m));
-  }
-  half8_t P[4];
-  const half2_t ones = {(half_t)1.0f, (half_t)1.0f};
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    half2_t w[4];
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int r = 8 * (k & 1) + 2 * u;
-      w[u] = pack_h2(s[k >> 1][r], s[k >> 1][r + 1]);
-      st.l = __builtin_amdgcn_fdot2(w[u], ones, st.l, false);
-    }
-    P[k] = as_h8(w[0], w[1], w[2], w[3]);
-  }
+    for (int tb = 0; tb < 2; ++tb) st.s[tb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lds_operand(t, (base ^ (32 * k)) + 8192 * tb), st.q[k], st.s[tb], 0, 0, 0);
+}
+// O^T += V^T P^T.  Chunks 2 k + h of rows 32 cb + i: the same, value_chunk of row 32 cb + i being that of row i with 2 cb flipped.
+__device__ __forceinline__ void tile_values(TileRows& st, ValueTile t, int lane) {
+  const int i = lane & 31, base = i * 128 + 16 * value_chunk(i, lane >> 5);
 #pragma unroll
   for (int k = 0; k < 4; ++k)
 #pragma unroll
-    for (int cb = 0; cb < 4; ++cb) {
-      const int ch = 32 * cb + i;
-      st.acc[cb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(as_h8(t.v[ch][value_chunk(ch, 2 * k + h)]), P[k], st.acc[cb], 0, 0, 0);
-    }
+    for (int cb = 0; cb < 4; ++cb) st.acc[cb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lds_operand(t, (base ^ (32 * (k ^ cb))) + 4096 * cb), st.p[k], st.acc[cb], 0, 0, 0);
 }
-
-// acc H, in binary32.
-__device__ __forceinline__ void rotate_tile_rows(TileRows& st, int lane) {
-  const float s32 = (lane & 32) != 0 ? -1.0f : 1.0f;
-#pragma unroll
-  for (int cb = 0; cb < 4; ++cb) {
-#pragma unroll
-    for (int hb = 1; hb < 16; hb *= 2)  // channel bits 0, 1 (r % 4) and 3, 4 (r / 4)
-#pragma unroll
-      for (int r = 0; r < 16; ++r)
-        if ((r & hb) == 0) {
-          const float a = st.acc[cb][r], b = st.acc[cb][r + hb];
-          st.acc[cb][r] = a + b;
-          st.acc[cb][r + hb] = a - b;
-        }
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {  // bit 2: the halves of the wave
-      float x, y;
-      pair_across<32>(st.acc[cb][r], x, y);
-      st.acc[cb][r] = __builtin_fmaf(y, s32, x) * kInvSqrtD;
-    }
-  }
-#pragma unroll
-  for (int hb = 1; hb < 4; hb *= 2)
-#pragma unroll
-    for (int cb = 0; cb < 4; ++cb)
-      if ((cb & hb) == 0) {
-        const float16_t a = st.acc[cb], b = st.acc[cb + hb];
-        st.acc[cb] = a + b;
-        st.acc[cb + hb] = a - b;
-      }
-}
-
-// Grid, one-dimensional: see tile_unit.
+// Grid, one-dimensional: see place_of_block.
 template <int BITS, bool SLIDING>
 __global__ __launch_bounds__(kTileThreads, 2) void tile_kernel(ContextCall a, int blocks) {
-  __shared__ __align__(16) Tiles tiles[2];
+  __shared__ __align__(16) Tiles tiles;
   const kvlinc_cache& c = a.cache;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
-  // Work items: split fastest, then (sequence, KV head), blocks of rows from the last (the longest) to the first.  Workgroups are dealt to
-  // the 8 XCDs in turn: where the pairs divide by 8, those of one pair are 8 apart, so that its tiles come from one L2.
-  const int pairs = c.B * c.H_kv;
-  int id = blockIdx.x, split, bh, block;
-  if (pairs % 8 == 0) {
-    const int x = id & 7, y = id >> 3, per = pairs / 8;
-    const int rest = y / a.splits;
-    split = y - rest * a.splits;
-    block = rest / per;
-    bh = (rest - block * per) * 8 + x;
-  } else {
-    const int rest = id / a.splits;
-    split = id - rest * a.splits;
-    block = rest / pairs;
-    bh = rest - block * pairs;
-  }
-  block = blocks - 1 - block;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const BlockPlace at_block = place_of_block(a, blocks);
+  const int split = at_block.split, bh = at_block.bh, block = at_block.block;
   const int b = bh / c.H_kv, kvh = bh - b * c.H_kv, gq = a.gq;
   const Lengths len = lengths_of(c, b);
   const int T = a.n_new != nullptr ? min(max(a.n_new[b], 0), a.T) : a.T;
   const int rows = T * gq, row0 = block * kTileRows;
   if (row0 >= rows) return;
   const int total = len.total();
-  const long long head0 = (long long)b * c.H_q + (long long)kvh * gq;
-
-  const int wave_row = row0 + 32 * wave, row = min(wave_row + (lane & 31), rows - 1);
-  const bool idle = wave_row >= rows;
-  const int my_i = row / gq, my_h = row - my_i * gq;
-  const long long place = (head0 + my_h) * a.T + my_i;
-  const int p = total + my_i, low = window_low(p, a.window);
-  // of the wave's rows: positions p_first .. p_last, the first token of the first row's window, and of the last row's
-  const int p_first = __builtin_amdgcn_readfirstlane(total + min(wave_row, rows - 1) / gq), p_last = __builtin_amdgcn_readfirstlane(total + min(wave_row + 31, rows - 1) / gq);
-  const int low_first = window_low(p_first, a.window), low_last = window_low(p_last, a.window);
+  const WaveRows wr = wave_rows(a, b, kvh, rows, row0 + 32 * wave, total, lane);
 
   TileRows st;
-  {
-    const uint4* src = reinterpret_cast<const uint4*>(a.q + place * kHeadDim) + h;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) st.q[k] = as_h8(src[2 * k]);
-  }
-  st.m = -INFINITY;
-  st.l = 0.0f;
-#pragma unroll
-  for (int cb = 0; cb < 4; ++cb)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) st.acc[cb][r] = 0.0f;
+  start_rows(st, a.q + wr.place * kHeadDim, lane);
 
   // Tiles that some row of the block sees: of the new rows, of the window, halves of groups; this split has first .. last - 1 of them.
   const int last_i = min(row0 + kTileRows - 1, rows - 1) / gq, low_block = window_low(total + row0 / gq, a.window);
@@ -359,130 +230,102 @@ __global__ __launch_bounds__(kTileThreads, 2) void tile_kernel(ContextCall a, in
   const int n_tiles = n_new + n_win + halves - half_low + n_sink;
   const int first = (int)((long long)n_tiles * split / a.splits), last = (int)((long long)n_tiles * (split + 1) / a.splits);
 
-  auto attend = [&](const Tiles& t, int at, int count) __attribute__((always_inline)) {
-    if (idle || at > p_last || (at + count <= low_first && at >= a.sinks)) return;
-    const bool masked = count < kTileTokens || at + kTileTokens - 1 > p_first || (at < low_last && at + kTileTokens > a.sinks);
-    attend_tile(st, t, at, count, masked, p, low, a.sinks, lane);
-  };
-
   const half_t* new_keys = a.k_new + (long long)bh * a.T * kHeadDim;
   const half_t* new_values = a.v_new + (long long)bh * a.T * kHeadDim;
   const half_t* k_win = reinterpret_cast<const half_t*>(c.k_res) + (long long)bh * c.R * kHeadDim;
   const half_t* v_win = reinterpret_cast<const half_t*>(c.v_res) + (long long)bh * c.R * kHeadDim;
   const uint32_t* rec0 = c.groups + (long long)bh * c.max_groups * Rec<BITS>::kWords;
-  auto half_of = [&](int item) { return item < n_sink ? item : item - n_sink + half_low; };
+  const int raw = n_new + n_win, newest = SLIDING && len.nq % kGroup == 0 && len.nr < kGroup ? len.groups() - 1 : -1;
+  auto half_of = [&](int it) { return it - raw < n_sink ? it - raw : it - raw - n_sink + half_low; };
 
-  // ---- raw tiles: the new rows, then the window ----
-  const int raw_end = min(last, n_new + n_win);
-  int item = first, buffer = 0;
-  bool rotated = first >= n_new;
-  if (item < raw_end) {
-    RawKeys rk;
-    RawValues rv;
-    auto request = [&](int it) __attribute__((always_inline)) {
+  Share<BITS> sh;
+  auto request = [&](int it) __attribute__((always_inline)) {
+    if (it < raw) {
       const bool fresh = it < n_new;
       const int t0 = (fresh ? new_from + it : win_from + it - n_new) * kTileTokens;
-      load_raw_keys(rk, (fresh ? new_keys : k_win) + (long long)t0 * kHeadDim, (fresh ? T : len.nr) - t0, tid);
-      if (fresh) load_raw_values(rv, new_values + (long long)t0 * kHeadDim, T - t0, tid);
-      else load_window_values(rv, v_win, t0 / 4, c.R / 4, tid);
+      load_raw_keys<BITS>(sh, (fresh ? new_keys : k_win) + (long long)t0 * kHeadDim, (fresh ? T : len.nr) - t0, tid);
+      if (fresh) load_raw_values<BITS>(sh, new_values + (long long)t0 * kHeadDim, T - t0, tid);
+      else load_window_values<BITS>(sh, v_win, t0 / 4, c.R / 4, tid);
+    } else {
+      const int hf = half_of(it);
+      load_packed<BITS>(sh, rec0 + (long long)(hf >> 1) * Rec<BITS>::kWords, hf & 1, tid);
+    }
+  };
+  auto put = [&](int it, int kb, int vb) __attribute__((always_inline)) {
+    if (it < raw) {
+      store_raw_keys<BITS>(sh, tiles.k[kb], tid);
+      if (it < n_new) store_raw_values<BITS>(sh, tiles.v[vb], tid);
+      else store_window_values<BITS>(sh, tiles.v[vb], tid);
+    } else {
+      const int hf = half_of(it);
+      store_packed<BITS>(sh, tiles.meta[wave], tiles.k[kb], tiles.v[vb], hf & 1, tid);
+      if (SLIDING && (hf >> 1) == newest) slide_values(tiles.v[vb], v_win, hf & 1, len.nr, tid);
+    }
+  };
+
+  // Tile `first` + k lies in key tile k % 2 and value tile k % 3.  Waves 0..3 put theirs one tile ahead of the softmax, waves 4..7, a phase
+  // behind them, two: all of a tile is there when waves 0..3 take its keys, and what it is written over has been read by all.
+  const int n = last - first, behind = wave >> 2;
+  bool rotated = first >= n_new;
+  if (n > 0) {
+    int to = 0, kb_put = 0, vb_put = 0;  // the next tile to put, and where
+    auto put_next = [&]() __attribute__((always_inline)) {
+      put(first + to, kb_put, vb_put);
+      ++to;
+      kb_put ^= 1;
+      vb_put = vb_put == 2 ? 0 : vb_put + 1;
+      if (to < n) request(first + to);
     };
-    auto put = [&](int it, Tiles& t) __attribute__((always_inline)) {
-      store_raw_keys(rk, t, tid);
-      if (it < n_new) store_raw_values(rv, t, tid);
-      else store_window_values(rv, t, tid);
-    };
-    request(item);
-    put(item, tiles[0]);
-    barrier_lds();
-    for (; item < raw_end; ++item) {
-      const bool more = item + 1 < raw_end;
-      if (more) request(item + 1);
-      if (item == n_new) {
+    request(first);
+#pragma unroll 1
+    for (int k = 0; k <= behind && to < n; ++k) put_next();
+    next_phase();
+    if (behind) next_phase();
+    // q has arrived from here on: left to its first use in the loop, the wait there would be for a tile under way, too
+#pragma unroll
+    for (int k = 0; k < 8; ++k) asm volatile("" : "+v"(st.q[k]));
+    if (!wr.idle) tile_scores(st, tiles.k[0], lane);
+    next_phase();
+    int vb = 0;
+#pragma unroll 1
+    for (int k = 0; k < n; ++k) {
+      // vector phase
+      const int item = first + k;
+      if (item == n_new && !rotated) {
         rotate_tile_rows(st, lane);
         rotated = true;
       }
-      const int t0 = item < n_new ? (new_from + item) * kTileTokens : (win_from + item - n_new) * kTileTokens;
-      attend(tiles[buffer], (item < n_new ? total : len.nq) + t0, min((item < n_new ? T : len.nr) - t0, kTileTokens));
-      buffer ^= 1;
-      if (more) put(item + 1, tiles[buffer]);
-      barrier_lds();
+      int at, count;
+      if (item < raw) {
+        const int t0 = (item < n_new ? new_from + item : win_from + item - n_new) * kTileTokens;
+        at = (item < n_new ? total : len.nq) + t0;
+        count = min((item < n_new ? T : len.nr) - t0, kTileTokens);
+      } else {
+        at = half_of(item) * kTileTokens;
+        count = min(len.nq - at, kTileTokens);
+      }
+      const bool live = wave_sees(wr, a, at, count);
+      if (live) tile_weights(st, at, count, wave_masked(wr, a, at, count), wr.p, wr.low, a.sinks, lane);
+      if (to < n) put_next();
+      next_phase();
+      // matrix phase
+      if (live) {
+        tile_values(st, tiles.v[vb], lane);
+        tile_scores(st, tiles.k[(k + 1) & 1], lane);  // (of the last tile: what the other key tile held; not used)
+        matrix_order<32>();
+      } else if (!wr.idle) {
+        tile_scores(st, tiles.k[(k + 1) & 1], lane);
+        matrix_order<16>();
+      }
+      vb = vb == 2 ? 0 : vb + 1;
+      next_phase();
     }
+    if (!behind) next_phase();
   }
-  // ---- halves of groups ----
   // (partial results of splits are in the cache's basis; a sequence without a cache that is not split stays in the new rows')
   const bool in_cache_basis = total > 0 || a.splits > 1;
   if (in_cache_basis && !rotated) rotate_tile_rows(st, lane);
-  if (item < last) {
-    const int skip = n_new + n_win;
-    const int newest = SLIDING && len.nq % kGroup == 0 && len.nr < kGroup ? len.groups() - 1 : -1;
-    Packed<BITS> pk;
-    auto request = [&](int it) __attribute__((always_inline)) {
-      const int hf = half_of(it - skip);
-      load_packed<BITS>(pk, rec0 + (long long)(hf >> 1) * Rec<BITS>::kWords, hf & 1, tid);
-    };
-    auto put = [&](int it, Tiles& t) __attribute__((always_inline)) {
-      const int hf = half_of(it - skip);
-      store_packed<BITS>(pk, t, hf & 1, tid);
-      if (SLIDING && (hf >> 1) == newest) slide_values(t, v_win, hf & 1, len.nr, tid);
-    };
-    request(item);
-    put(item, tiles[buffer]);
-    barrier_lds();
-    for (; item < last; ++item) {
-      const bool more = item + 1 < last;
-      if (more) request(item + 1);
-      const int at = half_of(item - skip) * kTileTokens;
-      attend(tiles[buffer], at, min(len.nq - at, kTileTokens));
-      buffer ^= 1;
-      if (more) put(item + 1, tiles[buffer]);
-      barrier_lds();
-    }
-  }
-
-  // ---- results ----
-  if (idle) return;
-  {
-    float x, y;
-    pair_across<32>(st.l, x, y);
-    st.l = x + y;
-  }
-  const bool mine = wave_row + (lane & 31) < rows;
-  if (a.splits > 1) {
-    if (!mine) return;
-    float* dst = a.part + (place * a.splits + split) * kPartStride;
-    if (h == 0) { dst[0] = st.m; dst[1] = st.l; }
-#pragma unroll
-    for (int cb = 0; cb < 4; ++cb)
-#pragma unroll
-      for (int r = 0; r < 16; r += 4)
-        *reinterpret_cast<float4*>(dst + 4 + 32 * cb + 2 * r + 4 * h) = make_float4(st.acc[cb][r], st.acc[cb][r + 1], st.acc[cb][r + 2], st.acc[cb][r + 3]);
-    return;
-  }
-  if (a.corr != nullptr) {  // {C_d, -, -, -, C_n[128]}, as e^0 terms: both sides relative to max(m, 0)
-    const float* corr = a.corr + place * kPartStride;
-    const float to = fmaxf(st.m, 0.0f), f = __builtin_amdgcn_exp2f(st.m - to), w = __builtin_amdgcn_exp2f(-to);
-    st.l = fmaf(w, corr[0], st.l * f);
-#pragma unroll
-    for (int cb = 0; cb < 4; ++cb)
-#pragma unroll
-      for (int r = 0; r < 16; r += 4) {
-        const float4 v = *reinterpret_cast<const float4*>(corr + 4 + 32 * cb + 2 * r + 4 * h);
-        st.acc[cb][r] = fmaf(w, v.x, st.acc[cb][r] * f);
-        st.acc[cb][r + 1] = fmaf(w, v.y, st.acc[cb][r + 1] * f);
-        st.acc[cb][r + 2] = fmaf(w, v.z, st.acc[cb][r + 2] * f);
-        st.acc[cb][r + 3] = fmaf(w, v.w, st.acc[cb][r + 3] * f);
-      }
-  }
-  if (in_cache_basis) rotate_tile_rows(st, lane);
-  if (!mine) return;
-  const float inv = 1.0f / st.l;
-  half_t* dst = a.out + place * kHeadDim;
-#pragma unroll
-  for (int cb = 0; cb < 4; ++cb)
-#pragma unroll
-    for (int r = 0; r < 16; r += 4)
-      *reinterpret_cast<uint2*>(dst + 32 * cb + 2 * r + 4 * h) =
-          make_uint2(as_u32(pack_h2(st.acc[cb][r] * inv, st.acc[cb][r + 1] * inv)), as_u32(pack_h2(st.acc[cb][r + 2] * inv, st.acc[cb][r + 3] * inv)));
+  store_results(st, a, wr, split, in_cache_basis, lane);
 }
 
 }  // namespace

@@ -113,12 +113,36 @@ def test_static_caches_with_a_partial_group(keep, R, n, window):
     run_case(850, 8, 2, [n, n - 3], [5, 20], 2, window, 3, keep=keep, R=R)
 
 
-@pytest.mark.parametrize("T", [3, 40])
+@pytest.mark.parametrize("bits", [2, 4])
+@pytest.mark.parametrize("n, T", [(0, 129), (0, 300), (1, 130), (128, 200), (300, 129), (1000, 260)])
+def test_more_rows_than_a_few_blocks(n, T, bits):
+    run_case(855, 8, 1, [n], [T], bits)
+
+
+@pytest.mark.parametrize("window, sinks", [(1, 0), (1, 1), (30, 3), (64, 64), (100, 5), (129, 130), (200, 1000), (5000, 4), (700, 0)])
+def test_windows_of_many_rows(window, sinks):
+    run_case(856, 7, 1, [900, 40, 0, 300], [160, 170, 33, 147], 2, window, sinks)
+
+
+@pytest.mark.parametrize("bits, corr, sliding", [(2, True, False), (4, True, False), (2, False, True), (4, False, True)])
+def test_variants_of_many_rows(bits, corr, sliding):
+    run_case(857, 8, 1, [700, 100, 0, 257], [150, 131, 129, 4], bits, corr=corr, sliding=sliding)
+
+
+def test_single_heads_and_many_rows():
+    run_case(858, 2, 2, [300, 129], [1100, 1030])
+
+
+@pytest.mark.parametrize("keep, R, n", [(32, 32, 100), (60, 64, 513)])
+def test_static_caches_and_many_rows(keep, R, n):
+    run_case(859, 8, 1, [n, n - 3], [150, 140], 2, 90, 3, keep=keep, R=R)
+
+
+@pytest.mark.parametrize("T", [3, 40, 300])
 def test_large_and_small_scores(T):
     # scores of some hundreds and next to none: the reference of a row moves by more than its head room, or not at all
-    run_case(860, 4, 2, [400], [T], scale=32.0)
-    run_case(860, 4, 2, [400], [T], scale=2.0 ** -12)
-    run_case(860, 4, 2, [400], [T], scale=0.0)
+    for scale in (32.0, 2.0 ** -12, 0.0):
+        run_case(860, 8, 2, [400], [T], scale=scale)
 
 
 @pytest.mark.parametrize("bound", [0, 5000, 2000])
