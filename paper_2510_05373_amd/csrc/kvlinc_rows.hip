@@ -27,42 +27,52 @@ constexpr int kRawTokens = 32;
 // The reference of a row is its largest score less kHeadroom when it is set, and is set anew when a score passes it by kHeadroom + kLag
 // (most blocks only compare): weights stay below 2^13, and p s with s < 2 below binary16's largest number.
 constexpr float kHeadroom = 8.0f, kLag = 5.0f;
+constexpr float kFusedBound = 0x1p20f;
 
 __device__ __forceinline__ int token_order(int i) { return 8 * ((i >> 2) & 1) + 2 * (i >> 3) + (i & 1) + 4 * ((i >> 1) & 1); }
 
 template <int BITS>
 struct Record {
-  uint4 kw[2 * BITS];  // key words: kw[4 plane + m] = token blocks 2 m (x, y) and 2 m + 1 (z, w)
-  uint4 ks[4], kz[4];  // key scale and zero-point of channels 32 g .. 32 g + 31
-  uint4 vw[2 * BITS];  // value words: channel blocks 2 m and 2 m + 1
-  uint4 sz[8];         // (scale, zero-point) of tokens 16 n + pi(4 g + r): sz[2 r], sz[2 r + 1] = n = 0..3, 4..7
+  u32x4_t kw[2 * BITS];  // key words: kw[4 plane + m] = token blocks 2 m (x, y) and 2 m + 1 (z, w)
+  u32x4_t vw[2 * BITS];  // value words: channel blocks 2 m and 2 m + 1
+  u32x4_t meta;          // 16 bytes of the record's 1 KB of scales and zero-points
 };
-__device__ __forceinline__ uint4 load_streamed(const uint4* p) {
-  const u32x4_t t = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(p));
-  return make_uint4(t[0], t[1], t[2], t[3]);
-}
 template <int BITS>
 __device__ __forceinline__ void load_key_part(Record<BITS>& r, const uint32_t* rec, int lane) {
-  const uint4* kt = reinterpret_cast<const uint4*>(rec + Rec<BITS>::kKeyTile) + token_order(lane & 15) + (lane & 48);
+  const u32x4_t* kt = reinterpret_cast<const u32x4_t*>(rec + Rec<BITS>::kKeyTile) + token_order(lane & 15) + (lane & 48);
 #pragma unroll
-  for (int m = 0; m < 2 * BITS; ++m) r.kw[m] = load_streamed(kt + 64 * m);
-  const uint4* s = reinterpret_cast<const uint4*>(rec + Rec<BITS>::kKeyScale) + 4 * (lane >> 4);
-  const uint4* z = reinterpret_cast<const uint4*>(rec + Rec<BITS>::kKeyZero) + 4 * (lane >> 4);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) { r.ks[i] = s[i]; r.kz[i] = z[i]; }
+  for (int m = 0; m < 2 * BITS; ++m) r.kw[m] = __builtin_nontemporal_load(kt + 64 * m);
+  r.meta = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(rec + Rec<BITS>::kKeyScale) + lane);
 }
 template <int BITS>
 __device__ __forceinline__ void load_value_part(Record<BITS>& r, const uint32_t* rec, int lane) {
-  const uint4* vt = reinterpret_cast<const uint4*>(rec + Rec<BITS>::kValueTile) + lane;
+  const u32x4_t* vt = reinterpret_cast<const u32x4_t*>(rec + Rec<BITS>::kValueTile) + lane;
 #pragma unroll
-  for (int m = 0; m < 2 * BITS; ++m) r.vw[m] = load_streamed(vt + 64 * m);
-  const uint4* sz = reinterpret_cast<const uint4*>(rec + Rec<BITS>::kValueSZ);
+  for (int m = 0; m < 2 * BITS; ++m) r.vw[m] = __builtin_nontemporal_load(vt + 64 * m);
+}
+static_assert(Rec<2>::kKeyZero == Rec<2>::kKeyScale + 64 && Rec<2>::kValueSZ == Rec<2>::kKeyScale + 128 && Rec<2>::kWords == Rec<2>::kKeyScale + 256, "256 words");
+
+// A wave's copy of a group's scales and zero-points in LDS: [0..15] key scales, [16..31] key zero-points, 8 channels each; [32 + 2 t + u]
+// value (scale, zero-point) of tokens 16 (4 u + i) + t, i = 0..3.  The exponent of the group's largest value scale is taken out of them on
+// the way (it goes to the codes, exactly: weight times scale then stays in binary16's range whatever the values' magnitude) and returned.
+template <int BITS>
+__device__ __forceinline__ int put_meta(const Record<BITS>& r, u32x4_t* meta, int lane) {
+  uint32_t top = 0;  // scales are not negative: their bit patterns order like the numbers
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int t = token_order(4 * (lane >> 4) + i);
-    r.sz[2 * i] = sz[2 * t];
-    r.sz[2 * i + 1] = sz[2 * t + 1];
-  }
+  for (int i = 0; i < 4; ++i) top = max(top, r.meta[i] & 0xffffu);
+  top = lane >= 32 ? top : 0u;
+  top = max(top, dpp_u<kRowRor1>(top));
+  top = max(top, dpp_u<kRowRor2>(top));
+  top = max(top, dpp_u<kRowRor4>(top));
+  top = max(top, dpp_u<kRowRor8>(top));
+  const int e = (int)(max(max(__builtin_amdgcn_readlane(top, 32), __builtin_amdgcn_readlane(top, 48)) >> 10, 3u)) - 15;  // -12 .. 15: the codes times 2^e are normal numbers
+  const half2_t unscale = {(half_t)(lane >= 32 ? bits_f32((uint32_t)(127 - e) << 23) : 1.0f), (half_t)1.0f};
+  u32x4_t w;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = as_u32(as_h2(r.meta[i]) * unscale);
+  meta[lane] = w;
+  __builtin_amdgcn_wave_barrier();  // (a wave's LDS instructions stay in order)
+  return e;
 }
 
 template <int NR>
@@ -122,43 +132,48 @@ __device__ __forceinline__ void window_values(Rows<NR>& st, const half_t* v_win,
 #pragma unroll
       for (int k = 0; k < NR; ++k) st.acc[k][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(V, P[k], st.acc[k][n], 0, 0, 0);
     }
+    asm volatile("" ::: "memory");  // (the next blocks' loads stay behind these products: all at once they spilled)
   }
 }
 
 // One group of 128 packed tokens, the first at position `at`, `count` of them there.  masked: some row does not see all of them.
 // SLIDING: tokens from fp16_from on take their values from the window.
-template <int BITS, int NR, bool SLIDING>
-__device__ __forceinline__ void group_scores(Rows<NR>& st, const Record<BITS>& rec, int at, int count, bool masked, int sinks, int lane,
-                                             float (&x)[NR][8][4]) {
-  const uint32_t S[16] = {rec.ks[0].x, rec.ks[0].y, rec.ks[0].z, rec.ks[0].w, rec.ks[1].x, rec.ks[1].y, rec.ks[1].z, rec.ks[1].w,
-                          rec.ks[2].x, rec.ks[2].y, rec.ks[2].z, rec.ks[2].w, rec.ks[3].x, rec.ks[3].y, rec.ks[3].z, rec.ks[3].w};
-  const uint32_t Z[16] = {rec.kz[0].x, rec.kz[0].y, rec.kz[0].z, rec.kz[0].w, rec.kz[1].x, rec.kz[1].y, rec.kz[1].z, rec.kz[1].w,
-                          rec.kz[2].x, rec.kz[2].y, rec.kz[2].z, rec.kz[2].w, rec.kz[3].x, rec.kz[3].y, rec.kz[3].z, rec.kz[3].w};
+template <int BITS, int NR>
+__device__ __forceinline__ void group_scores(Rows<NR>& st, const Record<BITS>& rec, const u32x4_t* meta, int at, int count, bool masked, int sinks,
+                                             int lane, float (&x)[NR][8][4], float (&base)[NR]) {
   half8_t hi[NR][4], lo[NR][4];
   float bias[NR];
+  {
+    float bz[NR], bs[NR];
 #pragma unroll
-  for (int k = 0; k < NR; ++k) {
-    float bz = 0.0f, bs = 0.0f;
+    for (int k = 0; k < NR; ++k) bz[k] = bs[k] = 0.0f;
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
-      const u32x4_t qq = __builtin_bit_cast(u32x4_t, st.q[k][s]);
-      uint32_t h[4], r[4];
+      const u32x4_t S = meta[4 * (lane >> 4) + s], Z = meta[16 + 4 * (lane >> 4) + s];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const half2_t a = as_h2(qq[i]), sc = as_h2(S[4 * s + i]);
-        const half2_t t = a * sc;
-        h[i] = as_u32(t);
-        r[i] = as_u32(__builtin_elementwise_fma(a, sc, -t));
-        bz = __builtin_amdgcn_fdot2(a, as_h2(Z[4 * s + i]), bz, false);
-        bs = __builtin_amdgcn_fdot2(a, sc, bs, false);
+      for (int k = 0; k < NR; ++k) {
+        const u32x4_t qq = __builtin_bit_cast(u32x4_t, st.q[k][s]);
+        u32x4_t h, r;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const half2_t a = as_h2(qq[i]), sc = as_h2(S[i]);
+          const half2_t t = a * sc;
+          h[i] = as_u32(t);
+          r[i] = as_u32(__builtin_elementwise_fma(a, sc, -t));
+          bz[k] = __builtin_amdgcn_fdot2(a, as_h2(Z[i]), bz[k], false);
+          bs[k] = __builtin_amdgcn_fdot2(a, sc, bs[k], false);
+        }
+        hi[k][s] = as_h8(h);
+        lo[k][s] = as_h8(r);
       }
-      hi[k][s] = as_h8(make_uint4(h[0], h[1], h[2], h[3]));
-      lo[k][s] = as_h8(make_uint4(r[0], r[1], r[2], r[3]));
     }
-    float v = fmaf(bs, Rec<BITS>::kCentre, bz), a, b;
-    pair_across<16>(v, a, b);
-    pair_across<32>(a + b, a, b);
-    bias[k] = (a + b) * st.unit[k];
+#pragma unroll
+    for (int k = 0; k < NR; ++k) {
+      float a, b;
+      pair_across<16>(fmaf(bs[k], Rec<BITS>::kCentre, bz[k]), a, b);
+      pair_across<32>(a + b, a, b);
+      bias[k] = (a + b) * st.unit[k];
+    }
   }
 #pragma unroll
   for (int m = 0; m < 4; ++m)
@@ -167,15 +182,12 @@ __device__ __forceinline__ void group_scores(Rows<NR>& st, const Record<BITS>& r
       half8_t A[4];
 #pragma unroll
       for (int w = 0; w < 2; ++w) {
-        Nibbles nb[BITS / 2];
-#pragma unroll
-        for (int pl = 0; pl < BITS / 2; ++pl) {
-          const uint4 t = rec.kw[4 * pl + m];
-          nb[pl] = nibbles_of(hf == 0 ? (w == 0 ? t.x : t.y) : (w == 0 ? t.z : t.w));
-        }
         uint32_t e[BITS / 2], o[BITS / 2];
 #pragma unroll
-        for (int pl = 0; pl < BITS / 2; ++pl) { e[pl] = nb[pl].first; o[pl] = nb[pl].second; }
+        for (int pl = 0; pl < BITS / 2; ++pl) {
+          const Nibbles nb = nibbles_of(rec.kw[4 * pl + m][2 * hf + w]);
+          e[pl] = nb.first; o[pl] = nb.second;
+        }
         A[2 * w] = as_h8(code_pair<BITS, 0>(e, 1.0f), code_pair<BITS, 1>(e, 1.0f), code_pair<BITS, 2>(e, 1.0f), code_pair<BITS, 3>(e, 1.0f));
         A[2 * w + 1] = as_h8(code_pair<BITS, 0>(o, 1.0f), code_pair<BITS, 1>(o, 1.0f), code_pair<BITS, 2>(o, 1.0f), code_pair<BITS, 3>(o, 1.0f));
       }
@@ -187,19 +199,21 @@ __device__ __forceinline__ void group_scores(Rows<NR>& st, const Record<BITS>& r
 #pragma unroll
         for (int s = 0; s < 4; ++s) d = __builtin_amdgcn_mfma_f32_16x16x32_f16(A[s], hi[k][s], d, 0, 0, 0);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) x[k][2 * m + hf][r] = fmaf(d[r], st.unit[k], bias[k]);
+        for (int r = 0; r < 4; ++r) x[k][2 * m + hf][r] = d[r];
       }
     }
   if (masked) {
 #pragma unroll
-    for (int n = 0; n < 8; ++n)
+    for (int k = 0; k < NR; ++k) {
+      const int end = min(count, st.p[k] - at + 1), from = st.low[k] - at, first = sinks - at;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int t = 16 * n + token_order(4 * (lane >> 4) + r);
+      for (int n = 0; n < 8; ++n)
 #pragma unroll
-        for (int k = 0; k < NR; ++k)
-          if (!seen(t, at, count, st.p[k], st.low[k], sinks)) x[k][n][r] = -INFINITY;
-      }
+        for (int r = 0; r < 4; ++r) {
+          const int t = 16 * n + token_order(4 * (lane >> 4) + r);
+          x[k][n][r] = (t < end) & ((t >= from) | (t < first)) ? x[k][n][r] : -INFINITY;
+        }
+    }
   }
 #pragma unroll
   for (int k = 0; k < NR; ++k) {
@@ -208,67 +222,64 @@ __device__ __forceinline__ void group_scores(Rows<NR>& st, const Record<BITS>& r
     for (int n = 0; n < 8; ++n)
 #pragma unroll
       for (int r = 0; r < 4; ++r) mx = fmaxf(mx, x[k][n][r]);
-    set_reference<NR>(st, k, mx);
+    set_reference<NR>(st, k, fmaf(mx, st.unit[k], bias[k]));
+    const float m = finite_reference(st.m[k]);
+    base[k] = bias[k] - m;
+    // References and biases thousands beyond what ordinary keys and queries give: the exponents are rounded as the reference was (the
+    // score itself, then its distance from the reference), or the exponent of the largest weight would be what the roundings leave.
+    if (__builtin_amdgcn_ballot_w64(fmaxf(fabsf(m), fabsf(bias[k])) > kFusedBound) != 0) {
+#pragma clang fp contract(off)
+      const float back = 1.0f / st.unit[k];
+#pragma unroll
+      for (int n = 0; n < 8; ++n)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) x[k][n][r] = (__builtin_fmaf(x[k][n][r], st.unit[k], bias[k]) - m) * back;
+      base[k] = 0.0f;
+    }
   }
 }
 
+// Scores become weights; O^T += V^T P^T of the group.  e: see put_meta.
 template <int BITS, int NR, bool SLIDING>
-__device__ __forceinline__ void group_values(Rows<NR>& st, const Record<BITS>& rec, float (&x)[NR][8][4], int fp16_from, const half_t* v_win,
-                                             int quads, int lane) {
-  // Value scales by token block, with the exponent of the largest of the group taken out (it goes to the codes, exactly): weight times
-  // scale stays in binary16's range whatever the values' magnitude.
-  uint32_t sz[8][4];
+__device__ __forceinline__ void group_values(Rows<NR>& st, const Record<BITS>& rec, const u32x4_t* meta, int e, float (&x)[NR][8][4], const float (&base)[NR],
+                                             int fp16_from, const half_t* v_win, int quads, int lane) {
+  const float scale = bits_f32((uint32_t)(127 + e) << 23);
+  half8_t P[NR][4];
+  float l[NR], ys[NR], zs[NR];
+#pragma unroll
+  for (int k = 0; k < NR; ++k) l[k] = ys[k] = zs[k] = 0.0f;
+  const half2_t ones = {(half_t)1.0f, (half_t)1.0f};
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
-    const uint4 a = rec.sz[2 * r], b = rec.sz[2 * r + 1];
-    sz[0][r] = a.x; sz[1][r] = a.y; sz[2][r] = a.z; sz[3][r] = a.w;
-    sz[4][r] = b.x; sz[5][r] = b.y; sz[6][r] = b.z; sz[7][r] = b.w;
-  }
-  uint32_t top = 0;  // scales are not negative: their bit patterns order like the numbers
+    const int t = token_order(4 * (lane >> 4) + r);
+    const u32x4_t z0 = meta[32 + 2 * t], z1 = meta[33 + 2 * t];
 #pragma unroll
-  for (int n = 0; n < 8; ++n)
+    for (int k = 0; k < NR; ++k)
 #pragma unroll
-    for (int r = 0; r < 4; ++r) top = max(top, sz[n][r] & 0xffffu);
-  {
-    const auto a = __builtin_amdgcn_permlane16_swap(top, top, false, false);
-    top = max(a[0], a[1]);
-    const auto b = __builtin_amdgcn_permlane32_swap(top, top, false, false);
-    top = max(b[0], b[1]);
-  }
-  const int e = (int)__builtin_amdgcn_readfirstlane(max(top >> 10, 3u)) - 15;  // -12 .. 15: the codes times 2^e are normal binary16 numbers
-  const float scale = bits_f32((uint32_t)(127 + e) << 23), unscale = bits_f32((uint32_t)(127 - e) << 23);
-  half8_t P[NR][4];
-#pragma unroll
-  for (int k = 0; k < NR; ++k) {
-    const float m = finite_reference(st.m[k]);
-    float l = 0.0f, ys = 0.0f, zs = 0.0f;
-#pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      uint32_t w[4];
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
+      for (int s = 0; s < 4; ++s) {
         float y[2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
           const int n = 2 * s + u;
-          const float p = __builtin_amdgcn_exp2f(x[k][n][r] - m);
-          x[k][n][r] = p;
-          l += p;
-          const half2_t t = as_h2(sz[n][r]);
-          float yy = p * ((float)t[0] * unscale), zz = (float)t[1];
-          bool coded = true;
-          if (SLIDING) coded = 16 * n + token_order(4 * (lane >> 4) + r) < fp16_from;
-          yy = coded ? yy : 0.0f;
-          y[u] = yy;
-          ys += yy;
-          zs = coded ? fmaf(p, zz, zs) : zs;
+          const half2_t sz = as_h2(n < 4 ? z0[n] : z1[n - 4]);
+          const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[k][n][r], st.unit[k], base[k]));
+          if (SLIDING) x[k][n][r] = p;
+          l[k] += p;
+          float yy = __builtin_fmaf(p, (float)sz[0], 0.0f);
+          const bool coded = !SLIDING || 16 * n + t < fp16_from;
+          y[u] = coded ? yy : 0.0f;
+          zs[k] = coded ? __builtin_fmaf(p, (float)sz[1], zs[k]) : zs[k];
         }
-        w[r] = as_u32(pack_h2(y[0], y[1]));
+        const half2_t w = pack_h2(y[0], y[1]);
+        ys[k] = __builtin_amdgcn_fdot2(w, ones, ys[k], false);
+        P[k][s][2 * r] = w[0];
+        P[k][s][2 * r + 1] = w[1];
       }
-      P[k][s] = as_h8(make_uint4(w[0], w[1], w[2], w[3]));
-    }
-    st.l[k] += l;
-    st.mid[k] += fmaf(ys * scale, Rec<BITS>::kCentre, zs);
+  }
+#pragma unroll
+  for (int k = 0; k < NR; ++k) {
+    st.l[k] += l[k];
+    st.mid[k] += fmaf(ys[k] * scale, Rec<BITS>::kCentre, zs[k]);
   }
 #pragma unroll
   for (int m = 0; m < 4; ++m)
@@ -277,8 +288,7 @@ __device__ __forceinline__ void group_values(Rows<NR>& st, const Record<BITS>& r
       uint32_t e0[BITS / 2], o0[BITS / 2], e1[BITS / 2], o1[BITS / 2];
 #pragma unroll
       for (int pl = 0; pl < BITS / 2; ++pl) {
-        const uint4 t = rec.vw[4 * pl + m];
-        const Nibbles a = nibbles_of(hf == 0 ? t.x : t.z), b = nibbles_of(hf == 0 ? t.y : t.w);
+        const Nibbles a = nibbles_of(rec.vw[4 * pl + m][2 * hf]), b = nibbles_of(rec.vw[4 * pl + m][2 * hf + 1]);
         e0[pl] = a.first; o0[pl] = a.second; e1[pl] = b.first; o1[pl] = b.second;
       }
       half8_t V[4];
@@ -428,6 +438,7 @@ __device__ __forceinline__ RowPlace row_place(int row, int gq) {
 // token at position total - 1.
 template <int BITS, int NR, bool PROMPT, bool SLIDING>
 __global__ __launch_bounds__(64 * kRowWaves, 2) void rows_kernel(ContextCall a) {
+  __shared__ __align__(16) u32x4_t sMeta[kRowWaves][64];
   const kvlinc_cache& c = a.cache;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4;
   const int pairs = c.B * c.H_kv, unit = blockIdx.x / a.splits, split = blockIdx.x - unit * a.splits;
@@ -520,13 +531,13 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void rows_kernel(ContextCall a) 
     load_value_part<BITS>(rec, rec0 + (long long)gr * Rec<BITS>::kWords, lane);
     for (;;) {
       const int at = gr * kGroup, count = min(len.nq - at, kGroup);
-      const bool masked = count < kGroup || (at < low_last && at + kGroup > a.sinks);
-      float x[NR][8][4];
-      group_scores<BITS, NR, SLIDING>(st, rec, at, count, masked, a.sinks, lane, x);
-      const int next = item + step < n_groups ? group_of(item + step) : gr;
-      const bool more = item + step < n_groups;
+      const bool masked = count < kGroup || (at < low_last && at + kGroup > a.sinks), more = item + step < n_groups;
+      const int e = put_meta<BITS>(rec, sMeta[wave], lane);
+      float x[NR][8][4], exponent_base[NR];
+      group_scores<BITS, NR>(st, rec, sMeta[wave], at, count, masked, a.sinks, lane, x, exponent_base);
+      const int next = more ? group_of(item + step) : gr;
       if (more) load_key_part<BITS>(rec, rec0 + (long long)next * Rec<BITS>::kWords, lane);
-      group_values<BITS, NR, SLIDING>(st, rec, x, gr == newest ? len.nr : kGroup, v_win, quads, lane);
+      group_values<BITS, NR, SLIDING>(st, rec, sMeta[wave], e, x, exponent_base, gr == newest ? len.nr : kGroup, v_win, quads, lane);
       if (!more) break;
       load_value_part<BITS>(rec, rec0 + (long long)next * Rec<BITS>::kWords, lane);
       item += step;
