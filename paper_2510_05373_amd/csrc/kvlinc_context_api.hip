@@ -12,7 +12,7 @@ inline bool bad_address(const void* p, uintptr_t a) { return p == nullptr || (re
 struct ContextPlan {
   // 16 rows a wave (kvlinc_rows.hip); blocks of 256 rows over tiles of codes (kvlinc_prompt.hip), or of rows dequantized first (kvlinc_dense.hip)
   enum Kind { kRows, kTiles, kDense } kind;
-  int splits;
+  int splits, waves;
   long long cached_rows, sink_rows;      // dequantized rows of a (sequence, KV head)
   int row_window;                        // see ContextCall
   size_t corr_floats, part_floats, row_halfs;  // row_halfs: of keys, and as many of values
@@ -38,8 +38,10 @@ ContextPlan plan_call(const kvlinc_cache& c, int T, int window, int sinks, int m
   p.kind = rows <= kFewRows ? ContextPlan::kRows : rows < kDenseRows ? ContextPlan::kTiles : ContextPlan::kDense;
   long long s, most;
   if (p.kind == ContextPlan::kRows) {
-    s = 512 / (pairs * ((rows + 15) / 16));
-    most = (groups + 3) / 4;
+    // Two workgroups of four waves a compute unit, or, where the pairs are few, one of eight: fewer splits to join.
+    p.waves = pairs <= 64 ? 8 : 4;
+    s = (p.waves == 8 ? 256 : 512) / pairs;
+    most = (groups + p.waves - 1) / p.waves;
   } else {
     s = 256 / (pairs * ((rows + 255) / 256));
     most = (groups + 1) / 2;
@@ -50,7 +52,7 @@ ContextPlan plan_call(const kvlinc_cache& c, int T, int window, int sinks, int m
   p.splits = (int)s;
   const size_t places = (size_t)c.B * c.H_q * T;
   p.corr_floats = c.S16 != nullptr ? places * kPartStride : 0;
-  p.part_floats = s > 1 ? places * s * kPartStride : 0;
+  p.part_floats = s > 1 || (p.kind == ContextPlan::kRows && p.corr_floats != 0) ? places * s * kPartStride : 0;
   if (p.kind == ContextPlan::kDense) {
     // all cached tokens; or those near the first row, and the sinks ahead of them where there can be such
     const long long cap = (long long)c.max_groups * kGroup + c.R, ctx = max_context > 0 && max_context < cap ? max_context : cap;
@@ -133,11 +135,12 @@ int kvlinc_prompt_attention(const kvlinc_cache* cache, const kvlinc_half* q, con
   a.v_new = reinterpret_cast<const _Float16*>(v_new);
   a.n_new = n_new;
   const hipStream_t s = static_cast<hipStream_t>(stream);
+  if (p.kind == ContextPlan::kRows) return launch_rows(a, p.waves, s);
   if (a.corr != nullptr) {
     const int rl = launch_prompt_correction(a, s);
     if (rl != KVLINC_OK) return rl;
   }
-  return p.kind == ContextPlan::kRows ? launch_rows(a, true, s) : p.kind == ContextPlan::kTiles ? launch_tiles(a, s) : launch_dense(a, s);
+  return p.kind == ContextPlan::kTiles ? launch_tiles(a, s) : launch_dense(a, s);
 }
 
 size_t kvlinc_decode_windowed_workspace_bytes(const kvlinc_cache* cache, int32_t window, int32_t sinks, int32_t max_context) {
@@ -151,7 +154,7 @@ int kvlinc_decode_attention_windowed(const kvlinc_cache* cache, const kvlinc_hal
   if (bad_address(q, 16) || bad_address(out, 16)) return KVLINC_EINVAL;
   const ContextPlan p = plan_call(*cache, 1, window, sinks, max_context);
   if (bad_workspace(workspace, workspace_bytes, p.bytes())) return KVLINC_EWORKSPACE;
-  return launch_rows(make_call(*cache, q, 1, window, sinks, out, workspace, p), false, static_cast<hipStream_t>(stream));
+  return launch_rows(make_call(*cache, q, 1, window, sinks, out, workspace, p), p.waves, static_cast<hipStream_t>(stream));
 }
 
 int kvlinc_cache_read(const kvlinc_cache* cache, const int32_t* first, int32_t T, void* k_out, void* v_out, int32_t dtype,

@@ -31,10 +31,10 @@ __host__ __device__ inline int window_base(int total, int window) {
   return low & ~(kTileTokens - 1);
 }
 
-int launch_rows(const ContextCall& a, bool prompt, hipStream_t stream);
+int launch_rows(const ContextCall& a, int waves, hipStream_t stream);  // up to 64 rows of a KV head; waves of a workgroup: 4 or 8
 int launch_tiles(const ContextCall& a, hipStream_t stream);
 int launch_dense(const ContextCall& a, hipStream_t stream);
-int launch_join(const ContextCall& a, bool prompt, hipStream_t stream);
+int launch_join(const ContextCall& a, hipStream_t stream);
 int launch_prompt_correction(const ContextCall& a, hipStream_t stream);
 int launch_read(const kvlinc_cache& c, const int32_t* first, int T, void* k_out, void* v_out, int dtype, bool rotated, hipStream_t stream);
 

@@ -214,7 +214,7 @@ int launch_dense(const ContextCall& a, hipStream_t stream) {
   const dim3 grid((unsigned)((long long)blocks * a.cache.B * a.cache.H_kv * a.splits));
   hipLaunchKernelGGL(dense_kernel, grid, dim3(kTileThreads), 0, stream, a, blocks);
   if (hipGetLastError() != hipSuccess) return KVLINC_EHIP;
-  return a.splits > 1 ? launch_join(a, true, stream) : KVLINC_OK;
+  return a.splits > 1 ? launch_join(a, stream) : KVLINC_OK;
 }
 
 }  // namespace kvlinc

@@ -337,7 +337,7 @@ int launch_tiles(const ContextCall& a, hipStream_t stream) {
   void (*kernel)(ContextCall, int) = a.cache.bits == 2 ? (sliding ? tile_kernel<2, true> : tile_kernel<2, false>) : (sliding ? tile_kernel<4, true> : tile_kernel<4, false>);
   hipLaunchKernelGGL(kernel, grid, dim3(kTileThreads), 0, stream, a, blocks);
   if (hipGetLastError() != hipSuccess) return KVLINC_EHIP;
-  return a.splits > 1 ? launch_join(a, true, stream) : KVLINC_OK;
+  return a.splits > 1 ? launch_join(a, stream) : KVLINC_OK;
 }
 
 }  // namespace kvlinc

@@ -1,8 +1,9 @@
-// Attention of few query rows, or of one query a sequence behind a sliding window, read directly from the packed cache.
+// Attention of few query rows (up to 64 of a KV head), or of one query a sequence behind a sliding window, read directly from the packed cache.
 //
-// Rows of a (sequence, KV head) are (token i, head h) pairs, row = i gq + h.  A wave takes blocks of tokens on its own, without a
-// barrier: groups of 128 packed tokens, or 32 raw ones (the cache's window, the new rows), and keeps a running maximum, sum and numerator
-// of its 16 NR rows; the workgroup's four waves are joined through LDS, the splits of a context through memory.
+// One launch.  Rows of a (sequence, KV head) are (token i, head h) pairs, row = i gq + h.  A workgroup has all rows of one and a split of its
+// tokens; a wave takes a block of 16 rows and blocks of tokens on its own, without a barrier: groups of 128 packed tokens, or 32 raw ones (the
+// cache's window, the new rows), and keeps a running maximum, sum and numerator.  The waves are joined through LDS, the splits and the
+// correction (a workgroup of its own, ahead of the others in the grid) through memory, by whoever arrives last at the counter of the pair.
 //
 // Both products run on v_mfma_f32_16x16x32_f16, transposed: S^T = K Q^T (rows = tokens, columns = query rows) and
 // O^T = V^T P^T (rows = channels, columns = query rows), so that a lane holds one query row, lane % 16, throughout, and the weights it
@@ -22,13 +23,16 @@
 namespace kvlinc {
 namespace {
 
-constexpr int kRowWaves = 4;
+constexpr int kMaxWaves = 8;
 constexpr int kRawTokens = 32;
 // The reference of a row is its largest score less kHeadroom when it is set, and is set anew when a score passes it by kHeadroom + kLag
 // (most blocks only compare): weights stay below 2^13, and p s with s < 2 below binary16's largest number.
 constexpr float kHeadroom = 8.0f, kLag = 5.0f;
 constexpr float kFusedBound = 0x1p20f;
 
+// Columns of the products: 16 rows of queries; or, of up to 8 or 4 rows, each row S = 2 or 4 times, column c with row c % (16 / S) and subset
+// c / (16 / S): the softmax of a column is then over the 16-token blocks n with n / (8 / S) = subset only, and a lane has 8 / S blocks' scores to
+// work on instead of 8.
 __device__ __forceinline__ int token_order(int i) { return 8 * ((i >> 2) & 1) + 2 * (i >> 3) + (i & 1) + 4 * ((i >> 1) & 1); }
 
 template <int BITS>
@@ -75,32 +79,15 @@ __device__ __forceinline__ int put_meta(const Record<BITS>& r, u32x4_t* meta, in
   return e;
 }
 
-template <int NR>
 struct Rows {
-  half8_t q[NR][4];       // query of this lane's row, channels 32 g + 8 step .. + 7, times 2^-e (largest magnitude in [1/2, 1))
-  float unit[NR];         // 2^e log2(e) / sqrt(d)
-  int p[NR], low[NR];     // position, first token of its window
-  float m[NR];            // reference (the same in the four lanes of a row), log2 domain; -inf: nothing seen yet
-  float l[NR], mid[NR];   // per-lane sums of the weights, and of weight times (zero-point + centre scale): the same for all channels
-  float4_t acc[NR][8];    // numerator of channels 16 n + 4 g + 0..3
+  half8_t q[4];       // query of this lane's row, channels 32 g + 8 step .. + 7, times 2^-e (largest magnitude in [1/2, 1))
+  float unit;      // 2^e log2(e) / sqrt(d)
+  int p, low;      // position, first token of its window
+  int subset;
+  float m;         // reference (the same in the four lanes of a column), log2 domain; -inf: nothing seen yet
+  float l, mid;    // per-lane sums of the weights, and of weight times (zero-point + centre scale): the same for all channels
+  float4_t acc[8]; // numerator of channels 16 n + 4 g + 0..3
 };
-
-template <int NR>
-__device__ __forceinline__ void set_reference(Rows<NR>& st, int k, float largest) {  // largest: of this lane's scores
-  if (__builtin_amdgcn_ballot_w64(largest > st.m[k] + (kHeadroom + kLag)) == 0) return;
-  float x, y;
-  pair_across<16>(largest, x, y);
-  pair_across<32>(fmaxf(x, y), x, y);
-  const float mx = fmaxf(x, y);
-  const float to = mx > st.m[k] + (kHeadroom + kLag) ? mx - kHeadroom : st.m[k];
-  const float f = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(st.m[k] - to);  // (0 where nothing was seen)
-  st.m[k] = to;
-  st.l[k] *= f;
-  st.mid[k] *= f;
-#pragma unroll
-  for (int n = 0; n < 8; ++n) st.acc[k][n] *= f;
-}
-__device__ __forceinline__ float finite_reference(float m) { return m == -INFINITY ? 0.0f : m; }
 
 // Token of register r, block n of the tile whose first token is `at`, or -1 beyond its `count` tokens; and whether a row sees it.
 __device__ __forceinline__ bool seen(int t, int at, int count, int p, int low, int sinks) {
@@ -108,258 +95,244 @@ __device__ __forceinline__ bool seen(int t, int at, int count, int p, int low, i
   return t < count && pos <= p && (pos >= low || pos < sinks);
 }
 
-// O^T += V^T P^T with the window's fp16 values of 16-token blocks first .. first + 2 count - 1 (two a product), weights w[n][r] by block.
+__device__ __forceinline__ void set_reference(Rows& st, float largest) {  // largest: of this lane's scores
+  if (__builtin_amdgcn_ballot_w64(largest > st.m + (kHeadroom + kLag)) == 0) return;
+  float x, y;
+  pair_across<16>(largest, x, y);
+  pair_across<32>(fmaxf(x, y), x, y);
+  const float mx = fmaxf(x, y);
+  const float to = mx > st.m + (kHeadroom + kLag) ? mx - kHeadroom : st.m;
+  const float f = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(st.m - to);  // (0 where nothing was seen)
+  st.m = to;
+  st.l *= f;
+  st.mid *= f;
+#pragma unroll
+  for (int n = 0; n < 8; ++n) st.acc[n] *= f;
+}
+__device__ __forceinline__ float finite_reference(float m) { return m == -INFINITY ? 0.0f : m; }
+
+// O^T += V^T P^T with the window's fp16 values of the 16-token blocks first .. first + NB - 1 (two a product), weights w[n][r] by block.
 // v_res is [slot / 4][channel][slot % 4]: a lane takes two neighbouring slots at a time.
-template <int NR, int NB>
-__device__ __forceinline__ void window_values(Rows<NR>& st, const half_t* v_win, int quads, int first, const float (&w)[NR][NB][4], int lane) {
+template <int NB>
+__device__ __forceinline__ void window_values(Rows& st, const half_t* v_win, int quads, int first, const float (&w)[NB][4], int lane) {
   const int g = lane >> 4, a = 8 * (g & 1) + 2 * (g >> 1);
 #pragma unroll
   for (int s = 0; s < NB / 2; ++s) {
-    half8_t P[NR];
-#pragma unroll
-    for (int k = 0; k < NR; ++k)
-      P[k] = as_h8(pack_h2(w[k][2 * s][0], w[k][2 * s][1]), pack_h2(w[k][2 * s][2], w[k][2 * s][3]), pack_h2(w[k][2 * s + 1][0], w[k][2 * s + 1][1]),
-                   pack_h2(w[k][2 * s + 1][2], w[k][2 * s + 1][3]));
+    const half8_t P = as_h8(pack_h2(w[2 * s][0], w[2 * s][1]), pack_h2(w[2 * s][2], w[2 * s][3]), pack_h2(w[2 * s + 1][0], w[2 * s + 1][1]),
+                            pack_h2(w[2 * s + 1][2], w[2 * s + 1][3]));
 #pragma unroll
     for (int n = 0; n < 8; ++n) {
-      uint32_t v[4];
+      u32x4_t v;
 #pragma unroll
       for (int u = 0; u < 4; ++u) {  // (slots beyond the window take its last quad's: their weights are 0 and the window is finite)
         const int slot = 16 * (first + 2 * s + (u >> 1)) + a + 4 * (u & 1);
         v[u] = *reinterpret_cast<const uint32_t*>(v_win + ((long long)min(slot >> 2, quads - 1) * kHeadDim + 16 * n + (lane & 15)) * 4 + (slot & 3));
       }
-      const half8_t V = as_h8(make_uint4(v[0], v[1], v[2], v[3]));
-#pragma unroll
-      for (int k = 0; k < NR; ++k) st.acc[k][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(V, P[k], st.acc[k][n], 0, 0, 0);
+      st.acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(as_h8(v), P, st.acc[n], 0, 0, 0);
     }
     asm volatile("" ::: "memory");  // (the next blocks' loads stay behind these products: all at once they spilled)
   }
 }
 
-// One group of 128 packed tokens, the first at position `at`, `count` of them there.  masked: some row does not see all of them.
-// SLIDING: tokens from fp16_from on take their values from the window.
-template <int BITS, int NR>
-__device__ __forceinline__ void group_scores(Rows<NR>& st, const Record<BITS>& rec, const u32x4_t* meta, int at, int count, bool masked, int sinks,
-                                             int lane, float (&x)[NR][8][4], float (&base)[NR]) {
-  half8_t hi[NR][4], lo[NR][4];
-  float bias[NR];
+// Scores of one group of 128 packed tokens, the first at position `at`, `count` of them there: x[i][r] = block subset (8 / S) + i, token
+// 16 n + pi(4 g + r), and with `base` the exponent of a weight, x unit + base.  masked: some row does not see all of them.
+template <int BITS, int S>
+__device__ __forceinline__ void group_scores(Rows& st, const Record<BITS>& rec, const u32x4_t* meta, int at, int count, bool masked, int sinks, int lane,
+                                             float (&x)[8 / S][4], float& base) {
+  constexpr int kBlocks = 8 / S;
+  half8_t hi[4], lo[4];
+  float bias;
   {
-    float bz[NR], bs[NR];
-#pragma unroll
-    for (int k = 0; k < NR; ++k) bz[k] = bs[k] = 0.0f;
+    float bz = 0.0f, bs = 0.0f;
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
-      const u32x4_t S = meta[4 * (lane >> 4) + s], Z = meta[16 + 4 * (lane >> 4) + s];
+      const u32x4_t sc = meta[4 * (lane >> 4) + s], z = meta[16 + 4 * (lane >> 4) + s];
+      const u32x4_t qq = __builtin_bit_cast(u32x4_t, st.q[s]);
+      u32x4_t h, r;
 #pragma unroll
-      for (int k = 0; k < NR; ++k) {
-        const u32x4_t qq = __builtin_bit_cast(u32x4_t, st.q[k][s]);
-        u32x4_t h, r;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const half2_t a = as_h2(qq[i]), sc = as_h2(S[i]);
-          const half2_t t = a * sc;
-          h[i] = as_u32(t);
-          r[i] = as_u32(__builtin_elementwise_fma(a, sc, -t));
-          bz[k] = __builtin_amdgcn_fdot2(a, as_h2(Z[i]), bz[k], false);
-          bs[k] = __builtin_amdgcn_fdot2(a, sc, bs[k], false);
-        }
-        hi[k][s] = as_h8(h);
-        lo[k][s] = as_h8(r);
+      for (int i = 0; i < 4; ++i) {
+        const half2_t a = as_h2(qq[i]), k = as_h2(sc[i]), t = a * k;
+        h[i] = as_u32(t);
+        r[i] = as_u32(__builtin_elementwise_fma(a, k, -t));
+        bz = __builtin_amdgcn_fdot2(a, as_h2(z[i]), bz, false);
+        bs = __builtin_amdgcn_fdot2(a, k, bs, false);
       }
+      hi[s] = as_h8(h);
+      lo[s] = as_h8(r);
     }
-#pragma unroll
-    for (int k = 0; k < NR; ++k) {
-      float a, b;
-      pair_across<16>(fmaf(bs[k], Rec<BITS>::kCentre, bz[k]), a, b);
-      pair_across<32>(a + b, a, b);
-      bias[k] = (a + b) * st.unit[k];
-    }
+    float a, b;
+    pair_across<16>(fmaf(bs, Rec<BITS>::kCentre, bz), a, b);
+    pair_across<32>(a + b, a, b);
+    bias = (a + b) * st.unit;
   }
 #pragma unroll
-  for (int m = 0; m < 4; ++m)
+  for (int n = 0; n < 8; ++n) {
+    half8_t A[4];
 #pragma unroll
-    for (int hf = 0; hf < 2; ++hf) {
-      half8_t A[4];
+    for (int w = 0; w < 2; ++w) {
+      uint32_t e[BITS / 2], o[BITS / 2];
 #pragma unroll
-      for (int w = 0; w < 2; ++w) {
-        uint32_t e[BITS / 2], o[BITS / 2];
-#pragma unroll
-        for (int pl = 0; pl < BITS / 2; ++pl) {
-          const Nibbles nb = nibbles_of(rec.kw[4 * pl + m][2 * hf + w]);
-          e[pl] = nb.first; o[pl] = nb.second;
-        }
-        A[2 * w] = as_h8(code_pair<BITS, 0>(e, 1.0f), code_pair<BITS, 1>(e, 1.0f), code_pair<BITS, 2>(e, 1.0f), code_pair<BITS, 3>(e, 1.0f));
-        A[2 * w + 1] = as_h8(code_pair<BITS, 0>(o, 1.0f), code_pair<BITS, 1>(o, 1.0f), code_pair<BITS, 2>(o, 1.0f), code_pair<BITS, 3>(o, 1.0f));
+      for (int pl = 0; pl < BITS / 2; ++pl) {
+        const Nibbles nb = nibbles_of(rec.kw[4 * pl + n / 2][2 * (n % 2) + w]);
+        e[pl] = nb.first; o[pl] = nb.second;
       }
-#pragma unroll
-      for (int k = 0; k < NR; ++k) {
-        float4_t d = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int s = 0; s < 4; ++s) d = __builtin_amdgcn_mfma_f32_16x16x32_f16(A[s], lo[k][s], d, 0, 0, 0);
-#pragma unroll
-        for (int s = 0; s < 4; ++s) d = __builtin_amdgcn_mfma_f32_16x16x32_f16(A[s], hi[k][s], d, 0, 0, 0);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) x[k][2 * m + hf][r] = d[r];
-      }
+      A[2 * w] = as_h8(code_pair<BITS, 0>(e, 1.0f), code_pair<BITS, 1>(e, 1.0f), code_pair<BITS, 2>(e, 1.0f), code_pair<BITS, 3>(e, 1.0f));
+      A[2 * w + 1] = as_h8(code_pair<BITS, 0>(o, 1.0f), code_pair<BITS, 1>(o, 1.0f), code_pair<BITS, 2>(o, 1.0f), code_pair<BITS, 3>(o, 1.0f));
     }
+    float4_t d = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int s = 0; s < 4; ++s) d = __builtin_amdgcn_mfma_f32_16x16x32_f16(A[s], lo[s], d, 0, 0, 0);
+#pragma unroll
+    for (int s = 0; s < 4; ++s) d = __builtin_amdgcn_mfma_f32_16x16x32_f16(A[s], hi[s], d, 0, 0, 0);
+    const bool own = S == 1 || n / kBlocks == st.subset;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) x[n % kBlocks][r] = n < kBlocks || own ? d[r] : x[n % kBlocks][r];
+  }
   if (masked) {
+    const int t0 = 16 * kBlocks * st.subset, end = min(count, st.p - at + 1) - t0, from = st.low - at - t0, first = sinks - at - t0;
 #pragma unroll
-    for (int k = 0; k < NR; ++k) {
-      const int end = min(count, st.p[k] - at + 1), from = st.low[k] - at, first = sinks - at;
+    for (int i = 0; i < kBlocks; ++i)
 #pragma unroll
-      for (int n = 0; n < 8; ++n)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int t = 16 * n + token_order(4 * (lane >> 4) + r);
-          x[k][n][r] = (t < end) & ((t >= from) | (t < first)) ? x[k][n][r] : -INFINITY;
-        }
-    }
+      for (int r = 0; r < 4; ++r) {
+        const int t = 16 * i + token_order(4 * (lane >> 4) + r);
+        x[i][r] = (t < end) & ((t >= from) | (t < first)) ? x[i][r] : -INFINITY;
+      }
   }
+  float mx = x[0][0];
 #pragma unroll
-  for (int k = 0; k < NR; ++k) {
-    float mx = x[k][0][0];
+  for (int i = 0; i < kBlocks; ++i)
 #pragma unroll
-    for (int n = 0; n < 8; ++n)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) mx = fmaxf(mx, x[k][n][r]);
-    set_reference<NR>(st, k, fmaf(mx, st.unit[k], bias[k]));
-    const float m = finite_reference(st.m[k]);
-    base[k] = bias[k] - m;
-    // References and biases thousands beyond what ordinary keys and queries give: the exponents are rounded as the reference was (the
-    // score itself, then its distance from the reference), or the exponent of the largest weight would be what the roundings leave.
-    if (__builtin_amdgcn_ballot_w64(fmaxf(fabsf(m), fabsf(bias[k])) > kFusedBound) != 0) {
+    for (int r = 0; r < 4; ++r) mx = fmaxf(mx, x[i][r]);
+  set_reference(st, fmaf(mx, st.unit, bias));
+  const float m = finite_reference(st.m);
+  base = bias - m;
+  // References and biases thousands beyond what ordinary keys and queries give: the exponents are rounded as the reference was (the score
+  // itself, then its distance from the reference), or the exponent of the largest weight would be what the roundings leave.
+  if (__builtin_amdgcn_ballot_w64(fmaxf(fabsf(m), fabsf(bias)) > kFusedBound) != 0) {
 #pragma clang fp contract(off)
-      const float back = 1.0f / st.unit[k];
+    const float back = 1.0f / st.unit;
 #pragma unroll
-      for (int n = 0; n < 8; ++n)
+    for (int i = 0; i < kBlocks; ++i)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) x[k][n][r] = (__builtin_fmaf(x[k][n][r], st.unit[k], bias[k]) - m) * back;
-      base[k] = 0.0f;
-    }
+      for (int r = 0; r < 4; ++r) x[i][r] = (__builtin_fmaf(x[i][r], st.unit, bias) - m) * back;
+    base = 0.0f;
   }
 }
 
-// Scores become weights; O^T += V^T P^T of the group.  e: see put_meta.
-template <int BITS, int NR, bool SLIDING>
-__device__ __forceinline__ void group_values(Rows<NR>& st, const Record<BITS>& rec, const u32x4_t* meta, int e, float (&x)[NR][8][4], const float (&base)[NR],
-                                             int fp16_from, const half_t* v_win, int quads, int lane) {
+// Scores become weights; O^T += V^T P^T of the group.  e: see put_meta.  SLIDING: tokens from fp16_from on take their values from the window.
+template <int BITS, int S, bool SLIDING>
+__device__ __forceinline__ void group_values(Rows& st, const Record<BITS>& rec, const u32x4_t* meta, int e, float (&x)[8 / S][4], float base, int fp16_from,
+                                             const half_t* v_win, int quads, int lane) {
+  constexpr int kBlocks = 8 / S;
   const float scale = bits_f32((uint32_t)(127 + e) << 23);
-  half8_t P[NR][4];
-  float l[NR], ys[NR], zs[NR];
-#pragma unroll
-  for (int k = 0; k < NR; ++k) l[k] = ys[k] = zs[k] = 0.0f;
+  uint32_t w[kBlocks / 2][4];  // weight times value scale of blocks 2 i and 2 i + 1
+  float l = 0.0f, ys = 0.0f, zs = 0.0f;
   const half2_t ones = {(half_t)1.0f, (half_t)1.0f};
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
     const int t = token_order(4 * (lane >> 4) + r);
-    const u32x4_t z0 = meta[32 + 2 * t], z1 = meta[33 + 2 * t];
+    const uint32_t* pairs = reinterpret_cast<const uint32_t*>(meta + 32 + 2 * t) + kBlocks * st.subset;
+    uint32_t sz[kBlocks];
+    if constexpr (S == 4) {
+      const u32x2_t v = *reinterpret_cast<const u32x2_t*>(pairs);
+      sz[0] = v[0]; sz[1] = v[1];
+    } else {
 #pragma unroll
-    for (int k = 0; k < NR; ++k)
+      for (int q = 0; q < kBlocks / 4; ++q) {
+        const u32x4_t v = reinterpret_cast<const u32x4_t*>(pairs)[q];
 #pragma unroll
-      for (int s = 0; s < 4; ++s) {
-        float y[2];
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const int n = 2 * s + u;
-          const half2_t sz = as_h2(n < 4 ? z0[n] : z1[n - 4]);
-          const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[k][n][r], st.unit[k], base[k]));
-          if (SLIDING) x[k][n][r] = p;
-          l[k] += p;
-          float yy = __builtin_fmaf(p, (float)sz[0], 0.0f);
-          const bool coded = !SLIDING || 16 * n + t < fp16_from;
-          y[u] = coded ? yy : 0.0f;
-          zs[k] = coded ? __builtin_fmaf(p, (float)sz[1], zs[k]) : zs[k];
-        }
-        const half2_t w = pack_h2(y[0], y[1]);
-        ys[k] = __builtin_amdgcn_fdot2(w, ones, ys[k], false);
-        P[k][s][2 * r] = w[0];
-        P[k][s][2 * r + 1] = w[1];
+        for (int i = 0; i < 4; ++i) sz[4 * q + i] = v[i];
       }
-  }
-#pragma unroll
-  for (int k = 0; k < NR; ++k) {
-    st.l[k] += l[k];
-    st.mid[k] += fmaf(ys[k] * scale, Rec<BITS>::kCentre, zs[k]);
-  }
-#pragma unroll
-  for (int m = 0; m < 4; ++m)
-#pragma unroll
-    for (int hf = 0; hf < 2; ++hf) {
-      uint32_t e0[BITS / 2], o0[BITS / 2], e1[BITS / 2], o1[BITS / 2];
-#pragma unroll
-      for (int pl = 0; pl < BITS / 2; ++pl) {
-        const Nibbles a = nibbles_of(rec.vw[4 * pl + m][2 * hf]), b = nibbles_of(rec.vw[4 * pl + m][2 * hf + 1]);
-        e0[pl] = a.first; o0[pl] = a.second; e1[pl] = b.first; o1[pl] = b.second;
-      }
-      half8_t V[4];
-      V[0] = as_h8(code_pair<BITS, 0>(e0, scale), code_pair<BITS, 0>(o0, scale), code_pair<BITS, 0>(e1, scale), code_pair<BITS, 0>(o1, scale));
-      V[1] = as_h8(code_pair<BITS, 1>(e0, scale), code_pair<BITS, 1>(o0, scale), code_pair<BITS, 1>(e1, scale), code_pair<BITS, 1>(o1, scale));
-      V[2] = as_h8(code_pair<BITS, 2>(e0, scale), code_pair<BITS, 2>(o0, scale), code_pair<BITS, 2>(e1, scale), code_pair<BITS, 2>(o1, scale));
-      V[3] = as_h8(code_pair<BITS, 3>(e0, scale), code_pair<BITS, 3>(o0, scale), code_pair<BITS, 3>(e1, scale), code_pair<BITS, 3>(o1, scale));
-#pragma unroll
-      for (int k = 0; k < NR; ++k)
-#pragma unroll
-        for (int s = 0; s < 4; ++s) st.acc[k][2 * m + hf] = __builtin_amdgcn_mfma_f32_16x16x32_f16(V[s], P[k][s], st.acc[k][2 * m + hf], 0, 0, 0);
     }
+#pragma unroll
+    for (int i = 0; i < kBlocks; i += 2) {
+      float y[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const half2_t p2 = as_h2(sz[i + u]);
+        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i + u][r], st.unit, base));
+        if (SLIDING) x[i + u][r] = p;
+        l += p;
+        const bool coded = !SLIDING || 16 * (kBlocks * st.subset + i + u) + t < fp16_from;
+        const float yy = __builtin_fmaf(p, (float)p2[0], 0.0f);
+        y[u] = coded ? yy : 0.0f;
+        zs = coded ? __builtin_fmaf(p, (float)p2[1], zs) : zs;
+      }
+      const half2_t pk = pack_h2(y[0], y[1]);
+      ys = __builtin_amdgcn_fdot2(pk, ones, ys, false);
+      w[i / 2][r] = as_u32(pk);
+    }
+  }
+  st.l += l;
+  st.mid += fmaf(ys * scale, Rec<BITS>::kCentre, zs);
+  half8_t P[4];  // step s: blocks 2 s and 2 s + 1; a column has those of its subset, and zero elsewhere
+#pragma unroll
+  for (int s = 0; s < 4; ++s) {
+    u32x4_t v;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) v[r] = S == 1 || 2 * s / kBlocks == st.subset ? w[s % (kBlocks / 2)][r] : 0u;
+    P[s] = as_h8(v);
+  }
+#pragma unroll
+  for (int n = 0; n < 8; ++n) {
+    uint32_t e0[BITS / 2], o0[BITS / 2], e1[BITS / 2], o1[BITS / 2];
+#pragma unroll
+    for (int pl = 0; pl < BITS / 2; ++pl) {
+      const Nibbles a = nibbles_of(rec.vw[4 * pl + n / 2][2 * (n % 2)]), b = nibbles_of(rec.vw[4 * pl + n / 2][2 * (n % 2) + 1]);
+      e0[pl] = a.first; o0[pl] = a.second; e1[pl] = b.first; o1[pl] = b.second;
+    }
+    half8_t V[4];
+    V[0] = as_h8(code_pair<BITS, 0>(e0, scale), code_pair<BITS, 0>(o0, scale), code_pair<BITS, 0>(e1, scale), code_pair<BITS, 0>(o1, scale));
+    V[1] = as_h8(code_pair<BITS, 1>(e0, scale), code_pair<BITS, 1>(o0, scale), code_pair<BITS, 1>(e1, scale), code_pair<BITS, 1>(o1, scale));
+    V[2] = as_h8(code_pair<BITS, 2>(e0, scale), code_pair<BITS, 2>(o0, scale), code_pair<BITS, 2>(e1, scale), code_pair<BITS, 2>(o1, scale));
+    V[3] = as_h8(code_pair<BITS, 3>(e0, scale), code_pair<BITS, 3>(o0, scale), code_pair<BITS, 3>(e1, scale), code_pair<BITS, 3>(o1, scale));
+#pragma unroll
+    for (int s = 0; s < 4; ++s) st.acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(V[s], P[s], st.acc[n], 0, 0, 0);
+  }
   if (SLIDING && fp16_from < kGroup) {
+    float p[8][4];
 #pragma unroll
-    for (int k = 0; k < NR; ++k)
+    for (int n = 0; n < 8; ++n)
 #pragma unroll
-      for (int n = 0; n < 8; ++n)
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-          if (16 * n + token_order(4 * (lane >> 4) + r) < fp16_from) x[k][n][r] = 0.0f;
-    window_values<NR, 8>(st, v_win, quads, 0, x, lane);
+      for (int r = 0; r < 4; ++r)
+        p[n][r] = (S == 1 || n / kBlocks == st.subset) && 16 * n + token_order(4 * (lane >> 4) + r) >= fp16_from ? x[n % kBlocks][r] : 0.0f;
+    window_values<8>(st, v_win, quads, 0, p, lane);
   }
 }
 
-// Scores of up to 32 raw key rows of 128 halves, `count` of them there; x[k][0..1].  Rows beyond count take the last one's keys.
-template <int NR>
-__device__ __forceinline__ void raw_scores(Rows<NR>& st, const half_t* keys, int at, int count, int sinks, int lane, float (&x)[NR][2][4]) {
+// Weights of up to 32 raw key rows of 128 halves, `count` of them there (all in subset 0).  Rows beyond count take the last one's keys.
+__device__ __forceinline__ void raw_weights(Rows& st, const half_t* keys, int at, int count, int sinks, int lane, float (&x)[2][4]) {
   const int g = lane >> 4;
 #pragma unroll
   for (int n = 0; n < 2; ++n) {
-    const uint4* row = reinterpret_cast<const uint4*>(keys + (long long)min(16 * n + token_order(lane & 15), count - 1) * kHeadDim + 32 * g);
-    half8_t K[4];
+    const u32x4_t* row = reinterpret_cast<const u32x4_t*>(keys + (long long)min(16 * n + token_order(lane & 15), count - 1) * kHeadDim + 32 * g);
+    float4_t d = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int s = 0; s < 4; ++s) K[s] = as_h8(row[s]);
+    for (int s = 0; s < 4; ++s) d = __builtin_amdgcn_mfma_f32_16x16x32_f16(as_h8(row[s]), st.q[s], d, 0, 0, 0);
 #pragma unroll
-    for (int k = 0; k < NR; ++k) {
-      float4_t d = {0.f, 0.f, 0.f, 0.f};
+    for (int r = 0; r < 4; ++r)
+      x[n][r] = st.subset == 0 && seen(16 * n + token_order(4 * g + r), at, count, st.p, st.low, sinks) ? d[r] * st.unit : -INFINITY;
+  }
+  float mx = x[0][0];
 #pragma unroll
-      for (int s = 0; s < 4; ++s) d = __builtin_amdgcn_mfma_f32_16x16x32_f16(K[s], st.q[k][s], d, 0, 0, 0);
+  for (int n = 0; n < 2; ++n)
 #pragma unroll
-      for (int r = 0; r < 4; ++r)
-        x[k][n][r] = seen(16 * n + token_order(4 * g + r), at, count, st.p[k], st.low[k], sinks) ? d[r] * st.unit[k] : -INFINITY;
+    for (int r = 0; r < 4; ++r) mx = fmaxf(mx, x[n][r]);
+  set_reference(st, mx);
+  const float m = finite_reference(st.m);
+#pragma unroll
+  for (int n = 0; n < 2; ++n)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      x[n][r] = __builtin_amdgcn_exp2f(x[n][r] - m);
+      st.l += x[n][r];
     }
-  }
-#pragma unroll
-  for (int k = 0; k < NR; ++k) {
-    float mx = x[k][0][0];
-#pragma unroll
-    for (int n = 0; n < 2; ++n)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) mx = fmaxf(mx, x[k][n][r]);
-    set_reference<NR>(st, k, mx);
-    const float m = finite_reference(st.m[k]);
-#pragma unroll
-    for (int n = 0; n < 2; ++n)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        x[k][n][r] = __builtin_amdgcn_exp2f(x[k][n][r] - m);
-        st.l[k] += x[k][n][r];
-      }
-  }
 }
 
 // O^T += V^T P^T with raw value rows of 128 halves.  A lane gathers the 8 values of a channel (16 lanes: 32 contiguous bytes a row).
-template <int NR>
-__device__ __forceinline__ void raw_values(Rows<NR>& st, const half_t* values, int count, const float (&w)[NR][2][4], int lane) {
+__device__ __forceinline__ void raw_values(Rows& st, const half_t* values, int count, const float (&w)[2][4], int lane) {
   const int g = lane >> 4;
-  half8_t P[NR];
-#pragma unroll
-  for (int k = 0; k < NR; ++k)
-    P[k] = as_h8(pack_h2(w[k][0][0], w[k][0][1]), pack_h2(w[k][0][2], w[k][0][3]), pack_h2(w[k][1][0], w[k][1][1]), pack_h2(w[k][1][2], w[k][1][3]));
+  const half8_t P = as_h8(pack_h2(w[0][0], w[0][1]), pack_h2(w[0][2], w[0][3]), pack_h2(w[1][0], w[1][1]), pack_h2(w[1][2], w[1][3]));
   const half_t* row[8];
 #pragma unroll
   for (int u = 0; u < 8; ++u)
@@ -369,61 +342,117 @@ __device__ __forceinline__ void raw_values(Rows<NR>& st, const half_t* values, i
     half8_t V;
 #pragma unroll
     for (int u = 0; u < 8; ++u) V[u] = row[u][16 * n];
-#pragma unroll
-    for (int k = 0; k < NR; ++k) st.acc[k][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(V, P[k], st.acc[k][n], 0, 0, 0);
+    st.acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(V, P, st.acc[n], 0, 0, 0);
   }
 }
 
 // acc H: channels 16 n + 4 g + r, seven butterfly stages and the factor 1 / sqrt(128), in binary32.
-template <int NR>
-__device__ __forceinline__ void rotate_rows(Rows<NR>& st, int lane) {
+__device__ __forceinline__ void rotate_rows(Rows& st, int lane) {
   const float s16 = (lane & 16) != 0 ? -1.0f : 1.0f, s32 = (lane & 32) != 0 ? -1.0f : 1.0f;
 #pragma unroll
-  for (int k = 0; k < NR; ++k) {
+  for (int n = 0; n < 8; ++n) {
+    const float4_t v = st.acc[n];
+    const float a0 = v[0] + v[1], a1 = v[0] - v[1], a2 = v[2] + v[3], a3 = v[2] - v[3];
+    float t[4] = {a0 + a2, a1 + a3, a0 - a2, a1 - a3};
 #pragma unroll
-    for (int n = 0; n < 8; ++n) {
-      const float4_t v = st.acc[k][n];
-      const float a0 = v[0] + v[1], a1 = v[0] - v[1], a2 = v[2] + v[3], a3 = v[2] - v[3];
-      float t[4] = {a0 + a2, a1 + a3, a0 - a2, a1 - a3};
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        float x, y;
-        pair_across<16>(t[r], x, y);
-        t[r] = __builtin_fmaf(y, s16, x);
-        pair_across<32>(t[r], x, y);
-        st.acc[k][n][r] = __builtin_fmaf(y, s32, x) * kInvSqrtD;
-      }
+    for (int r = 0; r < 4; ++r) {
+      float x, y;
+      pair_across<16>(t[r], x, y);
+      t[r] = __builtin_fmaf(y, s16, x);
+      pair_across<32>(t[r], x, y);
+      st.acc[n][r] = __builtin_fmaf(y, s32, x) * kInvSqrtD;
     }
-#pragma unroll
-    for (int h = 1; h < 8; h *= 2)
-#pragma unroll
-      for (int n = 0; n < 8; ++n)
-        if ((n & h) == 0) {
-          const float4_t a = st.acc[k][n], b = st.acc[k][n + h];
-          st.acc[k][n] = a + b;
-          st.acc[k][n + h] = a - b;
-        }
   }
+#pragma unroll
+  for (int h = 1; h < 8; h *= 2)
+#pragma unroll
+    for (int n = 0; n < 8; ++n)
+      if ((n & h) == 0) {
+        const float4_t a = st.acc[n], b = st.acc[n + h];
+        st.acc[n] = a + b;
+        st.acc[n + h] = a - b;
+      }
 }
 
-// One output row from its 128 numerators (16 lanes, 8 neighbouring channels each) and the correction, if any: normalised, rotated back.
-__device__ __forceinline__ void finish_row(float (&a)[8], float l, float m, const float* corr, int lane, half_t* out) {
-  if (corr != nullptr) {  // {C_d, -, -, -, C_n[128]}: added as e^0 terms (Eq. 5), both sides relative to max(m, 0)
-    const float to = fmaxf(m, 0.0f);
-    const float f = __builtin_amdgcn_exp2f(m - to), w = __builtin_amdgcn_exp2f(-to);
-    l = fmaf(w, corr[0], l * f);
-    const float4 c0 = *reinterpret_cast<const float4*>(corr + 4 + 8 * (lane & 15)), c1 = *reinterpret_cast<const float4*>(corr + 8 + 8 * (lane & 15));
-    const float c[8] = {c0.x, c0.y, c0.z, c0.w, c1.x, c1.y, c1.z, c1.w};
-#pragma unroll
-    for (int i = 0; i < 8; ++i) a[i] = fmaf(w, c[i], a[i] * f);
-  }
+// ---- results that one workgroup writes and another reads inside the launch ----------------------------------------------------------------
+// Stores and loads that go past the caches that are not coherent across the chip (sc0, sc1).  The partial results, and the correction's, of a
+// (sequence, KV head) lie together: [head][T][splits] resp. [head][T] rows of kPartStride floats.
+constexpr int kCoherent = 1 | 16, kPartBytes = 4 * kPartStride;
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(float* p, long long bytes) { return __builtin_amdgcn_make_buffer_rsrc(p, 0, (int)bytes, 0x00027000); }
+__device__ __forceinline__ void store4(__amdgpu_buffer_rsrc_t r, int at, float a, float b, float c, float d) {
+  __builtin_amdgcn_raw_buffer_store_b128(u32x4_t{__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b), __builtin_bit_cast(uint32_t, c), __builtin_bit_cast(uint32_t, d)}, r,
+                                         at, 0, kCoherent);
+}
+__device__ __forceinline__ void store2(__amdgpu_buffer_rsrc_t r, int at, float a, float b) {
+  __builtin_amdgcn_raw_buffer_store_b64(u32x2_t{__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b)}, r, at, 0, kCoherent);
+}
+__device__ __forceinline__ float4_t load4(__amdgpu_buffer_rsrc_t r, int at) { return __builtin_bit_cast(float4_t, __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, kCoherent)); }
+__device__ __forceinline__ float2v_t load2(__amdgpu_buffer_rsrc_t r, int at) { return __builtin_bit_cast(float2v_t, __builtin_amdgcn_raw_buffer_load_b64(r, at, 0, kCoherent)); }
+
+// One output row from its 128 numerators (16 lanes, 8 neighbouring channels each): normalised, rotated back.
+__device__ __forceinline__ void finish_row(float (&a)[8], float l, int lane, half_t* out) {
   lane8_butterflies(a);
   row16_butterflies<8>(a, lane);
   const float inv = l > 0.0f ? kInvSqrtD / l : 0.0f;
-  uint32_t h[4];
+  u32x4_t h;
 #pragma unroll
   for (int i = 0; i < 4; ++i) h[i] = as_u32(pack_h2(a[2 * i] * inv, a[2 * i + 1] * inv));
-  *reinterpret_cast<uint4*>(out + 8 * (lane & 15)) = make_uint4(h[0], h[1], h[2], h[3]);
+  *reinterpret_cast<u32x4_t*>(out + 8 * (lane & 15)) = h;
+}
+// The correction {C_d, -, -, -, C_n[128]} added as e^0 terms (Eq. 5), both sides relative to max(m, 0).
+__device__ __forceinline__ void add_correction(float (&a)[8], float& l, float m, float c_d, float4_t c0, float4_t c1) {
+  const float to = fmaxf(m, 0.0f), f = __builtin_amdgcn_exp2f(m - to), w = __builtin_amdgcn_exp2f(-to);
+  l = fmaf(w, c_d, l * f);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    a[i] = fmaf(w, c0[i], a[i] * f);
+    a[4 + i] = fmaf(w, c1[i], a[4 + i] * f);
+  }
+}
+constexpr int kMaxContextSplits = 32;
+// The splits of one row joined by 16 lanes: weights by lane, two splits each, then the numerators, eight splits under way at a time.
+__device__ __forceinline__ void join_row(__amdgpu_buffer_rsrc_t part, int at, int splits, float* weights /* LDS, 32 */, int lane, float (&o)[8], float& L, float& M) {
+  const int j = lane & 15;
+  float2v_t ml[2];
+#pragma unroll
+  for (int u = 0; u < 2; ++u) ml[u] = load2(part, at + min(j + 16 * u, splits - 1) * kPartBytes);
+  float m[2] = {j < splits ? ml[0][0] : -INFINITY, j + 16 < splits ? ml[1][0] : -INFINITY};
+  M = fmaxf(m[0], m[1]);
+  M = fmaxf(M, dpp_f<kRowRor1>(M));
+  M = fmaxf(M, dpp_f<kRowRor2>(M));
+  M = fmaxf(M, dpp_f<kRowRor4>(M));
+  M = fmaxf(M, dpp_f<kRowRor8>(M));
+  L = 0.0f;
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const float w = m[u] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[u] - M);
+    weights[j + 16 * u] = w;
+    L = fmaf(w, ml[u][1], L);
+  }
+  L += dpp_f<kRowRor1>(L);
+  L += dpp_f<kRowRor2>(L);
+  L += dpp_f<kRowRor4>(L);
+  L += dpp_f<kRowRor8>(L);
+  __builtin_amdgcn_wave_barrier();  // (the 16 lanes are of one wave)
+#pragma unroll
+  for (int i = 0; i < 8; ++i) o[i] = 0.0f;
+  for (int s0 = 0; s0 < splits; s0 += 8) {
+    float4_t u[8][2];
+#pragma unroll
+    for (int s = 0; s < 8; ++s)
+#pragma unroll
+      for (int k = 0; k < 2; ++k) u[s][k] = load4(part, at + min(s0 + s, splits - 1) * kPartBytes + 16 + 32 * j + 16 * k);
+#pragma unroll
+    for (int s = 0; s < 8; ++s) {
+      const float w = weights[s0 + s];  // (0 beyond the last)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        o[i] = fmaf(w, u[s][0][i], o[i]);
+        o[4 + i] = fmaf(w, u[s][1][i], o[4 + i]);
+      }
+    }
+  }
+  __builtin_amdgcn_wave_barrier();
 }
 
 struct RowPlace {
@@ -434,175 +463,332 @@ __device__ __forceinline__ RowPlace row_place(int row, int gq) {
   return RowPlace{i, row - i * gq};
 }
 
-// Grid, one-dimensional: split fastest, then (sequence, KV head), then the block of 16 NR rows.  PROMPT: rows are new tokens at positions total + i, and see their own rows; else one
-// token at position total - 1.
-template <int BITS, int NR, bool PROMPT, bool SLIDING>
-__global__ __launch_bounds__(64 * kRowWaves, 2) void rows_kernel(ContextCall a) {
-  __shared__ __align__(16) u32x4_t sMeta[kRowWaves][64];
+// ---- the correction of all rows of a pair (Sec. 3.2, Eq. 5-6), by one workgroup ----------------------------------------------------------------
+// Products as in kvlinc_prompt_correction.hip.  First the features, a wave a head and half of them at a time (16 tokens as columns), through LDS;
+// then C_n^T = S^T phi^T, a wave a block of 16 channels, so that the state is read once for all heads.
+constexpr int kFeatureStride = kRank + 8;  // halves of a row in LDS
+__device__ __forceinline__ float column_allmax(float v) {  // over the four lanes of a column
+  float x, y;
+  pair_across<16>(v, x, y);
+  pair_across<32>(fmaxf(x, y), x, y);
+  return fmaxf(x, y);
+}
+__device__ __forceinline__ float column_allsum(float v) {
+  float x, y;
+  pair_across<16>(v, x, y);
+  pair_across<32>(x + y, x, y);
+  return x + y;
+}
+__device__ __forceinline__ void correct_rows(const ContextCall& a, int b, int kvh, int T, int rows, int wave, int waves, int lane, half_t* features, float (*den)[64]) {
   const kvlinc_cache& c = a.cache;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4;
-  const int pairs = c.B * c.H_kv, unit = blockIdx.x / a.splits, split = blockIdx.x - unit * a.splits;
-  const int block = unit / pairs, bh = unit - block * pairs, b = bh / c.H_kv, kvh = bh - b * c.H_kv, gq = a.gq;
-  const Lengths len = lengths_of(c, b);
-  const int T = PROMPT ? (a.n_new != nullptr ? min(max(a.n_new[b], 0), a.T) : a.T) : 1;
-  const int rows = T * gq, row0 = block * 16 * NR;
-  if (row0 >= rows) return;
-  const int total = len.total(), base = PROMPT ? total : total - 1;
-  const long long head0 = (long long)b * c.H_q + (long long)kvh * gq;
-
-  Rows<NR> st;
+  const int j = lane & 15, g = lane >> 4, gq = a.gq;
+  const long long kv = (long long)b * c.H_kv + kvh, head0 = (long long)b * c.H_q + (long long)kvh * gq;
+  for (int unit = wave; unit < 2 * gq; unit += waves) {
+    const int h = unit >> 1, half = unit & 1;
+    const half_t* W = reinterpret_cast<const half_t*>(c.Wq) + (((long long)kvh * gq + h) * 2 + half) * kHeadDim * 128;
+    const float* P = c.P + kv * kRank + 128 * half;
+    for (int i0 = 0; i0 < T; i0 += 16) {
+      const u32x4_t* src = reinterpret_cast<const u32x4_t*>(a.q + ((head0 + h) * a.T + min(i0 + j, T - 1)) * kHeadDim) + g;
+      half8_t q[4];
 #pragma unroll
-  for (int k = 0; k < NR; ++k) {
-    const RowPlace at = row_place(min(row0 + 16 * k + (lane & 15), rows - 1), gq);
-    st.p[k] = base + at.i;
-    st.low[k] = window_low(st.p[k], a.window);
-    const uint4* src = reinterpret_cast<const uint4*>(a.q + ((head0 + at.h) * a.T + at.i) * kHeadDim + 32 * g);
-    uint4 raw[4];
-    uint32_t mx = 0;
+      for (int s = 0; s < 4; ++s) q[s] = as_h8(src[4 * s]);  // channels 32 s + 8 g + 0..7
+      float4_t d[2][4];  // [64-feature block][tile]: features 64 fb + 16 g + 4 r + i
 #pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      raw[s] = src[s];
-      const uint32_t w[4] = {raw[s].x, raw[s].y, raw[s].z, raw[s].w};
+      for (int fb = 0; fb < 2; ++fb) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) mx = max(mx, max(w[i] & 0x7fffu, (w[i] >> 16) & 0x7fffu));
-    }
-    const auto u = __builtin_amdgcn_permlane16_swap(mx, mx, false, false);
-    mx = max(u[0], u[1]);
-    const auto v = __builtin_amdgcn_permlane32_swap(mx, mx, false, false);
-    mx = max(v[0], v[1]);
-    const int e = (int)min(max(mx >> 10, 1u), 30u) - 14;  // largest magnitude in [2^(e-1), 2^e) (subnormal rows: below 2^-14, e = -13)
-    const float down = bits_f32((uint32_t)(127 - e) << 23);
-    st.unit[k] = bits_f32((uint32_t)(127 + e) << 23) * kLog2eSqrtD;
-    const half2_t down2 = pack_h2(down, down);
+        for (int i = 0; i < 4; ++i) d[fb][i] = float4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int s = 0; s < 4; ++s)
-      st.q[k][s] = as_h8(as_h2(raw[s].x) * down2, as_h2(raw[s].y) * down2, as_h2(raw[s].z) * down2, as_h2(raw[s].w) * down2);
-    st.m[k] = -INFINITY;
-    st.l[k] = st.mid[k] = 0.0f;
+        for (int s = 0; s < 4; ++s) {
+          u32x2_t w[8];
 #pragma unroll
-    for (int n = 0; n < 8; ++n) st.acc[k][n] = float4_t{0.f, 0.f, 0.f, 0.f};
-  }
-
-  // Blocks of tokens that some row sees: the new rows' (32 each), the window's (32 each), the groups.  `low` is that of the first row, the
-  // last row's position ends the new ones.
-  const int first_i = row0 / gq, last_i = min(row0 + 16 * NR - 1, rows - 1) / gq;
-  const int low = window_low(base + first_i, a.window), low_last = window_low(base + last_i, a.window);
-  const int new_from = PROMPT ? (a.sinks > total ? 0 : max(low - total, 0) / kRawTokens) : 0;
-  const int n_new = PROMPT ? (last_i + kRawTokens) / kRawTokens - new_from : 0;
-  const int win_from = a.sinks > len.nq ? 0 : min(max(low - len.nq, 0), len.nr) / kRawTokens;
-  const int n_win = (len.nr + kRawTokens - 1) / kRawTokens - win_from;
-  const int G = len.groups(), group_low = min(low / kGroup, G);
-  const int n_sink = a.window > 0 ? min((int)(((long long)a.sinks + kGroup - 1) / kGroup), group_low) : 0;
-  const int n_groups = G - group_low + n_sink;
-  const int step = kRowWaves * a.splits;
-  int item = split * kRowWaves + wave;
-
-  if (PROMPT) {
-    bool rotate = false;
-    const half_t* keys = a.k_new + (long long)bh * a.T * kHeadDim;
-    const half_t* values = a.v_new + (long long)bh * a.T * kHeadDim;
-    for (; item < n_new; item += step) {
-      const int t0 = (new_from + item) * kRawTokens;
-      float x[NR][2][4];
-      raw_scores<NR>(st, keys + (long long)t0 * kHeadDim, total + t0, min(T - t0, kRawTokens), a.sinks, lane, x);
-      raw_values<NR>(st, values + (long long)t0 * kHeadDim, min(T - t0, kRawTokens), x, lane);
-      rotate = true;
-    }
-    if (rotate) rotate_rows<NR>(st, lane);  // from here on the accumulators are in the cache's rotated basis
-  }
-  item -= n_new;
-  const half_t* k_win = reinterpret_cast<const half_t*>(c.k_res) + (long long)bh * c.R * kHeadDim;
-  const half_t* v_win = reinterpret_cast<const half_t*>(c.v_res) + (long long)bh * c.R * kHeadDim;
-  const int quads = c.R / 4;
-  for (; item < n_win; item += step) {
-    const int t0 = (win_from + item) * kRawTokens;
-    float x[NR][2][4];
-    raw_scores<NR>(st, k_win + t0 * kHeadDim, len.nq + t0, min(len.nr - t0, kRawTokens), a.sinks, lane, x);
-    window_values<NR, 2>(st, v_win, quads, t0 / 16, x, lane);
-  }
-  item -= n_win;
-  const uint32_t* rec0 = c.groups + (long long)bh * c.max_groups * Rec<BITS>::kWords;
-  const int newest = SLIDING && len.nq % kGroup == 0 && len.nr < kGroup ? G - 1 : -1;
-  auto group_of = [&](int it) { return it < n_sink ? it : it - n_sink + group_low; };
-  if (item < n_groups) {
-    Record<BITS> rec;
-    int gr = group_of(item);
-    load_key_part<BITS>(rec, rec0 + (long long)gr * Rec<BITS>::kWords, lane);
-    load_value_part<BITS>(rec, rec0 + (long long)gr * Rec<BITS>::kWords, lane);
-    for (;;) {
-      const int at = gr * kGroup, count = min(len.nq - at, kGroup);
-      const bool masked = count < kGroup || (at < low_last && at + kGroup > a.sinks), more = item + step < n_groups;
-      const int e = put_meta<BITS>(rec, sMeta[wave], lane);
-      float x[NR][8][4], exponent_base[NR];
-      group_scores<BITS, NR>(st, rec, sMeta[wave], at, count, masked, a.sinks, lane, x, exponent_base);
-      const int next = more ? group_of(item + step) : gr;
-      if (more) load_key_part<BITS>(rec, rec0 + (long long)next * Rec<BITS>::kWords, lane);
-      group_values<BITS, NR, SLIDING>(st, rec, sMeta[wave], e, x, exponent_base, gr == newest ? len.nr : kGroup, v_win, quads, lane);
-      if (!more) break;
-      load_value_part<BITS>(rec, rec0 + (long long)next * Rec<BITS>::kWords, lane);
-      item += step;
-      gr = next;
-    }
-  }
-
-  // ---- the four waves joined ----
-  constexpr int kAccStride = kHeadDim + 4;
-  __shared__ float sM[kRowWaves][16 * NR], sL[kRowWaves][16 * NR];
-  __shared__ __align__(16) float sAcc[kRowWaves][16][kAccStride];
+          for (int k = 0; k < 8; ++k) w[k] = *reinterpret_cast<const u32x2_t*>(W + (32 * s + 8 * g + k) * 128 + 64 * fb + 4 * j);
 #pragma unroll
-  for (int k = 0; k < NR; ++k) {
-    float l = st.l[k], mid = st.mid[k], x, y;
-    pair_across<16>(l, x, y);
-    pair_across<32>(x + y, x, y);
-    l = x + y;
-    pair_across<16>(mid, x, y);
-    pair_across<32>(x + y, x, y);
-    mid = x + y;
-    if (g == 0) { sM[wave][16 * k + lane] = st.m[k]; sL[wave][16 * k + lane] = l; }
-    if (k > 0) __syncthreads();
+          for (int i = 0; i < 4; ++i) {
+            u32x4_t r;
 #pragma unroll
-    for (int n = 0; n < 8; ++n) {
-      const float4_t v = st.acc[k][n];
-      *reinterpret_cast<float4*>(&sAcc[wave][lane & 15][16 * n + 4 * g]) = make_float4(v[0] + mid, v[1] + mid, v[2] + mid, v[3] + mid);
-    }
-    __syncthreads();
-    const int r = 16 * k + (threadIdx.x >> 4), row = row0 + r, ch = 8 * (lane & 15);
-    float M = -INFINITY;
+            for (int k = 0; k < 4; ++k) r[k] = __builtin_amdgcn_perm(w[2 * k + 1][i >> 1], w[2 * k][i >> 1], (i & 1) == 0 ? 0x05040100u : 0x07060302u);
+            d[fb][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(as_h8(r), q[s], d[fb][i], 0, 0, 0);
+          }
+        }
+        asm volatile("" ::: "memory");  // (the loads of both blocks at once would spill)
+      }
+      float m = -INFINITY, z = 0.0f, p = 0.0f;
 #pragma unroll
-    for (int w = 0; w < kRowWaves; ++w) M = fmaxf(M, sM[w][r]);
-    float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, L = 0.0f;
-    if (M != -INFINITY) {
+      for (int fb = 0; fb < 2; ++fb)
 #pragma unroll
-      for (int w = 0; w < kRowWaves; ++w) {
-        const float f = __builtin_amdgcn_exp2f(sM[w][r] - M);  // 0 for a wave that has seen nothing
-        L = fmaf(f, sL[w][r], L);
-        const float4 u0 = *reinterpret_cast<const float4*>(&sAcc[w][r - 16 * k][ch]), u1 = *reinterpret_cast<const float4*>(&sAcc[w][r - 16 * k][ch + 4]);
-        o[0] = fmaf(f, u0.x, o[0]); o[1] = fmaf(f, u0.y, o[1]); o[2] = fmaf(f, u0.z, o[2]); o[3] = fmaf(f, u0.w, o[3]);
-        o[4] = fmaf(f, u1.x, o[4]); o[5] = fmaf(f, u1.y, o[5]); o[6] = fmaf(f, u1.z, o[6]); o[7] = fmaf(f, u1.w, o[7]);
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) m = fmaxf(m, d[fb][i][r]);
+      m = column_allmax(m);
+#pragma unroll
+      for (int fb = 0; fb < 2; ++fb)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float4_t w = *reinterpret_cast<const float4_t*>(P + 64 * fb + 16 * g + 4 * r);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float e = __builtin_amdgcn_exp2f((d[fb][i][r] - m) * 1.4426950408889634f);
+            d[fb][i][r] = e;
+            z += e;
+            p = fmaf(e, w[i], p);
+          }
+        }
+      const float inv = 1.0f / column_allsum(z);
+      p = column_allsum(p) * inv;
+      const int row = (i0 + j) * gq + h;
+      if (i0 + j < T) {
+        if (g == 0) den[half][row] = p;
+#pragma unroll
+        for (int fb = 0; fb < 2; ++fb)
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+            *reinterpret_cast<half8_t*>(features + row * kFeatureStride + 128 * half + 64 * fb + 16 * g + 8 * e) =
+                as_h8(pack_h2(d[fb][0][2 * e] * inv, d[fb][1][2 * e] * inv), pack_h2(d[fb][2][2 * e] * inv, d[fb][3][2 * e] * inv),
+                      pack_h2(d[fb][0][2 * e + 1] * inv, d[fb][1][2 * e + 1] * inv), pack_h2(d[fb][2][2 * e + 1] * inv, d[fb][3][2 * e + 1] * inv));
       }
     }
-    if (row < rows) {
-      const RowPlace at = row_place(row, gq);
-      const long long place = (head0 + at.h) * a.T + at.i;
-      if (a.splits == 1) {
-        finish_row(o, L, M, a.corr != nullptr ? a.corr + place * kPartStride : nullptr, lane, a.out + place * kHeadDim);
-      } else {
-        float* dst = a.part + (place * a.splits + split) * kPartStride;
-        if ((lane & 15) == 0) { dst[0] = M; dst[1] = L; }
-        *reinterpret_cast<float4*>(dst + 4 + ch) = make_float4(o[0], o[1], o[2], o[3]);
-        *reinterpret_cast<float4*>(dst + 8 + ch) = make_float4(o[4], o[5], o[6], o[7]);
+  }
+  __syncthreads();
+  const half_t* S = reinterpret_cast<const half_t*>(c.S16) + kv * (128 * 64 * 4);
+  const __amdgpu_buffer_rsrc_t out = buffer_of(a.corr + head0 * a.T * kPartStride, (long long)gq * a.T * kPartBytes);
+  for (int n = wave; n < 8; n += waves) {
+    half8_t A[8];  // features 32 s + 8 g + 0..7 of channel 16 n + j: two tiles of S16 ([channel % 64][feature % 4])
+#pragma unroll
+    for (int s = 0; s < 8; ++s) {
+      const int tile = ((s >> 1) * 2 + n / 4) * 16 + 8 * (s & 1) + 2 * g, ch = 16 * (n % 4) + j;
+      const u32x2_t s0 = *reinterpret_cast<const u32x2_t*>(S + (tile * 64 + ch) * 4), s1 = *reinterpret_cast<const u32x2_t*>(S + ((tile + 1) * 64 + ch) * 4);
+      A[s] = as_h8(u32x4_t{s0[0], s0[1], s1[0], s1[1]});
+    }
+    for (int r0 = 0; r0 < rows; r0 += 16) {
+      const int row = r0 + j;
+      float4_t d = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int s = 0; s < 8; ++s)
+        d = __builtin_amdgcn_mfma_f32_16x16x32_f16(A[s], *reinterpret_cast<const half8_t*>(features + min(row, rows - 1) * kFeatureStride + 32 * s + 8 * g), d, 0, 0, 0);
+      if (row < rows) {
+        const RowPlace at = row_place(row, gq);
+        const int place = (at.h * a.T + at.i) * kPartBytes;
+        if (n == 0 && g == 0) store2(out, place, den[0][row] + den[1][row], 0.0f);
+        store4(out, place + 16 + 64 * n + 16 * g, d[0], d[1], d[2], d[3]);
       }
     }
   }
 }
 
-// The splits of 16 rows joined, 16 lanes a row.  Row = ((b H_kv + g) gq + h) T + i.
-template <bool PROMPT>
+// Grid, one-dimensional: with the correction, one workgroup a (sequence, KV head) for it; then the splits, pairs fastest.  Queries are new tokens
+// at positions total + i, which see their own rows (k_new), or one token at position total - 1.  Up to 64 rows a pair.
+template <int BITS, int S, bool SLIDING>
+__global__ __launch_bounds__(64 * kMaxWaves, 2) void rows_kernel(ContextCall a) {
+  constexpr int kBlockRows = 16 / S, kAccStride = kHeadDim + 4;
+  __shared__ __align__(16) u32x4_t sMeta[kMaxWaves][64];
+  __shared__ __align__(16) float sAcc[kMaxWaves][16][kAccStride];
+  __shared__ float sM[kMaxWaves][16], sL[kMaxWaves][16];
+  __shared__ int sLast;
+  static_assert(sizeof(sAcc) >= 64 * kFeatureStride * sizeof(half_t) && sizeof(sMeta) >= 32 * kMaxContextSplits * sizeof(float) && sizeof(sM) + sizeof(sL) >= 2 * 64 * sizeof(float), "shared in turn");
+  const kvlinc_cache& c = a.cache;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = blockDim.x >> 6, g = lane >> 4;
+  const int pairs = c.B * c.H_kv, n_corr = a.corr != nullptr ? pairs : 0;
+  const bool correction = (int)blockIdx.x < n_corr;
+  const int unit = correction ? blockIdx.x : blockIdx.x - n_corr, split = correction ? 0 : unit / pairs, bh = unit - split * pairs;
+  const int b = bh / c.H_kv, kvh = bh - b * c.H_kv, gq = a.gq;
+  const Lengths len = lengths_of(c, b);
+  const bool prompt = a.k_new != nullptr;
+  const int T = prompt && a.n_new != nullptr ? min(max(a.n_new[b], 0), a.T) : a.T;
+  const int rows = T * gq;
+  if (rows == 0) return;  // (nobody arrives for such a sequence)
+  const long long head0 = (long long)b * c.H_q + (long long)kvh * gq;
+  const int total = len.total();
+  // blocks of rows that the waves share: 1, 2 or 4, whatever this sequence's number of rows
+  const int all_blocks = (a.T * gq + kBlockRows - 1) / kBlockRows, blocks = all_blocks <= 2 ? all_blocks : 4;
+  const bool direct = a.splits == 1 && a.corr == nullptr;
+  const __amdgpu_buffer_rsrc_t part = buffer_of(a.part + (direct ? 0 : head0 * a.T * a.splits * kPartStride), direct ? 0 : (long long)gq * a.T * a.splits * kPartBytes);
+
+  if (correction) {
+    correct_rows(a, b, kvh, T, rows, wave, waves, lane, reinterpret_cast<half_t*>(&sAcc[0][0][0]), reinterpret_cast<float (*)[64]>(&sM[0][0]));
+  } else {
+    const int block = wave % blocks, walker = wave / blocks, walkers = waves / blocks;
+    const int row0 = block * kBlockRows;
+    Rows st;
+    st.subset = S == 1 ? 0 : (lane & 15) / kBlockRows;
+    st.m = -INFINITY;
+    st.l = st.mid = 0.0f;
+#pragma unroll
+    for (int n = 0; n < 8; ++n) st.acc[n] = float4_t{0.f, 0.f, 0.f, 0.f};
+    if (row0 < rows) {
+      const int base = prompt ? total : total - 1;
+      {
+        const RowPlace at = row_place(min(row0 + (lane & (kBlockRows - 1)), rows - 1), gq);
+        st.p = base + at.i;
+        st.low = window_low(st.p, a.window);
+        const u32x4_t* src = reinterpret_cast<const u32x4_t*>(a.q + ((head0 + at.h) * a.T + at.i) * kHeadDim + 32 * g);
+        u32x4_t raw[4];
+        uint32_t mx = 0;
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+          raw[s] = src[s];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) mx = max(mx, max(raw[s][i] & 0x7fffu, (raw[s][i] >> 16) & 0x7fffu));
+        }
+        const auto u = __builtin_amdgcn_permlane16_swap(mx, mx, false, false);
+        mx = max(u[0], u[1]);
+        const auto v = __builtin_amdgcn_permlane32_swap(mx, mx, false, false);
+        mx = max(v[0], v[1]);
+        const int e = (int)min(max(mx >> 10, 1u), 30u) - 14;  // largest magnitude in [2^(e-1), 2^e) (subnormal rows: below 2^-14, e = -13)
+        const float down = bits_f32((uint32_t)(127 - e) << 23);
+        st.unit = bits_f32((uint32_t)(127 + e) << 23) * kLog2eSqrtD;
+        const half2_t down2 = pack_h2(down, down);
+#pragma unroll
+        for (int s = 0; s < 4; ++s) st.q[s] = as_h8(as_h2(raw[s][0]) * down2, as_h2(raw[s][1]) * down2, as_h2(raw[s][2]) * down2, as_h2(raw[s][3]) * down2);
+      }
+      // Blocks of tokens that some row sees: the new rows' (32 each), the window's (32 each), the groups.  `low` is that of the first row, the
+      // last row's position ends the new ones.
+      const int first_i = row0 / gq, last_i = min(row0 + kBlockRows - 1, rows - 1) / gq;
+      const int low = window_low(base + first_i, a.window), low_last = window_low(base + last_i, a.window);
+      const int new_from = prompt ? (a.sinks > total ? 0 : max(low - total, 0) / kRawTokens) : 0;
+      const int n_new = prompt ? (last_i + kRawTokens) / kRawTokens - new_from : 0;
+      const int win_from = a.sinks > len.nq ? 0 : min(max(low - len.nq, 0), len.nr) / kRawTokens;
+      const int n_win = (len.nr + kRawTokens - 1) / kRawTokens - win_from;
+      const int G = len.groups(), group_low = min(low / kGroup, G);
+      const int n_sink = a.window > 0 ? min((int)(((long long)a.sinks + kGroup - 1) / kGroup), group_low) : 0;
+      const int n_groups = G - group_low + n_sink;
+      const int step = walkers * a.splits;
+      int item = split * walkers + walker;
+
+      if (prompt) {
+        bool rotate = false;
+        const half_t* keys = a.k_new + (long long)bh * a.T * kHeadDim;
+        const half_t* values = a.v_new + (long long)bh * a.T * kHeadDim;
+        for (; item < n_new; item += step) {
+          const int t0 = (new_from + item) * kRawTokens;
+          float x[2][4];
+          raw_weights(st, keys + (long long)t0 * kHeadDim, total + t0, min(T - t0, kRawTokens), a.sinks, lane, x);
+          raw_values(st, values + (long long)t0 * kHeadDim, min(T - t0, kRawTokens), x, lane);
+          rotate = true;
+        }
+        if (rotate) rotate_rows(st, lane);  // from here on the accumulators are in the cache's rotated basis
+      }
+      item -= n_new;
+      const half_t* k_win = reinterpret_cast<const half_t*>(c.k_res) + (long long)bh * c.R * kHeadDim;
+      const half_t* v_win = reinterpret_cast<const half_t*>(c.v_res) + (long long)bh * c.R * kHeadDim;
+      const int quads = c.R / 4;
+      for (; item < n_win; item += step) {
+        const int t0 = (win_from + item) * kRawTokens;
+        float x[2][4];
+        raw_weights(st, k_win + t0 * kHeadDim, len.nq + t0, min(len.nr - t0, kRawTokens), a.sinks, lane, x);
+        window_values<2>(st, v_win, quads, t0 / 16, x, lane);
+      }
+      item -= n_win;
+      const uint32_t* rec0 = c.groups + (long long)bh * c.max_groups * Rec<BITS>::kWords;
+      const int newest = SLIDING && len.nq % kGroup == 0 && len.nr < kGroup ? G - 1 : -1;
+      auto group_of = [&](int it) { return it < n_sink ? it : it - n_sink + group_low; };
+      if (item < n_groups) {
+        Record<BITS> rec;
+        int gr = group_of(item);
+        load_key_part<BITS>(rec, rec0 + (long long)gr * Rec<BITS>::kWords, lane);
+        load_value_part<BITS>(rec, rec0 + (long long)gr * Rec<BITS>::kWords, lane);
+        for (;;) {
+          const int at = gr * kGroup, count = min(len.nq - at, kGroup);
+          const bool masked = count < kGroup || (at < low_last && at + kGroup > a.sinks), more = item + step < n_groups;
+          const int e = put_meta<BITS>(rec, sMeta[wave], lane);
+          float x[8 / S][4], exponent_base;
+          group_scores<BITS, S>(st, rec, sMeta[wave], at, count, masked, a.sinks, lane, x, exponent_base);
+          const int next = more ? group_of(item + step) : gr;
+          if (more) load_key_part<BITS>(rec, rec0 + (long long)next * Rec<BITS>::kWords, lane);
+          group_values<BITS, S, SLIDING>(st, rec, sMeta[wave], e, x, exponent_base, gr == newest ? len.nr : kGroup, v_win, quads, lane);
+          if (!more) break;
+          load_value_part<BITS>(rec, rec0 + (long long)next * Rec<BITS>::kWords, lane);
+          item += step;
+          gr = next;
+        }
+      }
+    }
+
+    // ---- the waves joined ----
+    {
+      float x, y;
+      pair_across<16>(st.l, x, y);
+      pair_across<32>(x + y, x, y);
+      const float l = x + y;
+      pair_across<16>(st.mid, x, y);
+      pair_across<32>(x + y, x, y);
+      const float mid = x + y;
+      if (g == 0) { sM[wave][lane] = st.m; sL[wave][lane] = l; }
+#pragma unroll
+      for (int n = 0; n < 8; ++n) {
+        const float4_t v = st.acc[n];
+        *reinterpret_cast<float4_t*>(&sAcc[wave][lane & 15][16 * n + 4 * g]) = float4_t{v[0] + mid, v[1] + mid, v[2] + mid, v[3] + mid};
+      }
+    }
+    __syncthreads();
+    const int ch = 8 * (lane & 15);
+    for (int slot = tid >> 4; slot < blocks * kBlockRows; slot += blockDim.x >> 4) {
+      const int blk = slot / kBlockRows, r = slot % kBlockRows, row = slot;
+      if (row >= rows) continue;  // (the 16 lanes of a row go together)
+      float M = -INFINITY;
+      for (int w = blk; w < waves; w += blocks)
+#pragma unroll
+        for (int u = 0; u < S; ++u) M = fmaxf(M, sM[w][u * kBlockRows + r]);
+      float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, L = 0.0f;
+      if (M != -INFINITY) {
+        for (int w = blk; w < waves; w += blocks)
+#pragma unroll
+          for (int u = 0; u < S; ++u) {
+            const int col = u * kBlockRows + r;
+            const float f = __builtin_amdgcn_exp2f(sM[w][col] - M);  // 0 for a column that has seen nothing
+            L = fmaf(f, sL[w][col], L);
+            const float4_t u0 = *reinterpret_cast<const float4_t*>(&sAcc[w][col][ch]), u1 = *reinterpret_cast<const float4_t*>(&sAcc[w][col][ch + 4]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              o[i] = fmaf(f, u0[i], o[i]);
+              o[4 + i] = fmaf(f, u1[i], o[4 + i]);
+            }
+          }
+      }
+      const RowPlace at = row_place(row, gq);
+      if (direct) {
+        finish_row(o, L, lane, a.out + ((head0 + at.h) * a.T + at.i) * kHeadDim);
+      } else {
+        const int place = ((at.h * a.T + at.i) * a.splits + split) * kPartBytes;
+        if ((lane & 15) == 0) store2(part, place, M, L);
+        store4(part, place + 16 + 4 * ch, o[0], o[1], o[2], o[3]);
+        store4(part, place + 32 + 4 * ch, o[4], o[5], o[6], o[7]);
+      }
+    }
+    if (direct) return;
+  }
+
+  // ---- whoever arrives last at the pair's counter joins its splits and the correction, and clears the counter ----
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wave's results are where everybody sees them
+  __syncthreads();
+  if (tid == 0) sLast = __hip_atomic_fetch_add(c.split_done + bh, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM) == a.splits - 1 + (a.corr != nullptr ? 1 : 0);
+  __syncthreads();
+  if (!__builtin_amdgcn_readfirstlane(sLast)) return;
+  const __amdgpu_buffer_rsrc_t corr = buffer_of(a.corr + (a.corr != nullptr ? head0 * a.T * kPartStride : 0), a.corr != nullptr ? (long long)gq * a.T * kPartBytes : 0);
+  float* weights = reinterpret_cast<float*>(&sMeta[0][0]) + kMaxContextSplits * (tid >> 4);
+  for (int row = tid >> 4; row < rows; row += blockDim.x >> 4) {
+    const RowPlace at = row_place(row, gq);
+    const int place = at.h * a.T + at.i, ch = 8 * (lane & 15);
+    float c_d = 0.0f;
+    float4_t c0 = {0.f, 0.f, 0.f, 0.f}, c1 = c0;
+    if (a.corr != nullptr) {
+      c_d = load2(corr, place * kPartBytes)[0];
+      c0 = load4(corr, place * kPartBytes + 16 + 4 * ch);
+      c1 = load4(corr, place * kPartBytes + 32 + 4 * ch);
+    }
+    float o[8], L, M;
+    join_row(part, place * a.splits * kPartBytes, a.splits, weights, lane, o, L, M);
+    if (a.corr != nullptr) add_correction(o, L, M, c_d, c0, c1);
+    finish_row(o, L, lane, a.out + ((head0 + at.h) * a.T + at.i) * kHeadDim);
+  }
+  if (tid == 0) c.split_done[bh] = 0;
+}
+
+// The splits of a launch over blocks of 256 rows joined, 16 rows a workgroup.  Row = (b H_q + h) T + i.
 __global__ __launch_bounds__(256) void join_kernel(ContextCall a, long long n_rows) {
-  const int lane = threadIdx.x & 63;
+  const int lane = threadIdx.x & 63, ch = 8 * (lane & 15);
   const long long place = (long long)blockIdx.x * 16 + (threadIdx.x >> 4);
   if (place >= n_rows) return;
-  if (PROMPT && a.n_new != nullptr) {
+  if (a.n_new != nullptr) {
     const long long h = place / a.T;
     if (place - h * a.T >= a.n_new[h / a.cache.H_q]) return;
   }
@@ -611,40 +797,45 @@ __global__ __launch_bounds__(256) void join_kernel(ContextCall a, long long n_ro
   for (int s = 0; s < a.splits; ++s) M = fmaxf(M, p[s * kPartStride]);
   float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, L = 0.0f;
   if (M != -INFINITY)
+#pragma unroll 4
     for (int s = 0; s < a.splits; ++s) {
       const float* src = p + s * kPartStride;
       const float f = __builtin_amdgcn_exp2f(src[0] - M);
       L = fmaf(f, src[1], L);
-      const float4 u0 = *reinterpret_cast<const float4*>(src + 4 + 8 * (lane & 15)), u1 = *reinterpret_cast<const float4*>(src + 8 + 8 * (lane & 15));
-      o[0] = fmaf(f, u0.x, o[0]); o[1] = fmaf(f, u0.y, o[1]); o[2] = fmaf(f, u0.z, o[2]); o[3] = fmaf(f, u0.w, o[3]);
-      o[4] = fmaf(f, u1.x, o[4]); o[5] = fmaf(f, u1.y, o[5]); o[6] = fmaf(f, u1.z, o[6]); o[7] = fmaf(f, u1.w, o[7]);
+      const float4_t u0 = *reinterpret_cast<const float4_t*>(src + 4 + ch), u1 = *reinterpret_cast<const float4_t*>(src + 8 + ch);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        o[i] = fmaf(f, u0[i], o[i]);
+        o[4 + i] = fmaf(f, u1[i], o[4 + i]);
+      }
     }
-  finish_row(o, L, M, a.corr != nullptr ? a.corr + place * kPartStride : nullptr, lane, a.out + place * kHeadDim);
+  if (a.corr != nullptr) {
+    const float* corr = a.corr + place * kPartStride;
+    add_correction(o, L, M, corr[0], *reinterpret_cast<const float4_t*>(corr + 4 + ch), *reinterpret_cast<const float4_t*>(corr + 8 + ch));
+  }
+  finish_row(o, L, lane, a.out + place * kHeadDim);
 }
 
 }  // namespace
 
-template <int BITS, int NR, bool PROMPT>
-static void launch_rows_of(const ContextCall& a, dim3 grid, hipStream_t stream) {
+template <int BITS, int S>
+static void launch_rows_of(const ContextCall& a, dim3 grid, int waves, hipStream_t stream) {
   const bool sliding = (a.cache.flags & KVLINC_FLAG_SLIDING_VALUES) != 0;
-  if (sliding) hipLaunchKernelGGL((rows_kernel<BITS, NR, PROMPT, true>), grid, dim3(64 * kRowWaves), 0, stream, a);
-  else hipLaunchKernelGGL((rows_kernel<BITS, NR, PROMPT, false>), grid, dim3(64 * kRowWaves), 0, stream, a);
+  if (sliding) hipLaunchKernelGGL((rows_kernel<BITS, S, true>), grid, dim3(64 * waves), 0, stream, a);
+  else hipLaunchKernelGGL((rows_kernel<BITS, S, false>), grid, dim3(64 * waves), 0, stream, a);
 }
 
-int launch_rows(const ContextCall& a, bool prompt, hipStream_t stream) {
-  const long long rows = (long long)a.T * a.gq;
-  const dim3 grid((unsigned)(a.splits * (long long)a.cache.B * a.cache.H_kv * ((rows + 15) / 16)));
-  if (a.cache.bits == 2) prompt ? launch_rows_of<2, 1, true>(a, grid, stream) : launch_rows_of<2, 1, false>(a, grid, stream);
-  else prompt ? launch_rows_of<4, 1, true>(a, grid, stream) : launch_rows_of<4, 1, false>(a, grid, stream);
-  if (hipGetLastError() != hipSuccess) return KVLINC_EHIP;
-  return a.splits > 1 ? launch_join(a, prompt, stream) : KVLINC_OK;
+int launch_rows(const ContextCall& a, int waves, hipStream_t stream) {
+  const int rows = a.T * a.gq;
+  const dim3 grid((unsigned)((long long)a.cache.B * a.cache.H_kv * (a.splits + (a.corr != nullptr ? 1 : 0))));
+  if (a.cache.bits == 2) rows <= 4 ? launch_rows_of<2, 4>(a, grid, waves, stream) : rows <= 8 ? launch_rows_of<2, 2>(a, grid, waves, stream) : launch_rows_of<2, 1>(a, grid, waves, stream);
+  else rows <= 4 ? launch_rows_of<4, 4>(a, grid, waves, stream) : rows <= 8 ? launch_rows_of<4, 2>(a, grid, waves, stream) : launch_rows_of<4, 1>(a, grid, waves, stream);
+  return hipGetLastError() == hipSuccess ? KVLINC_OK : KVLINC_EHIP;
 }
 
-int launch_join(const ContextCall& a, bool prompt, hipStream_t stream) {
+int launch_join(const ContextCall& a, hipStream_t stream) {
   const long long n = (long long)a.cache.B * a.cache.H_q * a.T;
-  const dim3 grid((unsigned)((n + 15) / 16));
-  if (prompt) hipLaunchKernelGGL(join_kernel<true>, grid, dim3(256), 0, stream, a, n);
-  else hipLaunchKernelGGL(join_kernel<false>, grid, dim3(256), 0, stream, a, n);
+  hipLaunchKernelGGL(join_kernel, dim3((unsigned)((n + 15) / 16)), dim3(256), 0, stream, a, n);
   return hipGetLastError() == hipSuccess ? KVLINC_OK : KVLINC_EHIP;
 }
 
