@@ -27,8 +27,14 @@ __device__ __forceinline__ half8_t as_h8(half2_t a, half2_t b, half2_t c, half2_
 struct Nibbles {
   uint32_t first, second;
 };
+__device__ __forceinline__ uint32_t code_bits() {
+  uint32_t m = 0xAAAAAAAAu;
+  asm("" : "+s"(m));  // (opaque, so that taking the code's bits and setting the others is one bit-field insert)
+  return m;
+}
 __device__ __forceinline__ Nibbles nibbles_of(uint32_t w) {
-  return Nibbles{(w & 0xAAAAAAAAu) | 0x11111111u, ((w << 1) & 0xAAAAAAAAu) | 0x11111111u};
+  const uint32_t m = code_bits();
+  return Nibbles{0x11111111u ^ (m & (w ^ 0x11111111u)), 0x11111111u ^ (m & ((w << 1) ^ 0x11111111u))};
 }
 // Byte SEL of such nibbles, two codes, as binary16: (code - 1.5) scale, scale a power of two.  One instruction, exact.
 template <int SEL>
