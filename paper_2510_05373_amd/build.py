@@ -24,13 +24,14 @@ OBJECTS = {
     "kvlinc_decode": ("kvlinc_decode.hip", []),
     "kvlinc_context_api": ("kvlinc_context_api.hip", []),
     "kvlinc_rows": ("kvlinc_rows.hip", []),
+    "kvlinc_windowed": ("kvlinc_windowed.hip", []),
     "kvlinc_prompt": ("kvlinc_prompt.hip", []),
     "kvlinc_dense": ("kvlinc_dense.hip", []),
     "kvlinc_prompt_correction": ("kvlinc_prompt_correction.hip", []),
     "kvlinc_read": ("kvlinc_read.hip", []),
     "kvlinc_decode_nolooks": ("kvlinc_decode.hip", ["-DKVLINC_LOOKS=0"]),
 }
-CONTEXT = ["kvlinc_context_api", "kvlinc_rows", "kvlinc_prompt", "kvlinc_dense", "kvlinc_prompt_correction", "kvlinc_read"]
+CONTEXT = ["kvlinc_context_api", "kvlinc_rows", "kvlinc_windowed", "kvlinc_prompt", "kvlinc_dense", "kvlinc_prompt_correction", "kvlinc_read"]
 LIBRARIES = {
     LIB_PATH: ["kvlinc_api", "kvlinc_append", "kvlinc_decode", *CONTEXT],
     NOLOOKS_PATH: ["kvlinc_api", "kvlinc_append", "kvlinc_decode_nolooks", *CONTEXT],

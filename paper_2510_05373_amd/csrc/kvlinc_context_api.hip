@@ -83,6 +83,19 @@ int check_prompt(const kvlinc_cache* c, int T, int window, int sinks) {
   if (c->S16 != nullptr && (window != 0 || (c->flags & KVLINC_FLAG_ALG1_LITERAL) != 0)) return KVLINC_EINVAL;
   return KVLINC_OK;
 }
+// Windowed decode: two workgroups of four waves a compute unit; a split has a group for each wave.
+ContextPlan plan_windowed(const kvlinc_cache& c, int window, int sinks, int max_context) {
+  const long long pairs = (long long)c.B * c.H_kv, groups = groups_met(c, 1, window, sinks, max_context);
+  long long s = 512 / pairs, most = (groups + 3) / 4;
+  if (s > most) s = most;
+  if (s > kMaxContextSplits) s = kMaxContextSplits;
+  if (s < 1) s = 1;
+  ContextPlan p{};
+  p.splits = (int)s;
+  p.part_floats = s > 1 ? (size_t)c.B * c.H_q * s * kPartStride : 0;
+  return p;
+}
+
 int check_windowed(const kvlinc_cache* c, int window, int sinks) {
   const int rc = kvlinc_cache_validate(c);
   if (rc != KVLINC_OK) return rc;
@@ -144,7 +157,7 @@ int kvlinc_prompt_attention(const kvlinc_cache* cache, const kvlinc_half* q, con
 }
 
 size_t kvlinc_decode_windowed_workspace_bytes(const kvlinc_cache* cache, int32_t window, int32_t sinks, int32_t max_context) {
-  return check_windowed(cache, window, sinks) == KVLINC_OK ? plan_call(*cache, 1, window, sinks, max_context).bytes() : 0;
+  return check_windowed(cache, window, sinks) == KVLINC_OK ? plan_windowed(*cache, window, sinks, max_context).bytes() : 0;
 }
 
 int kvlinc_decode_attention_windowed(const kvlinc_cache* cache, const kvlinc_half* q, int32_t window, int32_t sinks, kvlinc_half* out,
@@ -152,9 +165,9 @@ int kvlinc_decode_attention_windowed(const kvlinc_cache* cache, const kvlinc_hal
   const int rc = check_windowed(cache, window, sinks);
   if (rc != KVLINC_OK) return rc;
   if (bad_address(q, 16) || bad_address(out, 16)) return KVLINC_EINVAL;
-  const ContextPlan p = plan_call(*cache, 1, window, sinks, max_context);
+  const ContextPlan p = plan_windowed(*cache, window, sinks, max_context);
   if (bad_workspace(workspace, workspace_bytes, p.bytes())) return KVLINC_EWORKSPACE;
-  return launch_rows(make_call(*cache, q, 1, window, sinks, out, workspace, p), p.waves, static_cast<hipStream_t>(stream));
+  return launch_windowed(make_call(*cache, q, 1, window, sinks, out, workspace, p), static_cast<hipStream_t>(stream));
 }
 
 int kvlinc_cache_read(const kvlinc_cache* cache, const int32_t* first, int32_t T, void* k_out, void* v_out, int32_t dtype,

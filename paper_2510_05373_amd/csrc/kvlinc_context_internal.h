@@ -32,6 +32,7 @@ __host__ __device__ inline int window_base(int total, int window) {
 }
 
 int launch_rows(const ContextCall& a, int waves, hipStream_t stream);  // up to 64 rows of a KV head; waves of a workgroup: 4 or 8
+int launch_windowed(const ContextCall& a, hipStream_t stream);
 int launch_tiles(const ContextCall& a, hipStream_t stream);
 int launch_dense(const ContextCall& a, hipStream_t stream);
 int launch_join(const ContextCall& a, hipStream_t stream);

@@ -1,4 +1,4 @@
-// Attention of few query rows (up to 64 of a KV head), or of one query a sequence behind a sliding window, read directly from the packed cache.
+// Prompt attention of few query rows (up to 64 of a KV head), read directly from the packed cache.
 //
 // One launch.  Rows of a (sequence, KV head) are (token i, head h) pairs, row = i gq + h.  A workgroup has all rows of one and a split of its
 // tokens; a wave takes a block of 16 rows and blocks of tokens on its own, without a barrier: groups of 128 packed tokens, or 32 raw ones (the
@@ -18,7 +18,7 @@
 #include <hip/hip_runtime.h>
 
 #include "kvlinc_codes.h"
-#include "kvlinc_context_internal.h"
+#include "kvlinc_join.h"
 
 namespace kvlinc {
 namespace {
@@ -374,87 +374,6 @@ __device__ __forceinline__ void rotate_rows(Rows& st, int lane) {
       }
 }
 
-// ---- results that one workgroup writes and another reads inside the launch ----------------------------------------------------------------
-// Stores and loads that go past the caches that are not coherent across the chip (sc0, sc1).  The partial results, and the correction's, of a
-// (sequence, KV head) lie together: [head][T][splits] resp. [head][T] rows of kPartStride floats.
-constexpr int kCoherent = 1 | 16, kPartBytes = 4 * kPartStride;
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(float* p, long long bytes) { return __builtin_amdgcn_make_buffer_rsrc(p, 0, (int)bytes, 0x00027000); }
-__device__ __forceinline__ void store4(__amdgpu_buffer_rsrc_t r, int at, float a, float b, float c, float d) {
-  __builtin_amdgcn_raw_buffer_store_b128(u32x4_t{__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b), __builtin_bit_cast(uint32_t, c), __builtin_bit_cast(uint32_t, d)}, r,
-                                         at, 0, kCoherent);
-}
-__device__ __forceinline__ void store2(__amdgpu_buffer_rsrc_t r, int at, float a, float b) {
-  __builtin_amdgcn_raw_buffer_store_b64(u32x2_t{__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b)}, r, at, 0, kCoherent);
-}
-__device__ __forceinline__ float4_t load4(__amdgpu_buffer_rsrc_t r, int at) { return __builtin_bit_cast(float4_t, __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, kCoherent)); }
-__device__ __forceinline__ float2v_t load2(__amdgpu_buffer_rsrc_t r, int at) { return __builtin_bit_cast(float2v_t, __builtin_amdgcn_raw_buffer_load_b64(r, at, 0, kCoherent)); }
-
-// One output row from its 128 numerators (16 lanes, 8 neighbouring channels each): normalised, rotated back.
-__device__ __forceinline__ void finish_row(float (&a)[8], float l, int lane, half_t* out) {
-  lane8_butterflies(a);
-  row16_butterflies<8>(a, lane);
-  const float inv = l > 0.0f ? kInvSqrtD / l : 0.0f;
-  u32x4_t h;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) h[i] = as_u32(pack_h2(a[2 * i] * inv, a[2 * i + 1] * inv));
-  *reinterpret_cast<u32x4_t*>(out + 8 * (lane & 15)) = h;
-}
-// The correction {C_d, -, -, -, C_n[128]} added as e^0 terms (Eq. 5), both sides relative to max(m, 0).
-__device__ __forceinline__ void add_correction(float (&a)[8], float& l, float m, float c_d, float4_t c0, float4_t c1) {
-  const float to = fmaxf(m, 0.0f), f = __builtin_amdgcn_exp2f(m - to), w = __builtin_amdgcn_exp2f(-to);
-  l = fmaf(w, c_d, l * f);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    a[i] = fmaf(w, c0[i], a[i] * f);
-    a[4 + i] = fmaf(w, c1[i], a[4 + i] * f);
-  }
-}
-constexpr int kMaxContextSplits = 32;
-// The splits of one row joined by 16 lanes: weights by lane, two splits each, then the numerators, eight splits under way at a time.
-__device__ __forceinline__ void join_row(__amdgpu_buffer_rsrc_t part, int at, int splits, float* weights /* LDS, 32 */, int lane, float (&o)[8], float& L, float& M) {
-  const int j = lane & 15;
-  float2v_t ml[2];
-#pragma unroll
-  for (int u = 0; u < 2; ++u) ml[u] = load2(part, at + min(j + 16 * u, splits - 1) * kPartBytes);
-  float m[2] = {j < splits ? ml[0][0] : -INFINITY, j + 16 < splits ? ml[1][0] : -INFINITY};
-  M = fmaxf(m[0], m[1]);
-  M = fmaxf(M, dpp_f<kRowRor1>(M));
-  M = fmaxf(M, dpp_f<kRowRor2>(M));
-  M = fmaxf(M, dpp_f<kRowRor4>(M));
-  M = fmaxf(M, dpp_f<kRowRor8>(M));
-  L = 0.0f;
-#pragma unroll
-  for (int u = 0; u < 2; ++u) {
-    const float w = m[u] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[u] - M);
-    weights[j + 16 * u] = w;
-    L = fmaf(w, ml[u][1], L);
-  }
-  L += dpp_f<kRowRor1>(L);
-  L += dpp_f<kRowRor2>(L);
-  L += dpp_f<kRowRor4>(L);
-  L += dpp_f<kRowRor8>(L);
-  __builtin_amdgcn_wave_barrier();  // (the 16 lanes are of one wave)
-#pragma unroll
-  for (int i = 0; i < 8; ++i) o[i] = 0.0f;
-  for (int s0 = 0; s0 < splits; s0 += 8) {
-    float4_t u[8][2];
-#pragma unroll
-    for (int s = 0; s < 8; ++s)
-#pragma unroll
-      for (int k = 0; k < 2; ++k) u[s][k] = load4(part, at + min(s0 + s, splits - 1) * kPartBytes + 16 + 32 * j + 16 * k);
-#pragma unroll
-    for (int s = 0; s < 8; ++s) {
-      const float w = weights[s0 + s];  // (0 beyond the last)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        o[i] = fmaf(w, u[s][0][i], o[i]);
-        o[4 + i] = fmaf(w, u[s][1][i], o[4 + i]);
-      }
-    }
-  }
-  __builtin_amdgcn_wave_barrier();
-}
-
 struct RowPlace {
   int i, h;  // token of the call, head of the KV head
 };
@@ -575,8 +494,7 @@ __device__ __forceinline__ void correct_rows(const ContextCall& a, int b, int kv
   }
 }
 
-// Grid, one-dimensional: with the correction, one workgroup a (sequence, KV head) for it; then the splits, pairs fastest.  Queries are new tokens
-// at positions total + i, which see their own rows (k_new), or one token at position total - 1.  Up to 64 rows a pair.
+// Grid, one-dimensional: with the correction, one workgroup a (sequence, KV head) for it; then the splits, pairs fastest.  Up to 64 rows a pair.
 template <int BITS, int S, bool SLIDING>
 __global__ __launch_bounds__(64 * kMaxWaves, 2) void rows_kernel(ContextCall a) {
   constexpr int kBlockRows = 16 / S, kAccStride = kHeadDim + 4;
@@ -592,8 +510,7 @@ __global__ __launch_bounds__(64 * kMaxWaves, 2) void rows_kernel(ContextCall a) 
   const int unit = correction ? blockIdx.x : blockIdx.x - n_corr, split = correction ? 0 : unit / pairs, bh = unit - split * pairs;
   const int b = bh / c.H_kv, kvh = bh - b * c.H_kv, gq = a.gq;
   const Lengths len = lengths_of(c, b);
-  const bool prompt = a.k_new != nullptr;
-  const int T = prompt && a.n_new != nullptr ? min(max(a.n_new[b], 0), a.T) : a.T;
+  const int T = a.n_new != nullptr ? min(max(a.n_new[b], 0), a.T) : a.T;
   const int rows = T * gq;
   if (rows == 0) return;  // (nobody arrives for such a sequence)
   const long long head0 = (long long)b * c.H_q + (long long)kvh * gq;
@@ -615,10 +532,9 @@ __global__ __launch_bounds__(64 * kMaxWaves, 2) void rows_kernel(ContextCall a) 
 #pragma unroll
     for (int n = 0; n < 8; ++n) st.acc[n] = float4_t{0.f, 0.f, 0.f, 0.f};
     if (row0 < rows) {
-      const int base = prompt ? total : total - 1;
       {
         const RowPlace at = row_place(min(row0 + (lane & (kBlockRows - 1)), rows - 1), gq);
-        st.p = base + at.i;
+        st.p = total + at.i;
         st.low = window_low(st.p, a.window);
         const u32x4_t* src = reinterpret_cast<const u32x4_t*>(a.q + ((head0 + at.h) * a.T + at.i) * kHeadDim + 32 * g);
         u32x4_t raw[4];
@@ -643,9 +559,9 @@ __global__ __launch_bounds__(64 * kMaxWaves, 2) void rows_kernel(ContextCall a) 
       // Blocks of tokens that some row sees: the new rows' (32 each), the window's (32 each), the groups.  `low` is that of the first row, the
       // last row's position ends the new ones.
       const int first_i = row0 / gq, last_i = min(row0 + kBlockRows - 1, rows - 1) / gq;
-      const int low = window_low(base + first_i, a.window), low_last = window_low(base + last_i, a.window);
-      const int new_from = prompt ? (a.sinks > total ? 0 : max(low - total, 0) / kRawTokens) : 0;
-      const int n_new = prompt ? (last_i + kRawTokens) / kRawTokens - new_from : 0;
+      const int low = window_low(total + first_i, a.window), low_last = window_low(total + last_i, a.window);
+      const int new_from = a.sinks > total ? 0 : max(low - total, 0) / kRawTokens;
+      const int n_new = (last_i + kRawTokens) / kRawTokens - new_from;
       const int win_from = a.sinks > len.nq ? 0 : min(max(low - len.nq, 0), len.nr) / kRawTokens;
       const int n_win = (len.nr + kRawTokens - 1) / kRawTokens - win_from;
       const int G = len.groups(), group_low = min(low / kGroup, G);
@@ -654,7 +570,7 @@ __global__ __launch_bounds__(64 * kMaxWaves, 2) void rows_kernel(ContextCall a) 
       const int step = walkers * a.splits;
       int item = split * walkers + walker;
 
-      if (prompt) {
+      {
         bool rotate = false;
         const half_t* keys = a.k_new + (long long)bh * a.T * kHeadDim;
         const half_t* values = a.v_new + (long long)bh * a.T * kHeadDim;
