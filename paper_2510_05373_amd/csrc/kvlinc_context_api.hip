@@ -40,7 +40,7 @@ ContextPlan plan_call(const kvlinc_cache& c, int T, int window, int sinks, int m
   if (p.kind == ContextPlan::kRows) {
     // Two workgroups of four waves a compute unit, or, where the pairs are few, one of eight: fewer splits to join.
     p.waves = pairs <= 64 ? 8 : 4;
-    s = (p.waves == 8 ? 256 : 512) / pairs;
+    s = (p.waves == 8 ? 256 : 512) / pairs - (c.S16 != nullptr ? 1 : 0);  // (the correction's workgroups are some of them)
     most = (groups + p.waves - 1) / p.waves;
   } else {
     s = 256 / (pairs * ((rows + 255) / 256));
