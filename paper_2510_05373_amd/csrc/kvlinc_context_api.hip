@@ -43,8 +43,11 @@ ContextPlan plan_call(const kvlinc_cache& c, int T, int window, int sinks, int m
     s = (p.waves == 8 ? 256 : 512) / pairs - (c.S16 != nullptr ? 1 : 0);  // (the correction's workgroups are some of them)
     most = (groups + p.waves - 1) / p.waves;
   } else {
+    // One workgroup a compute unit.  A split of less than 8 tiles costs more to write and join than it saves.  (Without a bound the cache is
+    // taken to have room for the rows, no more: that is a guess for the number of splits, not for what is reserved.)
+    const long long cached = max_context > 0 ? groups * kGroup : groups * kGroup - T;
     s = 256 / (pairs * ((rows + 255) / 256));
-    most = (groups + 1) / 2;
+    most = ((cached < 0 ? 0 : cached) + T / 2) / (8 * kTileTokens);  // (causal: half of the rows on average)
   }
   if (s > most) s = most;
   if (s > kMaxContextSplits) s = kMaxContextSplits;
