@@ -43,13 +43,24 @@ __device__ __forceinline__ void add_correction(float (&a)[8], float& l, float m,
   }
 }
 constexpr int kMaxContextSplits = 32;
-// The splits of one row joined by 16 lanes: weights by lane, two splits each, then the numerators, eight splits under way at a time.
+// The splits of one row joined by 16 lanes: weights by lane, two splits each, and the numerators, kSplitsAhead splits under way at a time, the
+// first of them requested together with the maxima.  (A trip to memory, past the caches, is about 2 us of a launch; 16 splits at a time spilled, and
+// drafts took 15 % longer.)
+constexpr int kSplitsAhead = 8;
 __device__ __forceinline__ void join_row(__amdgpu_buffer_rsrc_t part, int at, int splits, float* weights /* LDS, 32 */, int lane, float (&o)[8], float& L, float& M) {
   const int j = lane & 15;
+  float4_t u[kSplitsAhead][2];
+  auto request = [&](int s0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int s = 0; s < kSplitsAhead; ++s)
+#pragma unroll
+      for (int k = 0; k < 2; ++k) u[s][k] = load4(part, at + min(s0 + s, splits - 1) * kPartBytes + 16 + 32 * j + 16 * k);
+  };
   float2v_t ml[2];
 #pragma unroll
-  for (int u = 0; u < 2; ++u) ml[u] = load2(part, at + min(j + 16 * u, splits - 1) * kPartBytes);
-  float m[2] = {j < splits ? ml[0][0] : -INFINITY, j + 16 < splits ? ml[1][0] : -INFINITY};
+  for (int k = 0; k < 2; ++k) ml[k] = load2(part, at + min(j + 16 * k, splits - 1) * kPartBytes);
+  request(0);
+  const float m[2] = {j < splits ? ml[0][0] : -INFINITY, j + 16 < splits ? ml[1][0] : -INFINITY};
   M = fmaxf(m[0], m[1]);
   M = fmaxf(M, dpp_f<kRowRor1>(M));
   M = fmaxf(M, dpp_f<kRowRor2>(M));
@@ -57,10 +68,10 @@ __device__ __forceinline__ void join_row(__amdgpu_buffer_rsrc_t part, int at, in
   M = fmaxf(M, dpp_f<kRowRor8>(M));
   L = 0.0f;
 #pragma unroll
-  for (int u = 0; u < 2; ++u) {
-    const float w = m[u] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[u] - M);
-    weights[j + 16 * u] = w;
-    L = fmaf(w, ml[u][1], L);
+  for (int k = 0; k < 2; ++k) {
+    const float w = m[k] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[k] - M);
+    weights[j + 16 * k] = w;
+    L = fmaf(w, ml[k][1], L);
   }
   L += dpp_f<kRowRor1>(L);
   L += dpp_f<kRowRor2>(L);
@@ -69,14 +80,10 @@ __device__ __forceinline__ void join_row(__amdgpu_buffer_rsrc_t part, int at, in
   __builtin_amdgcn_wave_barrier();  // (the 16 lanes are of one wave)
 #pragma unroll
   for (int i = 0; i < 8; ++i) o[i] = 0.0f;
-  for (int s0 = 0; s0 < splits; s0 += 8) {
-    float4_t u[8][2];
+#pragma unroll 1
+  for (int s0 = 0;;) {
 #pragma unroll
-    for (int s = 0; s < 8; ++s)
-#pragma unroll
-      for (int k = 0; k < 2; ++k) u[s][k] = load4(part, at + min(s0 + s, splits - 1) * kPartBytes + 16 + 32 * j + 16 * k);
-#pragma unroll
-    for (int s = 0; s < 8; ++s) {
+    for (int s = 0; s < kSplitsAhead; ++s) {
       const float w = weights[s0 + s];  // (0 beyond the last)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -84,6 +91,9 @@ __device__ __forceinline__ void join_row(__amdgpu_buffer_rsrc_t part, int at, in
         o[4 + i] = fmaf(w, u[s][1][i], o[4 + i]);
       }
     }
+    s0 += kSplitsAhead;
+    if (s0 >= splits) break;
+    request(s0);
   }
   __builtin_amdgcn_wave_barrier();
 }

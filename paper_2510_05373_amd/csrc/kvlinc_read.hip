@@ -29,22 +29,35 @@ __device__ __forceinline__ BF16 rounded<BF16>(float v) {  // to nearest even (fi
   return BF16{(uint16_t)((u + 0x7fffu + ((u >> 16) & 1u)) >> 16)};
 }
 
-// 32 rows of a wave in LDS, 16 bytes more than a row apart
+// 16 rows of a wave in LDS, 16 bytes more than a row apart; a wave fills and stores them twice for its 32 tokens (twice the rows: half the
+// workgroups on a compute unit).
+constexpr int kRowsHeld = 16;
 template <typename OUT>
 struct WaveRows {
   static constexpr int kStride = kHeadDim + 16 / sizeof(OUT);
-  OUT x[32][kStride];
+  OUT x[kRowsHeld][kStride];
 };
-// token_of(r): position of row r; written if from <= position < to
+// Where rows go: those of positions from .. to - 1.  Stores past the caches: a large range written through them takes nearly twice as long (16
+// sequences of 8k tokens, 8 heads: 246 us, 140 so), and rows that the next launch reads (kvlinc_dense.hip) are read no slower.
+template <typename OUT>
+struct Target {
+  OUT* out;
+  long long first;
+  int from, to, at;  // at: position of the block
+};
 template <typename OUT, typename F>
-__device__ __forceinline__ void store_rows(const WaveRows<OUT>& rows, OUT* out, long long first, int from, int to, int lane, F token_of) {
+__device__ __forceinline__ void store_rows(const WaveRows<OUT>& rows, const Target<OUT>& d, int lane, F token_of) {  // token_of(r): of row r, in the block
   constexpr int kLanes = kHeadDim * sizeof(OUT) / 16;  // lanes a row takes, 16 bytes each
+  __builtin_amdgcn_wave_barrier();  // (a wave's LDS instructions stay in order)
 #pragma unroll
-  for (int r0 = 0; r0 < 32; r0 += 64 / kLanes) {
-    const int r = r0 + lane / kLanes, t = token_of(r);
-    if (t >= from && t < to)
-      reinterpret_cast<uint4*>(out + (t - first) * kHeadDim)[lane % kLanes] = reinterpret_cast<const uint4*>(&rows.x[r][0])[lane % kLanes];
+  for (int r0 = 0; r0 < kRowsHeld; r0 += 64 / kLanes) {
+    const int r = r0 + lane / kLanes, t = d.at + token_of(r);
+    if (t < d.from || t >= d.to) continue;
+    const u32x4_t v = reinterpret_cast<const u32x4_t*>(&rows.x[r][0])[lane % kLanes];
+    u32x4_t* dst = reinterpret_cast<u32x4_t*>(d.out + (t - d.first) * kHeadDim) + lane % kLanes;
+    __builtin_nontemporal_store(v, dst);
   }
+  __builtin_amdgcn_wave_barrier();
 }
 
 template <int BITS, int SEL>
@@ -56,7 +69,7 @@ __device__ __forceinline__ void key_pairs(const uint32_t (&e)[BITS / 2], const u
 
 // Keys: wave w has tokens 32 w .. 32 w + 31; a lane two of them, 32 channels each.
 template <int BITS, typename OUT>
-__device__ __forceinline__ void read_keys(const uint32_t* rec, WaveRows<OUT>& rows, int wave, int lane) {
+__device__ __forceinline__ void read_keys(const uint32_t* rec, WaveRows<OUT>& rows, const Target<OUT>& to, int wave, int lane) {
   const int j = lane & 15, g = lane >> 4;
   uint32_t s[16], z[16];
 #pragma unroll
@@ -82,10 +95,11 @@ __device__ __forceinline__ void read_keys(const uint32_t* rec, WaveRows<OUT>& ro
       const int at = 8 * (q % 2) + 4 * u;
       if (u == 0) { key_pairs<BITS, 0>(e, s, z, at, v); key_pairs<BITS, 1>(e, s, z, at, v); key_pairs<BITS, 2>(e, s, z, at, v); key_pairs<BITS, 3>(e, s, z, at, v); }
       else { key_pairs<BITS, 0>(o, s, z, at, v); key_pairs<BITS, 1>(o, s, z, at, v); key_pairs<BITS, 2>(o, s, z, at, v); key_pairs<BITS, 3>(o, s, z, at, v); }
-      OUT* dst = &rows.x[16 * (q / 2) + j][32 * g + 16 * (q % 2) + 8 * u];
+      OUT* dst = &rows.x[j][32 * g + 16 * (q % 2) + 8 * u];
 #pragma unroll
       for (int i = 0; i < 8; ++i) dst[i] = rounded<OUT>(v[i]);
     }
+    if (q % 2 == 1) store_rows<OUT>(rows, to, lane, [&](int r) { return 32 * wave + 16 * (q / 2) + r; });
   }
 }
 
@@ -113,7 +127,7 @@ __device__ __forceinline__ void rotate_codes(half2_t (&v)[2], int lane) {
   }
 }
 
-// Values: wave w has tokens 16 i + 4 w + 0..3 (i = 0..7), row 4 i + t of its rows; a lane channels 32 u + 16 n + j of all of them.
+// Values: wave w has tokens 16 i + 4 w + 0..3 (i = 0..7), two of the four (t) at a time, row 2 i + t % 2 of its rows; a lane channels 32 u + 16 n + j of all of them.
 template <int BITS, typename OUT, bool ROTATED, int SEL>
 __device__ __forceinline__ void value_pairs(const uint32_t (&e)[2][BITS / 2], const uint32_t* sz, int t, WaveRows<OUT>& rows, int lane) {
   const int j = lane & 15, u = lane >> 4;
@@ -129,12 +143,12 @@ __device__ __forceinline__ void value_pairs(const uint32_t (&e)[2][BITS / 2], co
       float v;
       if constexpr (ROTATED) v = fmaf(s, x + Rec<BITS>::kCentre, (float)p[1]);
       else v = fmaf(s, x, n == 0 && lane == 0 ? 128.0f * mid : 0.0f) * kInvSqrtD;
-      rows.x[4 * (2 * SEL + k) + t][32 * u + 16 * n + j] = rounded<OUT>(v);
+      rows.x[2 * (2 * SEL + k) + (t & 1)][32 * u + 16 * n + j] = rounded<OUT>(v);
     }
   }
 }
 template <int BITS, typename OUT, bool ROTATED>
-__device__ __forceinline__ void read_values(const uint32_t* rec, WaveRows<OUT>& rows, int wave, int lane) {
+__device__ __forceinline__ void read_values(const uint32_t* rec, WaveRows<OUT>& rows, const Target<OUT>& to, int wave, int lane) {
   const int j = lane & 15, u = lane >> 4;
 #pragma unroll
   for (int hg = 0; hg < 2; ++hg) {
@@ -163,6 +177,7 @@ __device__ __forceinline__ void read_values(const uint32_t* rec, WaveRows<OUT>& 
       value_pairs<BITS, OUT, ROTATED, 2>(e, sz, t, rows, lane);
       value_pairs<BITS, OUT, ROTATED, 3>(e, sz, t, rows, lane);
     }
+    store_rows<OUT>(rows, to, lane, [&](int r) { return 16 * (r >> 1) + 4 * wave + 2 * hg + (r & 1); });
   }
 }
 
@@ -194,15 +209,9 @@ __global__ __launch_bounds__(256) void read_kernel(kvlinc_cache c, ReadRange ran
   const int packed = sliding ? min(len.nq, max(len.total() - kGroup, 0)) : len.nq;
   if (from < packed) {
     const uint32_t* rec = c.groups + ((long long)bh * c.max_groups + block) * Rec<BITS>::kWords;
-    if (values) {
-      read_values<BITS, OUT, ROTATED>(rec, all[wave], wave, lane);
-      __builtin_amdgcn_wave_barrier();
-      store_rows<OUT>(all[wave], out, first, from, min(to, packed), lane, [&](int r) { return (int)at + 16 * (r >> 2) + 4 * wave + (r & 3); });
-    } else {
-      read_keys<BITS, OUT>(rec, all[wave], wave, lane);
-      __builtin_amdgcn_wave_barrier();
-      store_rows<OUT>(all[wave], out, first, from, min(to, packed), lane, [&](int r) { return (int)at + 32 * wave + r; });
-    }
+    const Target<OUT> target = {out, first, from, min(to, packed), (int)at};
+    if (values) read_values<BITS, OUT, ROTATED>(rec, all[wave], target, wave, lane);
+    else read_keys<BITS, OUT>(rec, all[wave], target, wave, lane);
   }
   const int raw = max(from, packed);
   if (raw >= to) return;
