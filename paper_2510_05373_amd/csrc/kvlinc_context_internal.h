@@ -39,8 +39,8 @@ int launch_join(const ContextCall& a, hipStream_t stream);
 int launch_prompt_correction(const ContextCall& a, hipStream_t stream);
 int launch_read(const kvlinc_cache& c, const int32_t* first, int T, void* k_out, void* v_out, int dtype, bool rotated, hipStream_t stream);
 
-// Tokens window_base(total, window) .. + T - 1 of every sequence as binary16 rows, values in the rotated basis, to rows from_row .. of
-// [B H_kv][rows][128].
-int launch_read_rows(const kvlinc_cache& c, int window, int from_row, int T, int rows, _Float16* k_rows, _Float16* v_rows, hipStream_t stream);
+// The first `lead` tokens of every sequence and, behind them, those from window_base(total, window) on, as binary16 rows
+// [B H_kv][rows][128], values in the rotated basis.
+int launch_read_rows(const kvlinc_cache& c, int window, int lead, int rows, _Float16* k_rows, _Float16* v_rows, hipStream_t stream);
 
 }  // namespace kvlinc

@@ -203,12 +203,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void dense_kernel(ContextCall a, i
 
 int launch_dense(const ContextCall& a, hipStream_t stream) {
   // the cached tokens that some row sees, as rows: the sinks (if they lie apart), and what is near
-  half_t *k = const_cast<half_t*>(a.k_rows), *v = const_cast<half_t*>(a.v_rows);
-  if (a.sink_rows > 0) {
-    const int rc = launch_read_rows(a.cache, 0, 0, a.sink_rows, a.cached_rows, k, v, stream);
-    if (rc != KVLINC_OK) return rc;
-  }
-  const int rc = launch_read_rows(a.cache, a.row_window, a.sink_rows, a.cached_rows - a.sink_rows, a.cached_rows, k, v, stream);
+  const int rc = launch_read_rows(a.cache, a.row_window, a.sink_rows, a.cached_rows, const_cast<half_t*>(a.k_rows), const_cast<half_t*>(a.v_rows), stream);
   if (rc != KVLINC_OK) return rc;
   const int blocks = (int)(((long long)a.T * a.gq + kTileRows - 1) / kTileRows);
   const dim3 grid((unsigned)((long long)blocks * a.cache.B * a.cache.H_kv * a.splits));

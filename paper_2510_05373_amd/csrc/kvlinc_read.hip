@@ -186,23 +186,25 @@ __device__ __forceinline__ void read_values(const uint32_t* rec, WaveRows<OUT>& 
 struct ReadRange {
   const int32_t* first_of;  // first token of each sequence; NULL: window_base(tokens, window)
   int window, T;            // T rows
+  int lead, lead_blocks;    // ahead of them: the first `lead` tokens, blocks of 128 of those
   long long pair_rows;      // rows from one (sequence, KV head) to the next
   int blocks, per_tensor;
 };
 template <int BITS, typename OUT, bool ROTATED>
 __global__ __launch_bounds__(256) void read_kernel(kvlinc_cache c, ReadRange range, OUT* k_out, OUT* v_out) {
-  const int T = range.T, blocks = range.blocks, per_tensor = range.per_tensor;
+  const int blocks = range.blocks, per_tensor = range.per_tensor;
   __shared__ __align__(16) WaveRows<OUT> all[4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const bool values = k_out == nullptr || (int)blockIdx.x >= per_tensor;
   const int id = (int)blockIdx.x >= per_tensor ? blockIdx.x - per_tensor : blockIdx.x;
-  const int bh = id / blocks, b = bh / c.H_kv;
+  const int bh = id / blocks, b = bh / c.H_kv, in_pair = id - bh * blocks;
+  const bool lead = in_pair < range.lead_blocks;
   const Lengths len = lengths_of(c, b);
-  const long long first = range.first_of != nullptr ? max(range.first_of[b], 0) : window_base(len.total(), range.window);
-  const long long block = first / kGroup + (id - bh * blocks), at = block * kGroup;
-  const long long end = min(first + T, (long long)len.total());
+  const long long first = lead ? 0 : range.first_of != nullptr ? max(range.first_of[b], 0) : window_base(len.total(), range.window);
+  const long long block = first / kGroup + in_pair - (lead ? 0 : range.lead_blocks), at = block * kGroup;
+  const long long end = min(first + (lead ? range.lead : range.T), (long long)len.total());
   if (at >= end) return;
-  OUT* out = (values ? v_out : k_out) + bh * range.pair_rows * kHeadDim;
+  OUT* out = (values ? v_out : k_out) + (bh * range.pair_rows + (lead ? 0 : range.lead)) * kHeadDim;
   const int from = (int)max(first, at), to = (int)min(end, at + kGroup);  // positions this workgroup writes
   // with sliding values, the newest 128 tokens' values are the window's: token t in slot t % 128
   const bool sliding = (c.flags & KVLINC_FLAG_SLIDING_VALUES) != 0 && values && len.nq % kGroup == 0;
@@ -260,7 +262,7 @@ __global__ __launch_bounds__(256) void read_kernel(kvlinc_cache c, ReadRange ran
 template <int BITS, typename OUT>
 int launch_read_of(const kvlinc_cache& c, ReadRange r, void* k_out, void* v_out, bool rotated, hipStream_t stream) {
   // (a range that does not start on a block of 128 touches one more)
-  const long long blocks = ((long long)r.T + kGroup - 1) / kGroup + (r.first_of != nullptr || r.window > 0 ? 1 : 0);
+  const long long blocks = r.lead_blocks + ((long long)r.T + kGroup - 1) / kGroup + (r.first_of != nullptr || r.window > 0 ? 1 : 0);
   const long long per_tensor = blocks * c.B * c.H_kv, grid = per_tensor * ((k_out != nullptr) + (v_out != nullptr));
   if (grid >= (1ll << 24)) return KVLINC_EINVAL;  // 2^32 threads: more than the outputs of any card
   r.blocks = (int)blocks;
@@ -274,7 +276,7 @@ int launch_read_of(const kvlinc_cache& c, ReadRange r, void* k_out, void* v_out,
 }  // namespace
 
 int launch_read(const kvlinc_cache& c, const int32_t* first, int T, void* k_out, void* v_out, int dtype, bool rotated, hipStream_t stream) {
-  const ReadRange r = {first, 0, T, T, 0, 0};
+  const ReadRange r = {first, 0, T, 0, 0, T, 0, 0};
   switch (dtype) {
     case KVLINC_F16: return c.bits == 2 ? launch_read_of<2, half_t>(c, r, k_out, v_out, rotated, stream) : launch_read_of<4, half_t>(c, r, k_out, v_out, rotated, stream);
     case KVLINC_BF16: return c.bits == 2 ? launch_read_of<2, BF16>(c, r, k_out, v_out, rotated, stream) : launch_read_of<4, BF16>(c, r, k_out, v_out, rotated, stream);
@@ -282,10 +284,9 @@ int launch_read(const kvlinc_cache& c, const int32_t* first, int T, void* k_out,
   }
 }
 
-int launch_read_rows(const kvlinc_cache& c, int window, int from_row, int T, int rows, half_t* k_rows, half_t* v_rows, hipStream_t stream) {
-  const ReadRange r = {nullptr, window, T, rows, 0, 0};
-  half_t *k = k_rows + (long long)from_row * kHeadDim, *v = v_rows + (long long)from_row * kHeadDim;
-  return c.bits == 2 ? launch_read_of<2, half_t>(c, r, k, v, true, stream) : launch_read_of<4, half_t>(c, r, k, v, true, stream);
+int launch_read_rows(const kvlinc_cache& c, int window, int lead, int rows, half_t* k_rows, half_t* v_rows, hipStream_t stream) {
+  const ReadRange r = {nullptr, window, rows - lead, lead, (lead + kGroup - 1) / kGroup, rows, 0, 0};
+  return c.bits == 2 ? launch_read_of<2, half_t>(c, r, k_rows, v_rows, true, stream) : launch_read_of<4, half_t>(c, r, k_rows, v_rows, true, stream);
 }
 
 }  // namespace kvlinc
