@@ -44,10 +44,12 @@ size_t kvlinc_prompt_workspace_bytes(const kvlinc_cache* cache, int32_t T, int32
  *                  read as 0, one above T as T.)  Rows from n_new[b] on are not read, and not written in `out`.
  *   T              rows per (sequence, head), 1 .. 2^24
  *   window, sinks  >= 0, see above
- *   out            [B, H_q, T, 128] fp16, in the original value basis; not one of the inputs
+ *   out            [B, H_q, T, 128] fp16, in the original value basis; memory of its own (KVLINC_EINVAL if an input's)
  *   workspace      device scratch of at least kvlinc_prompt_workspace_bytes(cache, T, window, sinks, max_context) bytes, 16-byte
  *                  aligned, contents undefined before and after; NULL where that is 0
- *   max_context    host-side upper bound on the tokens a sequence holds before the call (<= 0: capacity); it only sizes the launch
+ *   max_context    host-side upper bound on the tokens a sequence holds before the call (<= 0: capacity).  It sizes the launch and,
+ *                  from T * H_q / H_kv = 1024 on, the room for dequantized tokens (512 bytes each): those of a sequence that
+ *                  holds more than it was promised to are left out of the sums.
  *
  * out[b, h, i] = ( sum_t w_t V_t + phi_q(q) S H^T ) / ( sum_t w_t + phi_q(q) P ),  w_t = exp(q K_t / sqrt 128)
  * over the tokens that row i sees; the phi terms (Eq. 5) with the adapters only.  The states S, P stand for all quantized tokens:
@@ -70,7 +72,7 @@ size_t kvlinc_decode_windowed_workspace_bytes(const kvlinc_cache* cache, int32_t
  * One decode step of a layer with a sliding window: kvlinc_decode_attention (the query's own token, at position n - 1, is already
  * appended) over the tokens that the window and the sinks leave visible.  Only their groups are read.
  *
- *   q, out         [B, H_q, 128] fp16
+ *   q, out         [B, H_q, 128] fp16; out may be q
  *   window, sinks  >= 0, see above; window = 0: all tokens
  *   workspace      at least kvlinc_decode_windowed_workspace_bytes(cache, window, sinks, max_context) bytes, 16-byte aligned
  *   max_context    host-side upper bound on n_quant + n_res (<= 0: capacity); it only sizes the launch
@@ -86,7 +88,7 @@ int kvlinc_decode_attention_windowed(const kvlinc_cache* cache, const kvlinc_hal
  *   first          [B] int32 on the device: row i is token first[b] + i; NULL = 0 for all.  (A value below 0 is read as 0.)
  *   T              rows, 1 .. 2^30
  *   k_out, v_out   [B, H_kv, T, 128] of type dtype (KVLINC_F16, KVLINC_BF16, KVLINC_F32); either may be NULL.  Rows of tokens
- *                  that the sequence does not hold are left as they are.
+ *                  that the sequence does not hold are left as they are.  The two do not overlap.
  *   rotated        0: values in the original basis, V_t;  1: in the rotated basis they are stored in.
  *
  * A number is dequantized and rotated in binary32 and rounded to dtype once; one beyond the largest finite binary16 number (the

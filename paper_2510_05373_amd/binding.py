@@ -272,18 +272,26 @@ class KVLincCache:
             raise KVLincError("%s has to be contiguous" % name)
         return t
 
-    def _on(self, stream):
-        """The cache's device current, and `stream`, if one is given: what is allocated inside belongs to the stream that uses it."""
+    def _on(self, stream, *tensors):
+        """The cache's device current, and `stream`, if one is given: what is allocated inside belongs to the stream that uses it, and the
+        caller's tensors are not handed out again before it is done with them."""
         import contextlib
         import torch
         dev = self.groups.device
         if dev.type != "cuda":
             raise KVLincError("the cache is on %s: the kernels need a GPU" % dev)
+        if stream is not None and not hasattr(stream, "cuda_stream"):
+            stream = torch.cuda.ExternalStream(int(stream), device=dev)
+        if stream is not None and stream.device != dev:
+            raise KVLincError("the stream is on %s, the cache on %s" % (stream.device, dev))
         scope = contextlib.ExitStack()
         if torch.cuda.current_device() != dev.index:
             scope.enter_context(torch.cuda.device(dev))
         if stream is not None:
-            scope.enter_context(torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream), device=dev)))
+            scope.enter_context(torch.cuda.stream(stream))
+            for t in tensors:
+                if t is not None:
+                    t.record_stream(stream)
         return scope
 
     @staticmethod
@@ -319,7 +327,7 @@ class KVLincCache:
             self._tensor(n_new, "n_new", (self.B,), (torch.int32,))
         if out is not None:
             self._tensor(out, "out", q.shape, half)
-        with self._on(stream):
+        with self._on(stream, q, k_new, v_new, n_new, out):
             if out is None:
                 out = torch.empty_like(q) if n_new is None else torch.zeros_like(q)
             ws = self._context_workspace(kvlinc_prompt_workspace_bytes(self, T, window, sinks, max_context))
@@ -336,7 +344,7 @@ class KVLincCache:
         self._tensor(q, "q", (self.B, self.H_q, 128), half)
         if out is not None:
             self._tensor(out, "out", q.shape, half)
-        with self._on(stream):
+        with self._on(stream, q, out):
             if out is None:
                 out = torch.empty_like(q)
             ws = self._context_workspace(kvlinc_decode_windowed_workspace_bytes(self, window, sinks, max_context))
@@ -368,7 +376,7 @@ class KVLincCache:
                 self._tensor(t, name, shape, (dtype,))
         if first is not None:
             self._tensor(first, "first", (self.B,), (torch.int32,))
-        with self._on(stream):
+        with self._on(stream, first, k_out, v_out):
             if not given:
                 k_out, v_out = (torch.zeros(shape, dtype=dtype, device=self.groups.device) for _ in range(2))
             rc = kvlinc_cache_read(self, first, T, k_out, v_out, types[dtype], int(bool(rotated)), stream)

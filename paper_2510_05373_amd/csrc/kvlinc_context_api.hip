@@ -8,6 +8,12 @@ namespace {
 
 inline bool bad_address(const void* p, uintptr_t a) { return p == nullptr || (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
 
+// Whether rows [.., 128] of two tensors share memory.
+bool overlap(const void* p, long long p_bytes, const void* q, long long q_bytes) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+  return a < b + (uintptr_t)q_bytes && b < a + (uintptr_t)p_bytes;
+}
+
 // What a call makes of its sizes: splits of a context, scratch.
 struct ContextPlan {
   // 16 rows a wave (kvlinc_rows.hip); blocks of 256 rows over tiles of codes (kvlinc_prompt.hip), or of rows dequantized first (kvlinc_dense.hip)
@@ -72,10 +78,11 @@ ContextPlan plan_call(const kvlinc_cache& c, int T, int window, int sinks, int m
   return p;
 }
 
-// The grids of a call stay below 2^32 threads (rows beyond that would not fit any card's memory).
+// The grids of a call stay below 2^32 threads (rows beyond that would not fit any card's memory), positions below 2^31.
 bool too_many(const kvlinc_cache& c, int T) {
   const long long gq = c.H_q / c.H_kv;
-  return (long long)c.B * c.H_kv >= (1ll << 24) || (long long)c.B * c.H_kv * ((T * gq + 15) / 16) >= (1ll << 24);
+  return (long long)c.B * c.H_kv >= (1ll << 24) || (long long)c.B * c.H_kv * ((T * gq + 15) / 16) >= (1ll << 24) ||
+         c.max_groups * kGroup + c.R + T > INT32_MAX - 2 * kGroup;
 }
 
 int check_prompt(const kvlinc_cache* c, int T, int window, int sinks) {
@@ -144,6 +151,8 @@ int kvlinc_prompt_attention(const kvlinc_cache* cache, const kvlinc_half* q, con
   if (rc != KVLINC_OK) return rc;
   if (bad_address(q, 16) || bad_address(k_new, 16) || bad_address(v_new, 16) || bad_address(out, 16)) return KVLINC_EINVAL;
   if (n_new != nullptr && bad_address(n_new, 4)) return KVLINC_EINVAL;
+  const long long q_bytes = (long long)cache->B * cache->H_q * T * kHeadDim * 2, kv_bytes = q_bytes / (cache->H_q / cache->H_kv);
+  if (overlap(out, q_bytes, q, q_bytes) || overlap(out, q_bytes, k_new, kv_bytes) || overlap(out, q_bytes, v_new, kv_bytes)) return KVLINC_EINVAL;
   const ContextPlan p = plan_call(*cache, T, window, sinks, max_context);
   if (bad_workspace(workspace, workspace_bytes, p.bytes())) return KVLINC_EWORKSPACE;
   ContextCall a = make_call(*cache, q, T, window, sinks, out, workspace, p);
@@ -168,6 +177,9 @@ int kvlinc_decode_attention_windowed(const kvlinc_cache* cache, const kvlinc_hal
   const int rc = check_windowed(cache, window, sinks);
   if (rc != KVLINC_OK) return rc;
   if (bad_address(q, 16) || bad_address(out, 16)) return KVLINC_EINVAL;
+  // (a head's workgroups have all read q when the last of them writes its row)
+  const long long bytes = (long long)cache->B * cache->H_q * kHeadDim * 2;
+  if (q != out && overlap(out, bytes, q, bytes)) return KVLINC_EINVAL;
   const ContextPlan p = plan_windowed(*cache, window, sinks, max_context);
   if (bad_workspace(workspace, workspace_bytes, p.bytes())) return KVLINC_EWORKSPACE;
   return launch_windowed(make_call(*cache, q, 1, window, sinks, out, workspace, p), static_cast<hipStream_t>(stream));
@@ -181,6 +193,8 @@ int kvlinc_cache_read(const kvlinc_cache* cache, const int32_t* first, int32_t T
   if (k_out == nullptr && v_out == nullptr) return KVLINC_EINVAL;
   if ((k_out != nullptr && bad_address(k_out, 16)) || (v_out != nullptr && bad_address(v_out, 16))) return KVLINC_EINVAL;
   if (first != nullptr && bad_address(first, 4)) return KVLINC_EINVAL;
+  const long long bytes = (long long)cache->B * cache->H_kv * T * kHeadDim * (dtype == KVLINC_F32 ? 4 : 2);
+  if (k_out != nullptr && v_out != nullptr && overlap(k_out, bytes, v_out, bytes)) return KVLINC_EINVAL;
   return launch_read(*cache, first, T, k_out, v_out, dtype, rotated != 0, static_cast<hipStream_t>(stream));
 }
 

@@ -261,8 +261,9 @@ __global__ __launch_bounds__(256) void read_kernel(kvlinc_cache c, ReadRange ran
 
 template <int BITS, typename OUT>
 int launch_read_of(const kvlinc_cache& c, ReadRange r, void* k_out, void* v_out, bool rotated, hipStream_t stream) {
-  // (a range that does not start on a block of 128 touches one more)
-  const long long blocks = r.lead_blocks + ((long long)r.T + kGroup - 1) / kGroup + (r.first_of != nullptr || r.window > 0 ? 1 : 0);
+  // (a range that does not start on a block of 128 touches one more; none has more than the cache)
+  const long long of_rows = ((long long)r.T + kGroup - 1) / kGroup, of_cache = c.max_groups + 1;
+  const long long blocks = r.lead_blocks + (of_rows < of_cache ? of_rows : of_cache) + (r.first_of != nullptr || r.window > 0 ? 1 : 0);
   const long long per_tensor = blocks * c.B * c.H_kv, grid = per_tensor * ((k_out != nullptr) + (v_out != nullptr));
   if (grid >= (1ll << 24)) return KVLINC_EINVAL;  // 2^32 threads: more than the outputs of any card
   r.blocks = (int)blocks;

@@ -96,12 +96,12 @@ __device__ __forceinline__ bool seen(int t, int at, int count, int p, int low, i
 }
 
 __device__ __forceinline__ void set_reference(Rows& st, float largest) {  // largest: of this lane's scores
-  if (__builtin_amdgcn_ballot_w64(largest > st.m + (kHeadroom + kLag)) == 0) return;
+  if (__builtin_amdgcn_ballot_w64(largest - st.m > kHeadroom + kLag) == 0) return;  // (a difference: m + 13 is m + 16 where steps are that wide)
   float x, y;
   pair_across<16>(largest, x, y);
   pair_across<32>(fmaxf(x, y), x, y);
   const float mx = fmaxf(x, y);
-  const float to = mx > st.m + (kHeadroom + kLag) ? mx - kHeadroom : st.m;
+  const float to = mx - st.m > kHeadroom + kLag ? (fabsf(mx) > kFusedBound ? mx : mx - kHeadroom) : st.m;
   const float f = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(st.m - to);  // (0 where nothing was seen)
   st.m = to;
   st.l *= f;

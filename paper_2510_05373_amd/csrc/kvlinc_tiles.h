@@ -32,11 +32,11 @@ struct TileRows {
 };
 
 __device__ __forceinline__ void raise_reference(TileRows& st, float largest) {  // largest score of this lane, log2 domain
-  if (__builtin_amdgcn_ballot_w64(largest > st.m + (kHeadroom + kLag)) == 0) return;
+  if (__builtin_amdgcn_ballot_w64(largest - st.m > kHeadroom + kLag) == 0) return;  // (a difference: m + 13 is m + 16 where steps are that wide)
   float x, y;
   pair_across<32>(largest, x, y);
   const float mx = fmaxf(x, y);
-  const float to = mx > st.m + (kHeadroom + kLag) ? mx - kHeadroom : st.m;
+  const float to = mx - st.m > kHeadroom + kLag ? (fabsf(mx) > kFusedBound ? mx : mx - kHeadroom) : st.m;
   const float f = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(st.m - to);
   st.m = to;
   st.l *= f;

@@ -152,3 +152,31 @@ def test_decode_windowed_checks_its_tensors(cache, over):
 def test_read_checks_its_tensors(cache, over):
     with pytest.raises(kv.KVLincError):
         cache.read(**over)
+
+
+# ---- memory that a call would both read and write, and positions beyond 31 bits --------------------------------------------------
+
+def test_an_output_over_an_input_is_refused():
+    c = plain()  # q and out: B H_q T 128 halves, k_new and v_new: B H_kv T 128
+    q_bytes, kv_bytes = c.B * c.H_q * 4 * 256, c.B * c.H_kv * 4 * 256
+    at = 0x800000
+    for over in (dict(q=at), dict(q=at + q_bytes - 16), dict(q=at - q_bytes + 16), dict(k=at), dict(k=at - kv_bytes + 16), dict(v=at + q_bytes - 16)):
+        assert prompt(c, out=at, **over) == kb.KVLINC_EINVAL
+    # next to one another: looked at further (and refused for its workspace, nothing is launched)
+    assert prompt(fake_struct(), out=at, q=at + q_bytes, k=at - kv_bytes, v=at - kv_bytes, size=0) == kb.KVLINC_EWORKSPACE
+    one = c.B * c.H_q * 256
+    c = plain(max_groups=256)
+    assert windowed(c, q=at, out=at + one - 16, window=4096) == kb.KVLINC_EINVAL
+    assert windowed(c, q=at + 16, out=at, window=4096) == kb.KVLINC_EINVAL
+    assert windowed(c, q=at, out=at, window=4096, size=0) == kb.KVLINC_EWORKSPACE  # the same memory is allowed
+    for dtype, size in ((kb.KVLINC_F16, 2), (kb.KVLINC_BF16, 2), (kb.KVLINC_F32, 4)):
+        assert read(plain(), k=at, v=at + c.B * c.H_kv * 4 * 128 * size - 16, dtype=dtype) == kb.KVLINC_EINVAL
+    assert read(plain(), k=at, v=at) == kb.KVLINC_EINVAL
+
+
+def test_positions_have_31_bits():
+    for groups in (1 << 24, (1 << 24) - 1):
+        c = plain(max_groups=groups, B=1, H_q=1, H_kv=1)
+        assert prompt(c) == kb.KVLINC_EINVAL and windowed(c) == kb.KVLINC_EINVAL
+        assert kb.kvlinc_prompt_workspace_bytes(c, 4) == 0 and kb.kvlinc_decode_windowed_workspace_bytes(c, 16) == 0
+    assert kb.kvlinc_prompt_workspace_bytes(plain(max_groups=(1 << 24) - 4, B=1, H_q=1, H_kv=1), 1) > 0
