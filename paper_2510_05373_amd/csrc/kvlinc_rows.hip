@@ -595,14 +595,16 @@ __global__ __launch_bounds__(64 * kMaxWaves, 2) void rows_kernel(ContextCall a) 
       }
       item -= n_win;
       const uint32_t* rec0 = c.groups + (long long)bh * c.max_groups * Rec<BITS>::kWords;
-      const int newest = SLIDING && len.nq % kGroup == 0 && len.nr < kGroup ? G - 1 : -1;
       auto group_of = [&](int it) { return it < n_sink ? it : it - n_sink + group_low; };
+      // (the newest group, the last item, is left to the code below where its tokens from n_res on take the window's values: in the loop that
+      // code's registers spilled, and drafts over 16 sequences of 8k tokens took 41 us, 4 bits 71)
+      const int plain = SLIDING && len.nq % kGroup == 0 && len.nr < kGroup && n_groups > 0 && group_of(n_groups - 1) == G - 1 ? n_groups - 1 : n_groups;
       if (item < n_groups) {
         Record<BITS> rec;
         int gr = group_of(item);
         load_key_part<BITS>(rec, rec0 + (long long)gr * Rec<BITS>::kWords, lane);
         load_value_part<BITS>(rec, rec0 + (long long)gr * Rec<BITS>::kWords, lane);
-        for (;;) {
+        while (item < plain) {
           const int at = gr * kGroup, count = min(len.nq - at, kGroup);
           const bool masked = count < kGroup || (at < low_last && at + kGroup > a.sinks), more = item + step < n_groups;
           const int e = put_meta<BITS>(rec, sMeta[wave], lane);
@@ -610,11 +612,17 @@ __global__ __launch_bounds__(64 * kMaxWaves, 2) void rows_kernel(ContextCall a) 
           group_scores<BITS, S>(st, rec, sMeta[wave], at, count, masked, a.sinks, lane, x, exponent_base);
           const int next = more ? group_of(item + step) : gr;
           if (more) load_key_part<BITS>(rec, rec0 + (long long)next * Rec<BITS>::kWords, lane);
-          group_values<BITS, S, SLIDING>(st, rec, sMeta[wave], e, x, exponent_base, gr == newest ? len.nr : kGroup, v_win, quads, lane);
-          if (!more) break;
-          load_value_part<BITS>(rec, rec0 + (long long)next * Rec<BITS>::kWords, lane);
+          group_values<BITS, S, false>(st, rec, sMeta[wave], e, x, exponent_base, kGroup, v_win, quads, lane);
+          if (more) load_value_part<BITS>(rec, rec0 + (long long)next * Rec<BITS>::kWords, lane);
           item += step;
           gr = next;
+        }
+        if (SLIDING && item < n_groups) {
+          const int at = gr * kGroup;
+          const int e = put_meta<BITS>(rec, sMeta[wave], lane);
+          float x[8 / S][4], exponent_base;
+          group_scores<BITS, S>(st, rec, sMeta[wave], at, kGroup, at < low_last && at + kGroup > a.sinks, a.sinks, lane, x, exponent_base);
+          group_values<BITS, S, true>(st, rec, sMeta[wave], e, x, exponent_base, len.nr, v_win, quads, lane);
         }
       }
     }
