@@ -57,7 +57,8 @@ __device__ __forceinline__ void load_value_part(Record<BITS>& r, const uint32_t*
 static_assert(Rec<2>::kKeyZero == Rec<2>::kKeyScale + 64 && Rec<2>::kValueSZ == Rec<2>::kKeyScale + 128 && Rec<2>::kWords == Rec<2>::kKeyScale + 256, "256 words");
 
 // A wave's copy of a group's scales and zero-points in LDS: [0..15] key scales, [16..31] key zero-points, 8 channels each; [32 + 2 t + u]
-// value (scale, zero-point) of tokens 16 (4 u + i) + t, i = 0..3.  The exponent of the group's largest value scale is taken out of them on
+// value (scale, middle) of tokens 16 (4 u + i) + t, i = 0..3, the middle z + centre s in binary16: a value is s (code - centre) + middle, and a
+// weight's rounding counts with the first part only.  The exponent of the group's largest value scale is taken out of them on
 // the way (it goes to the codes, exactly: weight times scale then stays in binary16's range whatever the values' magnitude) and returned.
 template <int BITS>
 __device__ __forceinline__ int put_meta(const Record<BITS>& r, u32x4_t* meta, int lane) {
@@ -70,10 +71,13 @@ __device__ __forceinline__ int put_meta(const Record<BITS>& r, u32x4_t* meta, in
   top = max(top, dpp_u<kRowRor4>(top));
   top = max(top, dpp_u<kRowRor8>(top));
   const int e = (int)(max(max(__builtin_amdgcn_readlane(top, 32), __builtin_amdgcn_readlane(top, 48)) >> 10, 3u)) - 15;  // -12 .. 15: the codes times 2^e are normal numbers
-  const half2_t unscale = {(half_t)(lane >= 32 ? bits_f32((uint32_t)(127 - e) << 23) : 1.0f), (half_t)1.0f};
+  const half_t unscale = (half_t)(lane >= 32 ? bits_f32((uint32_t)(127 - e) << 23) : 1.0f), centre = (half_t)(lane >= 32 ? Rec<BITS>::kCentre : 0.0f);
   u32x4_t w;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) w[i] = as_u32(as_h2(r.meta[i]) * unscale);
+  for (int i = 0; i < 4; ++i) {
+    const half2_t v = as_h2(r.meta[i]);
+    w[i] = as_u32(half2_t{v[0] * unscale, __builtin_elementwise_fma(v[0], centre, v[1])});
+  }
   meta[lane] = w;
   __builtin_amdgcn_wave_barrier();  // (a wave's LDS instructions stay in order)
   return e;
@@ -85,7 +89,7 @@ struct Rows {
   int p, low;      // position, first token of its window
   int subset;
   float m;         // reference (the same in the four lanes of a column), log2 domain; -inf: nothing seen yet
-  float l, mid;    // per-lane sums of the weights, and of weight times (zero-point + centre scale): the same for all channels
+  float l, mid;    // per-lane sums of the weights, and of weight times middle: the same for all channels
   float4_t acc[8]; // numerator of channels 16 n + 4 g + 0..3
 };
 
@@ -226,8 +230,7 @@ __device__ __forceinline__ void group_values(Rows& st, const Record<BITS>& rec, 
   constexpr int kBlocks = 8 / S;
   const float scale = bits_f32((uint32_t)(127 + e) << 23);
   uint32_t w[kBlocks / 2][4];  // weight times value scale of blocks 2 i and 2 i + 1
-  float l = 0.0f, ys = 0.0f, zs = 0.0f;
-  const half2_t ones = {(half_t)1.0f, (half_t)1.0f};
+  float l = 0.0f, mid = 0.0f;
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
     const int t = token_order(4 * (lane >> 4) + r);
@@ -256,15 +259,13 @@ __device__ __forceinline__ void group_values(Rows& st, const Record<BITS>& rec, 
         const bool coded = !SLIDING || 16 * (kBlocks * st.subset + i + u) + t < fp16_from;
         const float yy = __builtin_fmaf(p, (float)p2[0], 0.0f);
         y[u] = coded ? yy : 0.0f;
-        zs = coded ? __builtin_fmaf(p, (float)p2[1], zs) : zs;
+        mid = coded ? __builtin_fmaf(p, (float)p2[1], mid) : mid;
       }
-      const half2_t pk = pack_h2(y[0], y[1]);
-      ys = __builtin_amdgcn_fdot2(pk, ones, ys, false);
-      w[i / 2][r] = as_u32(pk);
+      w[i / 2][r] = as_u32(pack_h2(y[0], y[1]));
     }
   }
   st.l += l;
-  st.mid += fmaf(ys * scale, Rec<BITS>::kCentre, zs);
+  st.mid += mid;
   half8_t P[4];  // step s: blocks 2 s and 2 s + 1; a column has those of its subset, and zero elsewhere
 #pragma unroll
   for (int s = 0; s < 4; ++s) {
