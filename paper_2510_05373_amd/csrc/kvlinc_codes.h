@@ -48,6 +48,19 @@ __device__ __forceinline__ half2_t code_pair(const uint32_t (&plane)[BITS / 2], 
   else return nibble_pair<SEL>(plane[0], 4.0f * scale) + nibble_pair<SEL>(plane[1], scale);
 }
 
+// Eight numbers over a scale, a power of two, as FP4 (E2M1) ones, the first in the lowest bits; a tie goes to the even one.
+__device__ __forceinline__ uint32_t fp4_of(const float (&v)[8], float scale) {
+  uint32_t w = 0;
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[0], v[1], scale, 0);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[2], v[3], scale, 1);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[4], v[5], scale, 2);
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[6], v[7], scale, 3);
+}
+
+// Exponent (biased by 127) of a scale for what the rounding to binary16 leaves of numbers up to one of these bits: half a step of it is
+// 2^(field - 26), 4 of the scale.
+__device__ __forceinline__ uint32_t low_scale_of(uint32_t largest) { return max(largest >> 10, 1u) + 99u; }
+
 // Butterflies between the 16 lanes of a DPP row, strides 1, 2, 4, 8, NV vectors at once.
 template <int NV>
 __device__ __forceinline__ void row16_butterflies(float (&v)[NV], int lane) {

@@ -22,7 +22,10 @@ struct ContextPlan {
   long long cached_rows, sink_rows;      // dequantized rows of a (sequence, KV head)
   int row_window;                        // see ContextCall
   size_t corr_floats, part_floats, row_halfs;  // row_halfs: of keys, and as many of values
-  size_t bytes() const { return (corr_floats + part_floats) * sizeof(float) + 2 * row_halfs * sizeof(_Float16); }
+  size_t low_words() const { return row_halfs / 8; }  // 4 bits each; and 4 bytes a row
+  size_t bytes() const {
+    return (corr_floats + part_floats + low_words() + row_halfs / kHeadDim) * sizeof(float) + 2 * row_halfs * sizeof(_Float16);
+  }
 };
 
 // Groups a row of queries meets in a context of the bound.
@@ -124,6 +127,8 @@ ContextCall make_call(const kvlinc_cache& c, const kvlinc_half* q, int T, int wi
   if (p.row_halfs != 0) {  // (the parts before are multiples of 16 bytes)
     a.k_rows = reinterpret_cast<_Float16*>(static_cast<float*>(workspace) + p.corr_floats + p.part_floats);
     a.v_rows = a.k_rows + p.row_halfs;
+    a.k_low = reinterpret_cast<uint32_t*>(a.v_rows + p.row_halfs);
+    a.k_low_scale = a.k_low + p.low_words();
   }
   a.cached_rows = (int)p.cached_rows;
   a.sink_rows = (int)p.sink_rows;

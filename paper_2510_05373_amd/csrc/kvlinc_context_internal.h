@@ -19,8 +19,11 @@ struct ContextCall {
   _Float16* out;
   // dequantized tokens [B H_kv][cached_rows][128], values in the rotated basis (launch_dense only): sink_rows rows of the first tokens, then
   // those from window_base on
-  const _Float16* k_rows;
-  const _Float16* v_rows;
+  _Float16* k_rows;
+  _Float16* v_rows;
+  // what the rounding of a key to binary16 leaves [B H_kv][cached_rows][128] as FP4 numbers, and the scales of each 32 of them (see low_scores)
+  uint32_t* k_low;
+  uint32_t* k_low_scale;  // [B H_kv][cached_rows] x 4 bytes
   int cached_rows, sink_rows, row_window;  // row_window: the window that window_base takes, 0 where the rows are all cached tokens
 };
 
@@ -39,8 +42,6 @@ int launch_join(const ContextCall& a, hipStream_t stream);
 int launch_prompt_correction(const ContextCall& a, hipStream_t stream);
 int launch_read(const kvlinc_cache& c, const int32_t* first, int T, void* k_out, void* v_out, int dtype, bool rotated, hipStream_t stream);
 
-// The first `lead` tokens of every sequence and, behind them, those from window_base(total, window) on, as binary16 rows
-// [B H_kv][rows][128], values in the rotated basis.
-int launch_read_rows(const kvlinc_cache& c, int window, int lead, int rows, _Float16* k_rows, _Float16* v_rows, hipStream_t stream);
+int launch_read_rows(const ContextCall& a, hipStream_t stream);  // k_rows .. k_low_scale
 
 }  // namespace kvlinc

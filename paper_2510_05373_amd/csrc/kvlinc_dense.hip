@@ -21,12 +21,16 @@ constexpr int kTileBytes = kTileTokens * kHeadDim * 2;
 struct DenseTiles {
   char k[kDenseBuffers][kTileBytes];
   char v[kDenseBuffers][kTileBytes];
+  LowTile low[kDenseBuffers];
 };
 
 // 1 KB from memory to LDS, 16 bytes a lane, in lane order from `lds` on.  (In assembly: the compiler would otherwise wait for the tile under
 // way ahead of every LDS read that it cannot tell from it.  There is no register to write.  The waits are in landed().)
 __device__ __forceinline__ void load_to_lds(const void* base, uint32_t offset, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory", "m0");
+}
+__device__ __forceinline__ void load_words_to_lds(const void* base, uint32_t offset, uint32_t lds) {  // 4 bytes a lane
+  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory", "m0");
 }
 // All but the newest N of this wave's loads have arrived.
 template <int N>
@@ -93,6 +97,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void dense_kernel(ContextCall a, i
 
   TileRows st;
   start_rows(st, a.q + wr.place * kHeadDim, lane);
+  if (total > 0) start_low(st, a.q + wr.place * kHeadDim, lane);
 
   // Tiles that some row of the block sees: of the new rows; of the sinks; of the tokens from `near` on.  Positions of the workspace's rows:
   // 0 .. near_row - 1 are the sinks' (tokens 0 ..), from near_row on the tokens from `near` on.
@@ -111,6 +116,8 @@ __global__ __launch_bounds__(kTileThreads, 2) void dense_kernel(ContextCall a, i
   const half_t* new_values = a.v_new + (long long)bh * a.T * kHeadDim;
   const half_t* old_keys = a.k_rows + (long long)bh * a.cached_rows * kHeadDim;
   const half_t* old_values = a.v_rows + (long long)bh * a.cached_rows * kHeadDim;
+  const u32x4_t* low_rows = reinterpret_cast<const u32x4_t*>(a.k_low) + (long long)bh * a.cached_rows * 4;
+  const uint32_t* low_scales = a.k_low_scale + (long long)bh * a.cached_rows;
 
   struct Tile { int at, row, count; bool fresh; };  // position of its first token, row in its source, tokens
   auto tile_of = [&](int it) {
@@ -136,6 +143,9 @@ __global__ __launch_bounds__(kTileThreads, 2) void dense_kernel(ContextCall a, i
   const uint32_t lds_k = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)&tiles.k[0][0] + 1024 * wave;
   const uint32_t lds_v = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)&tiles.v[0][0] + 1024 * wave;
   const int my_row = 4 * wave + (lane >> 4), my_chunk = 16 * ((lane & 15) ^ flip(my_row));  // (flip(row + 32) is the same)
+  // Of the low parts, waves 0..3 bring a quarter each, rows 16 w + l / 4, and waves 4..7 the scales (the same 256 bytes: their loads are as many).
+  const uint32_t lds_low = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)&tiles.low[0] + (wave < 4 ? 1024 * wave : (int)sizeof(tiles.low[0].k));
+  const int low_row = wave < 4 ? 16 * wave + (lane >> 2) : lane, low_at = 16 * low_chunk(low_row, lane & 3);
   auto bring = [&](int it, int buffer) __attribute__((always_inline)) {
     const Tile t = tile_of(it);
     const half_t* keys = (t.fresh ? new_keys : old_keys) + (long long)t.row * kHeadDim;
@@ -145,6 +155,9 @@ __global__ __launch_bounds__(kTileThreads, 2) void dense_kernel(ContextCall a, i
     load_to_lds(keys, o1, lds_k + kTileBytes * buffer + 8192);
     load_to_lds(values, o0, lds_v + kTileBytes * buffer);
     load_to_lds(values, o1, lds_v + kTileBytes * buffer + 8192);
+    if (t.fresh) return;
+    if (wave < 4) load_to_lds(low_rows + (long long)t.row * 4, 64 * min(low_row, t.count - 1) + low_at, lds_low + (int)sizeof(LowTile) * buffer);
+    else load_words_to_lds(low_scales + t.row, 4 * min(low_row, t.count - 1), lds_low + (int)sizeof(LowTile) * buffer);
   };
 
   // Tile `first` + k lies in buffer k % 4.  Waves 0..3 bring theirs two tiles ahead of the softmax, waves 4..7, a phase behind them, three: all
@@ -161,6 +174,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void dense_kernel(ContextCall a, i
     next_phase();
     if (behind) next_phase();
     if (!wr.idle) dense_scores(st, tiles.k[0], lane);
+    if (!wr.idle && first >= n_new) low_scores(st, tiles.low[0], lane);
     next_phase();
 #pragma unroll 1
     for (int k = 0; k < n; ++k) {
@@ -178,8 +192,10 @@ __global__ __launch_bounds__(kTileThreads, 2) void dense_kernel(ContextCall a, i
       const Tile t = tile_of(item);
       const bool live = wave_sees(wr, a, t.at, t.count);
       if (live) tile_weights(st, t.at, t.count, wave_masked(wr, a, t.at, t.count), wr.p, wr.low, a.sinks, lane);
-      if (more) landed<4>();  // the tile before the one just asked for
-      else landed<0>();
+      // the tile before the one just asked for
+      if (!more) landed<0>();
+      else if (first + to <= n_new) landed<4>();
+      else landed<5>();
       next_phase();
       // matrix phase
       if (live) {
@@ -190,6 +206,8 @@ __global__ __launch_bounds__(kTileThreads, 2) void dense_kernel(ContextCall a, i
         dense_scores(st, tiles.k[(k + 1) & 3], lane);
         dense_order<false>();
       }
+      // (a block of its own: one for both kinds of tiles in each of the above kept two copies of the accumulators)
+      if (item + 1 >= n_new && !wr.idle) low_scores(st, tiles.low[(k + 1) & 3], lane);
       next_phase();
     }
     if (!behind) next_phase();
@@ -203,7 +221,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void dense_kernel(ContextCall a, i
 
 int launch_dense(const ContextCall& a, hipStream_t stream) {
   // the cached tokens that some row sees, as rows: the sinks (if they lie apart), and what is near
-  const int rc = launch_read_rows(a.cache, a.row_window, a.sink_rows, a.cached_rows, const_cast<half_t*>(a.k_rows), const_cast<half_t*>(a.v_rows), stream);
+  const int rc = launch_read_rows(a, stream);
   if (rc != KVLINC_OK) return rc;
   const int blocks = (int)(((long long)a.T * a.gq + kTileRows - 1) / kTileRows);
   const dim3 grid((unsigned)((long long)blocks * a.cache.B * a.cache.H_kv * a.splits));

@@ -67,9 +67,15 @@ __device__ __forceinline__ void key_pairs(const uint32_t (&e)[BITS / 2], const u
   for (int i = 0; i < 2; ++i) v[2 * SEL + i] = fmaf((float)ss[i], (float)c[i] + Rec<BITS>::kCentre, (float)zz[i]);
 }
 
+// Where what the rounding of keys leaves goes, or NULL: rows as those of the keys, see low_scores.
+struct LowTarget {
+  u32x4_t* rows;  // [4]
+  uint32_t* scale;
+};
+
 // Keys: wave w has tokens 32 w .. 32 w + 31; a lane two of them, 32 channels each.
-template <int BITS, typename OUT>
-__device__ __forceinline__ void read_keys(const uint32_t* rec, WaveRows<OUT>& rows, const Target<OUT>& to, int wave, int lane) {
+template <int BITS, typename OUT, bool LOW>
+__device__ __forceinline__ void read_keys(const uint32_t* rec, WaveRows<OUT>& rows, const Target<OUT>& to, const LowTarget& low, int wave, int lane) {
   const int j = lane & 15, g = lane >> 4;
   uint32_t s[16], z[16];
 #pragma unroll
@@ -78,6 +84,18 @@ __device__ __forceinline__ void read_keys(const uint32_t* rec, WaveRows<OUT>& ro
     s[4 * i] = a.x; s[4 * i + 1] = a.y; s[4 * i + 2] = a.z; s[4 * i + 3] = a.w;
     z[4 * i] = b.x; z[4 * i + 1] = b.y; z[4 * i + 2] = b.z; z[4 * i + 3] = b.w;
   }
+  uint32_t scale = 0;  // of this lane's 32 channels, for the whole group
+  if constexpr (LOW) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const half_t levels = (half_t)(float)Rec<BITS>::kLevels;
+      const uint32_t lowest = z[i] & 0x7fff7fffu, highest = as_u32(__builtin_elementwise_fma(as_h2(s[i]), half2_t{levels, levels}, as_h2(z[i]))) & 0x7fff7fffu;
+      top = max(top, max(max(lowest & 0xffffu, lowest >> 16), max(highest & 0xffffu, highest >> 16)));
+    }
+    scale = low_scale_of(top);
+  }
+  u32x4_t rest = {0, 0, 0, 0};
   uint4 w[BITS / 2];
 #pragma unroll
   for (int pl = 0; pl < BITS / 2; ++pl) w[pl] = reinterpret_cast<const uint4*>(rec + Rec<BITS>::kKeyTile + 1024 * pl)[64 * wave + lane];
@@ -98,6 +116,18 @@ __device__ __forceinline__ void read_keys(const uint32_t* rec, WaveRows<OUT>& ro
       OUT* dst = &rows.x[j][32 * g + 16 * (q % 2) + 8 * u];
 #pragma unroll
       for (int i = 0; i < 8; ++i) dst[i] = rounded<OUT>(v[i]);
+      if constexpr (LOW) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] -= (float)rounded<half_t>(v[i]);
+        rest[2 * (q % 2) + u] = fp4_of(v, bits_f32(scale << 23));
+      }
+    }
+    if constexpr (LOW) {
+      const int t = to.at + 32 * wave + 16 * (q / 2) + j;
+      if (q % 2 == 1 && t >= to.from && t < to.to) {
+        __builtin_nontemporal_store(rest, low.rows + (t - to.first) * 4 + g);
+        reinterpret_cast<uint8_t*>(low.scale + (t - to.first))[g] = (uint8_t)scale;
+      }
     }
     if (q % 2 == 1) store_rows<OUT>(rows, to, lane, [&](int r) { return 32 * wave + 16 * (q / 2) + r; });
   }
@@ -189,8 +219,9 @@ struct ReadRange {
   int lead, lead_blocks;    // ahead of them: the first `lead` tokens, blocks of 128 of those
   long long pair_rows;      // rows from one (sequence, KV head) to the next
   int blocks, per_tensor;
+  LowTarget low;
 };
-template <int BITS, typename OUT, bool ROTATED>
+template <int BITS, typename OUT, bool ROTATED, bool LOW>
 __global__ __launch_bounds__(256) void read_kernel(kvlinc_cache c, ReadRange range, OUT* k_out, OUT* v_out) {
   const int blocks = range.blocks, per_tensor = range.per_tensor;
   __shared__ __align__(16) WaveRows<OUT> all[4];
@@ -204,7 +235,9 @@ __global__ __launch_bounds__(256) void read_kernel(kvlinc_cache c, ReadRange ran
   const long long block = first / kGroup + in_pair - (lead ? 0 : range.lead_blocks), at = block * kGroup;
   const long long end = min(first + (lead ? range.lead : range.T), (long long)len.total());
   if (at >= end) return;
-  OUT* out = (values ? v_out : k_out) + (bh * range.pair_rows + (lead ? 0 : range.lead)) * kHeadDim;
+  const long long row0 = bh * range.pair_rows + (lead ? 0 : range.lead);
+  OUT* out = (values ? v_out : k_out) + row0 * kHeadDim;
+  const LowTarget low = {range.low.rows + row0 * 4, range.low.scale + row0};
   const int from = (int)max(first, at), to = (int)min(end, at + kGroup);  // positions this workgroup writes
   // with sliding values, the newest 128 tokens' values are the window's: token t in slot t % 128
   const bool sliding = (c.flags & KVLINC_FLAG_SLIDING_VALUES) != 0 && values && len.nq % kGroup == 0;
@@ -213,7 +246,7 @@ __global__ __launch_bounds__(256) void read_kernel(kvlinc_cache c, ReadRange ran
     const uint32_t* rec = c.groups + ((long long)bh * c.max_groups + block) * Rec<BITS>::kWords;
     const Target<OUT> target = {out, first, from, min(to, packed), (int)at};
     if (values) read_values<BITS, OUT, ROTATED>(rec, all[wave], target, wave, lane);
-    else read_keys<BITS, OUT>(rec, all[wave], target, wave, lane);
+    else read_keys<BITS, OUT, LOW>(rec, all[wave], target, low, wave, lane);
   }
   const int raw = max(from, packed);
   if (raw >= to) return;
@@ -226,6 +259,10 @@ __global__ __launch_bounds__(256) void read_kernel(kvlinc_cache c, ReadRange ran
       OUT* dst = out + (t - first) * kHeadDim + 2 * lane;
       dst[0] = rounded<OUT>((float)k[0]);
       dst[1] = rounded<OUT>((float)k[1]);
+      if constexpr (LOW) {  // (binary16 numbers as they are)
+        if (lane < 16) reinterpret_cast<uint32_t*>(low.rows + (t - first) * 4)[lane] = 0u;
+        else if (lane == 16) low.scale[t - first] = 0x7f7f7f7fu;
+      }
     }
     return;
   }
@@ -269,15 +306,17 @@ int launch_read_of(const kvlinc_cache& c, ReadRange r, void* k_out, void* v_out,
   r.blocks = (int)blocks;
   r.per_tensor = (int)per_tensor;
   OUT *k = static_cast<OUT*>(k_out), *v = static_cast<OUT*>(v_out);
-  if (rotated) hipLaunchKernelGGL((read_kernel<BITS, OUT, true>), dim3((unsigned)grid), dim3(256), 0, stream, c, r, k, v);
-  else hipLaunchKernelGGL((read_kernel<BITS, OUT, false>), dim3((unsigned)grid), dim3(256), 0, stream, c, r, k, v);
+  void (*kernel)(kvlinc_cache, ReadRange, OUT*, OUT*) = rotated ? read_kernel<BITS, OUT, true, false> : read_kernel<BITS, OUT, false, false>;
+  if constexpr (std::is_same<OUT, half_t>::value)
+    if (r.low.rows != nullptr) kernel = read_kernel<BITS, OUT, true, true>;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(256), 0, stream, c, r, k, v);
   return hipGetLastError() == hipSuccess ? KVLINC_OK : KVLINC_EHIP;
 }
 
 }  // namespace
 
 int launch_read(const kvlinc_cache& c, const int32_t* first, int T, void* k_out, void* v_out, int dtype, bool rotated, hipStream_t stream) {
-  const ReadRange r = {first, 0, T, 0, 0, T, 0, 0};
+  const ReadRange r = {first, 0, T, 0, 0, T, 0, 0, {nullptr, nullptr}};
   switch (dtype) {
     case KVLINC_F16: return c.bits == 2 ? launch_read_of<2, half_t>(c, r, k_out, v_out, rotated, stream) : launch_read_of<4, half_t>(c, r, k_out, v_out, rotated, stream);
     case KVLINC_BF16: return c.bits == 2 ? launch_read_of<2, BF16>(c, r, k_out, v_out, rotated, stream) : launch_read_of<4, BF16>(c, r, k_out, v_out, rotated, stream);
@@ -285,9 +324,10 @@ int launch_read(const kvlinc_cache& c, const int32_t* first, int T, void* k_out,
   }
 }
 
-int launch_read_rows(const kvlinc_cache& c, int window, int lead, int rows, half_t* k_rows, half_t* v_rows, hipStream_t stream) {
-  const ReadRange r = {nullptr, window, rows - lead, lead, (lead + kGroup - 1) / kGroup, rows, 0, 0};
-  return c.bits == 2 ? launch_read_of<2, half_t>(c, r, k_rows, v_rows, true, stream) : launch_read_of<4, half_t>(c, r, k_rows, v_rows, true, stream);
+int launch_read_rows(const ContextCall& a, hipStream_t stream) {
+  const ReadRange r = {nullptr, a.row_window, a.cached_rows - a.sink_rows, a.sink_rows, (a.sink_rows + kGroup - 1) / kGroup, a.cached_rows, 0, 0,
+                       {reinterpret_cast<u32x4_t*>(a.k_low), a.k_low_scale}};
+  return a.cache.bits == 2 ? launch_read_of<2, half_t>(a.cache, r, a.k_rows, a.v_rows, true, stream) : launch_read_of<4, half_t>(a.cache, r, a.k_rows, a.v_rows, true, stream);
 }
 
 }  // namespace kvlinc

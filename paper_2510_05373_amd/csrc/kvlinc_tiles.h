@@ -24,6 +24,8 @@ __device__ __forceinline__ void next_phase() {
 // ---- a wave's rows ----------------------------------------------------------------------------------------------------------------
 struct TileRows {
   half8_t q[8];      // channels 16 s + 8 h + 0..7 of this lane's row
+  u32x4_t q4[2];     // and, for the products of low_scores, channels 64 j + 32 h + 0..31 as FP4 numbers
+  int q4_scale;      // their scales in bytes j
   float m, l;        // reference (log2 domain), per-lane sum of the weights
   bool far;          // some row's reference is beyond kFusedBound (the same in all lanes)
   float16_t acc[4];  // numerator of channels 32 cb + 8 (r / 4) + 4 h + r % 4
@@ -61,6 +63,30 @@ __device__ __forceinline__ void matrix_order() {
   }
   __builtin_amdgcn_sched_group_barrier(0x008, kAhead, 0);
 }
+// ---- what dequantized keys lose --------------------------------------------------------------------------------------------------------
+// A key code * scale + zero-point rounded to binary16 is off by up to 2^-12 of itself, and a score by 2^-12 of a sum of |q k|: several times what
+// all other roundings of an output come to (8e-4 of its norm against 2.5e-4, 8192 cached tokens).  What the rounding leaves is kept as FP4 numbers
+// with a scale for every 32 channels, and their products with the query, in FP4 too, are added to the score: a tenth of the loss stays (2.6e-4), for
+// 4 products of twice the depth and a quarter of the bytes on top of a tile's 32.  (A second binary16 term would cost 16 products.)
+struct LowTile {
+  u32x4_t k[kTileTokens][4];      // 32 channels a chunk; chunk c of token t lies at low_chunk(t, c)
+  uint32_t scale[kTileTokens];    // byte c: exponent (biased by 127) of the scale of chunk c
+};
+__device__ __forceinline__ int low_chunk(int t, int c) { return c ^ ((t >> 2) & 3); }
+
+typedef int i32x8_t __attribute__((ext_vector_type(8)));
+__device__ __forceinline__ i32x8_t fp4_operand(u32x4_t v) { return i32x8_t{(int)v[0], (int)v[1], (int)v[2], (int)v[3], 0, 0, 0, 0}; }
+// v_mfma_scale_f32_32x32x64_f8f6f4: lane l has row l % 32, of the depth 32 (l / 32) .. + 31, under one scale.
+__device__ __forceinline__ void low_scores(TileRows& st, const LowTile& t, int lane) {
+  const int i = lane & 31, h = lane >> 5;
+#pragma unroll
+  for (int tb = 0; tb < 2; ++tb) {
+    const int scale = (int)(t.scale[32 * tb + i] >> (8 * h));
+    st.s[tb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fp4_operand(t.k[32 * tb + i][low_chunk(i, h)]), fp4_operand(st.q4[0]), st.s[tb], 4, 4, 0, scale, 0, st.q4_scale);
+    st.s[tb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fp4_operand(t.k[32 * tb + i][low_chunk(i, 2 + h)]), fp4_operand(st.q4[1]), st.s[tb], 4, 4, 2, scale, 1, st.q4_scale);
+  }
+}
+
 // Scores to weights.  masked: not every row sees all tokens of the tile, the first of which is at position `at` (p, low: of this lane's row).
 __device__ __forceinline__ void tile_weights(TileRows& st, int at, int count, bool masked, int p, int low, int sinks, int lane) {
   const int h = lane >> 5;
@@ -197,6 +223,33 @@ __device__ __forceinline__ bool wave_masked(const WaveRows& w, const ContextCall
   return count < kTileTokens || at + kTileTokens - 1 > w.p_first || (at < w.low_last && at + kTileTokens > a.sinks);
 }
 
+__device__ __forceinline__ void start_low(TileRows& st, const half_t* q, int lane) {
+  st.q4_scale = 0;
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const u32x4_t* part = reinterpret_cast<const u32x4_t*>(q + 64 * j + 32 * (lane >> 5));
+    u32x4_t x[4];
+    uint32_t top = 0;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      x[c] = part[c];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) top = max(top, max(x[c][i] & 0x7fffu, (x[c][i] >> 16) & 0x7fffu));
+    }
+    const uint32_t e = max(top >> 10, 1u) + 110u;  // the largest is 4 .. 8 of the scale (FP4 ends at 6: the few beyond lose a quarter)
+    const float scale = bits_f32(e << 23);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      uint32_t w = 0;
+      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(w, as_h2(x[c][0]), scale, 0);
+      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(w, as_h2(x[c][1]), scale, 1);
+      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(w, as_h2(x[c][2]), scale, 2);
+      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(w, as_h2(x[c][3]), scale, 3);
+      st.q4[j][c] = w;
+    }
+    st.q4_scale |= (int)(e << (8 * j));
+  }
+}
 __device__ __forceinline__ void start_rows(TileRows& st, const half_t* q, int lane) {
   const uint4* src = reinterpret_cast<const uint4*>(q) + (lane >> 5);
 #pragma unroll
