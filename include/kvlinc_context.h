@@ -48,15 +48,16 @@ size_t kvlinc_prompt_workspace_bytes(const kvlinc_cache* cache, int32_t T, int32
  *   workspace      device scratch of at least kvlinc_prompt_workspace_bytes(cache, T, window, sinks, max_context) bytes, 16-byte
  *                  aligned, contents undefined before and after; NULL where that is 0
  *   max_context    host-side upper bound on the tokens a sequence holds before the call (<= 0: capacity).  It sizes the launch and,
- *                  from T * H_q / H_kv = 1024 on, the room for dequantized tokens (512 bytes each): those of a sequence that
- *                  holds more than it was promised to are left out of the sums.
+ *                  for more than 512 rows a KV head (T * H_q / H_kv), the room for dequantized tokens (580 bytes each): those
+ *                  of a sequence that holds more than it was promised to are left out of the sums.
  *
  * out[b, h, i] = ( sum_t w_t V_t + phi_q(q) S H^T ) / ( sum_t w_t + phi_q(q) P ),  w_t = exp(q K_t / sqrt 128)
  * over the tokens that row i sees; the phi terms (Eq. 5) with the adapters only.  The states S, P stand for all quantized tokens:
  * with adapters, window > 0 is refused, and so is KVLINC_FLAG_ALG1_LITERAL.  The cache may end in a partial group.
  *
- * Arithmetic: matrix products of binary16 operands with binary32 sums; softmax weights, and keys and values where they are
- * dequantized ahead of a product, are rounded to binary16 once; running maximum, sums and numerators are binary32.
+ * Arithmetic: matrix products of binary16 operands with binary32 sums; softmax weights, and values where they are dequantized
+ * ahead of a product, are rounded to binary16 once; keys are held to 2^-12 of themselves and what that leaves to a few percent;
+ * running maximum, sums and numerators are binary32.
  * Keys and values must be finite: a non-finite one among the rows reaches all outputs of its sequence that are formed with it in
  * one block of up to 128 rows, those of earlier rows too (the append then refuses the sequence).  Results do not depend on
  * the order in which the workgroups run.

@@ -39,12 +39,20 @@ long long groups_met(const kvlinc_cache& c, int T, int window, int sinks, int ma
 }
 
 constexpr int kMaxContextSplits = 32;
-constexpr long long kFewRows = 64, kDenseRows = 1024;
+// Which of the three a call of so many rows a KV head takes, measured (us; 8 KV heads, 2 bits):
+//   rows                                   64            512            640            1000
+//   1 sequence, 32k cached tokens          rows 53       tiles 137      tiles 199      tiles 243
+//                                          tiles 65      dense 135      dense 165      dense 202
+//   8 sequences of 4k                      rows 35       tiles 136      tiles 236      tiles 243
+//                                          tiles 55      dense 149      dense 188      dense 214
+// Every block of 256 rows dequantizes the tiles it goes over anew: from the third block on it pays to have done that once for all.  A wave of
+// the first kind has 16 rows and the codes for itself alone: 64 rows are what its registers and four waves make of a pair.
+constexpr long long kFewRows = 64, kTiledRows = 2 * 256;
 ContextPlan plan_call(const kvlinc_cache& c, int T, int window, int sinks, int max_context) {
   const long long rows = (long long)T * (c.H_q / c.H_kv), pairs = (long long)c.B * c.H_kv;
   const long long groups = groups_met(c, T, window, sinks, max_context);
   ContextPlan p{};
-  p.kind = rows <= kFewRows ? ContextPlan::kRows : rows < kDenseRows ? ContextPlan::kTiles : ContextPlan::kDense;
+  p.kind = rows <= kFewRows ? ContextPlan::kRows : rows <= kTiledRows ? ContextPlan::kTiles : ContextPlan::kDense;
   long long s, most;
   if (p.kind == ContextPlan::kRows) {
     // Two workgroups of four waves a compute unit, or, where the pairs are few, one of eight: fewer splits to join.

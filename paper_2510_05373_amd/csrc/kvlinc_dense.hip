@@ -4,6 +4,8 @@
 // Rows, products, softmax and schedule are those of kvlinc_prompt.hip; what differs is how a tile comes to LDS: as it lies in memory, [token]
 // [128 channels], by loads that write LDS themselves, so that no wave spends a register or a vector instruction on it.  The value operand
 // (rows = channels) comes out of the row-major tile by transposing LDS reads.
+// What the keys' rounding to binary16 leaves comes with them (64 bytes of FP4 numbers and 4 of scales a token, see LowTile): 8k tokens over 24k
+// take 4.0 ms, 3.7 without it, at three times the error.
 #include <hip/hip_runtime.h>
 
 #include "kvlinc_tiles.h"
@@ -97,7 +99,8 @@ __global__ __launch_bounds__(kTileThreads, 2) void dense_kernel(ContextCall a, i
 
   TileRows st;
   start_rows(st, a.q + wr.place * kHeadDim, lane);
-  if (total > 0) start_low(st, a.q + wr.place * kHeadDim, lane);
+  LowQuery low;
+  if (total > 0) low = low_query(a.q + wr.place * kHeadDim, lane);
 
   // Tiles that some row of the block sees: of the new rows; of the sinks; of the tokens from `near` on.  Positions of the workspace's rows:
   // 0 .. near_row - 1 are the sinks' (tokens 0 ..), from near_row on the tokens from `near` on.
@@ -174,7 +177,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void dense_kernel(ContextCall a, i
     next_phase();
     if (behind) next_phase();
     if (!wr.idle) dense_scores(st, tiles.k[0], lane);
-    if (!wr.idle && first >= n_new) low_scores(st, tiles.low[0], lane);
+    if (!wr.idle && first >= n_new) low_scores(st, tiles.low[0], low, lane);
     next_phase();
 #pragma unroll 1
     for (int k = 0; k < n; ++k) {
@@ -207,7 +210,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void dense_kernel(ContextCall a, i
         dense_order<false>();
       }
       // (a block of its own: one for both kinds of tiles in each of the above kept two copies of the accumulators)
-      if (item + 1 >= n_new && !wr.idle) low_scores(st, tiles.low[(k + 1) & 3], lane);
+      if (item + 1 >= n_new && !wr.idle) low_scores(st, tiles.low[(k + 1) & 3], low, lane);
       next_phase();
     }
     if (!behind) next_phase();

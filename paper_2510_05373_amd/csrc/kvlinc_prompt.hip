@@ -8,8 +8,9 @@
 // channels), so that a lane holds one query row throughout, and its weights are the operand of the second product as they come: lane
 // half h has tokens 16 s + 8 u + 4 h + 0..3 (u = 0, 1) of the first, and the V tile lies in LDS in that order, [channel][step s][h][u].
 // The softmax is one pass: reference of a row raised only when a score passes it by kLag (see kvlinc_rows.hip), one multiply-add, one
-// exponential, half a maximum, half a sum and half a conversion a score.  Roundings to binary16: keys and values that are dequantized
-// (codes times scales; a second term would double the products) and the weights; scores, sums and numerators stay binary32.
+// exponential, half a maximum, half a sum and half a conversion a score.  Roundings to binary16: dequantized values (2^-12 of each; a second term
+// would be 16 products a tile more), the weights, and dequantized keys, whose loss is added back in FP4 (see LowTile); scores, sums and numerators
+// stay binary32.
 // The new rows come first, in their own basis; then the accumulators are rotated, and the cache's tiles follow.
 //
 // Schedule.  A wave's tile is a matrix phase (P V of the tile, K Q of the next) and a vector phase (softmax, its share of a later tile into
@@ -29,6 +30,10 @@ struct Tiles {
   u32x4_t k[2][kTileTokens][16];
   u32x4_t v[3][kHeadDim][8];
   u32x4_t meta[kTileWaves][64];
+  LowTile low[2];  // as the key tiles
+  // a wave's LowQuery (in registers all the time it made others spill, in every tile)
+  u32x4_t q_low[kTileWaves][2][64];
+  u32x4_t q_low_end[kTileWaves][64];
 };
 typedef u32x4_t (*KeyTile)[16];
 typedef u32x4_t (*ValueTile)[8];
@@ -54,16 +59,19 @@ struct Share {
 
 template <int BITS>
 __device__ __forceinline__ void load_raw_keys(Share<BITS>& s, const half_t* rows, int count, int tid) {
+  asm("" : "+v"(tid));
 #pragma unroll
   for (int u = 0; u < 2; ++u) s.x[u] = reinterpret_cast<const u32x4_t*>(rows + (long long)min((tid >> 4) + 32 * u, count - 1) * kHeadDim)[tid & 15];
 }
 template <int BITS>
 __device__ __forceinline__ void store_raw_keys(const Share<BITS>& s, KeyTile t, int tid) {
+  asm("" : "+v"(tid));
 #pragma unroll
   for (int u = 0; u < 2; ++u) t[(tid >> 4) + 32 * u][key_chunk((tid >> 4) + 32 * u, tid & 15)] = s.x[u];
 }
 template <int BITS>
 __device__ __forceinline__ void load_raw_values(Share<BITS>& s, const half_t* rows, int count, int tid) {
+  asm("" : "+v"(tid));
 #pragma unroll
   for (int u = 0; u < 4; ++u) {
     const u32x2_t w = reinterpret_cast<const u32x2_t*>(rows + (long long)min(4 * (tid >> 5) + u, count - 1) * kHeadDim)[tid & 31];
@@ -73,6 +81,7 @@ __device__ __forceinline__ void load_raw_values(Share<BITS>& s, const half_t* ro
 }
 template <int BITS>
 __device__ __forceinline__ void store_raw_values(const Share<BITS>& s, ValueTile t, int tid) {  // 4 tokens x 4 channels, turned over
+  asm("" : "+v"(tid));
   const int quad = tid >> 5, ch = 4 * (tid & 31);
   put_value_quad(t, ch, quad, low_halves(s.x[2][0], s.x[2][2]), low_halves(s.x[3][0], s.x[3][2]));
   put_value_quad(t, ch + 1, quad, high_halves(s.x[2][0], s.x[2][2]), high_halves(s.x[3][0], s.x[3][2]));
@@ -81,6 +90,7 @@ __device__ __forceinline__ void store_raw_values(const Share<BITS>& s, ValueTile
 }
 template <int BITS>
 __device__ __forceinline__ void load_window_values(Share<BITS>& s, const half_t* v_win, int quad0, int quads, int tid) {
+  asm("" : "+v"(tid));
 #pragma unroll
   for (int u = 0; u < 4; ++u) {
     const u32x2_t w = reinterpret_cast<const u32x2_t*>(v_win)[min(quad0 + 4 * u + (tid >> 7), quads - 1) * kHeadDim + (tid & 127)];
@@ -90,12 +100,14 @@ __device__ __forceinline__ void load_window_values(Share<BITS>& s, const half_t*
 }
 template <int BITS>
 __device__ __forceinline__ void store_window_values(const Share<BITS>& s, ValueTile t, int tid) {
+  asm("" : "+v"(tid));
 #pragma unroll
   for (int u = 0; u < 4; ++u) put_value_quad(t, tid & 127, 4 * u + (tid >> 7), s.x[2 + (u >> 1)][2 * (u & 1)], s.x[2 + (u >> 1)][2 * (u & 1) + 1]);
 }
 
 template <int BITS>
 __device__ __forceinline__ void load_packed(Share<BITS>& s, const uint32_t* rec, int half, int tid) {
+  asm("" : "+v"(tid));
   const int n = tid >> 6, j = tid & 15, q4 = (tid >> 4) & 3;
   s.x[0] = reinterpret_cast<const u32x4_t*>(rec + Rec<BITS>::kKeyScale)[tid & 63];
 #pragma unroll
@@ -114,9 +126,20 @@ __device__ __forceinline__ uint32_t dequantized(half2_t centred, uint32_t s, uin
   const half_t c = (half_t)Rec<BITS>::kCentre, top = (half_t)65504.0f;
   return as_u32(__builtin_elementwise_min(__builtin_elementwise_fma(centred + half2_t{c, c}, as_h2(s), as_h2(z)), half2_t{top, top}));
 }
+// Channels 2 SEL, 2 SEL + 1 of eight, and what their rounding leaves.
 template <int BITS, int SEL>
-__device__ __forceinline__ uint32_t key_pair(const uint32_t (&e)[BITS / 2], u32x4_t s, u32x4_t z) {
-  return dequantized<BITS>(code_pair<BITS, SEL>(e, 1.0f), s[SEL], z[SEL]);
+__device__ __forceinline__ uint32_t key_pair(const uint32_t (&e)[BITS / 2], u32x4_t s, u32x4_t z, float (&rest)[8]) {
+  const half2_t centred = code_pair<BITS, SEL>(e, 1.0f), ss = as_h2(s[SEL]), zz = as_h2(z[SEL]);
+  const uint32_t key = dequantized<BITS>(centred, s[SEL], z[SEL]);
+  const half_t c = (half_t)Rec<BITS>::kCentre;
+  const half2_t code = centred + half2_t{c, c};
+#pragma unroll
+  for (int i = 0; i < 2; ++i) rest[2 * SEL + i] = fmaf((float)code[i], (float)ss[i], (float)zz[i]) - (float)as_h2(key)[i];
+  return key;
+}
+template <int BITS>
+__device__ __forceinline__ u32x4_t key_chunk_of(const uint32_t (&e)[BITS / 2], u32x4_t s, u32x4_t z, float (&rest)[8]) {
+  return u32x4_t{key_pair<BITS, 0>(e, s, z, rest), key_pair<BITS, 1>(e, s, z, rest), key_pair<BITS, 2>(e, s, z, rest), key_pair<BITS, 3>(e, s, z, rest)};
 }
 // Tokens i' = 2 SEL, 2 SEL + 1 of a half (quads 4 i' + q4) from byte SEL of the value words.
 template <int BITS, int SEL>
@@ -133,7 +156,8 @@ __device__ __forceinline__ void value_quads(const uint32_t (&e)[2][BITS / 2], co
   put_value_quad(t, ch, 8 * SEL + 4 + q4, hi[0], hi[1]);
 }
 template <int BITS>
-__device__ __forceinline__ void store_packed(const Share<BITS>& s, u32x4_t* meta, KeyTile kt, ValueTile vt, int half, int tid) {
+__device__ __forceinline__ void store_packed(const Share<BITS>& s, u32x4_t* meta, KeyTile kt, LowTile& low, ValueTile vt, int half, int tid) {
+  asm("" : "+v"(tid));  // (addresses formed here, not kept over the loop)
   meta[tid & 63] = s.x[0];
   __builtin_amdgcn_wave_barrier();  // (a wave's LDS instructions stay in order)
   {
@@ -145,9 +169,26 @@ __device__ __forceinline__ void store_packed(const Share<BITS>& s, u32x4_t* meta
       e[pl] = n.first; o[pl] = n.second;
     }
     const u32x4_t s0 = meta[chunk], s1 = meta[chunk + 1], z0 = meta[16 + chunk], z1 = meta[17 + chunk];  // a chunk of 8 channels is 16 bytes here, too
-    kt[token][key_chunk(token, chunk)] = u32x4_t{key_pair<BITS, 0>(e, s0, z0), key_pair<BITS, 1>(e, s0, z0), key_pair<BITS, 2>(e, s0, z0), key_pair<BITS, 3>(e, s0, z0)};
-    kt[token][key_chunk(token, chunk + 1)] = u32x4_t{key_pair<BITS, 0>(o, s1, z1), key_pair<BITS, 1>(o, s1, z1), key_pair<BITS, 2>(o, s1, z1), key_pair<BITS, 3>(o, s1, z1)};
+    float r0[8], r1[8];
+    const u32x4_t k0 = key_chunk_of<BITS>(e, s0, z0, r0), k1 = key_chunk_of<BITS>(o, s1, z1, r1);
+    kt[token][key_chunk(token, chunk)] = k0;
+    kt[token][key_chunk(token, chunk + 1)] = k1;
+    // the largest of the token's 32 channels: this thread's 16 and its neighbour's (as integers, halves apart)
+    uint32_t even = 0, odd = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      even = max(even, max(k0[i] & 0x7fffu, k1[i] & 0x7fffu));
+      odd = max(odd, max(k0[i] & 0x7fff0000u, k1[i] & 0x7fff0000u));
+    }
+    uint32_t top = max(even, odd >> 16);
+    top = max(top, dpp_u<kQuadSwap1>(top));
+    const uint32_t scale = low_scale_of(top);
+    const float by = bits_f32(scale << 23);
+    const int g = chunk >> 2;
+    reinterpret_cast<u32x2_t*>(&low.k[token][low_chunk(token, g)])[tid & 1] = u32x2_t{fp4_of(r0, by), fp4_of(r1, by)};
+    if ((tid & 1) == 0) reinterpret_cast<uint8_t*>(&low.scale[token])[g] = (uint8_t)scale;
   }
+  __builtin_amdgcn_sched_barrier(0);
   const int ch = 16 * (tid >> 6) + (tid & 15), q4 = (tid >> 4) & 3;
   // word 8 t + n of the value pairs is token 16 n + t: tokens 16 i + 4 q4 + 2 hg + e, i = 4 half + 0..3, in 16 bytes
   const u32x4_t sz[4] = {meta[32 + 2 * (4 * q4) + half], meta[32 + 2 * (4 * q4 + 1) + half], meta[32 + 2 * (4 * q4 + 2) + half], meta[32 + 2 * (4 * q4 + 3) + half]};
@@ -182,6 +223,7 @@ __device__ __forceinline__ void slide_values(ValueTile t, const half_t* v_win, i
 // S^T = K Q^T of a tile.  A lane's chunks 2 k + h of rows i and 32 + i: key_chunk only flips address bits, so they are one address with
 // k in bits 5..7 flipped (chunk and i & 15 are four bits).
 __device__ __forceinline__ void tile_scores(TileRows& st, KeyTile t, int lane) {
+  asm("" : "+v"(lane));
   const int i = lane & 31, base = i * 256 + 16 * key_chunk(i, lane >> 5);
 #pragma unroll
   for (int tb = 0; tb < 2; ++tb)
@@ -194,6 +236,7 @@ __device__ __forceinline__ void tile_scores(TileRows& st, KeyTile t, int lane) {
 }
 // O^T += V^T P^T.  Chunks 2 k + h of rows 32 cb + i: the same, value_chunk of row 32 cb + i being that of row i with 2 cb flipped.
 __device__ __forceinline__ void tile_values(TileRows& st, ValueTile t, int lane) {
+  asm("" : "+v"(lane));
   const int i = lane & 31, base = i * 128 + 16 * value_chunk(i, lane >> 5);
 #pragma unroll
   for (int k = 0; k < 4; ++k)
@@ -217,7 +260,25 @@ __global__ __launch_bounds__(kTileThreads, 2) void tile_kernel(ContextCall a, in
   const WaveRows wr = wave_rows(a, b, kvh, rows, row0 + 32 * wave, total, lane);
 
   TileRows st;
+  int low_scale = 0;
   start_rows(st, a.q + wr.place * kHeadDim, lane);
+  if (len.nq > 0) {
+    const LowQuery q = low_query(a.q + wr.place * kHeadDim, lane);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) tiles.q_low[wave][j][lane] = u32x4_t{q.q[j][0], q.q[j][1], q.q[j][2], q.q[j][3]};
+    tiles.q_low_end[wave][lane] = u32x4_t{q.q[0][4], q.q[0][5], q.q[1][4], q.q[1][5]};
+    low_scale = q.scale;
+  }
+  auto add_low = [&](const LowTile& t) __attribute__((always_inline)) {
+    int lane = tid & 63;
+    asm("" : "+v"(lane));
+    const u32x4_t a0 = tiles.q_low[wave][0][lane], a1 = tiles.q_low[wave][1][lane], e = tiles.q_low_end[wave][lane];
+    LowQuery q;
+    q.q[0] = u32x6_t{a0[0], a0[1], a0[2], a0[3], e[0], e[1]};
+    q.q[1] = u32x6_t{a1[0], a1[1], a1[2], a1[3], e[2], e[3]};
+    q.scale = low_scale;
+    low_scores(st, t, q, lane);
+  };
 
   // Tiles that some row of the block sees: of the new rows, of the window, halves of groups; this split has first .. last - 1 of them.
   const int last_i = min(row0 + kTileRows - 1, rows - 1) / gq, low_block = window_low(total + row0 / gq, a.window);
@@ -258,7 +319,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void tile_kernel(ContextCall a, in
       else store_window_values<BITS>(sh, tiles.v[vb], tid);
     } else {
       const int hf = half_of(it);
-      store_packed<BITS>(sh, tiles.meta[wave], tiles.k[kb], tiles.v[vb], hf & 1, tid);
+      store_packed<BITS>(sh, tiles.meta[wave], tiles.k[kb], tiles.low[kb], tiles.v[vb], hf & 1, tid);
       if (SLIDING && (hf >> 1) == newest) slide_values(tiles.v[vb], v_win, hf & 1, len.nr, tid);
     }
   };
@@ -285,6 +346,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void tile_kernel(ContextCall a, in
 #pragma unroll
     for (int k = 0; k < 8; ++k) asm volatile("" : "+v"(st.q[k]));
     if (!wr.idle) tile_scores(st, tiles.k[0], lane);
+    if (!wr.idle && first >= raw) add_low(tiles.low[0]);
     next_phase();
     int vb = 0;
 #pragma unroll 1
@@ -306,6 +368,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void tile_kernel(ContextCall a, in
       }
       const bool live = wave_sees(wr, a, at, count);
       if (live) tile_weights(st, at, count, wave_masked(wr, a, at, count), wr.p, wr.low, a.sinks, lane);
+      __builtin_amdgcn_sched_barrier(0);
       if (to < n) put_next();
       next_phase();
       // matrix phase
@@ -317,6 +380,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void tile_kernel(ContextCall a, in
         tile_scores(st, tiles.k[(k + 1) & 1], lane);
         matrix_order<16>();
       }
+      if (item + 1 >= raw && !wr.idle) add_low(tiles.low[(k + 1) & 1]);
       vb = vb == 2 ? 0 : vb + 1;
       next_phase();
     }

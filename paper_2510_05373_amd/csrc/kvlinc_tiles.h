@@ -26,8 +26,6 @@ __device__ __forceinline__ void next_phase() {
 // ---- a wave's rows ----------------------------------------------------------------------------------------------------------------
 struct TileRows {
   half8_t q[8];      // channels 16 s + 8 h + 0..7 of this lane's row
-  u32x6_t q_low[2];  // and, for the products of low_scores, channels 64 j + 32 h + 0..31 as FP6 (E2M3) numbers
-  int q_low_scale;   // their scales in bytes j
   float m, l;        // reference (log2 domain), per-lane sum of the weights
   bool far;          // some row's reference is beyond kFusedBound (the same in all lanes)
   float16_t acc[4];  // numerator of channels 32 cb + 8 (r / 4) + 4 h + r % 4
@@ -79,8 +77,37 @@ __device__ __forceinline__ int low_chunk(int t, int c) { return c ^ ((t >> 2) & 
 typedef int i32x8_t __attribute__((ext_vector_type(8)));
 __device__ __forceinline__ i32x8_t fp6_operand(u32x6_t v) { return i32x8_t{(int)v[0], (int)v[1], (int)v[2], (int)v[3], (int)v[4], (int)v[5], 0, 0}; }
 __device__ __forceinline__ i32x8_t fp4_operand(u32x4_t v) { return i32x8_t{(int)v[0], (int)v[1], (int)v[2], (int)v[3], 0, 0, 0, 0}; }
+struct LowQuery {
+  u32x6_t q[2];  // channels 64 j + 32 h + 0..31 of this lane's row as FP6 (E2M3) numbers
+  int scale;     // exponents of their scales in bytes j
+};
+__device__ __forceinline__ LowQuery low_query(const half_t* q, int lane) {
+  LowQuery r;
+  r.scale = 0;
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const u32x4_t* part = reinterpret_cast<const u32x4_t*>(q + 64 * j + 32 * (lane >> 5));
+    u32x4_t x[4];
+    uint32_t top = 0;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      x[c] = part[c];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) top = max(top, max(x[c][i] & 0x7fffu, (x[c][i] >> 16) & 0x7fffu));
+    }
+    const uint32_t e = max(top >> 10, 1u) + 110u;  // the largest is 4 .. 8 of the scale (FP6 ends at 7.5)
+    half32_t v;
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[8 * c + i] = as_h8(x[c])[i];
+    r.q[j] = __builtin_amdgcn_cvt_scalef32_pk32_fp6_f16(v, bits_f32(e << 23));
+    r.scale |= (int)(e << (8 * j));
+  }
+  return r;
+}
 // v_mfma_scale_f32_32x32x64_f8f6f4: lane l has row l % 32, of the depth 32 (l / 32) .. + 31, under one scale.
-__device__ __forceinline__ void low_scores(TileRows& st, const LowTile& t, int lane) {
+__device__ __forceinline__ void low_scores(TileRows& st, const LowTile& t, const LowQuery& q, int lane) {
   const int i = lane & 31, h = lane >> 5;
   int scale[2];
   u32x4_t k[2][2];
@@ -91,9 +118,9 @@ __device__ __forceinline__ void low_scores(TileRows& st, const LowTile& t, int l
     for (int j = 0; j < 2; ++j) k[tb][j] = t.k[32 * tb + i][low_chunk(i, 2 * j + h)];
   }
 #pragma unroll
-  for (int tb = 0; tb < 2; ++tb) st.s[tb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fp4_operand(k[tb][0]), fp6_operand(st.q_low[0]), st.s[tb], 4, 2, 0, scale[tb], 0, st.q_low_scale);
+  for (int tb = 0; tb < 2; ++tb) st.s[tb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fp4_operand(k[tb][0]), fp6_operand(q.q[0]), st.s[tb], 4, 2, 0, scale[tb], 0, q.scale);
 #pragma unroll
-  for (int tb = 0; tb < 2; ++tb) st.s[tb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fp4_operand(k[tb][1]), fp6_operand(st.q_low[1]), st.s[tb], 4, 2, 2, scale[tb], 1, st.q_low_scale);
+  for (int tb = 0; tb < 2; ++tb) st.s[tb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fp4_operand(k[tb][1]), fp6_operand(q.q[1]), st.s[tb], 4, 2, 2, scale[tb], 1, q.scale);
   __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
   __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
 }
@@ -234,29 +261,6 @@ __device__ __forceinline__ bool wave_masked(const WaveRows& w, const ContextCall
   return count < kTileTokens || at + kTileTokens - 1 > w.p_first || (at < w.low_last && at + kTileTokens > a.sinks);
 }
 
-__device__ __forceinline__ void start_low(TileRows& st, const half_t* q, int lane) {
-  st.q_low_scale = 0;
-#pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    const u32x4_t* part = reinterpret_cast<const u32x4_t*>(q + 64 * j + 32 * (lane >> 5));
-    u32x4_t x[4];
-    uint32_t top = 0;
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      x[c] = part[c];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) top = max(top, max(x[c][i] & 0x7fffu, (x[c][i] >> 16) & 0x7fffu));
-    }
-    const uint32_t e = max(top >> 10, 1u) + 110u;  // the largest is 4 .. 8 of the scale (FP6 ends at 7.5)
-    half32_t v;
-#pragma unroll
-    for (int c = 0; c < 4; ++c)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[8 * c + i] = as_h8(x[c])[i];
-    st.q_low[j] = __builtin_amdgcn_cvt_scalef32_pk32_fp6_f16(v, bits_f32(e << 23));
-    st.q_low_scale |= (int)(e << (8 * j));
-  }
-}
 __device__ __forceinline__ void start_rows(TileRows& st, const half_t* q, int lane) {
   const uint4* src = reinterpret_cast<const uint4*>(q) + (lane >> 5);
 #pragma unroll

@@ -269,7 +269,7 @@ def test_windowed_decode_over_its_own_queries():
 
 # ---- the ends of the ranges ------------------------------------------------------------------------------------------------------
 
-@pytest.mark.parametrize("rows", [4, 5, 8, 9, 16, 17, 32, 33, 48, 49, 64, 65, 256, 257, 1023, 1024])
+@pytest.mark.parametrize("rows", [4, 5, 8, 9, 16, 17, 32, 33, 48, 49, 64, 65, 256, 257, 511, 512, 513, 1023, 1024])
 def test_numbers_of_rows_where_the_work_is_laid_out_anew(rows):
     run_case(980, 1, 1, [333], [rows])
 
@@ -285,6 +285,55 @@ def test_sinks_apart_from_the_window_and_many_rows(window, sinks, bits):
 @pytest.mark.parametrize("corr", [False, True])
 def test_long_contexts_in_splits(lengths, rows, H_q, H_kv, corr):
     run_case(982, H_q, H_kv, lengths, rows, corr=corr)
+
+
+@pytest.mark.parametrize("bits", [2, 4])
+@pytest.mark.parametrize("window, sinks, corr, sliding, keep", [(0, 0, False, False, 0), (100, 3, False, False, 0), (1, 200, False, True, 0), (700, 1, False, False, 60),
+                                                                (0, 0, True, False, 0), (0, 0, True, True, 0), (0, 0, False, False, 32)])
+def test_two_blocks_of_rows(window, sinks, corr, sliding, keep, bits):
+    run_case(992, 8, 2, [900, 130, 0, 385], [128, 100, 65, 3], bits, window, sinks, corr=corr, sliding=sliding, keep=keep, R=64 if keep else 128)
+
+
+@pytest.mark.parametrize("bits", [2, 4])
+@pytest.mark.parametrize("T", [3, 40, 300])
+def test_keys_of_different_magnitudes(T, bits):
+    # channels from 2^-10 to 2^10 of one another, and queries that even them out: every scale of the parts that the rounding of a key leaves
+    B, H_q, H_kv, n = 1, 4, 1, 400
+    K, V, q, k_new, v_new = ref.inputs(993, B, H_q, H_kv, [n], T)
+    gain = 2.0 ** np.random.default_rng(3).integers(-10, 11, 128)
+    K = [[(K[0][0].astype(np.float32) * gain).astype(np.float16)]]
+    k_new, q = (k_new.astype(np.float32) * gain).astype(np.float16), (q.astype(np.float32) / gain).astype(np.float16)
+    cache = filled(B, H_q, H_kv, K, V, 512, bits)
+    assert cache.status.item() == 0
+    got = cache.prompt_attention(to_dev(q), to_dev(k_new), to_dev(v_new)).cpu().numpy()
+    keys, values, _ = ref.tokens_of(K[0][0], V[0][0], o_cache.window_split(n)[0], bits)
+    keys, values = np.concatenate([keys, k_new[0, 0].astype(np.float64)]), np.concatenate([values, v_new[0, 0].astype(np.float64)])
+    for h in range(H_q):
+        y, tol = ref.attend(q[0, h], keys, values, n + np.arange(T))
+        ref.check_rows(got[0, h], y, tol, h)
+
+
+@pytest.mark.parametrize("bits", [2, 4])
+@pytest.mark.parametrize("H_q, H_kv, T", [(8, 2, 4), (8, 2, 40), (8, 2, 150)])
+def test_what_the_roundings_come_to(H_q, H_kv, T, bits):
+    # All rows together, as norms of independent roundings.  One is uniform in half a step, 2^-11 / sqrt(12) = 1.4e-4 relative where a binade
+    # starts and half of that where it ends: the output's, the weights', the values' (of s |code|, up to twice the value: counted as two), and a
+    # tenth of what binary16 keys would cost the scores, 2^-12 / sqrt(3) * sqrt(380 / 128) = 2.4e-4.  sqrt(1 + 1 + 4) * 1.4e-4 = 3.4e-4 at the most,
+    # and 1.4 times that for the rows that few tokens decide: their roundings are no average.  Binary16 keys alone: 8e-4.
+    B, n = 2, 1500
+    K, V, q, k_new, v_new = ref.inputs(994, B, H_q, H_kv, [n] * B, T)
+    cache = filled(B, H_q, H_kv, K, V, 2048, bits)
+    got = cache.prompt_attention(to_dev(q), to_dev(k_new), to_dev(v_new)).cpu().numpy()
+    num = den = 0.0
+    for b in range(B):
+        for g in range(H_kv):
+            keys, values, _ = ref.tokens_of(K[b][g], V[b][g], o_cache.window_split(n)[0], bits)
+            keys, values = np.concatenate([keys, k_new[b, g].astype(np.float64)]), np.concatenate([values, v_new[b, g].astype(np.float64)])
+            for h in range(g * (H_q // H_kv), (g + 1) * (H_q // H_kv)):
+                y, tol = ref.attend(q[b, h], keys, values, n + np.arange(T))
+                d2, y2 = ref.check_rows(got[b, h], y, tol, (b, h))
+                num, den = num + d2, den + y2
+    assert (num / den) ** 0.5 <= 4.8e-4, (num / den) ** 0.5
 
 
 @pytest.mark.parametrize("pairs", [3, 8, 16, 24])
