@@ -221,13 +221,21 @@ struct ReadRange {
   int blocks, per_tensor;
   LowTarget low;
 };
+// Workgroups are dealt to the 8 XCDs in turn; runs of 64 blocks (2 MB of binary16 rows) go to one of them, so that each writes few pages at a time:
+// 16 sequences of 8k tokens, 8 heads, outputs and records that no cache holds: 197 us without, 163 with runs of 16, 144 of 32, 142 of 64, 139 of 128
+// (longer runs share a batch of few sequences out less evenly).
+__device__ __forceinline__ int in_runs(int id, int all) {
+  constexpr int kRun = 64;
+  const int y = id >> 3, run = y / kRun;
+  return id < all - all % (8 * kRun) ? (run * 8 + (id & 7)) * kRun + (y - run * kRun) : id;
+}
 template <int BITS, typename OUT, bool ROTATED, bool LOW>
 __global__ __launch_bounds__(256) void read_kernel(kvlinc_cache c, ReadRange range, OUT* k_out, OUT* v_out) {
   const int blocks = range.blocks, per_tensor = range.per_tensor;
   __shared__ __align__(16) WaveRows<OUT> all[4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const bool values = k_out == nullptr || (int)blockIdx.x >= per_tensor;
-  const int id = (int)blockIdx.x >= per_tensor ? blockIdx.x - per_tensor : blockIdx.x;
+  const int id = in_runs((int)blockIdx.x >= per_tensor ? blockIdx.x - per_tensor : blockIdx.x, per_tensor);
   const int bh = id / blocks, b = bh / c.H_kv, in_pair = id - bh * blocks;
   const bool lead = in_pair < range.lead_blocks;
   const Lengths len = lengths_of(c, b);
