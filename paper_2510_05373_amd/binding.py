@@ -1,4 +1,5 @@
 """ctypes binding of libkvlinc.so.  Same names and argument order as include/kvlinc.h and include/kvlinc_context.h."""
+import contextlib
 import ctypes
 import os
 
@@ -185,6 +186,9 @@ def kvlinc_cache_read(cache, first, T, k_out, v_out, dtype=KVLINC_F16, rotated=0
                                  _stream(stream))
 
 
+_NOTHING = contextlib.nullcontext()
+
+
 class KVLincCache:
     """Device buffers of one layer's cache plus the descriptor that points at them (allocation only)."""
 
@@ -227,7 +231,9 @@ class KVLincCache:
             Wq=None if Wq is None else Wq.data_ptr(), Wk=None if Wk is None else Wk.data_ptr(),
             status=self.status.data_ptr(), split_done=self.split_done.data_ptr(), flags=int(flags))
         self._ws = None
-        self._context_ws = []  # scratch of prompt_attention and decode_windowed, the largest last
+        self._context_ws = None  # scratch of prompt_attention and decode_windowed, and the streams that have used it
+        self._context_streams = set()
+        self._captured_ws = []
 
     def bytes(self):
         ts = [self.groups, self.k_res, self.v_res]
@@ -262,51 +268,56 @@ class KVLincCache:
         return out
 
     # The calls below check their tensors: what the C entry points take is an address.
-    def _tensor(self, t, name, shape, dtypes):
+    def _tensor(self, t, name, shape, dtype):
         import torch
-        if not torch.is_tensor(t) or t.dtype not in dtypes or tuple(t.shape) != tuple(shape):
-            raise KVLincError("%s has to be a %s tensor of shape %s" % (name, " or ".join(str(d) for d in dtypes), tuple(shape)))
+        if not torch.is_tensor(t) or t.dtype != dtype or t.shape != shape:
+            raise KVLincError("%s has to be a %s tensor of shape %s" % (name, dtype, tuple(shape)))
         if t.device != self.groups.device:
             raise KVLincError("%s is on %s, the cache on %s" % (name, t.device, self.groups.device))
         if not t.is_contiguous():
             raise KVLincError("%s has to be contiguous" % name)
-        return t
 
     def _on(self, stream, *tensors):
         """The cache's device current, and `stream`, if one is given: what is allocated inside belongs to the stream that uses it, and the
         caller's tensors are not handed out again before it is done with them."""
-        import contextlib
         import torch
         dev = self.groups.device
         if dev.type != "cuda":
             raise KVLincError("the cache is on %s: the kernels need a GPU" % dev)
-        if stream is not None and not hasattr(stream, "cuda_stream"):
+        here = torch.cuda.current_device() == dev.index
+        if stream is None:
+            return _NOTHING if here else torch.cuda.device(dev)
+        if not hasattr(stream, "cuda_stream"):
             stream = torch.cuda.ExternalStream(int(stream), device=dev)
-        if stream is not None and stream.device != dev:
+        if stream.device != dev:
             raise KVLincError("the stream is on %s, the cache on %s" % (stream.device, dev))
-        scope = contextlib.ExitStack()
-        if torch.cuda.current_device() != dev.index:
-            scope.enter_context(torch.cuda.device(dev))
-        if stream is not None:
-            scope.enter_context(torch.cuda.stream(stream))
-            for t in tensors:
-                if t is not None:
-                    t.record_stream(stream)
-        return scope
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
+        return torch.cuda.stream(stream)  # (makes its device current, too)
 
     @staticmethod
     def _limits(window, sinks):
         if window < 0 or sinks < 0:
             raise KVLincError("window and sinks have to be 0 or more, not %s and %s" % (window, sinks))
 
-    def _context_workspace(self, need):
-        """Scratch of at least `need` bytes.  One that has become too small is kept: a captured graph may still use it."""
+    def _with_scratch(self, call, need):
+        """call(scratch) on the current stream, with the scratch at hand if it does (the library looks before it launches anything), else with
+        one of need() bytes.  One that a captured graph uses is kept as long as the cache."""
         import torch
-        if need == 0:
-            return None
-        if not self._context_ws or self._context_ws[-1].numel() * 4 < need:
-            self._context_ws.append(torch.empty((need + 3) // 4, dtype=torch.float32, device=self.groups.device))
-        return self._context_ws[-1]
+        ws = self._context_ws
+        rc = call(ws)
+        stream = _stream(None)
+        if rc == KVLINC_EWORKSPACE:
+            ws = self._context_ws = torch.empty((need() + 3) // 4, dtype=torch.float32, device=self.groups.device)
+            self._context_streams = {stream}
+            rc = call(ws)
+        elif ws is not None and stream not in self._context_streams:  # (not handed out again before this stream is done with it)
+            ws.record_stream(torch.cuda.current_stream())
+            self._context_streams.add(stream)
+        if ws is not None and torch.cuda.is_current_stream_capturing() and not any(ws is t for t in self._captured_ws):
+            self._captured_ws.append(ws)
+        return rc
 
     def prompt_attention(self, q, k_new, v_new, n_new=None, window=0, sinks=0, out=None, max_context=0, stream=None):
         """Attention of T new tokens of every sequence over the cache and, causally, their own rows; append them afterwards.
@@ -316,7 +327,7 @@ class KVLincCache:
         import torch
         if not torch.is_tensor(q) or q.dim() != 4:
             raise KVLincError("q has to be a tensor of shape [B, H_q, T, 128]")
-        T, half = q.shape[2], (torch.float16,)
+        T, half = q.shape[2], torch.float16
         self._limits(window, sinks)
         if T < 1:
             raise KVLincError("q has no rows")
@@ -324,14 +335,14 @@ class KVLincCache:
         self._tensor(k_new, "k_new", (self.B, self.H_kv, T, 128), half)
         self._tensor(v_new, "v_new", (self.B, self.H_kv, T, 128), half)
         if n_new is not None:
-            self._tensor(n_new, "n_new", (self.B,), (torch.int32,))
+            self._tensor(n_new, "n_new", (self.B,), torch.int32)
         if out is not None:
             self._tensor(out, "out", q.shape, half)
         with self._on(stream, q, k_new, v_new, n_new, out):
             if out is None:
                 out = torch.empty_like(q) if n_new is None else torch.zeros_like(q)
-            ws = self._context_workspace(kvlinc_prompt_workspace_bytes(self, T, window, sinks, max_context))
-            rc = kvlinc_prompt_attention(self, q, k_new, v_new, n_new, T, window, sinks, out, ws, None, max_context, stream)
+            rc = self._with_scratch(lambda ws: kvlinc_prompt_attention(self, q, k_new, v_new, n_new, T, window, sinks, out, ws, None, max_context, stream),
+                                    lambda: kvlinc_prompt_workspace_bytes(self, T, window, sinks, max_context))
         if rc != KVLINC_OK:
             raise KVLincError("kvlinc_prompt_attention: " + kvlinc_strerror(rc))
         return out
@@ -339,7 +350,7 @@ class KVLincCache:
     def decode_windowed(self, q, window, sinks=0, out=None, max_context=0, stream=None):
         """decode() over the newest `window` tokens and the first `sinks` ones (window = 0: all).  q: [B, H_q, 128] fp16."""
         import torch
-        half = (torch.float16,)
+        half = torch.float16
         self._limits(window, sinks)
         self._tensor(q, "q", (self.B, self.H_q, 128), half)
         if out is not None:
@@ -347,8 +358,8 @@ class KVLincCache:
         with self._on(stream, q, out):
             if out is None:
                 out = torch.empty_like(q)
-            ws = self._context_workspace(kvlinc_decode_windowed_workspace_bytes(self, window, sinks, max_context))
-            rc = kvlinc_decode_attention_windowed(self, q, window, sinks, out, ws, None, max_context, stream)
+            rc = self._with_scratch(lambda ws: kvlinc_decode_attention_windowed(self, q, window, sinks, out, ws, None, max_context, stream),
+                                    lambda: kvlinc_decode_windowed_workspace_bytes(self, window, sinks, max_context))
         if rc != KVLINC_OK:
             raise KVLincError("kvlinc_decode_attention_windowed: " + kvlinc_strerror(rc))
         return out
@@ -373,9 +384,9 @@ class KVLincCache:
         shape = (self.B, self.H_kv, int(T), 128)
         for t, name in ((k_out, "k_out"), (v_out, "v_out")):
             if t is not None:
-                self._tensor(t, name, shape, (dtype,))
+                self._tensor(t, name, shape, dtype)
         if first is not None:
-            self._tensor(first, "first", (self.B,), (torch.int32,))
+            self._tensor(first, "first", (self.B,), torch.int32)
         with self._on(stream, first, k_out, v_out):
             if not given:
                 k_out, v_out = (torch.zeros(shape, dtype=dtype, device=self.groups.device) for _ in range(2))

@@ -109,13 +109,23 @@ def test_decoding_is_what_it_was_after_these_calls():
 
 def test_workspaces_of_different_sizes():
     K, V, _, _, _ = ref.inputs(972, 1, 8, 1, [2000], 1)
-    cache, other = filled(1, 8, 1, K, V, 2304), filled(1, 8, 1, K, V, 2304)
-    calls = [inputs(1, 8, 1, T, T) for T in (2, 300, 60, 2, 900, 1)]
+    cache = filled(1, 8, 1, K, V, 2304)
+    sizes = (2, 300, 60, 2, 900, 1)
+    calls = [inputs(1, 8, 1, T, T) for T in sizes]
     got = [cache.prompt_attention(*c) for c in calls]
-    assert len(cache._context_ws) >= 3
     for c, g in zip(calls, got):
-        other._context_ws = []
-        assert same(other.prompt_attention(*c), g)
+        assert same(filled(1, 8, 1, K, V, 2304).prompt_attention(*c), g)
+
+
+def test_scratch_that_is_outgrown_is_given_back():
+    cache = kv.KVLincCache(1, 8, 2, 1 << 16)
+    args = inputs(1, 8, 2, 300)
+    torch.cuda.synchronize()
+    before = torch.cuda.memory_allocated()
+    for bound in range(1 << 12, 1 << 16, 1 << 12):  # (room for the dequantized tokens of the bound)
+        cache.prompt_attention(*args, max_context=bound, out=torch.empty_like(args[0]))
+    need = kv.kvlinc_prompt_workspace_bytes(cache, 300, max_context=15 << 12)
+    assert need > 2 * 15 * 4096 * 512 and torch.cuda.memory_allocated() - before < need + (1 << 22)
 
 
 # ---- graphs ----------------------------------------------------------------------------------------------------------------------
