@@ -7,7 +7,7 @@
 // Both products run on v_mfma_f32_32x32x16_f16, transposed: S^T = K Q^T (rows = tokens, columns = query rows) and O^T = V^T P^T (rows =
 // channels), so that a lane holds one query row throughout, and its weights are the operand of the second product as they come: lane
 // half h has tokens 16 s + 8 u + 4 h + 0..3 (u = 0, 1) of the first, and the V tile lies in LDS in that order, [channel][step s][h][u].
-// The softmax is one pass: reference of a row raised only when a score passes it by kLag (see kvlinc_rows.hip), one multiply-add, one
+// The softmax is one pass: reference of a row raised only when a score passes it by kHeadroom + kLag, one multiply-add, one
 // exponential, half a maximum, half a sum and half a conversion a score.  Roundings to binary16: dequantized values (2^-12 of each; a second term
 // would be 16 products a tile more), the weights, and dequantized keys, whose loss is added back in FP4 (see LowTile); scores, sums and numerators
 // stay binary32.

@@ -10,7 +10,7 @@ namespace {
 
 constexpr int kTileWaves = 8, kTileThreads = 64 * kTileWaves, kTileRows = 32 * kTileWaves;
 constexpr float kHeadroom = 8.0f, kLag = 5.0f;
-constexpr float kFusedBound = 0x1p20f;  // references beyond it: the exponent is rounded as the reference is (see scores_to_weights)
+constexpr float kFusedBound = 0x1p20f;  // references beyond it: the exponent is rounded as the reference is (see tile_weights)
 
 typedef float float16_t __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x6_t __attribute__((ext_vector_type(6)));
@@ -65,9 +65,10 @@ __device__ __forceinline__ void matrix_order() {
 }
 // ---- what dequantized keys lose --------------------------------------------------------------------------------------------------------
 // A key code * scale + zero-point rounded to binary16 is off by up to 2^-12 of itself, and a score by 2^-12 of a sum of |q k|: several times what
-// all other roundings of an output come to (8e-4 of its norm against 2.5e-4, 8192 cached tokens).  What the rounding leaves is kept as FP4 numbers
-// with a scale for every 32 channels, and their products with the query, in FP4 too, are added to the score: a tenth of the loss stays (2.6e-4), for
-// 4 products of twice the depth and a quarter of the bytes on top of a tile's 32.  (A second binary16 term would cost 16 products.)
+// all other roundings of an output come to (8.9e-4 of its norm against 2.5e-4, 512 tokens over 8192 cached ones).  What the rounding leaves is kept as
+// FP4 numbers with a scale for every 32 channels, and its products with the query, in FP6, are added to the scores: 2.9e-4 (4 bits 3.4e-4, by the
+// rounding of values).  That is 4 products of four times the depth on top of a tile's 32 and a quarter of the keys' bytes: 9 % of a long call, in the kernel
+// that unpacks the codes itself, 65 to 512 rows, a quarter.  (A second binary16 term would be 16 products, half of a tile's.)
 struct LowTile {
   u32x4_t k[kTileTokens][4];      // 32 channels a chunk; chunk c of token t lies at low_chunk(t, c)
   uint32_t scale[kTileTokens];    // byte c: exponent (biased by 127) of the scale of chunk c
