@@ -231,6 +231,7 @@ class KVLincCache:
             Wq=None if Wq is None else Wq.data_ptr(), Wk=None if Wk is None else Wk.data_ptr(),
             status=self.status.data_ptr(), split_done=self.split_done.data_ptr(), flags=int(flags))
         self._ws = None
+        self._device = self.groups.device
         self._context_ws = None  # scratch of prompt_attention and decode_windowed, and the streams that have used it
         self._context_streams = set()
         self._captured_ws = []
@@ -269,11 +270,16 @@ class KVLincCache:
 
     # The calls below check their tensors: what the C entry points take is an address.
     def _tensor(self, t, name, shape, dtype):
+        try:
+            if t.dtype is dtype and t.shape == shape and t.device == self._device and t.is_contiguous():
+                return
+        except AttributeError:
+            pass
         import torch
         if not torch.is_tensor(t) or t.dtype != dtype or t.shape != shape:
             raise KVLincError("%s has to be a %s tensor of shape %s" % (name, dtype, tuple(shape)))
-        if t.device != self.groups.device:
-            raise KVLincError("%s is on %s, the cache on %s" % (name, t.device, self.groups.device))
+        if t.device != self._device:
+            raise KVLincError("%s is on %s, the cache on %s" % (name, t.device, self._device))
         if not t.is_contiguous():
             raise KVLincError("%s has to be contiguous" % name)
 
@@ -281,7 +287,7 @@ class KVLincCache:
         """The cache's device current, and `stream`, if one is given: what is allocated inside belongs to the stream that uses it, and the
         caller's tensors are not handed out again before it is done with them."""
         import torch
-        dev = self.groups.device
+        dev = self._device
         if dev.type != "cuda":
             raise KVLincError("the cache is on %s: the kernels need a GPU" % dev)
         here = torch.cuda.current_device() == dev.index
@@ -302,16 +308,15 @@ class KVLincCache:
             raise KVLincError("window and sinks have to be 0 or more, not %s and %s" % (window, sinks))
 
     def _with_scratch(self, call, need):
-        """call(scratch) on the current stream, with the scratch at hand if it does (the library looks before it launches anything), else with
+        """call(scratch, stream) on the current stream, with the scratch at hand if it does (the library looks before it launches anything), else with
         one of need() bytes.  One that a captured graph uses is kept as long as the cache."""
         import torch
-        ws = self._context_ws
-        rc = call(ws)
-        stream = _stream(None)
+        ws, stream = self._context_ws, _stream(None)
+        rc = call(ws, stream)
         if rc == KVLINC_EWORKSPACE:
             ws = self._context_ws = torch.empty((need() + 3) // 4, dtype=torch.float32, device=self.groups.device)
             self._context_streams = {stream}
-            rc = call(ws)
+            rc = call(ws, stream)
         elif ws is not None and stream not in self._context_streams:  # (not handed out again before this stream is done with it)
             ws.record_stream(torch.cuda.current_stream())
             self._context_streams.add(stream)
@@ -341,7 +346,7 @@ class KVLincCache:
         with self._on(stream, q, k_new, v_new, n_new, out):
             if out is None:
                 out = torch.empty_like(q) if n_new is None else torch.zeros_like(q)
-            rc = self._with_scratch(lambda ws: kvlinc_prompt_attention(self, q, k_new, v_new, n_new, T, window, sinks, out, ws, None, max_context, stream),
+            rc = self._with_scratch(lambda ws, s: kvlinc_prompt_attention(self, q, k_new, v_new, n_new, T, window, sinks, out, ws, None, max_context, s),
                                     lambda: kvlinc_prompt_workspace_bytes(self, T, window, sinks, max_context))
         if rc != KVLINC_OK:
             raise KVLincError("kvlinc_prompt_attention: " + kvlinc_strerror(rc))
@@ -358,7 +363,7 @@ class KVLincCache:
         with self._on(stream, q, out):
             if out is None:
                 out = torch.empty_like(q)
-            rc = self._with_scratch(lambda ws: kvlinc_decode_attention_windowed(self, q, window, sinks, out, ws, None, max_context, stream),
+            rc = self._with_scratch(lambda ws, s: kvlinc_decode_attention_windowed(self, q, window, sinks, out, ws, None, max_context, s),
                                     lambda: kvlinc_decode_windowed_workspace_bytes(self, window, sinks, max_context))
         if rc != KVLINC_OK:
             raise KVLincError("kvlinc_decode_attention_windowed: " + kvlinc_strerror(rc))
