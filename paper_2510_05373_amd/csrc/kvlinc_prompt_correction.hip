@@ -1,12 +1,14 @@
 // The linear correction of prompt rows (Sec. 3.2, Eq. 5-6): C_n = phi_q(q) S and C_d = phi_q(q) P of every row, in the rotated basis.
 //
-// A wave takes 16 NT tokens of one head, both products on v_mfma_f32_16x16x32_f16 and transposed, so that a lane keeps one token
-// (column lane % 16) from the logits to the result and nothing goes through LDS:
+// A workgroup takes 128 tokens of one head, a wave 16, both products on v_mfma_f32_16x16x32_f16 and transposed, so that a lane keeps one token
+// (column lane % 16) from the logits to the result:
 //   logits^T = W^T q^T: row j of tile i (i = 0..3) of a block of 64 features is feature 4 j + i, so that a lane loads 4 neighbouring features
 //              of the 8 channels that it feeds, and its results are 16 neighbouring features, 16 g .. 16 g + 15 (g = lane / 16);
 //   C_n^T    = S^T phi^T: those are the positions it feeds, 8 in turn; S from its binary16 tile copy, 4 features in 8 bytes.
+// The eight waves bring the weights and the state to LDS together, half of the features at a time, as operands: read by every wave for itself, 128 KB
+// for 32 tokens, they took twice as long (8192 tokens of 32 heads with what reads the results: 200 us, 109 so; 128 tokens 24 and 11; 32 tokens a wave: 122).
 // The features are rounded to binary16 (2^-12 of each), as S is; logits, their softmax and the sums are binary32.
-// Bound: the weights and the state, 64 KB each, which every wave reads from L2 for 16 NT tokens: 8192 tokens of 32 heads 150 us (0.23 PFLOP/s, 4 % of their call).
+// Bound: the results, 528 bytes a row, written and read again (0.28 GB, 53 us of the 109), and the operands from L2.
 #include <hip/hip_runtime.h>
 
 #include "kvlinc_codes.h"
@@ -28,143 +30,113 @@ __device__ __forceinline__ float column_allsum(float v) {
   return x + y;
 }
 
-template <int NT>
-__global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void prompt_correction_kernel(ContextCall a, long long n_waves, int blocks) {
+constexpr int kCorrWaves = 8, kCorrTokens = 16 * kCorrWaves;
+// Grid: blocks of 128 tokens fastest, then (sequence, query head).
+__global__ __launch_bounds__(64 * kCorrWaves, 4) void prompt_correction_kernel(ContextCall a, int blocks) {
+  __shared__ u32x4_t sW[2][4][4][64];  // operands of a half of the features, as lanes take them: weights [64-feature block][32 channels][tile]
+  __shared__ u32x4_t sS[2][8][2][64];  // and the state [64-feature block][16 channels][8 features of a lane]
   const kvlinc_cache& c = a.cache;
-  const int lane = threadIdx.x & 63, j = lane & 15, g = lane >> 4;
-  const long long id = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (id >= n_waves) return;
-  const long long bh = id / blocks;  // b H_q + h
-  const int i0 = (int)(id - bh * blocks) * 16 * NT, b = (int)(bh / c.H_q), h = (int)(bh - (long long)b * c.H_q);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane & 15, g = lane >> 4;
+  const long long bh = blockIdx.x / blocks;  // b H_q + h
+  const int first = (int)(blockIdx.x - bh * blocks) * kCorrTokens, token = first + 16 * wave + j, b = (int)(bh / c.H_q), h = (int)(bh - (long long)b * c.H_q);
   const int T = a.n_new != nullptr ? min(max(a.n_new[b], 0), a.T) : a.T;
-  if (i0 >= T) return;
+  if (first >= T) return;
+  const bool idle = first + 16 * wave >= T;  // (the wave only helps to bring the operands)
   const long long kv = (long long)b * c.H_kv + h / a.gq;
 
-  half8_t q[NT][4];
+  half8_t q[4];  // channels 32 s + 8 g + 0..7
+  const u32x4_t* src = reinterpret_cast<const u32x4_t*>(a.q + (bh * a.T + min(token, T - 1)) * kHeadDim) + g;
 #pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    const uint4* src = reinterpret_cast<const uint4*>(a.q + (bh * a.T + min(i0 + 16 * t + j, T - 1)) * kHeadDim) + g;
+  for (int s = 0; s < 4; ++s) q[s] = as_h8(src[4 * s]);
+  float4_t acc[8];
+  float den = 0.0f;
 #pragma unroll
-    for (int s = 0; s < 4; ++s) q[t][s] = as_h8(src[4 * s]);  // channels 32 s + 8 g + 0..7
-  }
-  float4_t acc[NT][8];
-  float den[NT];
-#pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    den[t] = 0.0f;
-#pragma unroll
-    for (int n = 0; n < 8; ++n) acc[t][n] = float4_t{0.f, 0.f, 0.f, 0.f};
-  }
+  for (int n = 0; n < 8; ++n) acc[n] = float4_t{0.f, 0.f, 0.f, 0.f};
+  const half_t* S = reinterpret_cast<const half_t*>(c.S16) + kv * (128 * 64 * 4);
 #pragma unroll 1
   for (int half = 0; half < 2; ++half) {
     const half_t* W = reinterpret_cast<const half_t*>(c.Wq) + ((long long)h * 2 + half) * kHeadDim * 128;
-    float x[NT][2][4][4];  // [64-feature block][tile][row]
+    if (half != 0) __syncthreads();
+    {  // a wave has one block of features and 32 channels of the weights, and 16 channels of the state
+      const int fb = wave >> 2, s = wave & 3, n = wave;
+      u32x2_t w[8];
 #pragma unroll
-    for (int fb = 0; fb < 2; ++fb) {
-      float4_t d[NT][4];
+      for (int k = 0; k < 8; ++k) w[k] = *reinterpret_cast<const u32x2_t*>(W + (32 * s + 8 * g + k) * 128 + 64 * fb + 4 * j);
 #pragma unroll
-      for (int t = 0; t < NT; ++t)
+      for (int i = 0; i < 4; ++i) {
+        u32x4_t r;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) d[t][i] = float4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int s = 0; s < 4; ++s) {
-        uint2 w[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) w[k] = *reinterpret_cast<const uint2*>(W + (32 * s + 8 * g + k) * 128 + 64 * fb + 4 * j);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          uint32_t r[4];
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const uint32_t lo = i < 2 ? w[2 * k].x : w[2 * k].y, hi = i < 2 ? w[2 * k + 1].x : w[2 * k + 1].y;
-            r[k] = __builtin_amdgcn_perm(hi, lo, (i & 1) == 0 ? 0x05040100u : 0x07060302u);
-          }
-          const half8_t A = as_h8(make_uint4(r[0], r[1], r[2], r[3]));
-#pragma unroll
-          for (int t = 0; t < NT; ++t) d[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(A, q[t][s], d[t][i], 0, 0, 0);
-        }
+        for (int k = 0; k < 4; ++k) r[k] = __builtin_amdgcn_perm(w[2 * k + 1][i >> 1], w[2 * k][i >> 1], (i & 1) == 0 ? 0x05040100u : 0x07060302u);
+        sW[fb][s][i][lane] = r;
       }
 #pragma unroll
-      for (int t = 0; t < NT; ++t)
+      for (int f = 0; f < 2; ++f)
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) x[t][fb][i][r] = d[t][i][r];
-    }
-    half8_t phi[NT][2][2];  // [64-feature block][8 of the lane's 16 features]
-    const float* P = c.P + kv * kRank + 128 * half;
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      float m = -INFINITY, z = 0.0f;
-#pragma unroll
-      for (int fb = 0; fb < 2; ++fb)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) m = fmaxf(m, x[t][fb][i][r]);
-      m = column_allmax(m);
-      float p = 0.0f;
-#pragma unroll
-      for (int fb = 0; fb < 2; ++fb)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const float4 w = *reinterpret_cast<const float4*>(P + 64 * fb + 16 * g + 4 * r);
-          const float ww[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float e = __builtin_amdgcn_exp2f((x[t][fb][i][r] - m) * 1.4426950408889634f);
-            x[t][fb][i][r] = e;
-            z += e;
-            p = fmaf(e, ww[i], p);
-          }
+        for (int e = 0; e < 2; ++e) {  // tile (64-feature block, channel half, 4-feature step) of S16 holds [channel % 64][feature % 4]
+          const int tile = ((2 * half + f) * 2 + n / 4) * 16 + 4 * g + 2 * e, ch = 16 * (n % 4) + j;
+          const u32x2_t s0 = *reinterpret_cast<const u32x2_t*>(S + (tile * 64 + ch) * 4), s1 = *reinterpret_cast<const u32x2_t*>(S + ((tile + 1) * 64 + ch) * 4);
+          sS[f][n][e][lane] = u32x4_t{s0[0], s0[1], s1[0], s1[1]};
         }
-      const float inv = 1.0f / column_allsum(z);
-      den[t] = fmaf(column_allsum(p), inv, den[t]);
-#pragma unroll
-      for (int fb = 0; fb < 2; ++fb)
-#pragma unroll
-        for (int e = 0; e < 2; ++e)
-          phi[t][fb][e] = as_h8(pack_h2(x[t][fb][0][2 * e] * inv, x[t][fb][1][2 * e] * inv), pack_h2(x[t][fb][2][2 * e] * inv, x[t][fb][3][2 * e] * inv),
-                                pack_h2(x[t][fb][0][2 * e + 1] * inv, x[t][fb][1][2 * e + 1] * inv),
-                                pack_h2(x[t][fb][2][2 * e + 1] * inv, x[t][fb][3][2 * e + 1] * inv));
     }
-    // tile (64-feature block, channel half, 4-feature step) of S16 holds [channel % 64][feature % 4]
-    const half_t* S = reinterpret_cast<const half_t*>(c.S16) + kv * (128 * 64 * 4);
+    __syncthreads();
+    if (idle) continue;
+    float4_t x[2][4];  // [64-feature block][tile]
+#pragma unroll
+    for (int fb = 0; fb < 2; ++fb) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[fb][i] = float4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[fb][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(as_h8(sW[fb][s][i][lane]), q[s], x[fb][i], 0, 0, 0);
+    }
+    float m = -INFINITY, z = 0.0f, p = 0.0f;
 #pragma unroll
     for (int fb = 0; fb < 2; ++fb)
 #pragma unroll
-      for (int n = 0; n < 8; ++n)
+      for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const int tile = ((2 * half + fb) * 2 + n / 4) * 16 + 4 * g + 2 * e, ch = 16 * (n % 4) + j;
-          const uint2 s0 = *reinterpret_cast<const uint2*>(S + (tile * 64 + ch) * 4), s1 = *reinterpret_cast<const uint2*>(S + ((tile + 1) * 64 + ch) * 4);
-          const half8_t A = as_h8(make_uint4(s0.x, s0.y, s1.x, s1.y));
+        for (int r = 0; r < 4; ++r) m = fmaxf(m, x[fb][i][r]);
+    m = column_allmax(m);
+    const float* P = c.P + kv * kRank + 128 * half;
 #pragma unroll
-          for (int t = 0; t < NT; ++t) acc[t][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(A, phi[t][fb][e], acc[t][n], 0, 0, 0);
+    for (int fb = 0; fb < 2; ++fb)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float4_t w = *reinterpret_cast<const float4_t*>(P + 64 * fb + 16 * g + 4 * r);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float e = __builtin_amdgcn_exp2f((x[fb][i][r] - m) * 1.4426950408889634f);
+          x[fb][i][r] = e;
+          z += e;
+          p = fmaf(e, w[i], p);
         }
-  }
+      }
+    const float inv = 1.0f / column_allsum(z);
+    den = fmaf(column_allsum(p), inv, den);
 #pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    const int i = i0 + 16 * t + j;
-    if (i >= T) continue;
-    float* dst = a.corr + (bh * a.T + i) * kPartStride;
-    if (g == 0) dst[0] = den[t];
+    for (int fb = 0; fb < 2; ++fb)
 #pragma unroll
-    for (int n = 0; n < 8; ++n) *reinterpret_cast<float4_t*>(dst + 4 + 16 * n + 4 * g) = acc[t][n];
+      for (int e = 0; e < 2; ++e) {
+        const half8_t phi = as_h8(pack_h2(x[fb][0][2 * e] * inv, x[fb][1][2 * e] * inv), pack_h2(x[fb][2][2 * e] * inv, x[fb][3][2 * e] * inv),
+                                  pack_h2(x[fb][0][2 * e + 1] * inv, x[fb][1][2 * e + 1] * inv), pack_h2(x[fb][2][2 * e + 1] * inv, x[fb][3][2 * e + 1] * inv));
+#pragma unroll
+        for (int n = 0; n < 8; ++n) acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(as_h8(sS[fb][n][e][lane]), phi, acc[n], 0, 0, 0);
+      }
   }
+  if (token >= T) return;
+  float* dst = a.corr + (bh * a.T + token) * kPartStride;
+  if (g == 0) dst[0] = den;
+#pragma unroll
+  for (int n = 0; n < 8; ++n) *reinterpret_cast<float4_t*>(dst + 4 + 16 * n + 4 * g) = acc[n];
 }
 
 }  // namespace
 
 int launch_prompt_correction(const ContextCall& a, hipStream_t stream) {
-  // 32 tokens a wave share the operands; fewer rows than a wave for every SIMD of the chip that way go by 16.
-  const long long heads = (long long)a.cache.B * a.cache.H_q;
-  const bool wide = heads * ((a.T + 31) / 32) >= 1024;
-  const int blocks = wide ? (a.T + 31) / 32 : (a.T + 15) / 16;
-  const long long waves = heads * blocks;
-  const dim3 grid((unsigned)((waves + 3) / 4));
-  if (wide) hipLaunchKernelGGL(prompt_correction_kernel<2>, grid, dim3(256), 0, stream, a, waves, blocks);
-  else hipLaunchKernelGGL(prompt_correction_kernel<1>, grid, dim3(256), 0, stream, a, waves, blocks);
+  const int blocks = (a.T + kCorrTokens - 1) / kCorrTokens;
+  const dim3 grid((unsigned)((long long)a.cache.B * a.cache.H_q * blocks));
+  hipLaunchKernelGGL(prompt_correction_kernel, grid, dim3(64 * kCorrWaves), 0, stream, a, blocks);
   return hipGetLastError() == hipSuccess ? KVLINC_OK : KVLINC_EHIP;
 }
 
