@@ -5,11 +5,12 @@
 // [128 channels], by loads that write LDS themselves, so that no wave spends a register or a vector instruction on it.  The value operand
 // (rows = channels) comes out of the row-major tile by transposing LDS reads.
 // What the keys' rounding to binary16 leaves comes with them (64 bytes of FP4 numbers and 4 of scales a token, see LowTile): 8k tokens over 24k
-// take 4.0 ms, 3.7 without it, at three times the error.
+// took 3.7 ms without it, 4.05 with it, at a third of the error.
 //
 // Bound: the matrix and the vector phases, which take turns on a SIMD's two waves and are about as long; a long call also the power limit (8k tokens
-// over 24k: 1.67 GHz).  8k over 24k, 4 heads, with 0.15 ms of correction and 0.05 of dequantizing: 4.1 ms (0.94 PFLOP/s; a matrix product of 8192^3 from the library
-// reaches 1.19); four prompts of 1700 to 4096 tokens 400 us (0.86), 340 without the softmax, 312 without the products; one of 700 tokens 30 us.
+// over 24k: 1.67 GHz).  8k over 24k, 4 heads, with 0.08 ms of correction and 0.05 of dequantizing: 4.0 ms (0.98 PFLOP/s; a matrix product of 8192^3
+// from the library reaches 1.19); four prompts of 1700 to 4096 tokens 400 us (0.86), 340 without the softmax, 312 without the products; one of
+// 700 tokens 30 us.
 #include <hip/hip_runtime.h>
 
 #include "kvlinc_tiles.h"
