@@ -235,6 +235,7 @@ class KVLincCache:
         self._context_ws = None  # scratch of prompt_attention and decode_windowed, and the streams that have used it
         self._context_streams = set()
         self._captured_ws = []
+        self._seen_streams = set()  # those that a caller has named
 
     def bytes(self):
         ts = [self.groups, self.k_res, self.v_res]
@@ -285,7 +286,7 @@ class KVLincCache:
 
     def _on(self, stream, *tensors):
         """The cache's device current, and `stream`, if one is given: what is allocated inside belongs to the stream that uses it, and the
-        caller's tensors are not handed out again before it is done with them."""
+        caller's tensors and the cache's are not handed out again before it is done with them."""
         import torch
         dev = self._device
         if dev.type != "cuda":
@@ -300,12 +301,20 @@ class KVLincCache:
         for t in tensors:
             if t is not None:
                 t.record_stream(stream)
+        if stream.cuda_stream not in self._seen_streams:
+            for t in (self.groups, self.k_res, self.v_res, self.n_quant, self.n_res, self.status, self.split_done, self.Wq, self.Wk, self.S, self.S16, self.P):
+                if t is not None:
+                    t.record_stream(stream)
+            self._seen_streams.add(stream.cuda_stream)
         return torch.cuda.stream(stream)  # (makes its device current, too)
 
     @staticmethod
-    def _limits(window, sinks):
-        if window < 0 or sinks < 0:
-            raise KVLincError("window and sinks have to be 0 or more, not %s and %s" % (window, sinks))
+    def _limits(window, sinks, max_context):
+        """(They go to the library as 32 bits.)"""
+        if not (0 <= window < 1 << 31 and 0 <= sinks < 1 << 31):
+            raise KVLincError("window and sinks have to be 0 or more, below 2^31, not %s and %s" % (window, sinks))
+        if max_context >= 1 << 31:
+            raise KVLincError("max_context is below 2^31, not %s" % max_context)
 
     def _with_scratch(self, call, need):
         """call(scratch, stream) on the current stream, with the scratch at hand if it does (the library looks before it launches anything), else with
@@ -333,7 +342,7 @@ class KVLincCache:
         if not torch.is_tensor(q) or q.dim() != 4:
             raise KVLincError("q has to be a tensor of shape [B, H_q, T, 128]")
         T, half = q.shape[2], torch.float16
-        self._limits(window, sinks)
+        self._limits(window, sinks, max_context)
         if T < 1:
             raise KVLincError("q has no rows")
         self._tensor(q, "q", (self.B, self.H_q, T, 128), half)
@@ -356,7 +365,7 @@ class KVLincCache:
         """decode() over the newest `window` tokens and the first `sinks` ones (window = 0: all).  q: [B, H_q, 128] fp16."""
         import torch
         half = torch.float16
-        self._limits(window, sinks)
+        self._limits(window, sinks, max_context)
         self._tensor(q, "q", (self.B, self.H_q, 128), half)
         if out is not None:
             self._tensor(out, "out", q.shape, half)

@@ -180,3 +180,11 @@ def test_positions_have_31_bits():
         assert prompt(c) == kb.KVLINC_EINVAL and windowed(c) == kb.KVLINC_EINVAL
         assert kb.kvlinc_prompt_workspace_bytes(c, 4) == 0 and kb.kvlinc_decode_windowed_workspace_bytes(c, 16) == 0
     assert kb.kvlinc_prompt_workspace_bytes(plain(max_groups=(1 << 24) - 4, B=1, H_q=1, H_kv=1), 1) > 0
+
+
+@pytest.mark.parametrize("over", [dict(window=1 << 31), dict(window=(1 << 32) + 5), dict(window=4, sinks=1 << 32), dict(window=4, max_context=(1 << 32) + 64)])
+def test_numbers_of_more_than_32_bits_are_refused(cache, over):
+    with pytest.raises(kv.KVLincError, match="2\\^31"):
+        cache.prompt_attention(**prompt_args(**over))
+    with pytest.raises(kv.KVLincError, match="2\\^31"):
+        cache.decode_windowed(half(2, 8, 128), **over)

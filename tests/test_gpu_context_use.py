@@ -244,6 +244,23 @@ def test_a_stream_of_the_callers(raw):
         del filler
 
 
+def test_a_cache_that_is_dropped_while_a_stream_reads_it():
+    K, V, q, k_new, v_new = ref.inputs(995, 1, 8, 2, [2000], 4)
+    args = [to_dev(x) for x in (q, k_new, v_new)]
+    want = filled(1, 8, 2, K, V, 2304).prompt_attention(*args)
+    cache, side = filled(1, 8, 2, K, V, 2304), torch.cuda.Stream()
+    size = cache.groups.numel()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(20_000_000)
+    got = cache.prompt_attention(*args, stream=side)
+    del cache
+    filler = [torch.full((size,), -1, dtype=torch.int32, device="cuda") for _ in range(4)]
+    torch.cuda.synchronize()
+    assert same(got, want)
+    del filler
+
+
 def test_two_caches_on_two_streams():
     caches, args, want = [], [], []
     for i in range(2):
