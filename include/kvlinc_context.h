@@ -42,7 +42,8 @@ size_t kvlinc_prompt_workspace_bytes(const kvlinc_cache* cache, int32_t T, int32
  *   k_new, v_new   [B, H_kv, T, 128] fp16, raw rows as kvlinc_append_quantize takes them
  *   n_new          [B] int32 on the device: sequence b has its first n_new[b] (0..T) rows; NULL = T for all.  (A value below 0 is
  *                  read as 0, one above T as T.)  Rows from n_new[b] on are not read, and not written in `out`.
- *   T              rows per (sequence, head), 1 .. 2^24
+ *   T              rows per (sequence, head), 1 .. 2^24; T and the cache's capacity together below 2^31 - 256 tokens, B * H_kv *
+ *                  ceil(T * H_q / H_kv / 16) below 2^24
  *   window, sinks  >= 0, see above
  *   out            [B, H_q, T, 128] fp16, in the original value basis; memory of its own (KVLINC_EINVAL if an input's)
  *   workspace      device scratch of at least kvlinc_prompt_workspace_bytes(cache, T, window, sinks, max_context) bytes, 16-byte
@@ -73,7 +74,7 @@ size_t kvlinc_decode_windowed_workspace_bytes(const kvlinc_cache* cache, int32_t
  * One decode step of a layer with a sliding window: kvlinc_decode_attention (the query's own token, at position n - 1, is already
  * appended) over the tokens that the window and the sinks leave visible.  Only their groups are read.
  *
- *   q, out         [B, H_q, 128] fp16; out may be q
+ *   q, out         [B, H_q, 128] fp16; out may be q (other overlaps: KVLINC_EINVAL)
  *   window, sinks  >= 0, see above; window = 0: all tokens
  *   workspace      at least kvlinc_decode_windowed_workspace_bytes(cache, window, sinks, max_context) bytes, 16-byte aligned
  *   max_context    host-side upper bound on n_quant + n_res (<= 0: capacity); it only sizes the launch
