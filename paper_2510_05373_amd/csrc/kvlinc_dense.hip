@@ -32,12 +32,13 @@ struct DenseTiles {
 };
 
 // 1 KB from memory to LDS, 16 bytes a lane, in lane order from `lds` on.  (In assembly: the compiler would otherwise wait for the tile under
-// way ahead of every LDS read that it cannot tell from it.  There is no register to write.  The waits are in landed().)
+// way ahead of every LDS read that it cannot tell from it.  There is no register to write.  The waits are in landed(); a load that writes LDS needs one
+// wait state after a scalar write of m0, which the compiler adds to its own code only.)
 __device__ __forceinline__ void load_to_lds(const void* base, uint32_t offset, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory", "m0");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory", "m0");
 }
 __device__ __forceinline__ void load_words_to_lds(const void* base, uint32_t offset, uint32_t lds) {  // 4 bytes a lane
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory", "m0");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory", "m0");
 }
 // All but the newest N of this wave's loads have arrived.
 template <int N>
