@@ -88,6 +88,18 @@ __device__ __forceinline__ void lane8_butterflies(float (&v)[8]) {
       }
 }
 
+// Softmax sums relative to 2^m (m: log2 domain) and the correction, e^0 terms, in one quotient: (den + 2^-m C_d), both sides times 2^m, but by no
+// less than 2^-64: the sums count some token as 1 or more, C_d and C_n stay in range under 2^64, so the divisor is a normal number however little is
+// added.  Where nothing is added (C_d = 0: no quantized token yet) the factor cancels and is left out.  (Times 2^min(m, 0) the sums vanished for
+// rows whose logits are all below -82, and 0 / 0 was left.)
+struct Shares {
+  float softmax, correction;  // factors
+};
+__device__ __forceinline__ Shares shares_of(float m, float c_d) {
+  const float to = fmaxf(m, -64.0f);
+  return Shares{c_d != 0.0f ? __builtin_amdgcn_exp2f(m - to) : 1.0f, __builtin_amdgcn_exp2f(-to)};
+}
+
 // What a query sees: its position p, the window's first token, the sinks.  Token t <= p is seen if t >= low or t < sinks.
 __device__ __forceinline__ int window_low(int p, int window) { return window > 0 ? max(p - window + 1, 0) : 0; }
 

@@ -32,14 +32,14 @@ __device__ __forceinline__ void finish_row(float (&a)[8], float l, int lane, hal
   for (int i = 0; i < 4; ++i) h[i] = as_u32(pack_h2(a[2 * i] * inv, a[2 * i + 1] * inv));
   *reinterpret_cast<u32x4_t*>(out + 8 * (lane & 15)) = h;
 }
-// The correction {C_d, -, -, -, C_n[128]} added as e^0 terms (Eq. 5), both sides relative to max(m, 0).
+// The correction {C_d, -, -, -, C_n[128]} added (Eq. 5).
 __device__ __forceinline__ void add_correction(float (&a)[8], float& l, float m, float c_d, float4_t c0, float4_t c1) {
-  const float to = fmaxf(m, 0.0f), f = __builtin_amdgcn_exp2f(m - to), w = __builtin_amdgcn_exp2f(-to);
-  l = fmaf(w, c_d, l * f);
+  const Shares f = shares_of(m, c_d);
+  l = fmaf(f.correction, c_d, l * f.softmax);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    a[i] = fmaf(w, c0[i], a[i] * f);
-    a[4 + i] = fmaf(w, c1[i], a[4 + i] * f);
+    a[i] = fmaf(f.correction, c0[i], a[i] * f.softmax);
+    a[4 + i] = fmaf(f.correction, c1[i], a[4 + i] * f.softmax);
   }
 }
 constexpr int kMaxContextSplits = 32;

@@ -295,19 +295,19 @@ __device__ __forceinline__ void store_results(TileRows& st, const ContextCall& a
         *reinterpret_cast<float4*>(dst + 4 + 32 * cb + 2 * r + 4 * h) = make_float4(st.acc[cb][r], st.acc[cb][r + 1], st.acc[cb][r + 2], st.acc[cb][r + 3]);
     return;
   }
-  if (a.corr != nullptr) {  // {C_d, -, -, -, C_n[128]}, as e^0 terms: both sides relative to max(m, 0)
+  if (a.corr != nullptr) {  // {C_d, -, -, -, C_n[128]}
     const float* corr = a.corr + w.place * kPartStride;
-    const float to = fmaxf(st.m, 0.0f), f = __builtin_amdgcn_exp2f(st.m - to), g = __builtin_amdgcn_exp2f(-to);
-    st.l = fmaf(g, corr[0], st.l * f);
+    const Shares f = shares_of(st.m, corr[0]);
+    st.l = fmaf(f.correction, corr[0], st.l * f.softmax);
 #pragma unroll
     for (int cb = 0; cb < 4; ++cb)
 #pragma unroll
       for (int r = 0; r < 16; r += 4) {
         const float4 v = *reinterpret_cast<const float4*>(corr + 4 + 32 * cb + 2 * r + 4 * h);
-        st.acc[cb][r] = fmaf(g, v.x, st.acc[cb][r] * f);
-        st.acc[cb][r + 1] = fmaf(g, v.y, st.acc[cb][r + 1] * f);
-        st.acc[cb][r + 2] = fmaf(g, v.z, st.acc[cb][r + 2] * f);
-        st.acc[cb][r + 3] = fmaf(g, v.w, st.acc[cb][r + 3] * f);
+        st.acc[cb][r] = fmaf(f.correction, v.x, st.acc[cb][r] * f.softmax);
+        st.acc[cb][r + 1] = fmaf(f.correction, v.y, st.acc[cb][r + 1] * f.softmax);
+        st.acc[cb][r + 2] = fmaf(f.correction, v.z, st.acc[cb][r + 2] * f.softmax);
+        st.acc[cb][r + 3] = fmaf(f.correction, v.w, st.acc[cb][r + 3] * f.softmax);
       }
   }
   if (in_cache_basis) rotate_tile_rows(st, lane);
