@@ -3,8 +3,8 @@
  *
  * The conventions of kvlinc.h hold: device pointers of the caller, 16-byte aligned (counts: 4-byte), no allocation, no
  * synchronisation, 0 = enqueued, a negative code = rejected before any launch (KVLINC_EHIP: the runtime refused one).  The calls
- * read the cache and leave all of it as it is, but for split_done, which an attention call may count in and leaves at zero: two
- * calls on the same cache must not overlap in time.
+ * read the cache and leave all of it as it is, but for split_done, which an attention call may count in and leaves at zero (two
+ * calls on the same cache must not overlap in time), and for KVLINC_ST_BOUND in *status.
  *
  * Token t of a sequence that holds n = n_quant + n_res tokens: its key K_t is the dequantized code (t < n_quant) or the window's
  * fp16 row, its value V_t likewise, times H^T (the cache keeps rotated values; with KVLINC_FLAG_SLIDING_VALUES the newest 128
@@ -30,6 +30,11 @@ enum {
   KVLINC_F32 = 2
 };
 
+/* Bit of *status, beside those of kvlinc.h. */
+enum {
+  KVLINC_ST_BOUND = 16 /* kvlinc_prompt_attention: a sequence held more tokens than max_context said; its output rows are zeros */
+};
+
 /* Bytes of device scratch kvlinc_prompt_attention needs for T rows a sequence when no sequence holds more than max_context
  * tokens before the call (<= 0: the cache's full capacity).  0 on invalid arguments. */
 size_t kvlinc_prompt_workspace_bytes(const kvlinc_cache* cache, int32_t T, int32_t window, int32_t sinks, int32_t max_context);
@@ -49,8 +54,8 @@ size_t kvlinc_prompt_workspace_bytes(const kvlinc_cache* cache, int32_t T, int32
  *   workspace      device scratch of at least kvlinc_prompt_workspace_bytes(cache, T, window, sinks, max_context) bytes, 16-byte
  *                  aligned, contents undefined before and after; NULL where that is 0
  *   max_context    host-side upper bound on the tokens a sequence holds before the call (<= 0: capacity).  It sizes the launch and,
- *                  for more than 512 rows a KV head (T * H_q / H_kv), the room for dequantized tokens (580 bytes each): those
- *                  of a sequence that holds more than it was promised to are left out of the sums.
+ *                  for more than 512 rows a KV head (T * H_q / H_kv), the room for dequantized tokens (580 bytes each): a
+ *                  sequence that holds more than there is room for gets zeros in its rows, and KVLINC_ST_BOUND is set.
  *
  * out[b, h, i] = ( sum_t w_t V_t + phi_q(q) S H^T ) / ( sum_t w_t + phi_q(q) P ),  w_t = exp(q K_t / sqrt 128)
  * over the tokens that row i sees; the phi terms (Eq. 5) with the adapters only.  The states S, P stand for all quantized tokens:

@@ -12,6 +12,7 @@ KVLINC_FLAG_ALG1_LITERAL = 1
 KVLINC_FLAG_SLIDING_VALUES = 2
 KVLINC_F16, KVLINC_BF16, KVLINC_F32 = 0, 1, 2
 KVLINC_ST_CAPACITY, KVLINC_ST_NONFINITE, KVLINC_ST_STATIC, KVLINC_ST_STATE_RANGE = 1, 2, 4, 8
+KVLINC_ST_BOUND = 16
 
 
 class KVLincError(RuntimeError):

@@ -88,6 +88,26 @@ __device__ __forceinline__ void dense_order() {
   }
 }
 
+// Rows of a sequence that holds more tokens than the workspace has rows for: zeros, and a bit in the status word.
+__device__ __forceinline__ void refuse_rows(const ContextCall& a, const WaveRows& w, int split, int lane) {
+  if (w.idle) return;
+  if (lane == 0) atomicOr(a.cache.status, KVLINC_ST_BOUND);
+  if (!w.mine) return;
+  const int h = lane >> 5;
+  auto clear = [&](void* row, int bytes) __attribute__((always_inline)) {
+    for (int at = 16 * h; at < bytes; at += 32) *reinterpret_cast<uint4*>(static_cast<char*>(row) + at) = make_uint4(0, 0, 0, 0);
+  };
+  if (a.splits == 1) {
+    clear(a.out + w.place * kHeadDim, kHeadDim * 2);
+    return;
+  }
+  // (the join makes zeros of empty splits and an empty correction)
+  float* dst = a.part + (w.place * a.splits + split) * kPartStride;
+  clear(dst, kPartStride * 4);
+  if (h == 0) dst[0] = -INFINITY;
+  if (a.corr != nullptr) clear(a.corr + w.place * kPartStride, kPartStride * 4);
+}
+
 // Grid, one-dimensional: see place_of_block.
 __global__ __launch_bounds__(kTileThreads, 2) void dense_kernel(ContextCall a, int blocks) {
   __shared__ __align__(1024) DenseTiles tiles;
@@ -114,7 +134,11 @@ __global__ __launch_bounds__(kTileThreads, 2) void dense_kernel(ContextCall a, i
   const int new_from = a.sinks > total ? 0 : max(low_block - total, 0) / kTileTokens;
   const int n_new = last_i / kTileTokens + 1 - new_from;
   const int near = window_base(total, a.row_window), near_row = a.sink_rows;
-  const int held = min(total, near + a.cached_rows - near_row);  // (all of them: the rows are as many as the caller's bound)
+  const int held = min(total, near + a.cached_rows - near_row);  // (all of them, unless the caller's bound was too low)
+  if (held < total) {
+    refuse_rows(a, wr, split, lane);
+    return;
+  }
   const int n_sink = (min(a.sinks, near) + kTileTokens - 1) / kTileTokens;
   const int near_from = a.sinks > near ? 0 : (min(low_block, held) - near) / kTileTokens;
   const int n_near = (held - near + kTileTokens - 1) / kTileTokens - near_from;
