@@ -38,7 +38,6 @@ long long groups_met(const kvlinc_cache& c, int T, int window, int sinks, int ma
   return near < all ? near : all;
 }
 
-constexpr int kMaxContextSplits = 32;
 // Which of the three a call of so many rows a KV head takes, measured (us; 8 KV heads, 2 bits):
 //   rows                                   64            512            640            1000
 //   1 sequence, 32k cached tokens          rows 53       tiles 137      tiles 199      tiles 243

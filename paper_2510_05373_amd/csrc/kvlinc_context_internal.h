@@ -6,6 +6,9 @@
 
 namespace kvlinc {
 
+// Splits of a context at most: what a launch is planned with and what the joins are made for.
+constexpr int kMaxContextSplits = 32;
+
 // One call as the kernels take it.  Places: row (b, h, i) of q and out is place (b H_q + h) T + i.
 struct ContextCall {
   kvlinc_cache cache;

@@ -42,12 +42,12 @@ __device__ __forceinline__ void add_correction(float (&a)[8], float& l, float m,
     a[4 + i] = fmaf(f.correction, c1[i], a[4 + i] * f.softmax);
   }
 }
-constexpr int kMaxContextSplits = 32;
 // The splits of one row joined by 16 lanes: weights by lane, two splits each, and the numerators, kSplitsAhead splits under way at a time, the
 // first of them requested together with the maxima.  (A trip to memory, past the caches, is about 2 us of a launch; 16 splits at a time spilled, and
 // drafts took 15 % longer.)
 constexpr int kSplitsAhead = 8;
-__device__ __forceinline__ void join_row(__amdgpu_buffer_rsrc_t part, int at, int splits, float* weights /* LDS, 32 */, int lane, float (&o)[8], float& L, float& M) {
+__device__ __forceinline__ void join_row(__amdgpu_buffer_rsrc_t part, int at, int splits, float* weights /* LDS, kMaxContextSplits */, int lane, float (&o)[8], float& L, float& M) {
+  static_assert(kMaxContextSplits == 32, "a row's 16 lanes take two splits each");
   const int j = lane & 15;
   float4_t u[kSplitsAhead][2];
   auto request = [&](int s0) __attribute__((always_inline)) {

@@ -57,3 +57,18 @@ def test_loads_into_lds_keep_their_distance(source, tmp_path):
             if op.startswith("v_") and not op.startswith("v_mfma"):
                 assert not registers(target) & base, (line, code[i])
             gone += states(line)
+
+
+def test_the_plan_and_the_joins_share_their_largest_number_of_splits():
+    # (a row's join has room for 32 weights in LDS and reads two splits a lane)
+    csrc = os.path.join(ROOT, "paper_2510_05373_amd", "csrc")
+    text = "".join(open(os.path.join(csrc, f)).read() for f in sorted(os.listdir(csrc)) if f.endswith((".h", ".hip")))
+    assert re.findall(r"constexpr int kMaxContextSplits = (\d+);", text) == ["32"]
+    from paper_2510_05373_amd import binding as kb
+    from tests.test_library_abi import fake_struct
+    none = dict(S=0, S16=0, P=0, Wq=0, Wk=0)
+    longest = fake_struct(B=1, H_q=1, H_kv=1, max_groups=1 << 20, **none)
+    part = 132 * 4  # bytes of a split's partial result
+    assert kb.kvlinc_prompt_workspace_bytes(longest, 1) == 32 * part
+    assert kb.kvlinc_prompt_workspace_bytes(longest, 100) == 32 * part * 100
+    assert kb.kvlinc_decode_windowed_workspace_bytes(longest, 0) == 32 * part
