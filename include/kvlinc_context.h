@@ -93,7 +93,7 @@ int kvlinc_decode_attention_windowed(const kvlinc_cache* cache, const kvlinc_hal
  * Keys and values of T tokens of every sequence as a plain attention would take them.
  *
  *   first          [B] int32 on the device: row i is token first[b] + i; NULL = 0 for all.  (A value below 0 is read as 0.)
- *   T              rows, 1 .. 2^30
+ *   T              rows, 1 .. 2^30; B * H_kv * T at most 2^40
  *   k_out, v_out   [B, H_kv, T, 128] of type dtype (KVLINC_F16, KVLINC_BF16, KVLINC_F32); either may be NULL.  Rows of tokens
  *                  that the sequence does not hold are left as they are.  The two do not overlap.
  *   rotated        0: values in the original basis, V_t;  1: in the rotated basis they are stored in.

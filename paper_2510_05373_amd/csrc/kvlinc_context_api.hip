@@ -210,7 +210,9 @@ int kvlinc_cache_read(const kvlinc_cache* cache, const int32_t* first, int32_t T
   if (k_out == nullptr && v_out == nullptr) return KVLINC_EINVAL;
   if ((k_out != nullptr && bad_address(k_out, 16)) || (v_out != nullptr && bad_address(v_out, 16))) return KVLINC_EINVAL;
   if (first != nullptr && bad_address(first, 4)) return KVLINC_EINVAL;
-  const long long bytes = (long long)cache->B * cache->H_kv * T * kHeadDim * (dtype == KVLINC_F32 ? 4 : 2);
+  const long long rows = (long long)cache->B * cache->H_kv * T;  // below 2^55
+  if (rows > (1ll << 40)) return KVLINC_EINVAL;  // 2^48 bytes: beyond any address space, and below what 64 bits count
+  const long long bytes = rows * kHeadDim * (dtype == KVLINC_F32 ? 4 : 2);
   if (k_out != nullptr && v_out != nullptr && overlap(k_out, bytes, v_out, bytes)) return KVLINC_EINVAL;
   return launch_read(*cache, first, T, k_out, v_out, dtype, rotated != 0, static_cast<hipStream_t>(stream));
 }

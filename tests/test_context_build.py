@@ -10,10 +10,15 @@ ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 BUILD = os.path.join(ROOT, "paper_2510_05373_amd", "build.py")
 
 
-def assembly(source, tmp_path):
-    spec = importlib.util.spec_from_file_location("kvlinc_build_for_assembly", BUILD)
+def build_module():
+    spec = importlib.util.spec_from_file_location("kvlinc_build_by_path", BUILD)
     build = importlib.util.module_from_spec(spec)
     spec.loader.exec_module(build)
+    return build
+
+
+def assembly(source, tmp_path):
+    build = build_module()
     out = tmp_path / (source + ".s")
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     r = subprocess.run([hipcc, *build.COMMON, "--cuda-device-only", "-S", os.path.join(build.CSRC, source), "-o", str(out)],
