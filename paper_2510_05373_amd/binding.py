@@ -314,8 +314,8 @@ class KVLincCache:
         """(They go to the library as 32 bits.)"""
         if not (0 <= window < 1 << 31 and 0 <= sinks < 1 << 31):
             raise KVLincError("window and sinks have to be 0 or more, below 2^31, not %s and %s" % (window, sinks))
-        if max_context >= 1 << 31:
-            raise KVLincError("max_context is below 2^31, not %s" % max_context)
+        if not -1 << 31 <= max_context < 1 << 31:
+            raise KVLincError("max_context is below 2^31 either way, not %s" % max_context)
 
     def _with_scratch(self, call, need):
         """call(scratch, stream) on the current stream, with the scratch at hand if it does (the library looks before it launches anything), else with

@@ -188,3 +188,14 @@ def test_numbers_of_more_than_32_bits_are_refused(cache, over):
         cache.prompt_attention(**prompt_args(**over))
     with pytest.raises(kv.KVLincError, match="2\\^31"):
         cache.decode_windowed(half(2, 8, 128), **over)
+
+
+@pytest.mark.parametrize("bound", [-(1 << 31) - 1, -(1 << 32) + 64, -(1 << 40)])
+def test_bounds_far_below_zero_are_refused(cache, bound):
+    # (as 32 bits the second would be 64)
+    with pytest.raises(kv.KVLincError, match="2\\^31"):
+        cache.prompt_attention(**prompt_args(max_context=bound))
+    with pytest.raises(kv.KVLincError, match="2\\^31"):
+        cache.decode_windowed(half(2, 8, 128), 16, max_context=bound)
+    with pytest.raises(kv.KVLincError, match="GPU"):  # (looked at further: the cache is on the host)
+        cache.decode_windowed(half(2, 8, 128), 16, max_context=-1 << 31)
