@@ -56,6 +56,8 @@ size_t kvlinc_prompt_workspace_bytes(const kvlinc_cache* cache, int32_t T, int32
  *   max_context    host-side upper bound on the tokens a sequence holds before the call (<= 0: capacity).  It sizes the launch and,
  *                  for more than 512 rows a KV head (T * H_q / H_kv), the room for dequantized tokens (580 bytes each): a
  *                  sequence that holds more than there is room for gets zeros in its rows, and KVLINC_ST_BOUND is set.
+ *                  Where nothing is cached yet, 1 says so: without it a first prompt of that many rows reserves the room of a
+ *                  full cache (16 sequences of up to 131072 tokens, 8 KV heads: 9.7 GB) and looks through it.
  *
  * out[b, h, i] = ( sum_t w_t V_t + phi_q(q) S H^T ) / ( sum_t w_t + phi_q(q) P ),  w_t = exp(q K_t / sqrt 128)
  * over the tokens that row i sees; the phi terms (Eq. 5) with the adapters only.  The states S, P stand for all quantized tokens:

@@ -338,7 +338,11 @@ class KVLincCache:
         """Attention of T new tokens of every sequence over the cache and, causally, their own rows; append them afterwards.
 
         q: [B, H_q, T, 128], k_new, v_new: [B, H_kv, T, 128] fp16; n_new: [B] int32 on the device or None (all T).  Returns out, [B, H_q, T,
-        128] fp16; rows beyond n_new are left as they are (zero in an `out` made here).  window, sinks, max_context: kvlinc_context.h."""
+        128] fp16; rows beyond n_new are left as they are (zero in an `out` made here).  window, sinks: kvlinc_context.h.
+
+        max_context: the most tokens that any sequence holds before the call (0: whatever the cache has room for; 1 for an empty cache).  A call
+        of more than 512 rows of a KV head keeps 580 bytes of scratch for each of them and KV head; a sequence that holds more gets zeros, and
+        KVLINC_ST_BOUND is set in `status`."""
         import torch
         if not torch.is_tensor(q) or q.dim() != 4:
             raise KVLincError("q has to be a tensor of shape [B, H_q, T, 128]")

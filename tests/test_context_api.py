@@ -199,3 +199,9 @@ def test_bounds_far_below_zero_are_refused(cache, bound):
         cache.decode_windowed(half(2, 8, 128), 16, max_context=bound)
     with pytest.raises(kv.KVLincError, match="GPU"):  # (looked at further: the cache is on the host)
         cache.decode_windowed(half(2, 8, 128), 16, max_context=-1 << 31)
+
+
+def test_an_empty_cache_needs_no_room_for_cached_tokens():
+    c = plain(B=16, H_q=32, H_kv=8, max_groups=1024)
+    full, empty = (kb.kvlinc_prompt_workspace_bytes(c, 700, max_context=n) for n in (0, 1))
+    assert full >= 16 * 8 * 131072 * 580 and empty == 16 * 8 * 64 * 580  # (64 rows: a tile)
