@@ -211,7 +211,7 @@ def prepare(case, seed):
     groups = torch.cat((_planes(d["kc"], case["bits"]), _planes(values, case["bits"]), scales(d["ks"]), scales(d["kz"]), sz), -1).contiguous()
     state = {"case": case, "groups": groups, "k_res": d["k_win"].contiguous(),
              "v_res": d["v_win"].view(B, Hkv, 32, 4, 128).transpose(-1, -2).contiguous(),
-             "n_quant": _device_counts(d["nq"], dev), "n_res": _device_counts(d["nr"], dev), "longest": int((d["nq"] + d["nr"]).max())}
+             "n_quant": _device_counts(d["nq"], dev), "n_res": _device_counts(d["nr"], dev), "longest": max(1, int((d["nq"] + d["nr"]).max()))}
     for k in ("q", "k_new", "v_new", "Wq", "Wk", "P"):
         state[k] = d.get(k)
     if case["corr"]:  # tile (64-feature block, channel half, 4-feature step) holds [channel % 64][feature % 4]
