@@ -66,9 +66,9 @@ size_t kvlinc_prompt_workspace_bytes(const kvlinc_cache* cache, int32_t T, int32
  * Arithmetic: matrix products of binary16 operands with binary32 sums; softmax weights, and values where they are dequantized
  * ahead of a product, are rounded to binary16 once; keys are held to 2^-12 of themselves and what that leaves to a few percent;
  * running maximum, sums and numerators are binary32.
- * Keys and values must be finite: a non-finite one among the rows reaches all outputs of its sequence that are formed with it in
- * one block of up to 128 rows, those of earlier rows too (the append then refuses the sequence).  Results do not depend on
- * the order in which the workgroups run.
+ * A key or value among the new rows that is not finite makes the rows that see it not finite (but for a key that is infinite and
+ * gets the weight 0), and no others: earlier rows and rows whose window has passed it stay right.  (The append then refuses the sequence.)
+ * Results do not depend on the order in which the workgroups run.
  */
 int kvlinc_prompt_attention(const kvlinc_cache* cache, const kvlinc_half* q, const kvlinc_half* k_new, const kvlinc_half* v_new,
                             const int32_t* n_new, int32_t T, int32_t window, int32_t sinks, kvlinc_half* out, void* workspace,

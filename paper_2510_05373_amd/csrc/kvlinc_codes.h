@@ -100,6 +100,15 @@ __device__ __forceinline__ Shares shares_of(float m, float c_d) {
   return Shares{c_d != 0.0f ? __builtin_amdgcn_exp2f(m - to) : 1.0f, __builtin_amdgcn_exp2f(-to)};
 }
 
+// Bits 15 and 31: the halves of a word that are infinite or not a number; and the word with zeros in their places.  A value that a row does not see
+// must not reach it, and 0 times such a value is not a number.
+__device__ __forceinline__ uint32_t not_finite(uint32_t w) { return ((w & 0x7c007c00u) + 0x04000400u) & 0x80008000u; }
+__device__ __forceinline__ uint32_t finite_or_zero(uint32_t w) { return w & ~((not_finite(w) >> 15) * 0xffffu); }
+
+// Reference of a row as the others' parts are joined with it: that of a row whose scores are not numbers was never set (a maximum passes them by), and
+// -inf would leave its sum out.
+__device__ __forceinline__ float reference_of(float m, float l) { return l != l && m == -INFINITY ? 0.0f : m; }
+
 // What a query sees: its position p, the window's first token, the sinks.  Token t <= p is seen if t >= low or t < sinks.
 __device__ __forceinline__ int window_low(int p, int window) { return window > 0 ? max(p - window + 1, 0) : 0; }
 

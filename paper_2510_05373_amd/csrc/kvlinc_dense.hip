@@ -29,6 +29,8 @@ struct DenseTiles {
   char k[kDenseBuffers][kTileBytes];
   char v[kDenseBuffers][kTileBytes];
   LowTile low[kDenseBuffers];
+  uint32_t bad[kDenseBuffers][4];  // tokens 16 i .. 16 i + 15 whose values are not finite, a bit each (see look_over)
+  uint32_t again;
 };
 
 // 1 KB from memory to LDS, 16 bytes a lane, in lane order from `lds` on.  (In assembly: the compiler would otherwise wait for the tile under
@@ -86,6 +88,48 @@ __device__ __forceinline__ void dense_order() {
     if (VALUES && i < 16 - kFirst / 2) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
     else if (i < (VALUES ? 32 - kFirst / 2 : 16 - kFirst)) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
   }
+}
+
+// New values that are not finite must not reach rows that do not see them: 0 times such a value is not a number.  A block goes over its tiles without a
+// look at that, and once more, looking at every new value, if one of its rows has not come out finite (finite values leave all sums far below binary32's
+// largest number).  Looked at in the first place they took 1 to 4 % of a call (700 tokens 31.9 -> 33.4 us, four prompts of 1700 to 4096 395 -> 405); so it
+// is 0.5 % (32.3; 397).  (The kernel that unpacks codes has them in registers on their way and looks at once: a second time cost its short calls 1.5 us.)
+__device__ __forceinline__ bool rows_not_finite(const TileRows& st) {
+  float z = st.l * 0.0f;
+#pragma unroll
+  for (int cb = 0; cb < 4; ++cb)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) z = fmaf(st.acc[cb][r], 0.0f, z);
+  return __builtin_amdgcn_ballot_w64(z != 0.0f) != 0;
+}
+// Whether some wave of the block has to; `word`: LDS, 0 since before the last barrier but one.  Ends with all waves at one place.
+__device__ __forceinline__ bool some_wave(bool mine, uint32_t& word, int lane) {
+  if (mine && lane == 0) word = 1;
+  next_phase();
+  return __builtin_amdgcn_readfirstlane(word) != 0;
+}
+// The second time over a block's tiles (see rows_not_finite): waves 0..3 look at 16 rows of new values each ahead of the tile's products, a quarter
+// of a row a lane, put zeros in the place of what is not finite and note the token.
+__device__ __forceinline__ void look_over(char* t, uint32_t& bad, int wave, int lane) {
+  u32x4_t* row = reinterpret_cast<u32x4_t*>(t + 4096 * wave + 64 * lane);  // (which chunks they are does not matter)
+  u32x4_t x[4];
+  uint32_t here = 0;
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    x[c] = row[c];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) here |= not_finite(x[c][i]);
+  }
+  const uint64_t lanes = __builtin_amdgcn_ballot_w64(here != 0);
+  uint32_t tokens = 0;
+  if (lanes != 0) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) tokens |= (lanes >> (4 * i) & 15u) != 0 ? 1u << i : 0u;
+    if (here != 0)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) row[c] = u32x4_t{finite_or_zero(x[c][0]), finite_or_zero(x[c][1]), finite_or_zero(x[c][2]), finite_or_zero(x[c][3])};
+  }
+  if (lane == 0) bad = tokens;
 }
 
 // Rows of a sequence that holds more tokens than the workspace has rows for: zeros, and a bit in the status word.
@@ -196,8 +240,10 @@ __global__ __launch_bounds__(kTileThreads, 2) void dense_kernel(ContextCall a, i
   // Tile `first` + k lies in buffer k % 4.  Waves 0..3 bring theirs two tiles ahead of the softmax, waves 4..7, a phase behind them, three: all
   // of a tile is there when waves 0..3 take its keys, and what it is written over (four tiles before) has been read by all.
   const int n = last - first, behind = wave >> 2;
-  bool rotated = first >= n_new;
-  if (n > 0) {
+  bool rotated = first >= n_new, careful = false;
+  if (tid == 0) tiles.again = 0;
+#pragma unroll 1
+  while (n > 0) {
     int to = 0;
 #pragma unroll 1
     for (; to < 2 + behind && to < n; ++to) bring(first + to, to);
@@ -225,6 +271,8 @@ __global__ __launch_bounds__(kTileThreads, 2) void dense_kernel(ContextCall a, i
       const Tile t = tile_of(item);
       const bool live = wave_sees(wr, a, t.at, t.count);
       if (live) tile_weights(st, t.at, t.count, wave_masked(wr, a, t.at, t.count), wr.p, wr.low, a.sinks, lane);
+      const bool look = careful && t.fresh;
+      if (look && !behind) look_over(tiles.v[k & 3], tiles.bad[k & 3][wave], wave, lane);
       // the tile before the one just asked for
       if (!more) landed<0>();
       else if (first + to <= n_new) landed<4>();
@@ -240,10 +288,19 @@ __global__ __launch_bounds__(kTileThreads, 2) void dense_kernel(ContextCall a, i
         dense_order<false>();
       }
       // (a block of its own: one for both kinds of tiles in each of the above kept two copies of the accumulators)
+      if (look) {
+        const uint32_t(&b)[4] = tiles.bad[k & 3];
+        const uint64_t bad = b[0] | (uint64_t)b[1] << 16 | (uint64_t)b[2] << 32 | (uint64_t)b[3] << 48;
+        if (__builtin_amdgcn_readfirstlane((uint32_t)bad | (uint32_t)(bad >> 32)) != 0) spoil_rows(st, bad, t.at, wr.p, wr.low, a.sinks);
+      }
       if (item + 1 >= n_new && !wr.idle) low_scores(st, tiles.low[(k + 1) & 3], low, lane);
       next_phase();
     }
     if (!behind) next_phase();
+    if (careful || !some_wave(!wr.idle && rows_not_finite(st), tiles.again, lane)) break;
+    careful = true;
+    rotated = first >= n_new;
+    start_rows(st, a.q + wr.place * kHeadDim, lane);
   }
   const bool in_cache_basis = total > 0 || a.splits > 1;
   if (in_cache_basis && !rotated) rotate_tile_rows(st, lane);

@@ -26,7 +26,7 @@ __device__ __forceinline__ float2v_t load2(__amdgpu_buffer_rsrc_t r, int at) { r
 __device__ __forceinline__ void finish_row(float (&a)[8], float l, int lane, half_t* out) {
   lane8_butterflies(a);
   row16_butterflies<8>(a, lane);
-  const float inv = l > 0.0f ? kInvSqrtD / l : 0.0f;
+  const float inv = l != 0.0f ? kInvSqrtD / l : 0.0f;  // (0: no tokens)
   u32x4_t h;
 #pragma unroll
   for (int i = 0; i < 4; ++i) h[i] = as_u32(pack_h2(a[2 * i] * inv, a[2 * i + 1] * inv));

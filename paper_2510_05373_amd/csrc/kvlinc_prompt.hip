@@ -36,6 +36,8 @@ struct Tiles {
   // a wave's LowQuery (in registers all the time it made others spill, in every tile)
   u32x4_t q_low[kTileWaves][2][64];
   u32x4_t q_low_end[kTileWaves][64];
+  // new rows whose values are not finite, as the value tiles: bits 0..3 of byte i are tokens 4 i .. 4 i + 3
+  u32x4_t bad[3];
 };
 typedef u32x4_t (*KeyTile)[16];
 typedef u32x4_t (*ValueTile)[8];
@@ -81,10 +83,25 @@ __device__ __forceinline__ void load_raw_values(Share<BITS>& s, const half_t* ro
     s.x[2 + (u >> 1)][2 * (u & 1) + 1] = w[1];
   }
 }
+// 4 tokens x 4 channels, turned over.  What is not finite becomes 0, and its token is noted (see spoil_rows): 0.3 us of a call at most.
 template <int BITS>
-__device__ __forceinline__ void store_raw_values(const Share<BITS>& s, ValueTile t, int tid) {  // 4 tokens x 4 channels, turned over
+__device__ __forceinline__ void store_raw_values(Share<BITS>& s, ValueTile t, u32x4_t& bad, int tid) {
   asm("" : "+v"(tid));
   const int quad = tid >> 5, ch = 4 * (tid & 31);
+  uint32_t here = 0, tokens = 0;
+#pragma unroll
+  for (int u = 0; u < 4; ++u) here |= not_finite(s.x[2][u]) | not_finite(s.x[3][u]);
+  if (__builtin_amdgcn_ballot_w64(here != 0) != 0) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {  // (32 lanes have the channels of the same tokens)
+      const uint32_t a = s.x[2 + (u >> 1)][2 * (u & 1)], b = s.x[2 + (u >> 1)][2 * (u & 1) + 1];
+      const uint64_t lanes = __builtin_amdgcn_ballot_w64((not_finite(a) | not_finite(b)) != 0);
+      tokens |= (uint32_t)((tid & 32) != 0 ? lanes >> 32 : lanes & 0xffffffffu) != 0 ? 1u << u : 0u;
+      s.x[2 + (u >> 1)][2 * (u & 1)] = finite_or_zero(a);
+      s.x[2 + (u >> 1)][2 * (u & 1) + 1] = finite_or_zero(b);
+    }
+  }
+  if ((tid & 31) == 0) reinterpret_cast<uint8_t*>(&bad)[quad] = (uint8_t)tokens;
   put_value_quad(t, ch, quad, low_halves(s.x[2][0], s.x[2][2]), low_halves(s.x[3][0], s.x[3][2]));
   put_value_quad(t, ch + 1, quad, high_halves(s.x[2][0], s.x[2][2]), high_halves(s.x[3][0], s.x[3][2]));
   put_value_quad(t, ch + 2, quad, low_halves(s.x[2][1], s.x[2][3]), low_halves(s.x[3][1], s.x[3][3]));
@@ -317,7 +334,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void tile_kernel(ContextCall a, in
   auto put = [&](int it, int kb, int vb) __attribute__((always_inline)) {
     if (it < raw) {
       store_raw_keys<BITS>(sh, tiles.k[kb], tid);
-      if (it < n_new) store_raw_values<BITS>(sh, tiles.v[vb], tid);
+      if (it < n_new) store_raw_values<BITS>(sh, tiles.v[vb], tiles.bad[vb], tid);
       else store_window_values<BITS>(sh, tiles.v[vb], tid);
     } else {
       const int hf = half_of(it);
@@ -370,6 +387,15 @@ __global__ __launch_bounds__(kTileThreads, 2) void tile_kernel(ContextCall a, in
       }
       const bool live = wave_sees(wr, a, at, count);
       if (live) tile_weights(st, at, count, wave_masked(wr, a, at, count), wr.p, wr.low, a.sinks, lane);
+      if (item < n_new) {
+        const u32x4_t b = tiles.bad[vb];
+        if (__builtin_amdgcn_readfirstlane(b[0] | b[1] | b[2] | b[3]) != 0) {
+          uint64_t bad = 0;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) bad |= (uint64_t)(b[i >> 2] >> (8 * (i & 3)) & 15u) << (4 * i);
+          spoil_rows(st, bad, at, wr.p, wr.low, a.sinks);
+        }
+      }
       __builtin_amdgcn_sched_barrier(0);
       if (to < n) put_next();
       next_phase();

@@ -304,9 +304,11 @@ __device__ __forceinline__ void group_values(Rows& st, const Record<BITS>& rec, 
   }
 }
 
-// Weights of up to 32 raw key rows of 128 halves, `count` of them there (all in subset 0).  Rows beyond count take the last one's keys.
-__device__ __forceinline__ void raw_weights(Rows& st, const half_t* keys, int at, int count, int sinks, int lane, float (&x)[2][4]) {
+// Weights of up to 32 raw key rows of 128 halves, `count` of them there (all in subset 0).  Rows beyond count take the last one's keys.  Returns
+// which of the lane's tokens its row sees, bit 4 n + r.
+__device__ __forceinline__ uint32_t raw_weights(Rows& st, const half_t* keys, int at, int count, int sinks, int lane, float (&x)[2][4]) {
   const int g = lane >> 4;
+  uint32_t seen_bits = 0;
 #pragma unroll
   for (int n = 0; n < 2; ++n) {
     const u32x4_t* row = reinterpret_cast<const u32x4_t*>(keys + (long long)min(16 * n + token_order(lane & 15), count - 1) * kHeadDim + 32 * g);
@@ -314,8 +316,11 @@ __device__ __forceinline__ void raw_weights(Rows& st, const half_t* keys, int at
 #pragma unroll
     for (int s = 0; s < 4; ++s) d = __builtin_amdgcn_mfma_f32_16x16x32_f16(as_h8(row[s]), st.q[s], d, 0, 0, 0);
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
-      x[n][r] = st.subset == 0 && seen(16 * n + token_order(4 * g + r), at, count, st.p, st.low, sinks) ? d[r] * st.unit : -INFINITY;
+    for (int r = 0; r < 4; ++r) {
+      const bool is = st.subset == 0 && seen(16 * n + token_order(4 * g + r), at, count, st.p, st.low, sinks);
+      x[n][r] = is ? d[r] * st.unit : -INFINITY;
+      seen_bits |= is ? 1u << (4 * n + r) : 0u;
+    }
   }
   float mx = x[0][0];
 #pragma unroll
@@ -331,23 +336,45 @@ __device__ __forceinline__ void raw_weights(Rows& st, const half_t* keys, int at
       x[n][r] = __builtin_amdgcn_exp2f(x[n][r] - m);
       st.l += x[n][r];
     }
+  return seen_bits;
 }
 
-// O^T += V^T P^T with raw value rows of 128 halves.  A lane gathers the 8 values of a channel (16 lanes: 32 contiguous bytes a row).
-__device__ __forceinline__ void raw_values(Rows& st, const half_t* values, int count, const float (&w)[2][4], int lane) {
+// O^T += V^T P^T with raw value rows of 128 halves.  A lane gathers the 8 values of a channel (16 lanes: 32 contiguous bytes a row).  A row that
+// sees a value that is not finite becomes not a number; the others take it as 0.
+__device__ __forceinline__ void raw_values(Rows& st, const half_t* values, int count, const float (&w)[2][4], uint32_t seen_bits, int lane) {
   const int g = lane >> 4;
   const half8_t P = as_h8(pack_h2(w[0][0], w[0][1]), pack_h2(w[0][2], w[0][3]), pack_h2(w[1][0], w[1][1]), pack_h2(w[1][2], w[1][3]));
   const half_t* row[8];
 #pragma unroll
   for (int u = 0; u < 8; ++u)
     row[u] = values + (long long)min(16 * (u >> 2) + token_order(4 * g + (u & 3)), count - 1) * kHeadDim + (lane & 15);
+  u32x4_t V[8];
+  uint32_t bad = 0;
 #pragma unroll
   for (int n = 0; n < 8; ++n) {
-    half8_t V;
+    half8_t v;
 #pragma unroll
-    for (int u = 0; u < 8; ++u) V[u] = row[u][16 * n];
-    st.acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(V, P, st.acc[n], 0, 0, 0);
+    for (int u = 0; u < 8; ++u) v[u] = row[u][16 * n];
+    V[n] = __builtin_bit_cast(u32x4_t, v);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) bad |= not_finite(V[n][i]);
   }
+  if (__builtin_amdgcn_ballot_w64(bad != 0) != 0) {
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {  // (the 16 lanes of g have the channels of the same tokens)
+      uint32_t of_token = 0;
+#pragma unroll
+      for (int n = 0; n < 8; ++n) of_token |= not_finite(V[n][u >> 1]) >> (15 + 16 * (u & 1)) & 1u;
+      const uint64_t lanes = __builtin_amdgcn_ballot_w64(of_token != 0);
+      if ((lanes >> (16 * g) & 0xffffu) != 0 && (seen_bits >> u & 1u) != 0) st.l = NAN;
+    }
+#pragma unroll
+    for (int n = 0; n < 8; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) V[n][i] = finite_or_zero(V[n][i]);
+  }
+#pragma unroll
+  for (int n = 0; n < 8; ++n) st.acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(as_h8(V[n]), P, st.acc[n], 0, 0, 0);
 }
 
 // acc H: channels 16 n + 4 g + r, seven butterfly stages and the factor 1 / sqrt(128), in binary32.
@@ -581,8 +608,8 @@ __global__ __launch_bounds__(64 * kMaxWaves, 2) void rows_kernel(ContextCall a) 
         for (; item < n_new; item += step) {
           const int t0 = (new_from + item) * kRawTokens;
           float x[2][4];
-          raw_weights(st, keys + (long long)t0 * kHeadDim, total + t0, min(T - t0, kRawTokens), a.sinks, lane, x);
-          raw_values(st, values + (long long)t0 * kHeadDim, min(T - t0, kRawTokens), x, lane);
+          const uint32_t seen_bits = raw_weights(st, keys + (long long)t0 * kHeadDim, total + t0, min(T - t0, kRawTokens), a.sinks, lane, x);
+          raw_values(st, values + (long long)t0 * kHeadDim, min(T - t0, kRawTokens), x, seen_bits, lane);
           rotate = true;
         }
         if (rotate) rotate_rows(st, lane);  // from here on the accumulators are in the cache's rotated basis
@@ -640,7 +667,7 @@ __global__ __launch_bounds__(64 * kMaxWaves, 2) void rows_kernel(ContextCall a) 
       pair_across<16>(st.mid, x, y);
       pair_across<32>(x + y, x, y);
       const float mid = x + y;
-      if (g == 0) { sM[wave][lane] = st.m; sL[wave][lane] = l; }
+      if (g == 0) { sM[wave][lane] = reference_of(st.m, l); sL[wave][lane] = l; }
 #pragma unroll
       for (int n = 0; n < 8; ++n) {
         const float4_t v = st.acc[n];

@@ -232,6 +232,13 @@ __device__ __forceinline__ BlockPlace place_of_block(const ContextCall& a, int b
   return p;
 }
 
+// A row that sees one of the tokens of a tile whose values are not finite (`bad`, a bit each; in the tile they are zeros) becomes not a number.
+__device__ __forceinline__ uint64_t bits_below(int n) { return n <= 0 ? 0 : n >= 64 ? ~0ull : (1ull << n) - 1; }
+__device__ __forceinline__ void spoil_rows(TileRows& st, uint64_t bad, int at, int p, int low, int sinks) {
+  const uint64_t seen = bits_below(p - at + 1) & (~bits_below(low - at) | bits_below(sinks - at));
+  if ((seen & bad) != 0) st.l = NAN;
+}
+
 // The rows of a wave.
 struct WaveRows {
   bool idle, mine;          // no row of the wave, or this lane's, is one of the call's (lanes beyond the last row take it along)
@@ -287,7 +294,7 @@ __device__ __forceinline__ void store_results(TileRows& st, const ContextCall& a
   if (a.splits > 1) {
     if (!w.mine) return;
     float* dst = a.part + (w.place * a.splits + split) * kPartStride;
-    if (h == 0) { dst[0] = st.m; dst[1] = st.l; }
+    if (h == 0) { dst[0] = reference_of(st.m, st.l); dst[1] = st.l; }
 #pragma unroll
     for (int cb = 0; cb < 4; ++cb)
 #pragma unroll
