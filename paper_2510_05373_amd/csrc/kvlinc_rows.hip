@@ -9,10 +9,11 @@
 // O^T = V^T P^T (rows = channels, columns = query rows), so that a lane holds one query row, lane % 16, throughout, and the weights it
 // forms are the operand it feeds.  For that the tokens of a block of 16 are taken in the order pi(4 g + r) = 8 (g % 2) + 2 (g / 2) +
 // r % 2 + 4 (r / 2) (g = lane / 16): what a lane of the second product has of a value tile's words.
-// Codes become binary16 numbers code - centre in one instruction a pair and stay unscaled: the key scales ride on the query
-// (q s in two binary16 terms, the second what the first leaves: 2^-22 of it), the value scales on the weights.  With the scale on the
-// tile instead, every group would cost 128 multiply-adds a lane and 16 rows, where this takes 32; the second term keeps the scores as
-// exact as binary32 products of the scales would be.  Zero-points and centring are sums over channels resp. tokens.
+// Codes become binary16 numbers code - centre in one instruction a pair and stay unscaled: the key scales ride on the query (q s in two binary16
+// terms, the second what the first leaves: together 2^-22 of q s, or 2^-31 of the row's largest |q|, whichever is more), the value scales on the weights.
+// With the scale on the tile instead, every group would cost 128 multiply-adds a lane and 16 rows, where this takes 32; the second term keeps the scores
+// as exact as binary32 products of the scales would be.  Magnitudes that binary16 has no room for take the same products the long way (wide_operands).
+// Zero-points and centring are sums over channels resp. tokens.
 // Bound: vector instructions, some 740 a wave, 16 rows and group of 128 tokens (beside 96 products), two waves a SIMD; and for few pairs the join of
 // their splits, two trips to memory past the caches, 7 to 9 us.  16 sequences of 8k tokens, 8 KV heads of 4: 1 token 26 us, 4 tokens 28 (3.0 TB/s), with
 // the correction 30.5, 4 bits 41; one of 131072: 6 tokens (24 rows, two blocks that both unpack the codes) 51 us.
@@ -62,13 +63,19 @@ static_assert(Rec<2>::kKeyZero == Rec<2>::kKeyScale + 64 && Rec<2>::kValueSZ == 
 // A wave's copy of a group's scales and zero-points in LDS: [0..15] key scales, [16..31] key zero-points, 8 channels each; [32 + 2 t + u]
 // value (scale, middle) of tokens 16 (4 u + i) + t, i = 0..3, the middle z + centre s in binary16: a value is s (code - centre) + middle, and a
 // weight's rounding counts with the first part only.  The exponent of the group's largest value scale is taken out of them on
-// the way (it goes to the codes, exactly: weight times scale then stays in binary16's range whatever the values' magnitude) and returned.
+// the way (it goes to the codes, exactly: weight times scale then stays in binary16's range whatever the values' magnitude) and returned, with the
+// bits of the largest key scale.
+struct GroupMagnitudes {
+  int value_exponent;
+  uint32_t key_scale;
+};
 template <int BITS>
-__device__ __forceinline__ int put_meta(const Record<BITS>& r, u32x4_t* meta, int lane) {
-  uint32_t top = 0;  // scales are not negative: their bit patterns order like the numbers
-#pragma unroll
-  for (int i = 0; i < 4; ++i) top = max(top, r.meta[i] & 0xffffu);
-  top = lane >= 32 ? top : 0u;
+__device__ __forceinline__ GroupMagnitudes put_meta(const Record<BITS>& r, u32x4_t* meta, int lane) {
+  // scales are not negative: their bit patterns order like the numbers
+  typedef uint16_t ushort2_t __attribute__((ext_vector_type(2)));
+  const auto halves = [&](int i) { return __builtin_bit_cast(ushort2_t, r.meta[i]); };
+  const uint32_t both = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_elementwise_max(halves(0), halves(1)), __builtin_elementwise_max(halves(2), halves(3))));
+  uint32_t top = lane >= 32 ? both & 0xffffu : max(both & 0xffffu, both >> 16);  // (lanes 0..15: key scales; 32..63: value scales)
   top = max(top, dpp_u<kRowRor1>(top));
   top = max(top, dpp_u<kRowRor2>(top));
   top = max(top, dpp_u<kRowRor4>(top));
@@ -83,12 +90,17 @@ __device__ __forceinline__ int put_meta(const Record<BITS>& r, u32x4_t* meta, in
   }
   meta[lane] = w;
   __builtin_amdgcn_wave_barrier();  // (a wave's LDS instructions stay in order)
-  return e;
+  return GroupMagnitudes{e, (uint32_t)__builtin_amdgcn_readlane(top, 0)};
 }
 
+// Queries are scaled to have their largest magnitude in [2^5, 2^6): as small as binary16 can hold beside it are then 2^-30 of it, and products with key
+// scales below 2^10 stay below 65504.
+constexpr int kQueryTop = 6;
+constexpr uint32_t kFirstLargeScale = (15 + 16 - kQueryTop) << 10;  // 2^10 in binary16
 struct Rows {
-  half8_t q[4];       // query of this lane's row, channels 32 g + 8 step .. + 7, times 2^-e (largest magnitude in [1/2, 1))
-  float unit;      // 2^e log2(e) / sqrt(d)
+  half8_t q[4];       // query of this lane's row, channels 32 g + 8 step .. + 7, scaled
+  float unit;      // log2(e) / sqrt(d) over that scale
+  bool lossy;      // some query of the wave's rows is not held exactly (the same in all lanes)
   int p, low;      // position, first token of its window
   int subset;
   float m;         // reference (the same in the four lanes of a column), log2 domain; -inf: nothing seen yet
@@ -141,15 +153,64 @@ __device__ __forceinline__ void window_values(Rows& st, const half_t* v_win, int
   }
 }
 
+// The operands of a group's first product from the query as it is (q_row: this lane's channels): products with the key scales in binary32, the largest of
+// a row brought to [2^14, 2^15).  For queries whose smallest binary16 would lose beside the largest (one of 64 or more is needed for
+// that), and key scales from 2^10 on.  A call takes 10 to 16 % longer so (16 sequences of 8k tokens, 4 rows: 27.5 and 31.3 us; 6 over 131072: 50 and 58).
+template <int BITS>
+__device__ __forceinline__ void wide_operands(const half_t* q_row, const u32x4_t* meta, int lane, half8_t (&hi)[4], half8_t (&lo)[4], float& bias, float& unit) {
+  u32x4_t q[4];
+#pragma unroll
+  for (int s = 0; s < 4; ++s) q[s] = reinterpret_cast<const u32x4_t*>(q_row)[s];
+  float mx = 0.0f, bz = 0.0f, bs = 0.0f;
+#pragma unroll
+  for (int s = 0; s < 4; ++s) {
+    const u32x4_t sc = meta[4 * (lane >> 4) + s], z = meta[16 + 4 * (lane >> 4) + s];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const half2_t a = as_h2(q[s][i]), k = as_h2(sc[i]);
+      mx = fmaxf(mx, fmaxf(fabsf((float)a[0] * (float)k[0]), fabsf((float)a[1] * (float)k[1])));
+      bz = __builtin_amdgcn_fdot2(a, as_h2(z[i]), bz, false);
+      bs = __builtin_amdgcn_fdot2(a, k, bs, false);
+    }
+  }
+  float a, b;
+  pair_across<16>(fmaf(bs, Rec<BITS>::kCentre, bz), a, b);
+  pair_across<32>(a + b, a, b);
+  bias = (a + b) * kLog2eSqrtD;
+  pair_across<16>(mx, a, b);
+  pair_across<32>(fmaxf(a, b), a, b);
+  const uint32_t e = max(__builtin_bit_cast(uint32_t, fmaxf(a, b)) >> 23, 87u);  // (2^-40 at least: none is below 2^-48, and it may be 0)
+  const float scale = bits_f32((254u + 14u - e) << 23);
+  unit = bits_f32((e - 14u) << 23) * kLog2eSqrtD;
+#pragma unroll
+  for (int s = 0; s < 4; ++s) {
+    const u32x4_t sc = meta[4 * (lane >> 4) + s];
+    u32x4_t h, r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const half2_t a = as_h2(q[s][i]), k = as_h2(sc[i]);
+      const float p0 = (float)a[0] * (float)k[0] * scale, p1 = (float)a[1] * (float)k[1] * scale;
+      const half2_t t = pack_h2(p0, p1);
+      h[i] = as_u32(t);
+      r[i] = as_u32(pack_h2(p0 - (float)t[0], p1 - (float)t[1]));
+    }
+    hi[s] = as_h8(h);
+    lo[s] = as_h8(r);
+  }
+}
+
 // Scores of one group of 128 packed tokens, the first at position `at`, `count` of them there: x[i][r] = block subset (8 / S) + i, token
 // 16 n + pi(4 g + r), and with `base` the exponent of a weight, x unit + base.  masked: some row does not see all of them.
-template <int BITS, int S>
-__device__ __forceinline__ void group_scores(Rows& st, const Record<BITS>& rec, const u32x4_t* meta, int at, int count, bool masked, int sinks, int lane,
-                                             float (&x)[8 / S][4], float& base) {
+template <int BITS, int S, typename Q>
+__device__ __forceinline__ void group_scores(Rows& st, const Record<BITS>& rec, const u32x4_t* meta, uint32_t key_scale, Q q_row, int at, int count, bool masked, int sinks, int lane,
+                                             float (&x)[8 / S][4], float& unit, float& base) {
   constexpr int kBlocks = 8 / S;
   half8_t hi[4], lo[4];
   float bias;
-  {
+  if (st.lossy || key_scale >= kFirstLargeScale) {
+    wide_operands<BITS>(q_row(), meta, lane, hi, lo, bias, unit);
+  } else {
+    unit = st.unit;
     float bz = 0.0f, bs = 0.0f;
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
@@ -210,25 +271,25 @@ __device__ __forceinline__ void group_scores(Rows& st, const Record<BITS>& rec, 
   for (int i = 0; i < kBlocks; ++i)
 #pragma unroll
     for (int r = 0; r < 4; ++r) mx = fmaxf(mx, x[i][r]);
-  set_reference(st, fmaf(mx, st.unit, bias));
+  set_reference(st, fmaf(mx, unit, bias));
   const float m = finite_reference(st.m);
   base = bias - m;
   // References and biases thousands beyond what ordinary keys and queries give: the exponents are rounded as the reference was (the score
   // itself, then its distance from the reference), or the exponent of the largest weight would be what the roundings leave.
   if (__builtin_amdgcn_ballot_w64(fmaxf(fabsf(m), fabsf(bias)) > kFusedBound) != 0) {
 #pragma clang fp contract(off)
-    const float back = 1.0f / st.unit;
+    const float back = 1.0f / unit;
 #pragma unroll
     for (int i = 0; i < kBlocks; ++i)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) x[i][r] = (__builtin_fmaf(x[i][r], st.unit, bias) - m) * back;
+      for (int r = 0; r < 4; ++r) x[i][r] = (__builtin_fmaf(x[i][r], unit, bias) - m) * back;
     base = 0.0f;
   }
 }
 
-// Scores become weights; O^T += V^T P^T of the group.  e: see put_meta.  SLIDING: tokens from fp16_from on take their values from the window.
+// Scores become weights; O^T += V^T P^T of the group.  e: value_exponent of put_meta.  SLIDING: tokens from fp16_from on take their values from the window.
 template <int BITS, int S, bool SLIDING>
-__device__ __forceinline__ void group_values(Rows& st, const Record<BITS>& rec, const u32x4_t* meta, int e, float (&x)[8 / S][4], float base, int fp16_from,
+__device__ __forceinline__ void group_values(Rows& st, const Record<BITS>& rec, const u32x4_t* meta, int e, float (&x)[8 / S][4], float unit, float base, int fp16_from,
                                              const half_t* v_win, int quads, int lane) {
   constexpr int kBlocks = 8 / S;
   const float scale = bits_f32((uint32_t)(127 + e) << 23);
@@ -256,7 +317,7 @@ __device__ __forceinline__ void group_values(Rows& st, const Record<BITS>& rec, 
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         const half2_t p2 = as_h2(sz[i + u]);
-        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i + u][r], st.unit, base));
+        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i + u][r], unit, base));
         if (SLIDING) x[i + u][r] = p;
         l += p;
         const bool coded = !SLIDING || 16 * (kBlocks * st.subset + i + u) + t < fp16_from;
@@ -306,19 +367,30 @@ __device__ __forceinline__ void group_values(Rows& st, const Record<BITS>& rec, 
 
 // Weights of up to 32 raw key rows of 128 halves, `count` of them there (all in subset 0).  Rows beyond count take the last one's keys.  Returns
 // which of the lane's tokens its row sees, bit 4 n + r.
-__device__ __forceinline__ uint32_t raw_weights(Rows& st, const half_t* keys, int at, int count, int sinks, int lane, float (&x)[2][4]) {
+template <typename Q>
+__device__ __forceinline__ uint32_t raw_weights(Rows& st, Q q_row, const half_t* keys, int at, int count, int sinks, int lane, float (&x)[2][4]) {
   const int g = lane >> 4;
+  half8_t q[4];
+#pragma unroll
+  for (int s = 0; s < 4; ++s) q[s] = st.q[s];
+  float unit = st.unit;
+  if (st.lossy) {
+    const u32x4_t* src = reinterpret_cast<const u32x4_t*>(q_row());
+#pragma unroll
+    for (int s = 0; s < 4; ++s) q[s] = as_h8(src[s]);
+    unit = kLog2eSqrtD;
+  }
   uint32_t seen_bits = 0;
 #pragma unroll
   for (int n = 0; n < 2; ++n) {
     const u32x4_t* row = reinterpret_cast<const u32x4_t*>(keys + (long long)min(16 * n + token_order(lane & 15), count - 1) * kHeadDim + 32 * g);
     float4_t d = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int s = 0; s < 4; ++s) d = __builtin_amdgcn_mfma_f32_16x16x32_f16(as_h8(row[s]), st.q[s], d, 0, 0, 0);
+    for (int s = 0; s < 4; ++s) d = __builtin_amdgcn_mfma_f32_16x16x32_f16(as_h8(row[s]), q[s], d, 0, 0, 0);
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const bool is = st.subset == 0 && seen(16 * n + token_order(4 * g + r), at, count, st.p, st.low, sinks);
-      x[n][r] = is ? d[r] * st.unit : -INFINITY;
+      x[n][r] = is ? d[r] * unit : -INFINITY;
       seen_bits |= is ? 1u << (4 * n + r) : 0u;
     }
   }
@@ -563,11 +635,15 @@ __global__ __launch_bounds__(64 * kMaxWaves, 2) void rows_kernel(ContextCall a) 
 #pragma unroll
     for (int n = 0; n < 8; ++n) st.acc[n] = float4_t{0.f, 0.f, 0.f, 0.f};
     if (row0 < rows) {
-      {
+      auto q_row = [&]() __attribute__((always_inline)) {
         const RowPlace at = row_place(min(row0 + (lane & (kBlockRows - 1)), rows - 1), gq);
-        st.p = total + at.i;
+        return a.q + ((head0 + at.h) * a.T + at.i) * kHeadDim + 32 * g;
+      };
+      {
+        const int i = row_place(min(row0 + (lane & (kBlockRows - 1)), rows - 1), gq).i;
+        st.p = total + i;
         st.low = window_low(st.p, a.window);
-        const u32x4_t* src = reinterpret_cast<const u32x4_t*>(a.q + ((head0 + at.h) * a.T + at.i) * kHeadDim + 32 * g);
+        const u32x4_t* src = reinterpret_cast<const u32x4_t*>(q_row());
         u32x4_t raw[4];
         uint32_t mx = 0;
 #pragma unroll
@@ -581,11 +657,22 @@ __global__ __launch_bounds__(64 * kMaxWaves, 2) void rows_kernel(ContextCall a) 
         const auto v = __builtin_amdgcn_permlane32_swap(mx, mx, false, false);
         mx = max(v[0], v[1]);
         const int e = (int)min(max(mx >> 10, 1u), 30u) - 14;  // largest magnitude in [2^(e-1), 2^e) (subnormal rows: below 2^-14, e = -13)
-        const float down = bits_f32((uint32_t)(127 - e) << 23);
-        st.unit = bits_f32((uint32_t)(127 + e) << 23) * kLog2eSqrtD;
-        const half2_t down2 = pack_h2(down, down);
+        const int shift = min(kQueryTop - e, 15);             // (2^15: binary16's largest power of two; what is so small is held exactly)
+        const half2_t by = pack_h2(bits_f32((uint32_t)(127 + shift) << 23), bits_f32((uint32_t)(127 + shift) << 23));
+        const half2_t back = pack_h2(bits_f32((uint32_t)(127 - shift) << 23), bits_f32((uint32_t)(127 - shift) << 23));
+        st.unit = bits_f32((uint32_t)(127 - shift) << 23) * kLog2eSqrtD;
+        uint32_t lost = 0;
 #pragma unroll
-        for (int s = 0; s < 4; ++s) st.q[s] = as_h8(as_h2(raw[s][0]) * down2, as_h2(raw[s][1]) * down2, as_h2(raw[s][2]) * down2, as_h2(raw[s][3]) * down2);
+        for (int s = 0; s < 4; ++s) {
+          u32x4_t scaled;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            scaled[i] = as_u32(as_h2(raw[s][i]) * by);
+            lost |= as_u32(as_h2(scaled[i]) * back) ^ raw[s][i];
+          }
+          st.q[s] = as_h8(scaled);
+        }
+        st.lossy = __builtin_amdgcn_ballot_w64(lost != 0) != 0;
       }
       // Blocks of tokens that some row sees: the new rows' (32 each), the window's (32 each), the groups.  `low` is that of the first row, the
       // last row's position ends the new ones.
@@ -608,7 +695,7 @@ __global__ __launch_bounds__(64 * kMaxWaves, 2) void rows_kernel(ContextCall a) 
         for (; item < n_new; item += step) {
           const int t0 = (new_from + item) * kRawTokens;
           float x[2][4];
-          const uint32_t seen_bits = raw_weights(st, keys + (long long)t0 * kHeadDim, total + t0, min(T - t0, kRawTokens), a.sinks, lane, x);
+          const uint32_t seen_bits = raw_weights(st, q_row, keys + (long long)t0 * kHeadDim, total + t0, min(T - t0, kRawTokens), a.sinks, lane, x);
           raw_values(st, values + (long long)t0 * kHeadDim, min(T - t0, kRawTokens), x, seen_bits, lane);
           rotate = true;
         }
@@ -621,7 +708,7 @@ __global__ __launch_bounds__(64 * kMaxWaves, 2) void rows_kernel(ContextCall a) 
       for (; item < n_win; item += step) {
         const int t0 = (win_from + item) * kRawTokens;
         float x[2][4];
-        raw_weights(st, k_win + t0 * kHeadDim, len.nq + t0, min(len.nr - t0, kRawTokens), a.sinks, lane, x);
+        raw_weights(st, q_row, k_win + t0 * kHeadDim, len.nq + t0, min(len.nr - t0, kRawTokens), a.sinks, lane, x);
         window_values<2>(st, v_win, quads, t0 / 16, x, lane);
       }
       item -= n_win;
@@ -638,22 +725,22 @@ __global__ __launch_bounds__(64 * kMaxWaves, 2) void rows_kernel(ContextCall a) 
         while (item < plain) {
           const int at = gr * kGroup, count = min(len.nq - at, kGroup);
           const bool masked = count < kGroup || (at < low_last && at + kGroup > a.sinks), more = item + step < n_groups;
-          const int e = put_meta<BITS>(rec, sMeta[wave], lane);
-          float x[8 / S][4], exponent_base;
-          group_scores<BITS, S>(st, rec, sMeta[wave], at, count, masked, a.sinks, lane, x, exponent_base);
+          const GroupMagnitudes mag = put_meta<BITS>(rec, sMeta[wave], lane);
+          float x[8 / S][4], unit, exponent_base;
+          group_scores<BITS, S>(st, rec, sMeta[wave], mag.key_scale, q_row, at, count, masked, a.sinks, lane, x, unit, exponent_base);
           const int next = more ? group_of(item + step) : gr;
           if (more) load_key_part<BITS>(rec, rec0 + (long long)next * Rec<BITS>::kWords, lane);
-          group_values<BITS, S, false>(st, rec, sMeta[wave], e, x, exponent_base, kGroup, v_win, quads, lane);
+          group_values<BITS, S, false>(st, rec, sMeta[wave], mag.value_exponent, x, unit, exponent_base, kGroup, v_win, quads, lane);
           if (more) load_value_part<BITS>(rec, rec0 + (long long)next * Rec<BITS>::kWords, lane);
           item += step;
           gr = next;
         }
         if (SLIDING && item < n_groups) {
           const int at = gr * kGroup;
-          const int e = put_meta<BITS>(rec, sMeta[wave], lane);
-          float x[8 / S][4], exponent_base;
-          group_scores<BITS, S>(st, rec, sMeta[wave], at, kGroup, at < low_last && at + kGroup > a.sinks, a.sinks, lane, x, exponent_base);
-          group_values<BITS, S, true>(st, rec, sMeta[wave], e, x, exponent_base, len.nr, v_win, quads, lane);
+          const GroupMagnitudes mag = put_meta<BITS>(rec, sMeta[wave], lane);
+          float x[8 / S][4], unit, exponent_base;
+          group_scores<BITS, S>(st, rec, sMeta[wave], mag.key_scale, q_row, at, kGroup, at < low_last && at + kGroup > a.sinks, a.sinks, lane, x, unit, exponent_base);
+          group_values<BITS, S, true>(st, rec, sMeta[wave], mag.value_exponent, x, unit, exponent_base, len.nr, v_win, quads, lane);
         }
       }
     }
