@@ -62,9 +62,8 @@ static_assert(Rec<2>::kKeyZero == Rec<2>::kKeyScale + 64 && Rec<2>::kValueSZ == 
 
 // A wave's copy of a group's scales and zero-points in LDS: [0..15] key scales, [16..31] key zero-points, 8 channels each; [32 + 2 t + u]
 // value (scale, middle) of tokens 16 (4 u + i) + t, i = 0..3, the middle z + centre s in binary16: a value is s (code - centre) + middle, and a
-// weight's rounding counts with the first part only.  The exponent of the group's largest value scale is taken out of them on
-// the way (it goes to the codes, exactly: weight times scale then stays in binary16's range whatever the values' magnitude) and returned, with the
-// bits of the largest key scale.
+// weight's rounding counts with the first part only.  Returned: the exponent e of the group's largest value scale, which goes from the weights to the
+// codes (2^-e weight scale stays in binary16's range whatever the values' magnitude, and the codes times 2^e are exact), and the bits of the largest key scale.
 struct GroupMagnitudes {
   int value_exponent;
   uint32_t key_scale;
@@ -81,12 +80,12 @@ __device__ __forceinline__ GroupMagnitudes put_meta(const Record<BITS>& r, u32x4
   top = max(top, dpp_u<kRowRor4>(top));
   top = max(top, dpp_u<kRowRor8>(top));
   const int e = (int)(max(max(__builtin_amdgcn_readlane(top, 32), __builtin_amdgcn_readlane(top, 48)) >> 10, 3u)) - 15;  // -12 .. 15: the codes times 2^e are normal numbers
-  const half_t unscale = (half_t)(lane >= 32 ? bits_f32((uint32_t)(127 - e) << 23) : 1.0f), centre = (half_t)(lane >= 32 ? Rec<BITS>::kCentre : 0.0f);
+  const half_t centre = (half_t)(lane >= 32 ? Rec<BITS>::kCentre : 0.0f);
   u32x4_t w;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const half2_t v = as_h2(r.meta[i]);
-    w[i] = as_u32(half2_t{v[0] * unscale, __builtin_elementwise_fma(v[0], centre, v[1])});
+    w[i] = as_u32(half2_t{v[0], __builtin_elementwise_fma(v[0], centre, v[1])});
   }
   meta[lane] = w;
   __builtin_amdgcn_wave_barrier();  // (a wave's LDS instructions stay in order)
@@ -293,6 +292,7 @@ __device__ __forceinline__ void group_values(Rows& st, const Record<BITS>& rec, 
                                              const half_t* v_win, int quads, int lane) {
   constexpr int kBlocks = 8 / S;
   const float scale = bits_f32((uint32_t)(127 + e) << 23);
+  base -= (float)e;  // weights here: times 2^-e
   uint32_t w[kBlocks / 2][4];  // weight times value scale of blocks 2 i and 2 i + 1
   float l = 0.0f, mid = 0.0f;
 #pragma unroll
@@ -318,7 +318,7 @@ __device__ __forceinline__ void group_values(Rows& st, const Record<BITS>& rec, 
       for (int u = 0; u < 2; ++u) {
         const half2_t p2 = as_h2(sz[i + u]);
         const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i + u][r], unit, base));
-        if (SLIDING) x[i + u][r] = p;
+        if (SLIDING) x[i + u][r] = p * scale;
         l += p;
         const bool coded = !SLIDING || 16 * (kBlocks * st.subset + i + u) + t < fp16_from;
         const float yy = __builtin_fmaf(p, (float)p2[0], 0.0f);
@@ -328,8 +328,8 @@ __device__ __forceinline__ void group_values(Rows& st, const Record<BITS>& rec, 
       w[i / 2][r] = as_u32(pack_h2(y[0], y[1]));
     }
   }
-  st.l += l;
-  st.mid += mid;
+  st.l = fmaf(l, scale, st.l);
+  st.mid = fmaf(mid, scale, st.mid);
   half8_t P[4];  // step s: blocks 2 s and 2 s + 1; a column has those of its subset, and zero elsewhere
 #pragma unroll
   for (int s = 0; s < 4; ++s) {

@@ -62,3 +62,40 @@ def test_one_channel_of_large_keys(T, key, query):
     ek[5], eq[5] = key, query
     ek[64:], eq[64:] = -9, 10
     run(T, 2, ek, eq, rows_exact=T <= 12)
+
+
+@pytest.mark.parametrize("bits", [2, 4])
+@pytest.mark.parametrize("T", [1, 2, 3, 12, 40, 300])
+@pytest.mark.parametrize("large, small, window", [(8000.0, 2.0 ** -8, 0), (8000.0, 2.0 ** -8, 150), (1000.0, 2.0 ** -11, 0), (1.0, 1.0, 0)])
+def test_large_values_of_tokens_without_weight(T, bits, large, small, window):
+    # one token in 40 has values some 2^21 times the others', and keys against all queries: its weight is below e^-30, or it is out of the window
+    H_q, H_kv, n = 4, 1, 500
+    K, V, q, k_new, v_new = ref.inputs(1021, 1, H_q, H_kv, [n], T)
+    rng = np.random.default_rng(7)
+    sign = np.where(rng.random(128) < 0.5, -1.0, 1.0)
+    q = (2.0 * np.abs(q.astype(np.float64)) * sign).astype(np.float16)
+    K, V, v_new = K[0][0].astype(np.float64), V[0][0].astype(np.float64) * small, v_new.astype(np.float64) * small
+    at = np.arange(3, n, 40)
+    K[at], V[at] = -6.0 * sign, np.clip(V[at] / small, -2, 2) * large
+    if large > 1:
+        assert (q.astype(np.float64)[0] @ (6.0 * sign)).min() / np.sqrt(128.0) > 35
+    K, V, v_new = [[K.astype(np.float16)]], [[V.astype(np.float16)]], v_new.astype(np.float16)
+    cache = filled(1, H_q, H_kv, K, V, n + 128, bits)
+    assert cache.status.item() == 0
+    got = cache.prompt_attention(to_dev(q), to_dev(k_new), to_dev(v_new), window=window).cpu().numpy()
+    keys, values, _ = ref.tokens_of(K[0][0], V[0][0], o_cache.window_split(n)[0], bits)
+    keys, values = np.concatenate([keys, k_new[0, 0].astype(np.float64)]), np.concatenate([values, v_new[0, 0].astype(np.float64)])
+    t, p = np.arange(len(keys)), n + np.arange(T)[:, None]
+    seen, norms = (t <= p) & ((window == 0) | (p - t < window)), np.linalg.norm(values, axis=1)
+    for h in range(H_q):
+        y, _ = ref.attend(q[0, h], keys, values, n + np.arange(T), window)
+        x = q[0, h].astype(np.float64)
+        s = np.where(seen, x @ keys.T / np.sqrt(128.0), -np.inf)
+        w = np.exp(s - s.max(1, keepdims=True))
+        w /= w.sum(1, keepdims=True)
+        # a score's own error, 2^-11 (few rows: no part of it) and binary32's share of its parts (see context_reference), moves its weight, and the
+        # weighted mean of all of them the sum
+        d = ((2.0 ** -11 if T > 12 else 0.0) + 2.0 ** -14) * (np.abs(x) @ np.abs(keys).T) / np.sqrt(128.0)
+        moved = np.expm1(d + (w * d).sum(1, keepdims=True))
+        tol = ref.HALF_STEP * np.linalg.norm(y, axis=1) + (w * (2 * ref.HALF_STEP + moved)) @ norms + 128 ** 0.5 * 2.0 ** -25  # (a subnormal output)
+        ref.check_rows(got[0, h], y, tol, (T, bits, h))
