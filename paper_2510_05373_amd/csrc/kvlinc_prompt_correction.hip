@@ -1,34 +1,16 @@
 // The linear correction of prompt rows (Sec. 3.2, Eq. 5-6): C_n = phi_q(q) S and C_d = phi_q(q) P of every row, in the rotated basis.
 //
-// A workgroup takes 128 tokens of one head, a wave 16, both products on v_mfma_f32_16x16x32_f16 and transposed, so that a lane keeps one token
-// (column lane % 16) from the logits to the result:
-//   logits^T = W^T q^T: row j of tile i (i = 0..3) of a block of 64 features is feature 4 j + i, so that a lane loads 4 neighbouring features
-//              of the 8 channels that it feeds, and its results are 16 neighbouring features, 16 g .. 16 g + 15 (g = lane / 16);
-//   C_n^T    = S^T phi^T: those are the positions it feeds, 8 in turn; S from its binary16 tile copy, 4 features in 8 bytes.
+// A workgroup takes 128 tokens of one head, a wave 16, one a column of the products (kvlinc_features.h).
 // The eight waves bring the weights and the state to LDS together, half of the features at a time, as operands: read by every wave for itself, 128 KB
 // for 32 tokens, they took twice as long (8192 tokens of 32 heads with what reads the results: 200 us, 109 so; 128 tokens 24 and 11; 32 tokens a wave: 122).
-// The features are rounded to binary16 (2^-12 of each), as S is; logits, their softmax and the sums are binary32.
 // Bound: the results, 528 bytes a row, written and read again (0.28 GB, 53 us of the 109), and the operands from L2.
 #include <hip/hip_runtime.h>
 
-#include "kvlinc_codes.h"
 #include "kvlinc_context_internal.h"
+#include "kvlinc_features.h"
 
 namespace kvlinc {
 namespace {
-
-__device__ __forceinline__ float column_allmax(float v) {  // over the four lanes of a column
-  float x, y;
-  pair_across<16>(v, x, y);
-  pair_across<32>(fmaxf(x, y), x, y);
-  return fmaxf(x, y);
-}
-__device__ __forceinline__ float column_allsum(float v) {
-  float x, y;
-  pair_across<16>(v, x, y);
-  pair_across<32>(x + y, x, y);
-  return x + y;
-}
 
 constexpr int kCorrWaves = 8, kCorrTokens = 16 * kCorrWaves;
 // Grid: blocks of 128 tokens fastest, then (sequence, query head).
@@ -59,24 +41,14 @@ __global__ __launch_bounds__(64 * kCorrWaves, 4) void prompt_correction_kernel(C
     if (half != 0) __syncthreads();
     {  // a wave has one block of features and 32 channels of the weights, and 16 channels of the state
       const int fb = wave >> 2, s = wave & 3, n = wave;
-      u32x2_t w[8];
+      u32x4_t w[4];
+      weight_operands(W, s, fb, j, g, w);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) w[k] = *reinterpret_cast<const u32x2_t*>(W + (32 * s + 8 * g + k) * 128 + 64 * fb + 4 * j);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        u32x4_t r;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) r[k] = __builtin_amdgcn_perm(w[2 * k + 1][i >> 1], w[2 * k][i >> 1], (i & 1) == 0 ? 0x05040100u : 0x07060302u);
-        sW[fb][s][i][lane] = r;
-      }
+      for (int i = 0; i < 4; ++i) sW[fb][s][i][lane] = w[i];
 #pragma unroll
       for (int f = 0; f < 2; ++f)
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {  // tile (64-feature block, channel half, 4-feature step) of S16 holds [channel % 64][feature % 4]
-          const int tile = ((2 * half + f) * 2 + n / 4) * 16 + 4 * g + 2 * e, ch = 16 * (n % 4) + j;
-          const u32x2_t s0 = *reinterpret_cast<const u32x2_t*>(S + (tile * 64 + ch) * 4), s1 = *reinterpret_cast<const u32x2_t*>(S + ((tile + 1) * 64 + ch) * 4);
-          sS[f][n][e][lane] = u32x4_t{s0[0], s0[1], s1[0], s1[1]};
-        }
+        for (int e = 0; e < 2; ++e) sS[f][n][e][lane] = state_operand(S, 128 * half + 64 * f + 16 * g + 8 * e, 16 * n + j);
     }
     __syncthreads();
     if (idle) continue;
@@ -90,39 +62,14 @@ __global__ __launch_bounds__(64 * kCorrWaves, 4) void prompt_correction_kernel(C
 #pragma unroll
         for (int i = 0; i < 4; ++i) x[fb][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(as_h8(sW[fb][s][i][lane]), q[s], x[fb][i], 0, 0, 0);
     }
-    float m = -INFINITY, z = 0.0f, p = 0.0f;
+    half8_t phi[2][2];
+    den += column_features(x, c.P + kv * kRank + 128 * half, g, phi);
 #pragma unroll
     for (int fb = 0; fb < 2; ++fb)
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int e = 0; e < 2; ++e)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) m = fmaxf(m, x[fb][i][r]);
-    m = column_allmax(m);
-    const float* P = c.P + kv * kRank + 128 * half;
-#pragma unroll
-    for (int fb = 0; fb < 2; ++fb)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const float4_t w = *reinterpret_cast<const float4_t*>(P + 64 * fb + 16 * g + 4 * r);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float e = __builtin_amdgcn_exp2f((x[fb][i][r] - m) * 1.4426950408889634f);
-          x[fb][i][r] = e;
-          z += e;
-          p = fmaf(e, w[i], p);
-        }
-      }
-    const float inv = 1.0f / column_allsum(z);
-    den = fmaf(column_allsum(p), inv, den);
-#pragma unroll
-    for (int fb = 0; fb < 2; ++fb)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const half8_t phi = as_h8(pack_h2(x[fb][0][2 * e] * inv, x[fb][1][2 * e] * inv), pack_h2(x[fb][2][2 * e] * inv, x[fb][3][2 * e] * inv),
-                                  pack_h2(x[fb][0][2 * e + 1] * inv, x[fb][1][2 * e + 1] * inv), pack_h2(x[fb][2][2 * e + 1] * inv, x[fb][3][2 * e + 1] * inv));
-#pragma unroll
-        for (int n = 0; n < 8; ++n) acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(as_h8(sS[fb][n][e][lane]), phi, acc[n], 0, 0, 0);
-      }
+        for (int n = 0; n < 8; ++n) acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(as_h8(sS[fb][n][e][lane]), phi[fb][e], acc[n], 0, 0, 0);
   }
   if (token >= T) return;
   float* dst = a.corr + (bh * a.T + token) * kPartStride;

@@ -18,22 +18,19 @@
 // their splits, two trips to memory past the caches, 7 to 9 us.  16 sequences of 8k tokens, 8 KV heads of 4: 1 token 26 us, 4 tokens 28 (3.0 TB/s), with
 // the correction 30.5, 4 bits 41; one of 131072: 6 tokens (24 rows, two blocks that both unpack the codes) 51 us.
 // Weights are rounded to binary16 once, for the second product: 2^-12 of each at most, of no common sign.  They are kept near 2^8 (see
-// kHeadroom), where the smallest that count are normal numbers; sums of weights are taken before the rounding, in binary32.
+// kvlinc_reference.h), where the smallest that count are normal numbers; sums of weights are taken before the rounding, in binary32.
 #include <hip/hip_runtime.h>
 
 #include "kvlinc_codes.h"
+#include "kvlinc_features.h"
 #include "kvlinc_join.h"
+#include "kvlinc_reference.h"
 
 namespace kvlinc {
 namespace {
 
 constexpr int kMaxWaves = 8;
 constexpr int kRawTokens = 32;
-// The reference of a row is its largest score less kHeadroom when it is set, and is set anew when a score passes it by kHeadroom + kLag
-// (most blocks only compare): weights stay below 2^13, and p s with s < 2 below binary16's largest number.
-constexpr float kHeadroom = 8.0f, kLag = 5.0f;
-constexpr float kFusedBound = 0x1p20f;
-
 // Columns of the products: 16 rows of queries; or, of up to 8 or 4 rows, each row S = 2 or 4 times, column c with row c % (16 / S) and subset
 // c / (16 / S): the softmax of a column is then over the 16-token blocks n with n / (8 / S) = subset only, and a lane has 8 / S blocks' scores to
 // work on instead of 8.
@@ -114,13 +111,11 @@ __device__ __forceinline__ bool seen(int t, int at, int count, int p, int low, i
 }
 
 __device__ __forceinline__ void set_reference(Rows& st, float largest) {  // largest: of this lane's scores
-  if (__builtin_amdgcn_ballot_w64(largest - st.m > kHeadroom + kLag) == 0) return;  // (a difference: m + 13 is m + 16 where steps are that wide)
+  if (__builtin_amdgcn_ballot_w64(passes(largest, st.m)) == 0) return;
   float x, y;
   pair_across<16>(largest, x, y);
   pair_across<32>(fmaxf(x, y), x, y);
-  const float mx = fmaxf(x, y);
-  const float to = mx - st.m > kHeadroom + kLag ? (fabsf(mx) > kFusedBound ? mx : mx - kHeadroom) : st.m;
-  const float f = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(st.m - to);  // (0 where nothing was seen)
+  const float to = raised(fmaxf(x, y), st.m), f = raised_factor(st.m, to);
   st.m = to;
   st.l *= f;
   st.mid *= f;
@@ -486,21 +481,9 @@ __device__ __forceinline__ RowPlace row_place(int row, int gq) {
 }
 
 // ---- the correction of all rows of a pair (Sec. 3.2, Eq. 5-6), by one workgroup ----------------------------------------------------------------
-// Products as in kvlinc_prompt_correction.hip.  First the features, a wave a head and half of them at a time (16 tokens as columns), through LDS;
+// Products: kvlinc_features.h.  First the features, a wave a head and half of them at a time (16 tokens as columns), through LDS;
 // then C_n^T = S^T phi^T, a wave a block of 16 channels, so that the state is read once for all heads.
 constexpr int kFeatureStride = kRank + 8;  // halves of a row in LDS
-__device__ __forceinline__ float column_allmax(float v) {  // over the four lanes of a column
-  float x, y;
-  pair_across<16>(v, x, y);
-  pair_across<32>(fmaxf(x, y), x, y);
-  return fmaxf(x, y);
-}
-__device__ __forceinline__ float column_allsum(float v) {
-  float x, y;
-  pair_across<16>(v, x, y);
-  pair_across<32>(x + y, x, y);
-  return x + y;
-}
 __device__ __forceinline__ void correct_rows(const ContextCall& a, int b, int kvh, int T, int rows, int wave, int waves, int lane, half_t* features, float (*den)[64]) {
   const kvlinc_cache& c = a.cache;
   const int j = lane & 15, g = lane >> 4, gq = a.gq;
@@ -521,42 +504,15 @@ __device__ __forceinline__ void correct_rows(const ContextCall& a, int b, int kv
         for (int i = 0; i < 4; ++i) d[fb][i] = float4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
-          u32x2_t w[8];
+          u32x4_t w[4];
+          weight_operands(W, s, fb, j, g, w);
 #pragma unroll
-          for (int k = 0; k < 8; ++k) w[k] = *reinterpret_cast<const u32x2_t*>(W + (32 * s + 8 * g + k) * 128 + 64 * fb + 4 * j);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            u32x4_t r;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) r[k] = __builtin_amdgcn_perm(w[2 * k + 1][i >> 1], w[2 * k][i >> 1], (i & 1) == 0 ? 0x05040100u : 0x07060302u);
-            d[fb][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(as_h8(r), q[s], d[fb][i], 0, 0, 0);
-          }
+          for (int i = 0; i < 4; ++i) d[fb][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(as_h8(w[i]), q[s], d[fb][i], 0, 0, 0);
         }
         asm volatile("" ::: "memory");  // (the loads of both blocks at once would spill)
       }
-      float m = -INFINITY, z = 0.0f, p = 0.0f;
-#pragma unroll
-      for (int fb = 0; fb < 2; ++fb)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) m = fmaxf(m, d[fb][i][r]);
-      m = column_allmax(m);
-#pragma unroll
-      for (int fb = 0; fb < 2; ++fb)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const float4_t w = *reinterpret_cast<const float4_t*>(P + 64 * fb + 16 * g + 4 * r);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float e = __builtin_amdgcn_exp2f((d[fb][i][r] - m) * 1.4426950408889634f);
-            d[fb][i][r] = e;
-            z += e;
-            p = fmaf(e, w[i], p);
-          }
-        }
-      const float inv = 1.0f / column_allsum(z);
-      p = column_allsum(p) * inv;
+      half8_t phi[2][2];
+      const float p = column_features(d, P, g, phi);
       const int row = (i0 + j) * gq + h;
       if (i0 + j < T) {
         if (g == 0) den[half][row] = p;
@@ -564,9 +520,7 @@ __device__ __forceinline__ void correct_rows(const ContextCall& a, int b, int kv
         for (int fb = 0; fb < 2; ++fb)
 #pragma unroll
           for (int e = 0; e < 2; ++e)
-            *reinterpret_cast<half8_t*>(features + row * kFeatureStride + 128 * half + 64 * fb + 16 * g + 8 * e) =
-                as_h8(pack_h2(d[fb][0][2 * e] * inv, d[fb][1][2 * e] * inv), pack_h2(d[fb][2][2 * e] * inv, d[fb][3][2 * e] * inv),
-                      pack_h2(d[fb][0][2 * e + 1] * inv, d[fb][1][2 * e + 1] * inv), pack_h2(d[fb][2][2 * e + 1] * inv, d[fb][3][2 * e + 1] * inv));
+            *reinterpret_cast<half8_t*>(features + row * kFeatureStride + 128 * half + 64 * fb + 16 * g + 8 * e) = phi[fb][e];
       }
     }
   }
@@ -574,13 +528,9 @@ __device__ __forceinline__ void correct_rows(const ContextCall& a, int b, int kv
   const half_t* S = reinterpret_cast<const half_t*>(c.S16) + kv * (128 * 64 * 4);
   const __amdgpu_buffer_rsrc_t out = buffer_of(a.corr + head0 * a.T * kPartStride, (long long)gq * a.T * kPartBytes);
   for (int n = wave; n < 8; n += waves) {
-    half8_t A[8];  // features 32 s + 8 g + 0..7 of channel 16 n + j: two tiles of S16 ([channel % 64][feature % 4])
+    half8_t A[8];  // features 32 s + 8 g + 0..7 of channel 16 n + j
 #pragma unroll
-    for (int s = 0; s < 8; ++s) {
-      const int tile = ((s >> 1) * 2 + n / 4) * 16 + 8 * (s & 1) + 2 * g, ch = 16 * (n % 4) + j;
-      const u32x2_t s0 = *reinterpret_cast<const u32x2_t*>(S + (tile * 64 + ch) * 4), s1 = *reinterpret_cast<const u32x2_t*>(S + ((tile + 1) * 64 + ch) * 4);
-      A[s] = as_h8(u32x4_t{s0[0], s0[1], s1[0], s1[1]});
-    }
+    for (int s = 0; s < 8; ++s) A[s] = as_h8(state_operand(S, 32 * s + 8 * g, 16 * n + j));
     for (int r0 = 0; r0 < rows; r0 += 16) {
       const int row = r0 + j;
       float4_t d = {0.f, 0.f, 0.f, 0.f};

@@ -4,13 +4,12 @@
 
 #include "kvlinc_codes.h"
 #include "kvlinc_context_internal.h"
+#include "kvlinc_reference.h"
 
 namespace kvlinc {
 namespace {
 
 constexpr int kTileWaves = 8, kTileThreads = 64 * kTileWaves, kTileRows = 32 * kTileWaves;
-constexpr float kHeadroom = 8.0f, kLag = 5.0f;
-constexpr float kFusedBound = 0x1p20f;  // references beyond it: the exponent is rounded as the reference is (see tile_weights)
 
 typedef float float16_t __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x6_t __attribute__((ext_vector_type(6)));
@@ -34,12 +33,10 @@ struct TileRows {
 };
 
 __device__ __forceinline__ void raise_reference(TileRows& st, float largest) {  // largest score of this lane, log2 domain
-  if (__builtin_amdgcn_ballot_w64(largest - st.m > kHeadroom + kLag) == 0) return;  // (a difference: m + 13 is m + 16 where steps are that wide)
+  if (__builtin_amdgcn_ballot_w64(passes(largest, st.m)) == 0) return;
   float x, y;
   pair_across<32>(largest, x, y);
-  const float mx = fmaxf(x, y);
-  const float to = mx - st.m > kHeadroom + kLag ? (fabsf(mx) > kFusedBound ? mx : mx - kHeadroom) : st.m;
-  const float f = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(st.m - to);
+  const float to = raised(fmaxf(x, y), st.m), f = raised_factor(st.m, to);
   st.m = to;
   st.l *= f;
   st.far = __builtin_amdgcn_ballot_w64(to != -INFINITY && fabsf(to) > kFusedBound) != 0;
