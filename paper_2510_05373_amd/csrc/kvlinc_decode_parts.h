@@ -273,7 +273,9 @@ __device__ __forceinline__ void empty_state(WaveState<NB>& st) {
 // off[nb] = what the zero-points and the centring of the codes add to every score of the head: sc leaves it out.
 // valid: tokens of the group that exist (only the newest group of a sequence may be partial; the loop over the others passes
 // the constant).
-template <int NB, int BITS>
+// EXACT_OFFSETS: zero-points and scales each for themselves, in place of mid-points rounded to binary16 (2^-12 of them: keys with an offset of
+// 300 in some channels left outputs 1.5e-2 off, so 4e-4).
+template <int NB, int BITS, bool EXACT_OFFSETS = false>
 __device__ __forceinline__ void qk_phase(const KeyRegs<BITS>& g, int valid, const uint32_t (&qh)[NB][4], const Roles& lr,
                                          float (&sc)[NB][8], float (&off)[NB]) {
   const uint32_t S[4] = {g.ks.x, g.ks.y, g.ks.z, g.ks.w};
@@ -282,7 +284,7 @@ __device__ __forceinline__ void qk_phase(const KeyRegs<BITS>& g, int valid, cons
   int scale_a[NB];
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
-    float x[8], bz = 0.0f, mx = 0.0f;
+    float x[8], bz = 0.0f, bs = 0.0f, mx = 0.0f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       x[i] = fmaf((float)as_h2(qh[nb][i >> 1])[i & 1], (float)as_h2(S[i >> 1])[i & 1], 0.0f);  // exact; the fused form reads binary16 operands as they are
@@ -293,10 +295,16 @@ __device__ __forceinline__ void qk_phase(const KeyRegs<BITS>& g, int valid, cons
     // group's scores and small (keys are centred), its rounding (2^-12 of it) is of no account.
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
+      if constexpr (EXACT_OFFSETS) {
+        bz = __builtin_amdgcn_fdot2(as_h2(qh[nb][i]), as_h2(Z[i]), bz, false);
+        bs = __builtin_amdgcn_fdot2(as_h2(qh[nb][i]), as_h2(S[i]), bs, false);
+        continue;
+      }
       const half2_t mid = as_h2(S[i]) * half2_t{(half_t)Rec<BITS>::kCentre, (half_t)Rec<BITS>::kCentre} + as_h2(Z[i]);
       bz = __builtin_amdgcn_fdot2(as_h2(qh[nb][i]), mid, bz, false);
     }
     const uint32_t eb = block_exponent(xrow_umax(quad_umax(as_bits(mx))));  // over the 128 channels of the head
+    if constexpr (EXACT_OFFSETS) bz = fmaf(bs, Rec<BITS>::kCentre, bz);
     bz = xrow_allsum(quad_allsum(bz));
     uint32_t t[3][2];
     split_fp8x3(x, block_scale_bits(eb), t);

@@ -1,7 +1,7 @@
 // Windowed decode: one query a sequence over the newest tokens and the first few, read directly from the packed cache.
 //
 // The arithmetic is that of the decode kernel (kvlinc_decode.hip; shared in kvlinc_decode_parts.h): codes go to the matrix cores as FP4, queries
-// and weights as three FP8 terms, all query heads of a KV head share one pass.  What differs is which groups are walked: those with sinks, then
+// and weights as three FP8 terms, zero-points exact (EXACT_OFFSETS), all query heads of a KV head share one pass.  What differs is which groups are walked: those with sinks, then
 // those from the window's first token on, numbered one after the other; tokens of a group at the border that are not seen have their scores
 // taken out.  A sequence is cut into splits of these groups; the four waves of split 0 share the visible part of the fp16 window first.
 // One launch; the splits are joined by the workgroup that arrives last at the pair's counter.
@@ -94,7 +94,7 @@ __global__ __launch_bounds__(kThreads, BITS == 4 || (NB == 2 && SLIDING) ? 2 : 3
     const bool more = next < count;
     const uint32_t* src = rec0 + (long long)group_of(more ? next : idx) * kRecordWords;
     float sc[NB][8], off[NB], base[NB];
-    qk_phase<NB, BITS>(kr, min(kGroup, len.nq - at), qh, lr, sc, off);
+    qk_phase<NB, BITS, true>(kr, min(kGroup, len.nq - at), qh, lr, sc, off);
     if (more) load_keys(kr, src, lr);
     if (at < low && at + kGroup > a.sinks) hide_tokens<NB>(sc, at, low, a.sinks, lr);
     update_reference<NB>(sc, off, base, st, kSlack);
@@ -105,7 +105,7 @@ __global__ __launch_bounds__(kThreads, BITS == 4 || (NB == 2 && SLIDING) ? 2 : 3
   if (SLIDING && idx < count) {
     const int at = group_of(idx) * kGroup;
     float sc[NB][8], off[NB], base[NB];
-    qk_phase<NB, BITS>(kr, kGroup, qh, lr, sc, off);
+    qk_phase<NB, BITS, true>(kr, kGroup, qh, lr, sc, off);
     if (at < low && at + kGroup > a.sinks) hide_tokens<NB>(sc, at, low, a.sinks, lr);
     update_reference<NB>(sc, off, base, st, kSlack);
     pv_phase<NB, BITS, true>(vr, sc, base, lr, st, len.nr);
