@@ -274,7 +274,7 @@ __device__ __forceinline__ void empty_state(WaveState<NB>& st) {
 // valid: tokens of the group that exist (only the newest group of a sequence may be partial; the loop over the others passes
 // the constant).
 // EXACT_OFFSETS: zero-points and scales each for themselves, in place of mid-points rounded to binary16 (2^-12 of them: keys with an offset of
-// 300 in some channels left outputs 1.5e-2 off, so 4e-4).
+// 300 in some channels left outputs 1.5e-2 off, so 3e-4).
 template <int NB, int BITS, bool EXACT_OFFSETS = false>
 __device__ __forceinline__ void qk_phase(const KeyRegs<BITS>& g, int valid, const uint32_t (&qh)[NB][4], const Roles& lr,
                                          float (&sc)[NB][8], float (&off)[NB]) {
