@@ -61,11 +61,13 @@ size_t kvlinc_prompt_workspace_bytes(const kvlinc_cache* cache, int32_t T, int32
  *
  * out[b, h, i] = ( sum_t w_t V_t + phi_q(q) S H^T ) / ( sum_t w_t + phi_q(q) P ),  w_t = exp(q K_t / sqrt 128)
  * over the tokens that row i sees; the phi terms (Eq. 5) with the adapters only.  The states S, P stand for all quantized tokens:
- * with adapters, window > 0 is refused, and so is KVLINC_FLAG_ALG1_LITERAL.  The cache may end in a partial group.
+ * with adapters, window > 0 is refused, and so is KVLINC_FLAG_ALG1_LITERAL.  Where nothing is quantized yet (S = P = 0) it is the
+ * softmax alone, however low the logits.  The cache may end in a partial group.
  *
  * Arithmetic: matrix products of binary16 operands with binary32 sums; softmax weights, and values where they are dequantized
- * ahead of a product, are rounded to binary16 once; keys are held to 2^-12 of themselves and what that leaves to a few percent;
- * running maximum, sums and numerators are binary32.
+ * ahead of a product, are rounded to binary16 once; running maximum, sums and numerators are binary32.  Keys are exact for up to
+ * 64 rows of a KV head; for more they are binary16 numbers, and what that leaves is held to a few percent of 2^-12 of the
+ * largest of 32 channels (keys with an offset of 300 in some channels: outputs 1e-3 to 2e-3 of their norm off, without it 3e-4).
  * A key or value among the new rows that is not finite makes the rows that see it not finite (but for a key that is infinite and
  * gets the weight 0), and no others: earlier rows and rows whose window has passed it stay right.  (The append then refuses the sequence.)
  * Results do not depend on the order in which the workgroups run.

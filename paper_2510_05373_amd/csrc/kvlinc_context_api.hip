@@ -38,12 +38,13 @@ long long groups_met(const kvlinc_cache& c, int T, int window, int sinks, int ma
   return near < all ? near : all;
 }
 
+// (The figures beside the choices below are two sides of one run each, three states in turn so that no cache holds them.)
 // Which of the three a call of so many rows a KV head takes, measured (us; 8 KV heads, 2 bits):
 //   rows                                   64            512            640            1000
-//   1 sequence, 32k cached tokens          rows 53       tiles 137      tiles 199      tiles 243
-//                                          tiles 65      dense 135      dense 165      dense 202
-//   8 sequences of 4k                      rows 35       tiles 136      tiles 236      tiles 243
-//                                          tiles 55      dense 149      dense 188      dense 214
+//   1 sequence, 32k cached tokens          rows 53       tiles 137      tiles 200      tiles 245
+//                                          tiles 66      dense 149      dense 172      dense 213
+//   8 sequences of 4k                      rows 34       tiles 137      tiles 239      tiles 246
+//                                          tiles 56      dense 151      dense 190      dense 215
 // Every block of 256 rows dequantizes the tiles it goes over anew: from the third block on it pays to have done that once for all.  A wave of
 // the first kind has 16 rows and the codes for itself alone: 64 rows are what its registers and four waves make of a pair.
 constexpr long long kFewRows = 64, kTiledRows = 2 * 256;
@@ -55,15 +56,16 @@ ContextPlan plan_call(const kvlinc_cache& c, int T, int window, int sinks, int m
   long long s, most;
   if (p.kind == ContextPlan::kRows) {
     // Two workgroups of four waves a compute unit, or, where the pairs are few, one of eight: fewer splits to join (6 tokens over 131072, 8 pairs:
-    // 59.2 us with four, 53.4 with eight; 4 tokens, 64 pairs of 16k: 28.5 and 27.8; 128 of 8k: 27.9 and 28.2).
+    // 58.1 us with four, 50.5 with eight; 4 tokens, 64 pairs of 16k: 29.5 and 27.6; 128 of 8k: 29.6 and 28.6, with the correction 32.2 and 41.1; 512 pairs
+    // of 400 to 4096: 41 and 46).
     p.waves = pairs <= 64 ? 8 : 4;
     s = (p.waves == 8 ? 256 : 512) / pairs - (c.S16 != nullptr ? 1 : 0);  // (the correction's workgroups are some of them)
     most = (groups + p.waves - 1) / p.waves;
   } else {
-    // One workgroup a compute unit.  A split of less than 8 tiles costs more to write and join than it saves (one prompt of 700 tokens: 31 us, 38 with
-    // splits of 4; 300 tokens over 4096: 65 and 64), one over codes, whose tiles take longer, of less than 4 (64 tokens over 2048: 47 us with 8, 38 with
-    // 4, 38 with 2; over 8192: 57, 53, 54).  (Without a bound the cache is taken to have room for the rows, no more: that is a guess for
-    // the number of splits, not for what is reserved.)
+    // One workgroup a compute unit.  A split of less than 8 tiles costs more to write and join than it saves (one prompt of 700 tokens: 31 us, 34 in
+    // three splits; 300 tokens over 4096: 63 with 8, 4 and 2), one over codes, whose tiles take longer, of less than 4 (64 tokens over 8192: 54 us with 8, 48
+    // with 4 and with 2; over 2048, where two would be better still: 47, 37, 34).  (Without a bound the cache is taken to have room for the rows, no more:
+    // that is a guess for the number of splits, not for what is reserved.)
     const long long least = p.kind == ContextPlan::kTiles ? 4 : 8;
     const long long cached = max_context > 0 ? groups * kGroup : groups * kGroup - T;
     s = 256 / (pairs * ((rows + 255) / 256));
@@ -107,8 +109,8 @@ int check_prompt(const kvlinc_cache* c, int T, int window, int sinks) {
   if (c->S16 != nullptr && (window != 0 || (c->flags & KVLINC_FLAG_ALG1_LITERAL) != 0)) return KVLINC_EINVAL;
   return KVLINC_OK;
 }
-// Windowed decode: two workgroups of four waves a compute unit; a split has a group for each wave (one sequence, window 1024: 7.3 us, 7.2 with three
-// groups a wave; 2048: 7.3 and 8.5; 4 bits, 7 heads, 2048: 10.4 and 12.8).
+// Windowed decode: two workgroups of four waves a compute unit; a split has a group for each wave (from a graph: one sequence, window 1024: 7.3 us, 7.1
+// with three groups a wave; 2048: 7.6 and 8.9; 4 bits, 7 heads, 2048: 10.8 and 13.3).
 ContextPlan plan_windowed(const kvlinc_cache& c, int window, int sinks, int max_context) {
   const long long pairs = (long long)c.B * c.H_kv, groups = groups_met(c, 1, window, sinks, max_context);
   long long s = 512 / pairs, most = (groups + 3) / 4;

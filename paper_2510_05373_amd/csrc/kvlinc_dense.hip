@@ -8,9 +8,9 @@
 // took 3.7 ms without it, 4.05 with it, at a third of the error.
 //
 // Bound: the matrix and the vector phases, which take turns on a SIMD's two waves and are about as long; a long call also the power limit (8k tokens
-// over 24k: 1.67 GHz).  8k over 24k, 4 heads, with 0.08 ms of correction and 0.05 of dequantizing: 4.0 ms (0.98 PFLOP/s; a matrix product of 8192^3
-// from the library reaches 1.19); four prompts of 1700 to 4096 tokens 400 us (0.86), 340 without the softmax, 312 without the products; one of
-// 700 tokens 30 us.
+// over 24k: 1.67 GHz).  8k over 24k, 4 heads, with 0.08 ms of correction and 0.05 of dequantizing: 3.97 to 4.22 ms by the card (0.92 to 0.98 PFLOP/s; a
+// matrix product of 8192^3 from the library reaches 1.19); four prompts of 1700 to 4096 tokens 393 to 402 us (0.86), 340 without the softmax, 312 without
+// the products; one of 700 tokens 30.6 us.
 #include <hip/hip_runtime.h>
 
 #include "kvlinc_tiles.h"

@@ -13,7 +13,7 @@
 // stay binary32.
 // The new rows come first, in their own basis; then the accumulators are rotated, and the cache's tiles follow.
 //
-// Bound: vector instructions, softmax and unpacking: 128 tokens of 4 heads over 32k cached ones 137 us (0.5 PFLOP/s), 64 tokens 92 us.
+// Bound: vector instructions, softmax and unpacking: 128 tokens of 4 heads over 32k cached ones 137 to 144 us by the card (0.5 PFLOP/s), 64 tokens 90.
 //
 // Schedule.  A wave's tile is a matrix phase (P V of the tile, K Q of the next) and a vector phase (softmax, its share of a later tile into
 // LDS), about as long as each other.  The two waves of a SIMD take them in turn: waves 4..7 run one phase behind waves 0..3, with a barrier

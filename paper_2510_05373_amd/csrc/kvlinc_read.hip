@@ -6,6 +6,7 @@
 // codes, multiples of 1/2 below 1024, are exact in binary16, two tokens an instruction.  H 1 = sqrt(128) e_0 leaves the zero-point to channel 0.
 // So a number is rounded once in binary32 and once to its type.  Bound: bytes written (256 to 512 a token and tensor against 32 to 64
 // read); rows go through LDS so that a wave stores whole lines.
+// 16 sequences of 8k tokens, 8 heads, 2 bits: binary16 and bfloat16 138 us, rotated 133, binary32 209 (5.5 TB/s), rotated 198; 4 bits 145.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>

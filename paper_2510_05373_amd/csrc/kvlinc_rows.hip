@@ -15,8 +15,8 @@
 // as exact as binary32 products of the scales would be.  Magnitudes that binary16 has no room for take the same products the long way (wide_operands).
 // Zero-points and centring are sums over channels resp. tokens.
 // Bound: vector instructions, some 740 a wave, 16 rows and group of 128 tokens (beside 96 products), two waves a SIMD; and for few pairs the join of
-// their splits, two trips to memory past the caches, 7 to 9 us.  16 sequences of 8k tokens, 8 KV heads of 4: 1 token 26 us, 4 tokens 28 (3.0 TB/s), with
-// the correction 30.5, 4 bits 41; one of 131072: 6 tokens (24 rows, two blocks that both unpack the codes) 51 us.
+// their splits, two trips to memory past the caches, 7 to 9 us.  16 sequences of 8k tokens, 8 KV heads of 4: 1 token 27 us, 4 tokens 28.5 (3.0 TB/s), with
+// the correction 30.5, 4 bits 41; one of 131072: 6 tokens (24 rows, two blocks that both unpack the codes), correction, 51 us.
 // Weights are rounded to binary16 once, for the second product: 2^-12 of each at most, of no common sign.  They are kept near 2^8 (see
 // kvlinc_reference.h), where the smallest that count are normal numbers; sums of weights are taken before the rounding, in binary32.
 #include <hip/hip_runtime.h>

@@ -158,6 +158,7 @@ __device__ __forceinline__ void tile_weights(TileRows& st, int at, int count, bo
   for (int tb = 0; tb < 2; ++tb)
 #pragma unroll
     for (int r = 0; r < 16; ++r) st.s[tb][r] = __builtin_amdgcn_exp2f(fmaf(st.s[tb][r], kLog2eSqrtD, base));
+  // (the sum takes the weights as rounded, in binary32: what all of them are rounded by in common cancels in the quotient)
   const half2_t ones = {(half_t)1.0f, (half_t)1.0f};
 #pragma unroll
   for (int k = 0; k < 4; ++k) {

@@ -1,12 +1,13 @@
 // Windowed decode: one query a sequence over the newest tokens and the first few, read directly from the packed cache.
 //
 // The arithmetic is that of the decode kernel (kvlinc_decode.hip; shared in kvlinc_decode_parts.h): codes go to the matrix cores as FP4, queries
-// and weights as three FP8 terms, zero-points exact (EXACT_OFFSETS), all query heads of a KV head share one pass.  What differs is which groups are walked: those with sinks, then
-// those from the window's first token on, numbered one after the other; tokens of a group at the border that are not seen have their scores
-// taken out.  A sequence is cut into splits of these groups; the four waves of split 0 share the visible part of the fp16 window first.
+// and weights as three FP8 terms, zero-points exact (EXACT_OFFSETS), all query heads of a KV head share one pass.  What differs is which groups are
+// walked: those with sinks, then those from the window's first token on, numbered one after the other; tokens of a group at the border that are not
+// seen have their scores taken out.  A sequence is cut into splits of these groups; the four waves of split 0 share the visible part of the fp16 window first.
 // One launch; the splits are joined by the workgroup that arrives last at the pair's counter.
-// Bound: bytes of the visible groups (64 sequences, window 4096, 2 bits: 29.6 us, 5.3 TB/s; 32 of 7 heads, window 8192, 4 bits: 33 us, 4.5 TB/s);
-// small windows: latency, a chain of counters, record, combine (and arrival, join): one sequence, window 1024: 7.6 us.
+// Bound: bytes of the visible groups (64 sequences, window 4096, 2 bits: 29.4 us, 5.4 TB/s; 32 of 7 heads, window 8192, 4 bits: 32.8 us, 4.6 TB/s;
+// with sliding values 1.9 and 3.5 us more); small windows: latency, a chain of counters, record, combine (and arrival, join): one sequence, window 1024:
+// 7.3 us, 7.6 with the host's calls.
 #include <hip/hip_runtime.h>
 
 #include "kvlinc_decode_parts.h"
