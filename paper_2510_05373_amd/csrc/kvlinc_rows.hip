@@ -69,7 +69,10 @@ template <int BITS>
 __device__ __forceinline__ GroupMagnitudes put_meta(const Record<BITS>& r, u32x4_t* meta, int lane) {
   // scales are not negative: their bit patterns order like the numbers
   typedef uint16_t ushort2_t __attribute__((ext_vector_type(2)));
-  const auto halves = [&](int i) { return __builtin_bit_cast(ushort2_t, r.meta[i]); };
+  const auto halves = [&](int i) {
+    const uint32_t w = r.meta[i];  // (a bit cast of r.meta[i] itself would take r.meta[0]: it goes by the address of the vector)
+    return __builtin_bit_cast(ushort2_t, w);
+  };
   const uint32_t both = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_elementwise_max(halves(0), halves(1)), __builtin_elementwise_max(halves(2), halves(3))));
   uint32_t top = lane >= 32 ? both & 0xffffu : max(both & 0xffffu, both >> 16);  // (lanes 0..15: key scales; 32..63: value scales)
   top = max(top, dpp_u<kRowRor1>(top));
