@@ -1,6 +1,7 @@
-"""ctypes binding of libkvlinc.so.  Same names and argument order as include/kvlinc.h and include/kvlinc_context.h."""
+"""ctypes binding of libkvlinc.so.  Same names and argument order as include/kvlinc.h, include/kvlinc_context.h and include/kvlinc_bounded.h."""
 import contextlib
 import ctypes
+import math
 import os
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -33,6 +34,17 @@ class CacheStruct(ctypes.Structure):
         ("status", ctypes.c_void_p), ("split_done", ctypes.c_void_p),
         ("flags", ctypes.c_int32),
     ]
+
+
+class RotationStruct(ctypes.Structure):
+    """Mirror of struct kvlinc_rotation."""
+    _fields_ = [("channels", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("magnitude", ctypes.c_float), ("freq", ctypes.c_void_p)]
+
+
+class RowsStruct(ctypes.Structure):
+    """Mirror of struct kvlinc_rows."""
+    _fields_ = [("in_", ctypes.c_void_p), ("out", ctypes.c_void_p), ("sequence_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+                ("token_stride", ctypes.c_int64)]
 
 
 def _load():
@@ -76,6 +88,21 @@ def _load():
     L.kvlinc_decode_attention_windowed.argtypes = [P, ptr, i32, i32, ptr, ptr, ctypes.c_size_t, i32, ptr]
     L.kvlinc_cache_read.restype = ctypes.c_int
     L.kvlinc_cache_read.argtypes = [P, ptr, i32, ptr, ptr, i32, i32, ptr]
+    f32, size, rows = ctypes.c_float, ctypes.c_size_t, ctypes.POINTER(RowsStruct)
+    L.kvlinc_rotary.restype = ctypes.c_int
+    L.kvlinc_rotary.argtypes = [P, ctypes.POINTER(RotationStruct), rows, rows, rows, i32, ptr, ptr, ptr, i32, i32, i32, ptr]
+    L.kvlinc_decode_mass_workspace_bytes.restype = size
+    L.kvlinc_decode_mass_workspace_bytes.argtypes = [P, i32]
+    L.kvlinc_decode_attention_mass.restype = ctypes.c_int
+    L.kvlinc_decode_attention_mass.argtypes = [P, ptr, ptr, ptr, f32, ptr, ptr, size, i32, ptr]
+    L.kvlinc_attention_mass_workspace_bytes.restype = size
+    L.kvlinc_attention_mass_workspace_bytes.argtypes = [P, i32, i32]
+    L.kvlinc_attention_mass.restype = ctypes.c_int
+    L.kvlinc_attention_mass.argtypes = [P, ptr, ptr, i32, ptr, f32, ptr, ptr, size, i32, ptr]
+    L.kvlinc_cache_evict_workspace_bytes.restype = size
+    L.kvlinc_cache_evict_workspace_bytes.argtypes = [P]
+    L.kvlinc_cache_evict.restype = ctypes.c_int
+    L.kvlinc_cache_evict.argtypes = [P, P, ptr, ptr, i32, i32, i32, i32, ptr, ptr, ptr, ptr, size, ptr]
     return L
 
 
@@ -185,6 +212,93 @@ def kvlinc_cache_read(cache, first, T, k_out, v_out, dtype=KVLINC_F16, rotated=0
     """k_out, v_out: [B, H_kv, T, 128] device tensors of the type dtype (KVLINC_F16, ...), either may be None; first: [B] int32 or None."""
     return lib.kvlinc_cache_read(ctypes.byref(_struct(cache)), _ptr(first), int(T), _ptr(k_out), _ptr(v_out), int(dtype), int(rotated),
                                  _stream(stream))
+
+
+def kvlinc_rotary(cache, rotation, q, k, v, T, n_new=None, first=None, depth=None, counted=1, dtype_in=KVLINC_F16, dtype_out=KVLINC_F16, stream=None):
+    """rotation: RotationStruct; q, k, v: RowsStruct or None; n_new, first: [B], depth: [B, T] int32 device tensors or None."""
+    return lib.kvlinc_rotary(_struct(cache), rotation, q, k, v, int(T), _ptr(n_new), _ptr(first), _ptr(depth), int(counted), int(dtype_in), int(dtype_out),
+                             _stream(stream))
+
+
+def kvlinc_decode_mass_workspace_bytes(cache, max_context=0):
+    return lib.kvlinc_decode_mass_workspace_bytes(ctypes.byref(_struct(cache)), int(max_context))
+
+
+def kvlinc_decode_attention_mass(cache, q, out, mass, decay, mass_out, workspace, workspace_bytes=None, max_context=0, stream=None):
+    """q, out: [B, H_q, 128] fp16; mass, mass_out: [B, H_kv, max_groups + 1] fp32; device tensors (contiguous), mass may be None."""
+    return lib.kvlinc_decode_attention_mass(ctypes.byref(_struct(cache)), _ptr(q), _ptr(out), _ptr(mass), float(decay), _ptr(mass_out), _ptr(workspace),
+                                            _bytes_of(workspace, workspace_bytes), int(max_context), _stream(stream))
+
+
+def kvlinc_attention_mass_workspace_bytes(cache, T, max_context=0):
+    return lib.kvlinc_attention_mass_workspace_bytes(ctypes.byref(_struct(cache)), int(T), int(max_context))
+
+
+def kvlinc_attention_mass(cache, q, n_rows, T, mass, decay, mass_out, workspace, workspace_bytes=None, max_context=0, stream=None):
+    """q: [B, H_q, T, 128] fp16; n_rows: [B] int32 or None; mass, mass_out: [B, H_kv, max_groups + 1] fp32; device tensors (contiguous), mass may be None."""
+    return lib.kvlinc_attention_mass(ctypes.byref(_struct(cache)), _ptr(q), _ptr(n_rows), int(T), _ptr(mass), float(decay), _ptr(mass_out), _ptr(workspace),
+                                     _bytes_of(workspace, workspace_bytes), int(max_context), _stream(stream))
+
+
+def kvlinc_cache_evict_workspace_bytes(cache):
+    return lib.kvlinc_cache_evict_workspace_bytes(ctypes.byref(_struct(cache)))
+
+
+def kvlinc_cache_evict(cache, to, mass, mass_out, keep, limit, first, last, offset, offset_out, kept, workspace, workspace_bytes=None, stream=None):
+    """mass: [B, H_kv, max_groups + 1] fp32, mass_out the same of `to`; offset, offset_out: [B] int32 or None; kept: [B, H_kv, max_groups of `to`] int32 or None."""
+    return lib.kvlinc_cache_evict(ctypes.byref(_struct(cache)), ctypes.byref(_struct(to)), _ptr(mass), _ptr(mass_out), int(keep), int(limit), int(first),
+                                  int(last), _ptr(offset), _ptr(offset_out), _ptr(kept), _ptr(workspace), _bytes_of(workspace, workspace_bytes),
+                                  _stream(stream))
+
+
+def rotary_frequencies(channels=128, base=10000.0, scaling=None, factor=1.0, original=0, low=1.0, high=32.0):
+    """Angles per position of the channels / 2 pairs, base^(-2 i / channels), for KVLincRotary; for contexts `factor` times as long as those of `original`
+    tokens that a model has learnt, scaled
+      "linear"  all divided by the factor: positions in between;
+      "base"    the base times factor^(channels / (channels - 2)): the last pair divided by it, the first left as it is;
+      "parts"   pairs that turn more than `high` times in `original` tokens left as they are, those below `low` divided by the factor, a ramp between
+                (used with a magnitude of 0.1 ln(factor) + 1, or of 1)."""
+    if channels < 2 or channels > 128 or channels % 2:
+        raise KVLincError("channels has to be even, 2 .. 128, not %s" % channels)
+    if not base > 0.0 or not factor > 0.0:
+        raise KVLincError("base and factor have to be above 0, not %s and %s" % (base, factor))
+    if scaling not in (None, "linear", "base", "parts"):
+        raise KVLincError("scaling has to be None, 'linear', 'base' or 'parts', not %r" % (scaling,))
+    if scaling == "base" and channels > 2:
+        base = base * factor ** (channels / (channels - 2.0))
+    freq = [base ** (-2.0 * i / channels) for i in range(channels // 2)]
+    if scaling == "linear":
+        freq = [f / factor for f in freq]
+    elif scaling == "parts":
+        if not original > 0 or not high > low:
+            raise KVLincError("scaling by parts needs original > 0 and high > low, not %s, %s and %s" % (original, high, low))
+        kept = [min(1.0, max(0.0, (original * f / (2.0 * math.pi) - low) / (high - low))) for f in freq]
+        freq = [k * f + (1.0 - k) * f / factor for k, f in zip(kept, freq)]
+    return freq
+
+
+class KVLincRotary:
+    """Rotary positions as KVLincCache.rotary takes them: the angle per position of every pair, on the device.
+
+    freq: channels / 2 numbers (rotary_frequencies, or a model's own); interleaved: pairs are channels 2 i and 2 i + 1, else i and i + channels / 2;
+    magnitude: what the rotated channels are multiplied with."""
+
+    def __init__(self, freq, interleaved=False, magnitude=1.0, device="cuda"):
+        import torch
+        self.freq = torch.as_tensor(freq, dtype=torch.float64).to(device).contiguous()
+        self.channels = 2 * self.freq.numel()
+        if self.freq.dim() != 1 or not 2 <= self.channels <= 128:
+            raise KVLincError("freq has to be 1 to 64 numbers, not a tensor of shape %s" % (tuple(self.freq.shape),))
+        if not math.isfinite(magnitude):
+            raise KVLincError("magnitude has to be finite, not %s" % magnitude)
+        self.interleaved, self.magnitude = bool(interleaved), float(magnitude)
+        self.struct = RotationStruct(channels=self.channels, interleaved=int(self.interleaved), magnitude=self.magnitude, freq=self.freq.data_ptr())
+
+    def inverse(self):
+        """The rotation back."""
+        if self.magnitude == 0.0:
+            raise KVLincError("a magnitude of 0 has no inverse")
+        return KVLincRotary(-self.freq, self.interleaved, 1.0 / self.magnitude, self.freq.device)
 
 
 _NOTHING = contextlib.nullcontext()
@@ -413,3 +527,161 @@ class KVLincCache:
         if rc != KVLINC_OK:
             raise KVLincError("kvlinc_cache_read: " + kvlinc_strerror(rc))
         return k_out, v_out
+
+    # ---- long generation in a cache of bounded size (kvlinc_bounded.h) ----
+
+    def rotary(self, plan, q=None, k=None, v=None, n_new=None, first=None, depth=None, counted=True, q_out=None, k_out=None, v_out=None, dtype=None,
+               stream=None):
+        """Queries and keys of T new tokens of every sequence rotated to their positions, values taken along: (q_out, k_out, v_out), [B, heads, T, 128],
+        contiguous, in `dtype` (fp16), as append, prompt_attention and, at T = 1, the decode calls take them.
+
+        plan: KVLincRotary; q: [B, H_q, T, 128], k, v: [B, H_kv, T, 128], any of the three, fp16, bf16 or fp32, of any strides that are multiples of 16
+        bytes with contiguous rows (a projection's output [B, T, heads, 128] transposed, say).  n_new: [B] int32 or None (all T); rows beyond it
+        are left as they are (zero in outputs made here).  Row i is at position first[b] + depth[b, i] (None: 0; i) and, if counted, the tokens in
+        the cache."""
+        import torch
+        types = {torch.float16: KVLINC_F16, torch.bfloat16: KVLINC_BF16, torch.float32: KVLINC_F32}
+        if not isinstance(plan, KVLincRotary):
+            raise KVLincError("plan has to be a KVLincRotary")
+        if plan.freq.device != self._device:
+            raise KVLincError("the plan is on %s, the cache on %s" % (plan.freq.device, self._device))
+        heads, given = (self.H_q, self.H_kv, self.H_kv), (q, k, v)
+        some = next((t for t in given if t is not None), None)
+        if not torch.is_tensor(some) or some.dim() != 4 or some.dtype not in types:
+            raise KVLincError("q, k or v is needed, a tensor of shape [B, heads, T, 128] and type %s" % ", ".join(str(t) for t in types))
+        T = some.shape[2]
+        if T < 1:
+            raise KVLincError("there are no rows")
+        outs = [q_out, k_out, v_out]
+        if dtype is None:
+            dtype = next((t.dtype for t in outs if torch.is_tensor(t)), torch.float16)
+        if dtype not in types:
+            raise KVLincError("dtype has to be one of %s" % ", ".join(str(t) for t in types))
+        for t, out, h, name in zip(given, outs, heads, "qkv"):
+            shape = (self.B, h, T, 128)
+            if t is None:
+                if out is not None:
+                    raise KVLincError("%s_out without %s" % (name, name))
+                continue
+            if not torch.is_tensor(t) or t.dtype != some.dtype or t.shape != shape:
+                raise KVLincError("%s has to be a %s tensor of shape %s" % (name, some.dtype, shape))
+            if t.device != self._device:
+                raise KVLincError("%s is on %s, the cache on %s" % (name, t.device, self._device))
+            if t.stride(3) != 1:
+                raise KVLincError("the rows of %s have to be contiguous" % name)
+            if out is not None:
+                self._tensor(out, name + "_out", shape, dtype)
+        for t, name, shape in ((n_new, "n_new", (self.B,)), (first, "first", (self.B,)), (depth, "depth", (self.B, T))):
+            if t is not None:
+                self._tensor(t, name, shape, torch.int32)
+        with self._on(stream, plan.freq, n_new, first, depth, *given, *outs):
+            make = torch.empty if n_new is None else torch.zeros
+            rows = [None, None, None]
+            for i, (t, h) in enumerate(zip(given, heads)):
+                if t is not None:
+                    if outs[i] is None:
+                        outs[i] = make((self.B, h, T, 128), dtype=dtype, device=self._device)
+                    strides = (s if n > 1 else 0 for s, n in zip(t.stride(), t.shape[:3]))
+                    rows[i] = RowsStruct(t.data_ptr(), outs[i].data_ptr(), *strides)
+            rc = kvlinc_rotary(self, plan.struct, *rows, T, n_new, first, depth, bool(counted), types[some.dtype], types[dtype], stream)
+        if rc != KVLINC_OK:
+            raise KVLincError("kvlinc_rotary: " + kvlinc_strerror(rc))
+        return tuple(outs)
+
+    def new_mass(self):
+        """Accumulated attention weight of the groups, and of the window behind the last: zeros, [B, H_kv, max_groups + 1] fp32."""
+        import torch
+        return torch.zeros(self.B, self.H_kv, self.max_groups + 1, dtype=torch.float32, device=self._device)
+
+    def _mass_tensors(self, mass, mass_out, decay):
+        import torch
+        shape = (self.B, self.H_kv, self.max_groups + 1)
+        for t, name in ((mass, "mass"), (mass_out, "mass_out")):
+            if t is not None:
+                self._tensor(t, name, shape, torch.float32)
+        if not 0.0 <= decay <= 1.0:
+            raise KVLincError("decay has to be 0 to 1, not %s" % decay)
+
+    def decode_mass(self, q, mass, decay=1.0, mass_out=None, out=None, max_context=0, stream=None):
+        """One decode step over the whole cache that also accumulates the attention weight of every group: mass_out = decay mass + the weights of this
+        query (mass_out None: in mass itself; mass None: zeros).  q: [B, H_q, 128] fp16.  Returns out."""
+        import torch
+        half = torch.float16
+        self._limits(0, 0, max_context)
+        self._tensor(q, "q", (self.B, self.H_q, 128), half)
+        if mass_out is None:
+            mass_out = mass
+        if mass_out is None:
+            raise KVLincError("mass or mass_out is needed")
+        self._mass_tensors(mass, mass_out, decay)
+        if out is not None:
+            self._tensor(out, "out", q.shape, half)
+        with self._on(stream, q, out, mass, mass_out):
+            if out is None:
+                out = torch.empty_like(q)
+            rc = self._with_scratch(lambda ws, s: kvlinc_decode_attention_mass(self, q, out, mass, decay, mass_out, ws, None, max_context, s),
+                                    lambda: kvlinc_decode_mass_workspace_bytes(self, max_context))
+        if rc != KVLINC_OK:
+            raise KVLincError("kvlinc_decode_attention_mass: " + kvlinc_strerror(rc))
+        return out
+
+    def attention_mass(self, q, mass=None, n_rows=None, decay=1.0, mass_out=None, max_context=0, stream=None):
+        """The attention weight that the groups receive from T query rows of every sequence, its newest tokens, which the cache already holds: mass_out =
+        decay mass + their weights (mass_out None: in mass itself, or a new one; mass None: zeros).  q: [B, H_q, T, 128] fp16; n_rows: [B] int32 or None
+        (all T).  max_context: the most tokens that any sequence holds (0: whatever the cache has room for); one that holds more adds
+        nothing, and KVLINC_ST_BOUND is set in `status`.  Returns mass_out."""
+        import torch
+        if not torch.is_tensor(q) or q.dim() != 4:
+            raise KVLincError("q has to be a tensor of shape [B, H_q, T, 128]")
+        T = q.shape[2]
+        self._limits(0, 0, max_context)
+        if T < 1:
+            raise KVLincError("q has no rows")
+        self._tensor(q, "q", (self.B, self.H_q, T, 128), torch.float16)
+        if n_rows is not None:
+            self._tensor(n_rows, "n_rows", (self.B,), torch.int32)
+        if mass_out is None:
+            mass_out = mass
+        self._mass_tensors(mass, mass_out, decay)
+        with self._on(stream, q, n_rows, mass, mass_out):
+            if mass_out is None:
+                mass_out = self.new_mass()
+            rc = self._with_scratch(lambda ws, s: kvlinc_attention_mass(self, q, n_rows, T, mass, decay, mass_out, ws, None, max_context, s),
+                                    lambda: kvlinc_attention_mass_workspace_bytes(self, T, max_context))
+        if rc != KVLINC_OK:
+            raise KVLincError("kvlinc_attention_mass: " + kvlinc_strerror(rc))
+        return mass_out
+
+    def evict(self, mass, keep, limit=None, first=1, last=1, to=None, mass_out=None, offset=None, offset_out=None, kept=None, stream=None):
+        """Sequences of more than `limit` groups (None: keep) cut to `keep` of them, of each KV head the first, the newest `last` and those with the largest
+        mass: in place, or into the cache `to`.  mass: [B, H_kv, max_groups + 1] fp32, as decode_mass and attention_mass leave it; mass_out: where that
+        of what is kept goes, in the shape of `to` (None: in mass itself, in place only).  offset, offset_out: [B] int32 or None, tokens dropped so
+        far (offset_out None: in offset itself), what rotary takes as `first`.  kept: [B, H_kv, max_groups of `to`] int32 or None, the slots that the
+        groups had.  Returns the cache."""
+        import torch
+        if to is None:
+            to = self
+        if not isinstance(to, KVLincCache):
+            raise KVLincError("to has to be a KVLincCache")
+        if to._device != self._device:
+            raise KVLincError("to is on %s, the cache on %s" % (to._device, self._device))
+        limit = keep if limit is None else limit
+        for x, name in ((keep, "keep"), (limit, "limit"), (first, "first"), (last, "last")):
+            if not 0 <= x < 1 << 31:
+                raise KVLincError("%s has to be 0 or more, below 2^31, not %s" % (name, x))
+        if mass_out is None and to is self:
+            mass_out = mass
+        if offset_out is None:
+            offset_out = offset
+        self._tensor(mass, "mass", (self.B, self.H_kv, self.max_groups + 1), torch.float32)
+        to._tensor(mass_out, "mass_out", (to.B, to.H_kv, to.max_groups + 1), torch.float32)
+        for t, name, shape in ((offset, "offset", (self.B,)), (offset_out, "offset_out", (self.B,)), (kept, "kept", (to.B, to.H_kv, to.max_groups))):
+            if t is not None:
+                self._tensor(t, name, shape, torch.int32)
+        theirs = () if to is self else (to.groups, to.k_res, to.v_res, to.n_quant, to.n_res)
+        with self._on(stream, mass, mass_out, offset, offset_out, kept, *theirs):
+            rc = self._with_scratch(lambda ws, s: kvlinc_cache_evict(self, to, mass, mass_out, keep, limit, first, last, offset, offset_out, kept, ws, None, s),
+                                    lambda: kvlinc_cache_evict_workspace_bytes(self))
+        if rc != KVLINC_OK:
+            raise KVLincError("kvlinc_cache_evict: " + kvlinc_strerror(rc))
+        return to

@@ -29,12 +29,18 @@ OBJECTS = {
     "kvlinc_dense": ("kvlinc_dense.hip", []),
     "kvlinc_prompt_correction": ("kvlinc_prompt_correction.hip", []),
     "kvlinc_read": ("kvlinc_read.hip", []),
+    "kvlinc_bounded_api": ("kvlinc_bounded_api.hip", []),
+    "kvlinc_rotary": ("kvlinc_rotary.hip", []),
+    "kvlinc_decode_mass": ("kvlinc_decode_mass.hip", []),
+    "kvlinc_attention_mass": ("kvlinc_attention_mass.hip", []),
+    "kvlinc_evict": ("kvlinc_evict.hip", []),
     "kvlinc_decode_nolooks": ("kvlinc_decode.hip", ["-DKVLINC_LOOKS=0"]),
 }
 CONTEXT = ["kvlinc_context_api", "kvlinc_rows", "kvlinc_windowed", "kvlinc_prompt", "kvlinc_dense", "kvlinc_prompt_correction", "kvlinc_read"]
+BOUNDED = ["kvlinc_bounded_api", "kvlinc_rotary", "kvlinc_decode_mass", "kvlinc_attention_mass", "kvlinc_evict"]
 LIBRARIES = {
-    LIB_PATH: ["kvlinc_api", "kvlinc_append", "kvlinc_decode", *CONTEXT],
-    NOLOOKS_PATH: ["kvlinc_api", "kvlinc_append", "kvlinc_decode_nolooks", *CONTEXT],
+    LIB_PATH: ["kvlinc_api", "kvlinc_append", "kvlinc_decode", *CONTEXT, *BOUNDED],
+    NOLOOKS_PATH: ["kvlinc_api", "kvlinc_append", "kvlinc_decode_nolooks", *CONTEXT, *BOUNDED],
 }
 PROBE_SOURCE = "kvlinc_readprobe.hip"
 

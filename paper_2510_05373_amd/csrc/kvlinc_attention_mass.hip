@@ -1,0 +1,334 @@
+// What query rows add to the accumulated attention weight of the groups, without their output rows.
+//
+// Three launches.  scores_kernel leaves, for every row and slot (a group, or the window), log2 of the row's sum of weights over the slot's tokens;
+// rows_kernel makes of them the same over all tokens that the row sees; and columns_kernel sums 2^(the first - the second) over the rows of a slot.
+// So the weights are formed once, groups do not wait for one another, and what goes through memory is 4 bytes a row and group.
+//
+// scores_kernel.  S^T = K Q^T on v_mfma_f32_16x16x32_f16, operands and exactness as in kvlinc_rows.hip.  A wave unpacks a group's key tile into
+// 128 registers, and goes over blocks of 16 rows with it: query times key scales in two terms, 64 products, 32 exponentials a lane.  A column's
+// reference is one that an earlier group has left, as long as the sums it gives stay below 2^14; only where they do not, the largest score is looked
+// for and the weights are formed again: what a row's larger weights leave of a slot below 2^-126 of them is nothing.
+#include <hip/hip_runtime.h>
+
+#include "kvlinc_bounded_internal.h"
+#include "kvlinc_row_parts.h"
+
+namespace kvlinc {
+namespace {
+
+constexpr int kScoreWaves = 4, kMostBlocks = 8;           // blocks of 16 rows of a workgroup
+constexpr int kQueryStride = kHeadDim + 8;                // halves of a row in LDS
+constexpr float kMostSum = 0x1p14f;
+
+// Rows and tokens of a sequence.
+struct Place {
+  Lengths len;
+  int rows, T;  // rows of a KV head, rows of a query head
+  __device__ __forceinline__ int position(int row, int gq) const { return len.total() - T + row / gq; }
+};
+__device__ __forceinline__ Place place_of(const MassCall& a, int b) {
+  const Lengths len = lengths_of(a.cache, b);
+  const int T = a.n_rows != nullptr ? min(max(a.n_rows[b], 0), a.T) : a.T;
+  const bool fits = len.groups() < a.slots;
+  return Place{len, fits ? T * a.gq : 0, T};
+}
+
+template <int BITS>
+struct KeyPart {
+  u32x4_t kw[2 * BITS];
+  u32x4_t meta;  // lanes 0..31: scales, zero-points
+};
+template <int BITS>
+__device__ __forceinline__ void load_keys_of(KeyPart<BITS>& r, const uint32_t* rec, int lane) {
+  const u32x4_t* kt = reinterpret_cast<const u32x4_t*>(rec + Rec<BITS>::kKeyTile) + token_order(lane & 15) + (lane & 48);
+#pragma unroll
+  for (int m = 0; m < 2 * BITS; ++m) r.kw[m] = kt[64 * m];
+  r.meta = reinterpret_cast<const u32x4_t*>(rec + Rec<BITS>::kKeyScale)[lane & 31];
+}
+
+// Scores of a tile of 128 tokens (operands A) become the columns' sums of weights.  hide(n, r): the token of x[n][r] is not seen.
+struct Column {
+  float m;  // reference; -inf: nothing seen yet
+};
+template <bool TWO, typename H>
+__device__ __forceinline__ float tile_sum(Column& col, const half8_t (&A)[8][4], const half8_t (&hi)[4], const half8_t (&lo)[4], float unit, float bias, bool masked, H hide) {
+  float4_t x[8];
+#pragma unroll
+  for (int n = 0; n < 8; ++n) x[n] = float4_t{0.f, 0.f, 0.f, 0.f};
+  if constexpr (TWO) {
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+#pragma unroll
+      for (int n = 0; n < 8; ++n) x[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(A[n][s], lo[s], x[n], 0, 0, 0);
+  }
+#pragma unroll
+  for (int s = 0; s < 4; ++s)
+#pragma unroll
+    for (int n = 0; n < 8; ++n) x[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(A[n][s], hi[s], x[n], 0, 0, 0);
+  if (masked) {
+#pragma unroll
+    for (int n = 0; n < 8; ++n)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) x[n][r] = hide(n, r) ? -INFINITY : x[n][r];
+  }
+  float l = 0.0f;
+  {
+    const float base = bias - col.m;
+#pragma unroll
+    for (int n = 0; n < 8; ++n)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) l += __builtin_amdgcn_exp2f(fmaf(x[n][r], unit, base));
+  }
+  if (__builtin_amdgcn_ballot_w64(!(l <= kMostSum) || fmaxf(fabsf(bias), fabsf(col.m)) > kFusedBound) != 0) {
+    float mx = -INFINITY;
+#pragma unroll
+    for (int n = 0; n < 8; ++n)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        x[n][r] = fmaf(x[n][r], unit, bias);
+        mx = fmaxf(mx, x[n][r]);
+      }
+    float a, b;
+    pair_across<16>(mx, a, b);
+    pair_across<32>(fmaxf(a, b), a, b);
+    col.m = raised(fmaxf(a, b), col.m);
+    const float m = finite_reference(col.m);
+    l = 0.0f;
+#pragma unroll
+    for (int n = 0; n < 8; ++n)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) l += __builtin_amdgcn_exp2f(x[n][r] - m);
+  }
+  float a, b;
+  pair_across<16>(l, a, b);
+  pair_across<32>(a + b, a, b);
+  return a + b;
+}
+
+// Grid, one-dimensional: pairs fastest, then runs of kScoreWaves splits of the slots, then sets of a.blocks blocks of rows.
+template <int BITS>
+__global__ __launch_bounds__(64 * kScoreWaves, 2) void scores_kernel(MassCall a, int blocks, int runs) {
+  __shared__ __align__(16) half_t sQuery[kMostBlocks * 16][kQueryStride];
+  __shared__ __align__(16) u32x4_t sMeta[kScoreWaves][32];
+  __shared__ float sUnit[kMostBlocks * 16], sRef[kScoreWaves][kMostBlocks * 16];
+  __shared__ int sPosition[kMostBlocks * 16], sLossy[kMostBlocks];
+  const kvlinc_cache& c = a.cache;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), j = lane & 15, g = lane >> 4;
+  const int pairs = c.B * c.H_kv, unit_id = blockIdx.x / pairs, bh = blockIdx.x - unit_id * pairs, set = unit_id / runs, split = (unit_id - set * runs) * kScoreWaves + wave;
+  const int b = bh / c.H_kv, gq = a.gq, row0 = 16 * blocks * set;
+  const Place at = place_of(a, b);
+  if (row0 >= at.rows) return;
+  const int G = at.len.groups(), splits = runs * kScoreWaves, n_blocks = min(blocks, (at.rows - row0 + 15) / 16);
+  const long long head0 = (long long)bh * gq;
+  auto query_of = [&](int row) {  // (rows beyond the last take its query)
+    const RowPlace p = row_place(min(row, at.rows - 1), gq);
+    return a.q + ((head0 + p.h) * a.T + p.i) * kHeadDim;
+  };
+
+  // ---- the rows to LDS, as load_query of kvlinc_row_parts.h has them ----
+  if (tid < kMostBlocks) sLossy[tid] = 0;
+  __syncthreads();
+  for (int row = tid >> 4; row < 16 * n_blocks; row += 4 * kScoreWaves) {
+    const u32x4_t raw = reinterpret_cast<const u32x4_t*>(query_of(row0 + row))[lane & 15];
+    uint32_t mx = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) mx = max(mx, max(raw[i] & 0x7fffu, (raw[i] >> 16) & 0x7fffu));
+    mx = max(mx, dpp_u<kRowRor1>(mx));
+    mx = max(mx, dpp_u<kRowRor2>(mx));
+    mx = max(mx, dpp_u<kRowRor4>(mx));
+    mx = max(mx, dpp_u<kRowRor8>(mx));
+    const QueryScale by = query_scale(mx);
+    u32x4_t scaled;
+    uint32_t lost = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      scaled[i] = as_u32(as_h2(raw[i]) * by.by);
+      lost |= as_u32(as_h2(scaled[i]) * by.back) ^ raw[i];
+    }
+    *reinterpret_cast<u32x4_t*>(&sQuery[row][8 * (lane & 15)]) = scaled;
+    if (lost != 0) sLossy[row / 16] = 1;
+    if ((lane & 15) == 0) {
+      sUnit[row] = by.unit;
+      sPosition[row] = at.position(min(row0 + row, at.rows - 1), gq);
+    }
+  }
+  for (int k = 0; k < n_blocks; ++k) sRef[wave][16 * k + j] = -INFINITY;
+  __syncthreads();
+
+  float* lse = a.lse + bh * a.slots * a.rows + row0;
+  const uint32_t* rec0 = c.groups + (long long)bh * c.max_groups * Rec<BITS>::kWords;
+  // (a block of rows goes over a slot whose first token its last row sees)
+  auto last_position = [&](int k) { return __builtin_amdgcn_readfirstlane(sPosition[16 * k + 15]); };
+  auto leave = [&](int slot, int k, const Column& col, float sum) __attribute__((always_inline)) {
+    sRef[wave][16 * k + j] = col.m;  // (the same in the four lanes of a column: each reads what it has written)
+    if (g == 0) lse[(long long)slot * a.rows + 16 * k + j] = finite_reference(col.m) + __builtin_amdgcn_logf(sum);
+  };
+  const int newest = last_position(n_blocks - 1);
+  KeyPart<BITS> rec;
+  int slot = split;
+  if (slot < G) load_keys_of<BITS>(rec, rec0 + (long long)slot * Rec<BITS>::kWords, lane);
+  for (; slot < G && slot * kGroup <= newest; slot += splits) {
+    const int first = slot * kGroup, count = min(at.len.nq - first, kGroup);
+    if (lane < 32) sMeta[wave][lane] = rec.meta;
+    wave_order();
+    // scales are not negative: their bit patterns order like the numbers
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) top = max(top, max(rec.meta[i] & 0xffffu, rec.meta[i] >> 16));
+    top = max(top, dpp_u<kRowRor1>(top));
+    top = max(top, dpp_u<kRowRor2>(top));
+    top = max(top, dpp_u<kRowRor4>(top));
+    top = max(top, dpp_u<kRowRor8>(top));
+    const uint32_t key_scale = (uint32_t)__builtin_amdgcn_readlane(top, 0);  // (lanes 0..15 have the scales)
+    half8_t A[8][4];
+#pragma unroll
+    for (int n = 0; n < 8; ++n) key_operands<BITS>(rec.kw, n, A[n]);
+    const int next = slot + splits < G ? slot + splits : slot;
+    load_keys_of<BITS>(rec, rec0 + (long long)next * Rec<BITS>::kWords, lane);
+    for (int k = 0; k < n_blocks; ++k) {
+      if (first > last_position(k)) continue;
+      const int row = row0 + 16 * k + j;
+      half8_t q[4], hi[4], lo[4];
+#pragma unroll
+      for (int s = 0; s < 4; ++s) q[s] = *reinterpret_cast<const half8_t*>(&sQuery[16 * k + j][32 * g + 8 * s]);
+      float bias, unit;
+      row_operands<BITS>(q, sUnit[16 * k + j], sLossy[k] != 0, [&]() __attribute__((always_inline)) { return query_of(row) + 32 * g; }, &sMeta[wave][0], key_scale, lane, hi, lo, bias, unit);
+      Column col = {sRef[wave][16 * k + j]};
+      const bool masked = count < kGroup || first + kGroup - 1 > __builtin_amdgcn_readfirstlane(sPosition[16 * k]);
+      const int end = min(count, sPosition[16 * k + j] - first + 1);
+      const float sum = tile_sum<true>(col, A, hi, lo, unit, bias, masked, [&](int n, int r) { return 16 * n + token_order(4 * g + r) >= end; });
+      leave(slot, k, col, sum);
+    }
+    wave_order();
+  }
+  // ---- the window, by the wave whose turn it is ----
+  if (at.len.nr > 0 && G % splits == split && at.len.nq <= newest) {
+    const half_t* keys = reinterpret_cast<const half_t*>(c.k_res) + (long long)bh * c.R * kHeadDim;
+    half8_t A[8][4];
+#pragma unroll
+    for (int n = 0; n < 8; ++n) {
+      const half_t* row = keys + (long long)min(16 * n + token_order(j), at.len.nr - 1) * kHeadDim + 32 * g;
+#pragma unroll
+      for (int s = 0; s < 4; ++s) A[n][s] = as_h8(reinterpret_cast<const u32x4_t*>(row)[s]);
+    }
+    for (int k = 0; k < n_blocks; ++k) {
+      if (at.len.nq > last_position(k)) continue;
+      const int row = row0 + 16 * k + j;
+      half8_t q[4];
+      float unit = sUnit[16 * k + j];
+#pragma unroll
+      for (int s = 0; s < 4; ++s) q[s] = *reinterpret_cast<const half8_t*>(&sQuery[16 * k + j][32 * g + 8 * s]);
+      if (sLossy[k] != 0) {
+        const u32x4_t* src = reinterpret_cast<const u32x4_t*>(query_of(row) + 32 * g);
+#pragma unroll
+        for (int s = 0; s < 4; ++s) q[s] = as_h8(src[s]);
+        unit = kLog2eSqrtD;
+      }
+      Column col = {sRef[wave][16 * k + j]};
+      const int end = min(at.len.nr, sPosition[16 * k + j] - at.len.nq + 1);
+      const float sum = tile_sum<false>(col, A, q, q, unit, 0.0f, true, [&](int n, int r) { return 16 * n + token_order(4 * g + r) >= end; });
+      leave(G, k, col, sum);
+    }
+  }
+}
+
+// Slots whose first token a row at position p sees: groups 0 .. n - 1, and the window.
+struct Seen {
+  int groups;
+  bool window;
+};
+__device__ __forceinline__ Seen seen_by(const Lengths& len, int p) { return Seen{p < 0 ? 0 : min(p / kGroup + 1, len.groups()), len.nr > 0 && p >= len.nq}; }
+
+// log2 of a row's sum over all it sees.  Grid: pairs by runs of 64 rows, pairs fastest; a lane a row, the slots shared by the waves.
+constexpr int kRowWaves = 16;
+__global__ __launch_bounds__(64 * kRowWaves) void rows_kernel(MassCall a) {
+  __shared__ float sM[kRowWaves][64], sL[kRowWaves][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, pairs = a.cache.B * a.cache.H_kv, run = blockIdx.x / pairs, bh = blockIdx.x - run * pairs;
+  const int row = 64 * run + lane;
+  const Place at = place_of(a, bh / a.cache.H_kv);
+  if (64 * run >= at.rows) return;
+  const Seen see = seen_by(at.len, row < at.rows ? at.position(row, a.gq) : -1);
+  const int G = at.len.groups(), slots = see.groups;
+  const float* lse = a.lse + bh * a.slots * a.rows + min(row, at.rows - 1);
+  // two passes, the second from the caches: the largest first
+  constexpr int kAhead = 8;
+  float m = -INFINITY;
+  for (int s0 = wave; s0 < slots; s0 += kAhead * kRowWaves) {
+    float v[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) v[i] = lse[(long long)min(s0 + i * kRowWaves, slots - 1) * a.rows];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) m = fmaxf(m, v[i]);
+  }
+  const bool window = wave == 0 && see.window;
+  const float of_window = window ? lse[(long long)G * a.rows] : -INFINITY;
+  m = finite_reference(fmaxf(m, of_window));
+  float l = window ? __builtin_amdgcn_exp2f(of_window - m) : 0.0f;
+  for (int s0 = wave; s0 < slots; s0 += kAhead * kRowWaves) {
+    float v[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) v[i] = lse[(long long)min(s0 + i * kRowWaves, slots - 1) * a.rows];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) l += s0 + i * kRowWaves < slots ? __builtin_amdgcn_exp2f(v[i] - m) : 0.0f;
+  }
+  sM[wave][lane] = l == 0.0f ? -INFINITY : m;
+  sL[wave][lane] = l;
+  __syncthreads();
+  if (wave != 0 || row >= at.rows) return;
+  float M = -INFINITY, L = 0.0f;
+#pragma unroll
+  for (int w = 0; w < kRowWaves; ++w) M = fmaxf(M, sM[w][lane]);
+  const float to = finite_reference(M);
+#pragma unroll
+  for (int w = 0; w < kRowWaves; ++w) L = fmaf(__builtin_amdgcn_exp2f(sM[w][lane] - to), sL[w][lane], L);
+  a.row_lse[(long long)bh * a.rows + row] = to + __builtin_amdgcn_logf(L);
+}
+
+// The mass.  Grid: a wave a slot, those of a pair one after the other.
+constexpr int kColumnWaves = 4;
+__global__ __launch_bounds__(64 * kColumnWaves) void columns_kernel(MassCall a, long long columns) {
+  const int lane = threadIdx.x & 63;
+  const long long column = (long long)blockIdx.x * kColumnWaves + (threadIdx.x >> 6);
+  if (column >= columns) return;
+  const long long bh = column / (a.cache.max_groups + 1);
+  const int slot = (int)(column - bh * (a.cache.max_groups + 1)), b = (int)(bh / a.cache.H_kv);
+  const Place at = place_of(a, b);
+  const int G = at.len.groups();
+  if (slot > G) return;
+  if (slot == G && G >= a.slots && bh % a.cache.H_kv == 0 && lane == 0) atomicOr(a.cache.status, KVLINC_ST_BOUND);
+  const int first = slot < G ? slot * kGroup : at.len.nq;  // rows before that of the first token do not see it
+  const int from = at.rows == 0 ? 0 : max(first - (at.len.total() - at.T), 0) * a.gq;
+  const float* lse = a.lse + (bh * a.slots + slot) * a.rows;
+  const float* of_row = a.row_lse + bh * a.rows;
+  float w = 0.0f;
+  if (slot < G || at.len.nr > 0)
+    for (int row = from + lane; row < at.rows; row += 64) w += __builtin_amdgcn_exp2f(lse[row] - of_row[row]);
+  w = wave_allsum(w);
+  if (lane == 0) a.mass_out[column] = a.mass != nullptr ? fmaf(a.decay, a.mass[column], w) : w;
+}
+
+}  // namespace
+
+int launch_attention_mass(const MassCall& a, hipStream_t stream) {
+  const long long pairs = (long long)a.cache.B * a.cache.H_kv, row_blocks = a.rows / 16;
+  // Some 2048 waves, two a SIMD; blocks of rows share an unpacked tile where there are more of them and of groups than that.
+  long long blocks = pairs * row_blocks * a.slots / 2048;
+  blocks = blocks < 1 ? 1 : blocks > kMostBlocks ? kMostBlocks : blocks;
+  if (blocks > row_blocks) blocks = row_blocks;
+  const long long sets = (row_blocks + blocks - 1) / blocks;
+  long long splits = 2048 / (pairs * sets);
+  if (splits > a.slots) splits = a.slots;
+  if (splits < 1) splits = 1;
+  const long long runs = (splits + kScoreWaves - 1) / kScoreWaves;
+  const dim3 grid((unsigned)(pairs * sets * runs)), block(64 * kScoreWaves);
+  if (a.cache.bits == 2) hipLaunchKernelGGL((scores_kernel<2>), grid, block, 0, stream, a, (int)blocks, (int)runs);
+  else hipLaunchKernelGGL((scores_kernel<4>), grid, block, 0, stream, a, (int)blocks, (int)runs);
+  if (hipGetLastError() != hipSuccess) return KVLINC_EHIP;
+  hipLaunchKernelGGL(rows_kernel, dim3((unsigned)(pairs * ((a.rows + 63) / 64))), dim3(64 * kRowWaves), 0, stream, a);
+  if (hipGetLastError() != hipSuccess) return KVLINC_EHIP;
+  const long long columns = pairs * (a.cache.max_groups + 1);
+  hipLaunchKernelGGL(columns_kernel, dim3((unsigned)((columns + kColumnWaves - 1) / kColumnWaves)), block, 0, stream, a, columns);
+  return hipGetLastError() == hipSuccess ? KVLINC_OK : KVLINC_EHIP;
+}
+
+}  // namespace kvlinc

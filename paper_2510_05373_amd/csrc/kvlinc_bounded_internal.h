@@ -1,0 +1,66 @@
+// Internal declarations of the calls of kvlinc_bounded.h (not part of the C ABI).
+#pragma once
+
+#include "kvlinc_bounded.h"
+#include "kvlinc_internal.h"
+
+namespace kvlinc {
+
+// ---- positions ----
+struct RotaryRows {
+  const void* in;
+  void* out;
+  long long sequence_stride, head_stride, token_stride;
+  int heads;  // 0: no such rows
+};
+struct RotaryCall {
+  RotaryRows rows[3];  // queries, keys, values
+  const double* freq;
+  const int32_t* n_quant;  // NULL: positions are not counted from the cache
+  const int32_t* n_res;
+  const int32_t* first;
+  const int32_t* depth;
+  const int32_t* n_new;
+  float magnitude;
+  int channels, B, T, heads, steps;  // heads: of all three; steps: of 8 heads that a wave takes
+};
+int launch_rotary(const RotaryCall& a, bool interleaved, int dtype_in, int dtype_out, hipStream_t stream);
+
+// ---- accumulated attention weight ----
+// One call as the kernels take it.  Slots of a (sequence, KV head): a group each, and the window's behind the last.
+struct MassCall {
+  kvlinc_cache cache;
+  const _Float16* q;
+  const int32_t* n_rows;
+  const float* mass;  // NULL: zeros
+  float* mass_out;
+  float decay;
+  int T, gq, splits;
+  _Float16* out;
+  float* part;        // decode: partial results of the splits as in kvlinc_context_internal.h; splits > 1 only
+  unsigned long long* sums;  // decode: [B H_kv][slots][16] pairs {reference, sum of weights} of a column, see kvlinc_decode_mass.hip
+  float* lse;         // rows: [B H_kv][slots][rows] log2 of a row's sum of weights over the slot's tokens
+  float* row_lse;     // rows: [B H_kv][rows] the same over all tokens it sees
+  long long slots;
+  int rows;           // of a (sequence, KV head), up to a multiple of 16
+};
+int launch_decode_mass(const MassCall& a, int waves, hipStream_t stream);
+int launch_attention_mass(const MassCall& a, hipStream_t stream);
+
+// ---- eviction ----
+struct EvictCall {
+  kvlinc_cache from, to;
+  const float* mass;
+  float* mass_out;
+  int keep, limit, first, last;
+  const int32_t* offset;
+  int32_t* offset_out;
+  int32_t* kept;
+  int32_t* source;  // [B H_kv][stride] slots of the kept groups
+  int32_t* count;   // [B H_kv][2] how many, and the first that has another slot than before
+  long long stride;
+  bool in_place;
+};
+int launch_evict(const EvictCall& a, hipStream_t stream);
+
+}  // namespace kvlinc

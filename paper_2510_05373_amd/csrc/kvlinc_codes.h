@@ -100,6 +100,9 @@ __device__ __forceinline__ Shares shares_of(float m, float c_d) {
   return Shares{c_d != 0.0f ? __builtin_amdgcn_exp2f(m - to) : 1.0f, __builtin_amdgcn_exp2f(-to)};
 }
 
+// A wave's LDS instructions stay in order; so that the compiler leaves them there where one lane reads what another has written.
+__device__ __forceinline__ void wave_order() { asm volatile("" ::: "memory"); }
+
 // Bits 15 and 31: the halves of a word that are infinite or not a number; and the word with zeros in their places.  A value that a row does not see
 // must not reach it, and 0 times such a value is not a number.
 __device__ __forceinline__ uint32_t not_finite(uint32_t w) { return ((w & 0x7c007c00u) + 0x04000400u) & 0x80008000u; }
