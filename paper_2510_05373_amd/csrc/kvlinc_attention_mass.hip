@@ -4,11 +4,17 @@
 // rows_kernel makes of them the same over all tokens that the row sees; and columns_kernel sums 2^(the first - the second) over the rows of a slot.
 // So the weights are formed once, groups do not wait for one another, and what goes through memory is 4 bytes a row and group.
 //
-// scores_kernel.  S^T = K Q^T on v_mfma_f32_16x16x32_f16, operands and exactness as in kvlinc_rows.hip.  A wave unpacks a group's key tile into
-// 128 registers, and goes over blocks of 16 rows with it: query times key scales in two terms, 64 products, 32 exponentials a lane.  A column's
-// reference is one that an earlier group has left, as long as the sums it gives stay below 2^14; only where they do not, the largest score is looked
-// for and the weights are formed again: what a row's larger weights leave of a slot below 2^-126 of them is nothing.
+// scores_kernel.  S^T = K Q^T on v_mfma_f32_16x16x32_f16: codes as binary16 numbers, query times key scales in two binary16 terms (exactness as in
+// kvlinc_rows.hip).  A wave unpacks a group's key tile into 128 registers and goes over blocks of 16 rows with it: 64 products, 32 exponentials a lane.
+// Zero-points and centring are two sums over channels, products of rows, too.  Vector work goes ahead of products (s_setprio): the two waves of a
+// SIMD, with the same steps to do, otherwise do them side by side, products then vector work, and neither fills the other's gaps (2048 rows over 32768
+// tokens: 887 us, 810 so).  The second term as FP6 numbers, half of the matrix work, was 793 (its conversion takes 20 issue slots) and 30 times less
+// exact; four FP6 terms and codes as they lie 1085.
+// A column's reference is one that an earlier group has left, as long as the sums it gives stay below 2^14; only where they do not, the largest score is
+// looked for and the weights are formed again: what a row's larger weights leave of a slot below 2^-126 of them is nothing.
 #include <hip/hip_runtime.h>
+
+#include <type_traits>
 
 #include "kvlinc_bounded_internal.h"
 #include "kvlinc_row_parts.h"
@@ -46,39 +52,18 @@ __device__ __forceinline__ void load_keys_of(KeyPart<BITS>& r, const uint32_t* r
   r.meta = reinterpret_cast<const u32x4_t*>(rec + Rec<BITS>::kKeyScale)[lane & 31];
 }
 
-// Scores of a tile of 128 tokens (operands A) become the columns' sums of weights.  hide(n, r): the token of x[n][r] is not seen.
+// Scores of a tile of 128 tokens become a column's sum of weights relative to col.m (-inf: nothing seen yet), which may be raised.
 struct Column {
-  float m;  // reference; -inf: nothing seen yet
+  float m;
 };
-template <bool TWO, typename H>
-__device__ __forceinline__ float tile_sum(Column& col, const half8_t (&A)[8][4], const half8_t (&hi)[4], const half8_t (&lo)[4], float unit, float bias, bool masked, H hide) {
-  float4_t x[8];
+__device__ __forceinline__ float tile_sum(Column& col, float4_t (&x)[8], float unit, float bias) {
+  float4_t l4 = {0.f, 0.f, 0.f, 0.f};
+  const float base = bias - col.m;
 #pragma unroll
-  for (int n = 0; n < 8; ++n) x[n] = float4_t{0.f, 0.f, 0.f, 0.f};
-  if constexpr (TWO) {
+  for (int n = 0; n < 8; ++n)
 #pragma unroll
-    for (int s = 0; s < 4; ++s)
-#pragma unroll
-      for (int n = 0; n < 8; ++n) x[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(A[n][s], lo[s], x[n], 0, 0, 0);
-  }
-#pragma unroll
-  for (int s = 0; s < 4; ++s)
-#pragma unroll
-    for (int n = 0; n < 8; ++n) x[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(A[n][s], hi[s], x[n], 0, 0, 0);
-  if (masked) {
-#pragma unroll
-    for (int n = 0; n < 8; ++n)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) x[n][r] = hide(n, r) ? -INFINITY : x[n][r];
-  }
-  float l = 0.0f;
-  {
-    const float base = bias - col.m;
-#pragma unroll
-    for (int n = 0; n < 8; ++n)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) l += __builtin_amdgcn_exp2f(fmaf(x[n][r], unit, base));
-  }
+    for (int r = 0; r < 4; ++r) l4[r] += __builtin_amdgcn_exp2f(fmaf(x[n][r], unit, base));
+  float l = (l4[0] + l4[1]) + (l4[2] + l4[3]);
   if (__builtin_amdgcn_ballot_w64(!(l <= kMostSum) || fmaxf(fabsf(bias), fabsf(col.m)) > kFusedBound) != 0) {
     float mx = -INFINITY;
 #pragma unroll
@@ -104,14 +89,21 @@ __device__ __forceinline__ float tile_sum(Column& col, const half8_t (&A)[8][4],
   pair_across<32>(a + b, a, b);
   return a + b;
 }
+// Tokens 16 n + pi(4 g + r) from `end` on are not seen.
+__device__ __forceinline__ void hide_from(float4_t (&x)[8], int end, int g) {
+#pragma unroll
+  for (int n = 0; n < 8; ++n)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) x[n][r] = 16 * n + token_order(4 * g + r) >= end ? -INFINITY : x[n][r];
+}
 
 // Grid, one-dimensional: pairs fastest, then runs of kScoreWaves splits of the slots, then sets of a.blocks blocks of rows.
 template <int BITS>
 __global__ __launch_bounds__(64 * kScoreWaves, 2) void scores_kernel(MassCall a, int blocks, int runs) {
   __shared__ __align__(16) half_t sQuery[kMostBlocks * 16][kQueryStride];
-  __shared__ __align__(16) u32x4_t sMeta[kScoreWaves][32];
+  __shared__ __align__(16) u32x4_t sMeta[kScoreWaves][33];  // key scales, zero-points, zeros
   __shared__ float sUnit[kMostBlocks * 16], sRef[kScoreWaves][kMostBlocks * 16];
-  __shared__ int sPosition[kMostBlocks * 16], sLossy[kMostBlocks];
+  __shared__ int sPosition[kMostBlocks * 16], sLossy;
   const kvlinc_cache& c = a.cache;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), j = lane & 15, g = lane >> 4;
   const int pairs = c.B * c.H_kv, unit_id = blockIdx.x / pairs, bh = blockIdx.x - unit_id * pairs, set = unit_id / runs, split = (unit_id - set * runs) * kScoreWaves + wave;
@@ -126,7 +118,7 @@ __global__ __launch_bounds__(64 * kScoreWaves, 2) void scores_kernel(MassCall a,
   };
 
   // ---- the rows to LDS, as load_query of kvlinc_row_parts.h has them ----
-  if (tid < kMostBlocks) sLossy[tid] = 0;
+  if (tid == 0) sLossy = 0;
   __syncthreads();
   for (int row = tid >> 4; row < 16 * n_blocks; row += 4 * kScoreWaves) {
     const u32x4_t raw = reinterpret_cast<const u32x4_t*>(query_of(row0 + row))[lane & 15];
@@ -146,24 +138,31 @@ __global__ __launch_bounds__(64 * kScoreWaves, 2) void scores_kernel(MassCall a,
       lost |= as_u32(as_h2(scaled[i]) * by.back) ^ raw[i];
     }
     *reinterpret_cast<u32x4_t*>(&sQuery[row][8 * (lane & 15)]) = scaled;
-    if (lost != 0) sLossy[row / 16] = 1;
+    if (lost != 0) sLossy = 1;
     if ((lane & 15) == 0) {
       sUnit[row] = by.unit;
       sPosition[row] = at.position(min(row0 + row, at.rows - 1), gq);
     }
   }
   for (int k = 0; k < n_blocks; ++k) sRef[wave][16 * k + j] = -INFINITY;
+  if (lane == 0) sMeta[wave][32] = u32x4_t{0, 0, 0, 0};
   __syncthreads();
 
   float* lse = a.lse + bh * a.slots * a.rows + row0;
   const uint32_t* rec0 = c.groups + (long long)bh * c.max_groups * Rec<BITS>::kWords;
-  // (a block of rows goes over a slot whose first token its last row sees)
-  auto last_position = [&](int k) { return __builtin_amdgcn_readfirstlane(sPosition[16 * k + 15]); };
+  const bool lossy = __builtin_amdgcn_readfirstlane(sLossy) != 0;
+  const int oldest = __builtin_amdgcn_readfirstlane(sPosition[0]), newest = __builtin_amdgcn_readfirstlane(sPosition[16 * n_blocks - 1]);
+  auto load_rows = [&](int k, half8_t (&q)[4]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int s = 0; s < 4; ++s) q[s] = *reinterpret_cast<const half8_t*>(&sQuery[16 * k + j][32 * g + 8 * s]);
+  };
   auto leave = [&](int slot, int k, const Column& col, float sum) __attribute__((always_inline)) {
     sRef[wave][16 * k + j] = col.m;  // (the same in the four lanes of a column: each reads what it has written)
     if (g == 0) lse[(long long)slot * a.rows + 16 * k + j] = finite_reference(col.m) + __builtin_amdgcn_logf(sum);
   };
-  const int newest = last_position(n_blocks - 1);
+  // What the zero-points and the centring add to a score is a product, too: of rows that are the zero-points (in every quarter's first row of the
+  // product) and the scales (in the second), so that every lane finds both sums of its column.
+  const int bias_at = (j & 3) == 0 ? 16 + 4 * g : (j & 3) == 1 ? 4 * g : 32, bias_step = (j & 3) < 2 ? 1 : 0;
   KeyPart<BITS> rec;
   int slot = split;
   if (slot < G) load_keys_of<BITS>(rec, rec0 + (long long)slot * Rec<BITS>::kWords, lane);
@@ -179,54 +178,91 @@ __global__ __launch_bounds__(64 * kScoreWaves, 2) void scores_kernel(MassCall a,
     top = max(top, dpp_u<kRowRor2>(top));
     top = max(top, dpp_u<kRowRor4>(top));
     top = max(top, dpp_u<kRowRor8>(top));
-    const uint32_t key_scale = (uint32_t)__builtin_amdgcn_readlane(top, 0);  // (lanes 0..15 have the scales)
+    const bool wide = lossy || (uint32_t)__builtin_amdgcn_readlane(top, 0) >= kFirstLargeScale;  // (lanes 0..15 have the scales)
+    const bool masked = count < kGroup || first + kGroup - 1 > oldest;
     half8_t A[8][4];
 #pragma unroll
     for (int n = 0; n < 8; ++n) key_operands<BITS>(rec.kw, n, A[n]);
     const int next = slot + splits < G ? slot + splits : slot;
     load_keys_of<BITS>(rec, rec0 + (long long)next * Rec<BITS>::kWords, lane);
-    for (int k = 0; k < n_blocks; ++k) {
-      if (first > last_position(k)) continue;
-      const int row = row0 + 16 * k + j;
-      half8_t q[4], hi[4], lo[4];
-#pragma unroll
-      for (int s = 0; s < 4; ++s) q[s] = *reinterpret_cast<const half8_t*>(&sQuery[16 * k + j][32 * g + 8 * s]);
-      float bias, unit;
-      row_operands<BITS>(q, sUnit[16 * k + j], sLossy[k] != 0, [&]() __attribute__((always_inline)) { return query_of(row) + 32 * g; }, &sMeta[wave][0], key_scale, lane, hi, lo, bias, unit);
+    auto block = [&](int k, auto general) __attribute__((always_inline)) {
+      constexpr bool kGeneral = decltype(general)::value;
+      float bias, unit = sUnit[16 * k + j];
       Column col = {sRef[wave][16 * k + j]};
-      const bool masked = count < kGroup || first + kGroup - 1 > __builtin_amdgcn_readfirstlane(sPosition[16 * k]);
-      const int end = min(count, sPosition[16 * k + j] - first + 1);
-      const float sum = tile_sum<true>(col, A, hi, lo, unit, bias, masked, [&](int n, int r) { return 16 * n + token_order(4 * g + r) >= end; });
+      half8_t hi[4], lo[4];
+      if (kGeneral && wide) {
+        wide_operands<BITS>(query_of(row0 + 16 * k + j) + 32 * g, &sMeta[wave][0], lane, hi, lo, bias, unit);
+      } else {
+        half8_t q[4];
+        load_rows(k, q);
+        float4_t d = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+          d = __builtin_amdgcn_mfma_f32_16x16x32_f16(as_h8(sMeta[wave][bias_at + s * bias_step]), q[s], d, 0, 0, 0);
+          const u32x4_t sc = sMeta[wave][4 * g + s], qq = __builtin_bit_cast(u32x4_t, q[s]);
+          u32x4_t h, r;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const half2_t x = as_h2(qq[i]), y = as_h2(sc[i]), t = x * y;
+            h[i] = as_u32(t);
+            r[i] = as_u32(__builtin_elementwise_fma(x, y, -t));
+          }
+          hi[s] = as_h8(h);
+          lo[s] = as_h8(r);
+        }
+        bias = fmaf(d[1], Rec<BITS>::kCentre, d[0]) * unit;
+      }
+      __builtin_amdgcn_s_setprio(0);
+      float4_t x[8];
+#pragma unroll
+      for (int n = 0; n < 8; ++n) x[n] = float4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+#pragma unroll
+        for (int n = 0; n < 8; ++n) x[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(A[n][s], lo[s], x[n], 0, 0, 0);
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+#pragma unroll
+        for (int n = 0; n < 8; ++n) x[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(A[n][s], hi[s], x[n], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_setprio(1);
+      if (kGeneral && masked) hide_from(x, min(count, sPosition[16 * k + j] - first + 1), g);
+      const float sum = tile_sum(col, x, unit, bias);
       leave(slot, k, col, sum);
+    };
+    if (wide || masked) {
+      for (int k = 0; k < n_blocks; ++k)  // (a block of rows goes over a slot whose first token its last row sees)
+        if (first <= __builtin_amdgcn_readfirstlane(sPosition[16 * k + 15])) block(k, std::true_type{});
+    } else {
+      for (int k = 0; k < n_blocks; ++k) block(k, std::false_type{});
     }
     wave_order();
   }
-  // ---- the window, by the wave whose turn it is ----
+  // ---- the window's raw rows, by the wave whose turn it is ----
   if (at.len.nr > 0 && G % splits == split && at.len.nq <= newest) {
     const half_t* keys = reinterpret_cast<const half_t*>(c.k_res) + (long long)bh * c.R * kHeadDim;
-    half8_t A[8][4];
-#pragma unroll
-    for (int n = 0; n < 8; ++n) {
-      const half_t* row = keys + (long long)min(16 * n + token_order(j), at.len.nr - 1) * kHeadDim + 32 * g;
-#pragma unroll
-      for (int s = 0; s < 4; ++s) A[n][s] = as_h8(reinterpret_cast<const u32x4_t*>(row)[s]);
-    }
     for (int k = 0; k < n_blocks; ++k) {
-      if (at.len.nq > last_position(k)) continue;
-      const int row = row0 + 16 * k + j;
+      if (at.len.nq > __builtin_amdgcn_readfirstlane(sPosition[16 * k + 15])) continue;
       half8_t q[4];
       float unit = sUnit[16 * k + j];
-#pragma unroll
-      for (int s = 0; s < 4; ++s) q[s] = *reinterpret_cast<const half8_t*>(&sQuery[16 * k + j][32 * g + 8 * s]);
-      if (sLossy[k] != 0) {
-        const u32x4_t* src = reinterpret_cast<const u32x4_t*>(query_of(row) + 32 * g);
+      load_rows(k, q);
+      if (lossy) {
+        const u32x4_t* src = reinterpret_cast<const u32x4_t*>(query_of(row0 + 16 * k + j) + 32 * g);
 #pragma unroll
         for (int s = 0; s < 4; ++s) q[s] = as_h8(src[s]);
         unit = kLog2eSqrtD;
       }
+      float4_t x[8];
+#pragma unroll
+      for (int n = 0; n < 8; ++n) {
+        const u32x4_t* row = reinterpret_cast<const u32x4_t*>(keys + (long long)min(16 * n + token_order(j), at.len.nr - 1) * kHeadDim + 32 * g);
+        x[n] = float4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = 0; s < 4; ++s) x[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(as_h8(row[s]), q[s], x[n], 0, 0, 0);
+      }
+      hide_from(x, min(at.len.nr, sPosition[16 * k + j] - at.len.nq + 1), g);
       Column col = {sRef[wave][16 * k + j]};
-      const int end = min(at.len.nr, sPosition[16 * k + j] - at.len.nq + 1);
-      const float sum = tile_sum<false>(col, A, q, q, unit, 0.0f, true, [&](int n, int r) { return 16 * n + token_order(4 * g + r) >= end; });
+      const float sum = tile_sum(col, x, unit, 0.0f);
       leave(G, k, col, sum);
     }
   }
@@ -301,8 +337,19 @@ __global__ __launch_bounds__(64 * kColumnWaves) void columns_kernel(MassCall a, 
   const float* lse = a.lse + (bh * a.slots + slot) * a.rows;
   const float* of_row = a.row_lse + bh * a.rows;
   float w = 0.0f;
-  if (slot < G || at.len.nr > 0)
-    for (int row = from + lane; row < at.rows; row += 64) w += __builtin_amdgcn_exp2f(lse[row] - of_row[row]);
+  if (slot < G || at.len.nr > 0) {
+    const auto add = [&](int row) __attribute__((always_inline)) {  // (rows of a pair begin at 64 bytes)
+      const float4_t v = *reinterpret_cast<const float4_t*>(lse + row), l = *reinterpret_cast<const float4_t*>(of_row + row);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w += row + i >= from && row + i < at.rows ? __builtin_amdgcn_exp2f(v[i] - l[i]) : 0.0f;
+    };
+    int row = (from & ~255) + 4 * lane;
+    for (; row + 3 * 256 < at.rows; row += 4 * 256) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) add(row + 256 * u);
+    }
+    for (; row < at.rows; row += 256) add(row);
+  }
   w = wave_allsum(w);
   if (lane == 0) a.mass_out[column] = a.mass != nullptr ? fmaf(a.decay, a.mass[column], w) : w;
 }
@@ -327,7 +374,7 @@ int launch_attention_mass(const MassCall& a, hipStream_t stream) {
   hipLaunchKernelGGL(rows_kernel, dim3((unsigned)(pairs * ((a.rows + 63) / 64))), dim3(64 * kRowWaves), 0, stream, a);
   if (hipGetLastError() != hipSuccess) return KVLINC_EHIP;
   const long long columns = pairs * (a.cache.max_groups + 1);
-  hipLaunchKernelGGL(columns_kernel, dim3((unsigned)((columns + kColumnWaves - 1) / kColumnWaves)), block, 0, stream, a, columns);
+  hipLaunchKernelGGL(columns_kernel, dim3((unsigned)((columns + kColumnWaves - 1) / kColumnWaves)), dim3(64 * kColumnWaves), 0, stream, a, columns);
   return hipGetLastError() == hipSuccess ? KVLINC_OK : KVLINC_EHIP;
 }
 
