@@ -320,6 +320,55 @@ __global__ __launch_bounds__(64 * kRowWaves) void rows_kernel(MassCall a) {
   a.row_lse[(long long)bh * a.rows + row] = to + __builtin_amdgcn_logf(L);
 }
 
+// Both of what follows scores_kernel in one launch, a workgroup a pair, where its numbers fit into LDS.
+constexpr int kPairThreads = 1024, kPairNumbers = 32768;
+__global__ __launch_bounds__(kPairThreads) void pair_kernel(MassCall a) {
+  extern __shared__ float sLse[];  // [slots][rows]
+  __shared__ float sM[kPairThreads], sL[kPairThreads];
+  const int tid = threadIdx.x, lane = tid & 63, bh = blockIdx.x, b = bh / a.cache.H_kv;
+  const Place at = place_of(a, b);
+  const int G = at.len.groups(), rows = a.rows;
+  // unlike scores_kernel's, numbers of slots that a row does not see are read here, and left
+  const auto first_of = [&](int slot) { return slot < G ? slot * kGroup : at.len.nq; };
+  const float* lse = a.lse + (long long)bh * a.slots * rows;
+  const int slots = at.rows == 0 ? 0 : G + (at.len.nr > 0 ? 1 : 0);
+  for (int i = 4 * tid; i < slots * rows; i += 4 * kPairThreads) *reinterpret_cast<float4_t*>(sLse + i) = *reinterpret_cast<const float4_t*>(lse + i);
+  __syncthreads();
+  // a row's sum: its slots shared by `parts` threads
+  const int parts = kPairThreads / rows, row = tid % rows, part = tid / rows;
+  float m = -INFINITY, l = 0.0f;
+  if (part < parts && row < at.rows) {
+    const int p = at.position(row, a.gq);
+    for (int s = part; s < slots; s += parts)
+      if (first_of(s) <= p) m = fmaxf(m, sLse[s * rows + row]);
+    const float to = finite_reference(m);
+    for (int s = part; s < slots; s += parts)
+      if (first_of(s) <= p) l += __builtin_amdgcn_exp2f(sLse[s * rows + row] - to);
+  }
+  sM[tid] = l == 0.0f ? -INFINITY : finite_reference(m);
+  sL[tid] = l;
+  __syncthreads();
+  float M = -INFINITY, L = 0.0f;
+  if (tid < rows) {
+    for (int i = 0; i < parts; ++i) M = fmaxf(M, sM[i * rows + tid]);
+    M = finite_reference(M);
+    for (int i = 0; i < parts; ++i) L = fmaf(__builtin_amdgcn_exp2f(sM[i * rows + tid] - M), sL[i * rows + tid], L);
+  }
+  __syncthreads();
+  if (tid < rows) sM[tid] = M + __builtin_amdgcn_logf(L);
+  __syncthreads();
+  for (int slot = tid >> 6; slot <= G; slot += kPairThreads / 64) {
+    const int from = max(first_of(slot) - (at.len.total() - at.T), 0) * a.gq;  // rows before that of the first token do not see it
+    float w = 0.0f;
+    if (slot < slots)
+      for (int r = from + lane; r < at.rows; r += 64) w += __builtin_amdgcn_exp2f(sLse[slot * rows + r] - sM[r]);
+    w = wave_allsum(w);
+    const long long column = (long long)bh * (a.cache.max_groups + 1) + slot;
+    if (lane == 0) a.mass_out[column] = a.mass != nullptr ? fmaf(a.decay, a.mass[column], w) : w;
+  }
+  if (G >= a.slots && bh % a.cache.H_kv == 0 && tid == 0) atomicOr(a.cache.status, KVLINC_ST_BOUND);
+}
+
 // The mass.  Grid: a wave a slot, those of a pair one after the other.
 constexpr int kColumnWaves = 4;
 __global__ __launch_bounds__(64 * kColumnWaves) void columns_kernel(MassCall a, long long columns) {
@@ -371,6 +420,10 @@ int launch_attention_mass(const MassCall& a, hipStream_t stream) {
   if (a.cache.bits == 2) hipLaunchKernelGGL((scores_kernel<2>), grid, block, 0, stream, a, (int)blocks, (int)runs);
   else hipLaunchKernelGGL((scores_kernel<4>), grid, block, 0, stream, a, (int)blocks, (int)runs);
   if (hipGetLastError() != hipSuccess) return KVLINC_EHIP;
+  if (a.rows <= kPairThreads && a.slots * a.rows <= kPairNumbers) {
+    hipLaunchKernelGGL(pair_kernel, dim3((unsigned)pairs), dim3(kPairThreads), (size_t)(a.slots * a.rows) * sizeof(float), stream, a);
+    return hipGetLastError() == hipSuccess ? KVLINC_OK : KVLINC_EHIP;
+  }
   hipLaunchKernelGGL(rows_kernel, dim3((unsigned)(pairs * ((a.rows + 63) / 64))), dim3(64 * kRowWaves), 0, stream, a);
   if (hipGetLastError() != hipSuccess) return KVLINC_EHIP;
   const long long columns = pairs * (a.cache.max_groups + 1);
