@@ -241,6 +241,13 @@ __global__ __launch_bounds__(64 * kScoreWaves, 2) void scores_kernel(MassCall a,
   // ---- the window's raw rows, by the wave whose turn it is ----
   if (at.len.nr > 0 && G % splits == split && at.len.nq <= newest) {
     const half_t* keys = reinterpret_cast<const half_t*>(c.k_res) + (long long)bh * c.R * kHeadDim;
+    half8_t A[8][4];
+#pragma unroll
+    for (int n = 0; n < 8; ++n) {
+      const u32x4_t* row = reinterpret_cast<const u32x4_t*>(keys + (long long)min(16 * n + token_order(j), at.len.nr - 1) * kHeadDim + 32 * g);
+#pragma unroll
+      for (int s = 0; s < 4; ++s) A[n][s] = as_h8(row[s]);
+    }
     for (int k = 0; k < n_blocks; ++k) {
       if (at.len.nq > __builtin_amdgcn_readfirstlane(sPosition[16 * k + 15])) continue;
       half8_t q[4];
@@ -254,12 +261,11 @@ __global__ __launch_bounds__(64 * kScoreWaves, 2) void scores_kernel(MassCall a,
       }
       float4_t x[8];
 #pragma unroll
-      for (int n = 0; n < 8; ++n) {
-        const u32x4_t* row = reinterpret_cast<const u32x4_t*>(keys + (long long)min(16 * n + token_order(j), at.len.nr - 1) * kHeadDim + 32 * g);
-        x[n] = float4_t{0.f, 0.f, 0.f, 0.f};
+      for (int n = 0; n < 8; ++n) x[n] = float4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int s = 0; s < 4; ++s) x[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(as_h8(row[s]), q[s], x[n], 0, 0, 0);
-      }
+      for (int s = 0; s < 4; ++s)
+#pragma unroll
+        for (int n = 0; n < 8; ++n) x[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(A[n][s], q[s], x[n], 0, 0, 0);
       hide_from(x, min(at.len.nr, sPosition[16 * k + j] - at.len.nq + 1), g);
       Column col = {sRef[wave][16 * k + j]};
       const float sum = tile_sum(col, x, unit, 0.0f);
