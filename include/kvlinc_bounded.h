@@ -86,7 +86,7 @@ size_t kvlinc_decode_mass_workspace_bytes(const kvlinc_cache* cache, int32_t max
  *   max_context    host-side upper bound on n_quant + n_res (<= 0: capacity); it only sizes the launch, results do not depend on it but for the
  *                  order of sums
  *
- * A sequence with no tokens yields zeros and decay mass.  Scores are those of exact products with the dequantized keys to about 2^-21 of their terms;
+ * A sequence with no tokens yields zeros and decay mass.  Scores are those of exact products with the dequantized keys to 2^-16 of each;
  * sums are binary32, and do not depend on the order in which the workgroups run.
  */
 int kvlinc_decode_attention_mass(const kvlinc_cache* cache, const kvlinc_half* q, kvlinc_half* out, const float* mass, float decay, float* mass_out,

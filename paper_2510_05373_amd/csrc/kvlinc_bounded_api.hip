@@ -45,9 +45,9 @@ long long groups_of_bound(const kvlinc_cache& c, int max_context) {
   return groups < c.max_groups ? groups : c.max_groups;
 }
 
-// Decode: as few-row prompt attention has its splits (plan_call in kvlinc_context_api.hip).
+// Decode: as windowed decode has its splits (plan_windowed in kvlinc_context_api.hip).
 struct DecodePlan {
-  int waves, splits;
+  int splits;
   long long slots;
   size_t part_floats, sums;
   size_t bytes() const { return part_floats * sizeof(float) + sums * sizeof(unsigned long long); }
@@ -55,16 +55,15 @@ struct DecodePlan {
 DecodePlan plan_decode(const kvlinc_cache& c, int max_context) {
   const long long pairs = pairs_of(c), groups = groups_of_bound(c, max_context);
   DecodePlan p{};
-  p.waves = pairs <= 64 ? 8 : 4;
-  long long s = (p.waves == 8 ? 256 : 512) / pairs;
-  const long long most = (groups + p.waves - 1) / p.waves;
+  long long s = 512 / pairs;
+  const long long most = (groups + 3) / 4;
   if (s > most) s = most;
   if (s > kMaxContextSplits) s = kMaxContextSplits;
   if (s < 1) s = 1;
   p.splits = (int)s;
   p.slots = c.max_groups + 4;  // (the window's 128 tokens in runs of 32; whatever max_context says, so that no sequence is too long for it)
   p.part_floats = s > 1 ? (size_t)(c.B * (long long)c.H_q * s) * kPartStride : 0;
-  p.sums = (size_t)(pairs * p.slots) * 16;
+  p.sums = (size_t)(pairs * p.slots) * 8;
   return p;
 }
 
@@ -194,8 +193,8 @@ int kvlinc_decode_attention_mass(const kvlinc_cache* cache, const kvlinc_half* q
   a.splits = p.splits;
   a.slots = p.slots;
   a.sums = static_cast<unsigned long long*>(workspace);
-  a.part = p.part_floats != 0 ? reinterpret_cast<float*>(a.sums + p.sums) : nullptr;  // (sums: a multiple of 128 bytes)
-  return launch_decode_mass(a, p.waves, static_cast<hipStream_t>(stream));
+  a.part = p.part_floats != 0 ? reinterpret_cast<float*>(a.sums + p.sums) : nullptr;  // (sums: a multiple of 64 bytes)
+  return launch_decode_mass(a, static_cast<hipStream_t>(stream));
 }
 
 size_t kvlinc_attention_mass_workspace_bytes(const kvlinc_cache* cache, int32_t T, int32_t max_context) {

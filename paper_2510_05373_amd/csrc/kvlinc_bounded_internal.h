@@ -38,13 +38,13 @@ struct MassCall {
   int T, gq, splits;
   _Float16* out;
   float* part;        // decode: partial results of the splits as in kvlinc_context_internal.h; splits > 1 only
-  unsigned long long* sums;  // decode: [B H_kv][slots][16] pairs {reference, sum of weights} of a column, see kvlinc_decode_mass.hip
+  unsigned long long* sums;  // decode: [B H_kv][slots][8] pairs {reference, sum of weights} of a head, see kvlinc_decode_mass.hip
   float* lse;         // rows: [B H_kv][slots][rows] log2 of a row's sum of weights over the slot's tokens
   float* row_lse;     // rows: [B H_kv][rows] the same over all tokens it sees
   long long slots;
   int rows;           // of a (sequence, KV head), up to a multiple of 16
 };
-int launch_decode_mass(const MassCall& a, int waves, hipStream_t stream);
+int launch_decode_mass(const MassCall& a, hipStream_t stream);
 int launch_attention_mass(const MassCall& a, hipStream_t stream);
 
 // ---- eviction ----

@@ -1,158 +1,156 @@
 // One decode step that also accumulates what attention weight every group of tokens has received.
 //
-// The walk over the packed cache is that of kvlinc_rows.hip (shared in kvlinc_row_parts.h) with one token a sequence: a wave takes groups of 128
-// packed tokens, or 32 of the window's, and the rows of a KV head, its 1 to 8 query heads, are the columns of the products, each 4 or 2 times for
-// different blocks of tokens.  Scores there are exact to about 2^-21 of their terms, which the weights need that are results themselves.
-// A weight is known only when the whole context has been seen.  So every wave leaves, for each group and column, its reference and its sum of weights, 128
+// The walk over the packed cache is that of kvlinc_windowed.hip without a window (shared in kvlinc_decode_parts.h): codes go to the matrix cores as
+// FP4, weights as three FP8 terms, zero-points exact, all query heads of a KV head share one pass.  Weights are results here, so query times key scale
+// has four terms (2^-16 of each product, see qk_phase), in the row of the matrix instruction that is spare.
+// A weight is known only when the whole context has been seen.  So every wave leaves, for each group and head, its reference and its sum of weights, 64
 // bytes a group beside the 9216 or 17408 it reads; and who joins the splits of a pair, and so knows the maximum M and the sum L of every head, makes
 //     mass[j] = decay mass[j] + sum over heads of 2^(reference - M) sum / L,
-// the columns and heads always in the same order.  No second pass over keys, no second launch.
+// always in the same order.  No second pass over keys, no second launch.
+// Bound: bytes of the groups.  32 sequences of 32k tokens, 7 heads, 4 bits: 119.0 us, 4.9 TB/s; with half of the tokens missing from the shortest 106.5
+// (the splits are made for the longest); 16 of 8k, 2 bits: 22.3 us, 3.6 TB/s, of which the chain of counters, first record, arrival, join and mass takes
+// 6; one of 300 tokens: 8.4 us, the host's calls.  (The walk of few-row attention, which unpacks the codes for binary16 products: 119.5 for the 106.5,
+// 28 for the 22.3.  Two workgroups a compute unit, 512 in all; with 1024 110 and 26, three a unit at 2 bits spill.)
 #include <hip/hip_runtime.h>
 
 #include "kvlinc_bounded_internal.h"
+#include "kvlinc_decode_parts.h"
 #include "kvlinc_join.h"
-#include "kvlinc_row_parts.h"
 
 namespace kvlinc {
 namespace {
 
-constexpr int kMaxWaves = 8;
+constexpr int kHalfMirror = 0x141;  // row_half_mirror: lane 7 - i of every 8
+constexpr int kSumHeads = 8;    // pairs {reference, sum} of a slot
+constexpr int kShare = 32;     // tokens of the window a wave takes, with a slot of their own
+constexpr int kSlotsAhead = 8;  // slots of a lane requested together
 
-// {reference, sum} of a column: stores and loads past the caches that are not coherent across the chip.
-__device__ __forceinline__ void put_sum(unsigned long long* at, float reference, float sum) {
-  const unsigned long long v = (unsigned long long)__builtin_bit_cast(uint32_t, sum) << 32 | __builtin_bit_cast(uint32_t, reference);
-  __hip_atomic_store(at, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
-}
-struct ColumnSum {
-  float reference, sum;
-};
-__device__ __forceinline__ ColumnSum get_sum(const unsigned long long* at) {
-  const unsigned long long v = __hip_atomic_load(at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
-  return ColumnSum{__builtin_bit_cast(float, (uint32_t)v), __builtin_bit_cast(float, (uint32_t)(v >> 32))};
-}
-__device__ __forceinline__ float column_sum(float v) {  // over the four lanes of a column
-  float x, y;
-  pair_across<16>(v, x, y);
-  pair_across<32>(x + y, x, y);
-  return x + y;
-}
+// {reference, sum} of a head: a store past the caches that are not coherent across the chip.
+__device__ __forceinline__ void put_sum(unsigned long long* at, float reference, float sum) { st_coherent2(reinterpret_cast<float*>(at), reference, sum); }
 
-// Grid, one-dimensional: pairs fastest, then the splits.
-template <int BITS, int S, bool SLIDING>
-__global__ __launch_bounds__(64 * kMaxWaves, 2) void decode_mass_kernel(MassCall a) {
-  constexpr int kRows = 16 / S, kAccStride = kHeadDim + 4;
-  __shared__ __align__(16) u32x4_t sMeta[kMaxWaves][64];
-  __shared__ __align__(16) float sAcc[kMaxWaves][16][kAccStride];
-  __shared__ float sM[kMaxWaves][16], sL[kMaxWaves][16];
-  __shared__ float sRowM[kRows], sRowL[kRows];
+// Grid, one-dimensional: (sequence, KV head) fastest, then the split.
+template <int NB, bool SLIDING, int BITS>
+__global__ __launch_bounds__(kThreads, 2) void decode_mass_kernel(MassCall a) {
+  constexpr int kCombine = 2 * kWaves * NB * 4 + kWaves * NB * 4 * kHeadDim, kRecordWords = Rec<BITS>::kWords, kTerms = 4;
+  __shared__ __align__(16) float lds[kCombine + kWaves * 2 * kExWords];
+  uint32_t (*ex)[2 * kExWords] = reinterpret_cast<uint32_t (*)[2 * kExWords]>(lds + kCombine);
+  __shared__ float sRowM[kSumHeads], sRowL[kSumHeads];
   __shared__ int sLast;
-  static_assert(sizeof(sMeta) >= 32 * kMaxContextSplits * sizeof(float), "shared in turn");
+  static_assert(kWaves * 2 * kExWords >= kThreads / 16 * kMaxContextSplits, "weights of the join");
   const kvlinc_cache& c = a.cache;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = blockDim.x >> 6, g = lane >> 4;
-  const int pairs = c.B * c.H_kv, split = blockIdx.x / pairs, bh = blockIdx.x - split * pairs;
-  const int b = bh / c.H_kv, gq = a.gq;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int pairs = c.B * c.H_kv, split = blockIdx.x / pairs, bh = blockIdx.x - split * pairs, b = bh / c.H_kv, gq = a.gq;
   const Lengths len = lengths_of(c, b);
-  const int total = len.total(), G = len.groups();
+  const int G = len.groups();
+  // every workgroup of the pair comes to the same number: a split has a group for each wave
+  const int n_splits = max(1, min(a.splits, (G + kWaves - 1) / kWaves));
+  if (split >= n_splits) return;
   const long long row0 = (long long)bh * gq;  // (one token a sequence: rows are heads)
-  unsigned long long* sums = a.sums + bh * a.slots * 16;
-  const bool direct = a.splits == 1;
-  const __amdgpu_buffer_rsrc_t part = buffer_of(a.part + (direct ? 0 : row0 * a.splits * kPartStride), direct ? 0 : (long long)gq * a.splits * kPartBytes);
+  unsigned long long* const sums = a.sums + bh * a.slots * kSumHeads;
 
-  {
-    Rows st;
-    st.subset = (lane & 15) / kRows;
-    st.m = -INFINITY;
-    st.l = st.mid = 0.0f;
+  const Roles lr = make_roles(lane, ex[wave]);
+  const uint32_t* rec0 = c.groups + (long long)bh * c.max_groups * kRecordWords;
+  GroupOrder order(n_splits, split, wave, BITS == 2 && n_splits > 1 ? 2 : 1);
+  int rd = split == 0 ? order.skip : 0, idx = order.group(rd);
+  KeyRegs<BITS> kr;
+  ValueRegs<BITS> vr;
+  if (idx < G) {
+    const uint32_t* src = rec0 + (long long)idx * kRecordWords;
+    load_keys(kr, src, lr);
+    load_values(vr, src, lr);
+  }
+  uint32_t qh[NB][4];  // q of the head this lane builds operands for (head 4 nb + ha, or the last one), channels c0 .. c0 + 7
 #pragma unroll
-    for (int n = 0; n < 8; ++n) st.acc[n] = float4_t{0.f, 0.f, 0.f, 0.f};
-    auto q_row = [&]() __attribute__((always_inline)) { return a.q + (row0 + min(lane & (kRows - 1), gq - 1)) * kHeadDim + 32 * g; };
-    load_query(st, q_row(), lane);
-    st.p = total - 1;
-    st.low = 0;
-    const int n_win = (len.nr + kRawTokens - 1) / kRawTokens, step = waves * a.splits;
-    int item = split * waves + wave;
-    const half_t* k_win = reinterpret_cast<const half_t*>(c.k_res) + (long long)bh * c.R * kHeadDim;
-    const half_t* v_win = reinterpret_cast<const half_t*>(c.v_res) + (long long)bh * c.R * kHeadDim;
-    const int quads = c.R / 4;
-    for (; item < n_win; item += step) {
-      const int t0 = item * kRawTokens;
-      float x[2][4];
-      raw_weights(st, q_row, k_win + t0 * kHeadDim, len.nq + t0, min(len.nr - t0, kRawTokens), 0, lane, x);
-      float sum = 0.0f;
+  for (int nb = 0; nb < NB; ++nb) {
+    const uint4 raw = *reinterpret_cast<const uint4*>(a.q + (row0 + min(nb * 4 + lr.ha, gq - 1)) * kHeadDim + lr.c0);
+    qh[nb][0] = raw.x; qh[nb][1] = raw.y; qh[nb][2] = raw.z; qh[nb][3] = raw.w;
+  }
+  // the spare term row of the weights' exchange regions reads as zero
 #pragma unroll
-      for (int i = 0; i < 8; ++i) sum += x[i / 4][i % 4];
-      sum = column_sum(sum);
-      if (g == 0) put_sum(sums + (long long)(G + item) * 16 + lane, st.m, sum);
-      window_values<2>(st, v_win, quads, t0 / 16, x, lane);
+  for (int k = 0; k < 4; ++k) ex[wave][(k >> 1) * kExWords + (2 * (k & 1) + (lane >> 5)) * kExHead + 96 + (lane & 31)] = 0u;
+  lds_order();
+  WaveState<NB> st;
+  empty_state<NB>(st);
+  const auto leave = [&](int slot, const float (&sum)[NB]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      const float s = row_allsum(sum[nb]);
+      if (lr.jd == 0) put_sum(sums + (long long)slot * kSumHeads + nb * 4 + lr.hd, st.m[nb], s);
     }
-    item -= n_win;
-    const uint32_t* rec0 = c.groups + (long long)bh * c.max_groups * Rec<BITS>::kWords;
-    // (the newest group is left to the code below where its tokens from n_res on take the window's values)
-    const int plain = SLIDING && len.nq % kGroup == 0 && len.nr < kGroup && G > 0 ? G - 1 : G;
-    if (item < G) {
-      Record<BITS> rec;
-      load_key_part<BITS>(rec, rec0 + (long long)item * Rec<BITS>::kWords, lane);
-      load_value_part<BITS>(rec, rec0 + (long long)item * Rec<BITS>::kWords, lane);
-      while (item < plain) {
-        const int at = item * kGroup, count = min(len.nq - at, kGroup);
-        const bool more = item + step < G;
-        const GroupMagnitudes mag = put_meta<BITS>(rec, sMeta[wave], lane);
-        float x[8 / S][4], unit, base;
-        group_scores<BITS, S>(st, rec, sMeta[wave], mag.key_scale, q_row, at, count, count < kGroup, 0, lane, x, unit, base);
-        const uint32_t* next = rec0 + (long long)(more ? item + step : item) * Rec<BITS>::kWords;
-        if (more) load_key_part<BITS>(rec, next, lane);
-        const float sum = column_sum(group_values<BITS, S, false>(st, rec, sMeta[wave], mag.value_exponent, x, unit, base, kGroup, v_win, quads, lane));
-        if (more) load_value_part<BITS>(rec, next, lane);
-        if (g == 0) put_sum(sums + (long long)item * 16 + lane, st.m, sum);
-        item += step;
-      }
-      if (SLIDING && item < G) {
-        const GroupMagnitudes mag = put_meta<BITS>(rec, sMeta[wave], lane);
-        float x[8 / S][4], unit, base;
-        group_scores<BITS, S>(st, rec, sMeta[wave], mag.key_scale, q_row, item * kGroup, kGroup, false, 0, lane, x, unit, base);
-        const float sum = column_sum(group_values<BITS, S, true>(st, rec, sMeta[wave], mag.value_exponent, x, unit, base, len.nr, v_win, quads, lane));
-        if (g == 0) put_sum(sums + (long long)item * 16 + lane, st.m, sum);
-      }
+  };
+  if (split == 0) {
+    const WindowShare sh = {kShare * wave, min(kShare * wave + kShare, len.nr)};
+    if (sh.first < sh.end) {
+      WindowRegs w;
+      request_window(w, c, bh, sh, lr);
+      window_part<NB>(w, qh, sh, lr, st);
+      leave(G + wave, st.l);
     }
+  }
+  const half_t* const v_win = reinterpret_cast<const half_t*>(c.v_res) + (long long)bh * c.R * kHeadDim;
+  float (*sM)[NB * 4] = reinterpret_cast<float (*)[NB * 4]>(lds);
+  float (*sL)[NB * 4] = reinterpret_cast<float (*)[NB * 4]>(lds + kWaves * NB * 4);
+  float (*sAcc)[NB * 4][kHeadDim] = reinterpret_cast<float (*)[NB * 4][kHeadDim]>(lds + 2 * kWaves * NB * 4);
+  // (the newest group is left to the code below where its tokens from n_res on take the window's values)
+  const int plain = SLIDING && len.nq % kGroup == 0 && len.nr < kGroup && G > 0 ? G - 1 : G;
+  while (idx < plain) {
+    const int next = order.group(++rd);
+    const bool more = next < G;
+    const uint32_t* src = rec0 + (long long)(more ? next : idx) * kRecordWords;
+    float sc[NB][8], off[NB], base[NB], sum[NB];
+    qk_phase<NB, BITS, true, kTerms>(kr, min(kGroup, len.nq - idx * kGroup), qh, lr, sc, off);
+    if (more) load_keys(kr, src, lr);
+    update_reference<NB>(sc, off, base, st, kSlack);
+    pv_phase<NB, BITS, false, kTerms>(vr, sc, base, lr, st, kGroup, sum);
+    if (more) load_values(vr, src, lr);
+    leave(idx, sum);
+    idx = next;
+  }
+  if (SLIDING && idx < G) {
+    float sc[NB][8], off[NB], base[NB], sum[NB];
+    qk_phase<NB, BITS, true, kTerms>(kr, kGroup, qh, lr, sc, off);
+    update_reference<NB>(sc, off, base, st, kSlack);
+    pv_phase<NB, BITS, true, kTerms>(vr, sc, base, lr, st, len.nr, sum);
+    leave(idx, sum);
+    pv_window_tail<NB>(v_win, sc, base, len.nr, lr, st, lane, sAcc[wave]);
+  }
 
-    // ---- the waves joined ----
-    const float l = column_sum(st.l), mid = column_sum(st.mid);
-    if (g == 0) { sM[wave][lane] = reference_of(st.m, l); sL[wave][lane] = l; }
+  // ---- the waves joined; one (m, l, numerators) a head ----
 #pragma unroll
-    for (int n = 0; n < 8; ++n) {
-      const float4_t v = st.acc[n];
-      *reinterpret_cast<float4_t*>(&sAcc[wave][lane & 15][16 * n + 4 * g]) = float4_t{v[0] + mid, v[1] + mid, v[2] + mid, v[3] + mid};
-    }
+  for (int nb = 0; nb < NB; ++nb) {
+    const float l = row_allsum(st.l[nb]), pz = row_allsum(st.pz[nb]);
+    const int h = nb * 4 + lr.hd;
+    if (lr.jd == 0) { sM[wave][h] = reference_of(st.m[nb], l); sL[wave][h] = l; }
+#pragma unroll
+    for (int n = 0; n < 8; ++n) sAcc[wave][h][16 * n + lr.jd] = st.acc[nb][n] + pz;
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wave's sums are where everybody sees them
   __syncthreads();
-  const int r = tid >> 4, ch = 8 * (lane & 15);  // 16 lanes a row
-  if (r < gq) {
-    float M = -INFINITY;
-    for (int w = 0; w < waves; ++w)
+  const bool direct = n_splits == 1;
+  const __amdgpu_buffer_rsrc_t part = buffer_of(a.part + (direct ? 0 : row0 * a.splits * kPartStride), direct ? 0 : (long long)gq * a.splits * kPartBytes);
+  const int h = tid >> 4, ch = 8 * (lane & 15);  // 16 lanes a head
+  if (h < gq) {
+    float M = -INFINITY, L = 0.0f, o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int u = 0; u < S; ++u) M = fmaxf(M, sM[w][u * kRows + r]);
-    float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, L = 0.0f;
+    for (int w = 0; w < kWaves; ++w) M = fmaxf(M, sM[w][h]);
     if (M != -INFINITY) {
-      for (int w = 0; w < waves; ++w)
 #pragma unroll
-        for (int u = 0; u < S; ++u) {
-          const int col = u * kRows + r;
-          const float f = __builtin_amdgcn_exp2f(sM[w][col] - M);  // 0 for a column that has seen nothing
-          L = fmaf(f, sL[w][col], L);
-          const float4_t u0 = *reinterpret_cast<const float4_t*>(&sAcc[w][col][ch]), u1 = *reinterpret_cast<const float4_t*>(&sAcc[w][col][ch + 4]);
+      for (int w = 0; w < kWaves; ++w) {
+        const float f = __builtin_amdgcn_exp2f(sM[w][h] - M);  // 0 for a wave without tokens
+        L = fmaf(f, sL[w][h], L);
+        const float4_t u0 = *reinterpret_cast<const float4_t*>(&sAcc[w][h][ch]), u1 = *reinterpret_cast<const float4_t*>(&sAcc[w][h][ch + 4]);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            o[i] = fmaf(f, u0[i], o[i]);
-            o[4 + i] = fmaf(f, u1[i], o[4 + i]);
-          }
+        for (int i = 0; i < 4; ++i) {
+          o[i] = fmaf(f, u0[i], o[i]);
+          o[4 + i] = fmaf(f, u1[i], o[4 + i]);
         }
+      }
     }
     if (direct) {
-      finish_row(o, L, lane, a.out + (row0 + r) * kHeadDim);
-      if ((lane & 15) == 0) { sRowM[r] = M; sRowL[r] = L; }
+      finish_row(o, L, lane, a.out + (row0 + h) * kHeadDim);
+      if ((lane & 15) == 0) { sRowM[h] = M; sRowL[h] = L; }
     } else {
-      const int place = (r * a.splits + split) * kPartBytes;
+      const int place = (h * a.splits + split) * kPartBytes;
       if ((lane & 15) == 0) store2(part, place, M, L);
       store4(part, place + 16 + 4 * ch, o[0], o[1], o[2], o[3]);
       store4(part, place + 32 + 4 * ch, o[4], o[5], o[6], o[7]);
@@ -163,53 +161,77 @@ __global__ __launch_bounds__(64 * kMaxWaves, 2) void decode_mass_kernel(MassCall
   if (!direct) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-    if (tid == 0) sLast = __hip_atomic_fetch_add(c.split_done + bh, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM) == a.splits - 1;
+    if (tid == 0) sLast = __hip_atomic_fetch_add(c.split_done + bh, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM) == n_splits - 1;
     __syncthreads();
     if (!__builtin_amdgcn_readfirstlane(sLast)) return;
-    if (r < gq) {
+  }
+
+  // ---- the mass: 8 lanes a slot, a head each, kSlotsAhead slots under way, the first of them requested together with the splits' results ----
+  const int head = tid & (kSumHeads - 1), n_win = (len.nr + kShare - 1) / kShare, entries = G + n_win;
+  const long long at = (long long)bh * (c.max_groups + 1);
+  float2 s[kSlotsAhead];
+  float before[kSlotsAhead];
+  const auto request = [&](int j0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < kSlotsAhead; ++i) {
+      const int j = j0 + i * (kThreads / kSumHeads);
+      s[i] = make_float2(0.0f, 0.0f);
+      before[i] = 0.0f;
+      if (j < entries && head < NB * 4) s[i] = ld_coherent2(reinterpret_cast<const float*>(sums + (long long)j * kSumHeads + head));
+      if (j < G && a.mass != nullptr) before[i] = a.mass[at + j];
+    }
+  };
+  request(tid / kSumHeads);
+  if (!direct) {
+    if (h < gq) {
       float o[8], L, M;
-      join_row(part, r * a.splits * kPartBytes, a.splits, reinterpret_cast<float*>(&sMeta[0][0]) + kMaxContextSplits * r, lane, o, L, M);
-      finish_row(o, L, lane, a.out + (row0 + r) * kHeadDim);
-      if ((lane & 15) == 0) { sRowM[r] = M; sRowL[r] = L; }
+      join_row(part, h * a.splits * kPartBytes, n_splits, reinterpret_cast<float*>(&ex[0][0]) + kMaxContextSplits * h, lane, o, L, M);
+      finish_row(o, L, lane, a.out + (row0 + h) * kHeadDim);
+      if ((lane & 15) == 0) { sRowM[h] = M; sRowL[h] = L; }
     }
     if (tid == 0) c.split_done[bh] = 0;
   }
   __syncthreads();
-
-  // ---- the mass: 16 lanes a slot, a column each ----
-  const int col = lane & 15, row = col % kRows;
-  const bool used = row < gq;
-  const float M = used ? sRowM[row] : 0.0f, L = used ? sRowL[row] : 0.0f;
+  const bool used = head < gq;
+  const float M = used ? sRowM[head] : 0.0f, L = used ? sRowL[head] : 0.0f;
   const float inv = L != 0.0f ? 1.0f / L : 0.0f;
-  const int n_win = (len.nr + kRawTokens - 1) / kRawTokens;
-  const long long at = (long long)bh * (c.max_groups + 1);
-  for (int j = tid >> 4; j <= G; j += blockDim.x >> 4) {
-    const int parts = j < G ? 1 : n_win;
-    float w = 0.0f;
-    for (int i = 0; i < parts; ++i) {
-      const ColumnSum s = get_sum(sums + (long long)(j + i) * 16 + col);
-      if (used && s.sum != 0.0f) w = fmaf(s.sum * inv, __builtin_amdgcn_exp2f(s.reference - M), w);
+  const auto weight_of = [&](float2 v) __attribute__((always_inline)) {
+    float w = used && v.y != 0.0f ? v.y * inv * __builtin_amdgcn_exp2f(v.x - M) : 0.0f;
+    w += dpp_f<kQuadSwap1>(w);
+    w += dpp_f<kQuadSwap2>(w);
+    return w + dpp_f<kHalfMirror>(w);
+  };
+  float* const sWindow = lds;  // (the combine buffer is read no more)
+  for (int j0 = tid / kSumHeads;; request(j0)) {
+#pragma unroll
+    for (int i = 0; i < kSlotsAhead; ++i) {
+      const int j = j0 + i * (kThreads / kSumHeads);
+      const float w = weight_of(s[i]);
+      if (head != 0 || j >= entries) continue;
+      if (j < G) a.mass_out[at + j] = fmaf(a.decay, before[i], w);
+      else sWindow[j - G] = w;
     }
-    w += dpp_f<kRowRor1>(w);
-    w += dpp_f<kRowRor2>(w);
-    w += dpp_f<kRowRor4>(w);
-    w += dpp_f<kRowRor8>(w);
-    if (col == 0) a.mass_out[at + j] = a.mass != nullptr ? fmaf(a.decay, a.mass[at + j], w) : w;
+    j0 += kSlotsAhead * (kThreads / kSumHeads);
+    if (j0 - tid / kSumHeads >= entries) break;  // (the same for the whole workgroup)
+  }
+  __syncthreads();
+  if (tid == 0) {
+    float w = 0.0f;
+    for (int i = 0; i < n_win; ++i) w += sWindow[i];
+    a.mass_out[at + G] = a.mass != nullptr ? fmaf(a.decay, a.mass[at + G], w) : w;
   }
 }
 
 }  // namespace
 
-template <int BITS, int S>
-static void launch_of(const MassCall& a, dim3 grid, int waves, hipStream_t stream) {
-  if ((a.cache.flags & KVLINC_FLAG_SLIDING_VALUES) != 0) hipLaunchKernelGGL((decode_mass_kernel<BITS, S, true>), grid, dim3(64 * waves), 0, stream, a);
-  else hipLaunchKernelGGL((decode_mass_kernel<BITS, S, false>), grid, dim3(64 * waves), 0, stream, a);
-}
-
-int launch_decode_mass(const MassCall& a, int waves, hipStream_t stream) {
+int launch_decode_mass(const MassCall& a, hipStream_t stream) {
   const dim3 grid((unsigned)((long long)a.cache.B * a.cache.H_kv * a.splits));
-  if (a.cache.bits == 2) a.gq <= 4 ? launch_of<2, 4>(a, grid, waves, stream) : launch_of<2, 2>(a, grid, waves, stream);
-  else a.gq <= 4 ? launch_of<4, 4>(a, grid, waves, stream) : launch_of<4, 2>(a, grid, waves, stream);
+  const bool sliding = (a.cache.flags & KVLINC_FLAG_SLIDING_VALUES) != 0;
+  void (*kernel)(MassCall) = a.cache.bits == 4 ? (a.gq > 4 ? (sliding ? decode_mass_kernel<2, true, 4> : decode_mass_kernel<2, false, 4>)
+                                                           : (sliding ? decode_mass_kernel<1, true, 4> : decode_mass_kernel<1, false, 4>))
+                                               : (a.gq > 4 ? (sliding ? decode_mass_kernel<2, true, 2> : decode_mass_kernel<2, false, 2>)
+                                                           : (sliding ? decode_mass_kernel<1, true, 2> : decode_mass_kernel<1, false, 2>));
+  hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, stream, a);
   return hipGetLastError() == hipSuccess ? KVLINC_OK : KVLINC_EHIP;
 }
 

@@ -106,7 +106,7 @@ __device__ __forceinline__ void lds_order() { asm volatile("" ::: "memory"); }
 // 8-byte chunks -- chunk u of (head, quarter g) = bytes 8 u .. 8 u + 7 = positions 64 (u / 2) + 16 g + 8 (u % 2) + 0..7 --
 // and handed over through LDS: the builder of (head h, quarter g, chunk u) writes its three terms at
 // ex[160 h + 32 term + 2 (4 g + u)], the holder of (head h, term, quarter g) reads 8 words at ex[160 h + 32 term + 8 g].
-// Term 3 of every head stays zero.  Word 128 of a head carries the block exponent where builder and holder differ.
+// Term 3 of every head stays zero where there are three.  Word 128 of a head carries the block exponent where builder and holder differ.
 constexpr int kExHead = 160;              // words per head in an exchange region (stride 640 B: two heads cover all banks)
 constexpr int kExWords = 4 * kExHead;     // one region: 4 heads
 constexpr int kExExp = 128;               // word of the block exponent
@@ -149,15 +149,16 @@ __device__ __forceinline__ Roles make_roles(int lane, uint32_t* ex_wave) {
   return r;
 }
 
-// x[0..7] as three FP8 terms: with sc = 2^e (sc_bits its binary32 pattern, e chosen so that |x| / sc < 256),
+// x[0..7] as three FP8 terms (or more): with sc = 2^e (sc_bits its binary32 pattern, e chosen so that |x| / sc < 256),
 // t_k = fp8((x - what t_0 .. t_{k-1} stand for) / (sc / 16^k)), round to nearest even.  Every residual is exact in
 // binary32 (the term agrees with it in its leading bits).  t[k][v] holds values 4 v .. 4 v + 3, lowest byte first.
-__device__ __forceinline__ void split_fp8x3(const float (&x)[8], uint32_t sc_bits, uint32_t (&t)[3][2]) {
+template <int TERMS>
+__device__ __forceinline__ void split_fp8(const float (&x)[8], uint32_t sc_bits, uint32_t (&t)[TERMS][2]) {
   float r[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) r[i] = x[i];
 #pragma unroll
-  for (int k = 0; k < 3; ++k) {
+  for (int k = 0; k < TERMS; ++k) {
     const float sc = as_f32(sc_bits - ((uint32_t)(4 * k) << 23));
 #pragma unroll
     for (int v = 0; v < 2; ++v) {
@@ -167,7 +168,7 @@ __device__ __forceinline__ void split_fp8x3(const float (&x)[8], uint32_t sc_bit
       w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, r[4 * v + 2], r[4 * v + 3], sc, true);
       const uint32_t bits = __builtin_bit_cast(uint32_t, w);
       t[k][v] = bits;
-      if (k < 2) {
+      if (k < TERMS - 1) {
         const float2_t f0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(bits, sc, false);
         const float2_t f1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(bits, sc, true);
         r[4 * v] -= f0[0]; r[4 * v + 1] -= f0[1];
@@ -179,14 +180,16 @@ __device__ __forceinline__ void split_fp8x3(const float (&x)[8], uint32_t sc_bit
 
 // Biased binary32 exponent eb of the largest magnitude of a block, from its bit pattern (kept away from the low end of
 // the range), for sc = 2^(eb - 127 - 7): |x| / sc < 256, inside FP8's range.  Row `term` then carries the block scale
-// byte eb - 7 - 4 term.
+// byte eb - 7 - 4 term.  (TOP for 7: |x| / sc < 2^(TOP + 1).)
 __device__ __forceinline__ uint32_t block_exponent(uint32_t mx_bits) { return max(mx_bits, as_bits(0x1p-100f)) >> 23; }
-__device__ __forceinline__ uint32_t block_scale_bits(uint32_t eb) { return (eb - 7u) << 23; }
+template <uint32_t TOP = 7u>
+__device__ __forceinline__ uint32_t block_scale_bits(uint32_t eb) { return (eb - TOP) << 23; }
 
-// Builder side of the hand-over: the three terms of this lane's chunk; holder side: the 8 operand registers.
-__device__ __forceinline__ void put_terms(uint32_t* ex, int at, const uint32_t (&t)[3][2]) {
+// Builder side of the hand-over: the terms of this lane's chunk; holder side: the 8 operand registers.
+template <int TERMS>
+__device__ __forceinline__ void put_terms(uint32_t* ex, int at, const uint32_t (&t)[TERMS][2]) {
 #pragma unroll
-  for (int k = 0; k < 3; ++k) *reinterpret_cast<u32x2_t*>(ex + at + 32 * k) = u32x2_t{t[k][0], t[k][1]};
+  for (int k = 0; k < TERMS; ++k) *reinterpret_cast<u32x2_t*>(ex + at + 32 * k) = u32x2_t{t[k][0], t[k][1]};
 }
 __device__ __forceinline__ v8i_t get_operand(const uint32_t* ex, int at) {
   const u32x4_t a = *reinterpret_cast<const u32x4_t*>(ex + at), b = *reinterpret_cast<const u32x4_t*>(ex + at + 4);
@@ -267,6 +270,11 @@ __device__ __forceinline__ void empty_state(WaveState<NB>& st) {
   }
 }
 
+template <int TERMS>
+__device__ __forceinline__ float sum_of_terms(float4_t d) {
+  return TERMS == 3 ? (d[0] + d[1]) + d[2] : (d[0] + d[1]) + (d[2] + d[3]);
+}
+
 // q K^T of one group for all heads (Alg. 1 line 7): sc[nb][n] = q.k of head 4 nb + hd, token 16 n + jd (the factor
 // log2(e) / sqrt(d) enters with the reference maximum, see exponent()).
 // qh = this lane's 8 query values (head 4 nb + ha, channels c0 ..) in binary16 pairs.
@@ -275,9 +283,15 @@ __device__ __forceinline__ void empty_state(WaveState<NB>& st) {
 // the constant).
 // EXACT_OFFSETS: zero-points and scales each for themselves, in place of mid-points rounded to binary16 (2^-12 of them: keys with an offset of
 // 300 in some channels left outputs 1.5e-2 off, so 3e-4).
-template <int NB, int BITS, bool EXACT_OFFSETS = false>
+// TERMS: of query times key scale, each 4 bits of it: three for outputs (2^-12), four, in the spare row, where the weights are results themselves (2^-16).
+// A matrix instruction drops what lies more than 13 bits below the exponent of its largest product (measured).  With |x| / sc < 256 that is, now and
+// then, a part of a small channel's first term: 2^-14 of a score, of no account beside three terms.  With |x| / sc < 8 and FP8's smallest step of 2^-9
+// nothing is dropped: a group's sum of weights 1.3e-5 off -> 4e-7 (a fifth term, in an instruction of its own: 1.5e-7 for 4 to 6 % of the time).
+template <int NB, int BITS, bool EXACT_OFFSETS = false, int TERMS = 3>
 __device__ __forceinline__ void qk_phase(const KeyRegs<BITS>& g, int valid, const uint32_t (&qh)[NB][4], const Roles& lr,
                                          float (&sc)[NB][8], float (&off)[NB]) {
+  static_assert(TERMS == 3 || TERMS == 4, "rows of the matrix instruction");
+  constexpr uint32_t kTop = TERMS == 3 ? 7u : 2u;  // |x| / sc < 2^(kTop + 1)
   const uint32_t S[4] = {g.ks.x, g.ks.y, g.ks.z, g.ks.w};
   const uint32_t Z[4] = {g.kz.x, g.kz.y, g.kz.z, g.kz.w};
   v8i_t A[NB];
@@ -306,8 +320,8 @@ __device__ __forceinline__ void qk_phase(const KeyRegs<BITS>& g, int valid, cons
     const uint32_t eb = block_exponent(xrow_umax(quad_umax(as_bits(mx))));  // over the 128 channels of the head
     if constexpr (EXACT_OFFSETS) bz = fmaf(bs, Rec<BITS>::kCentre, bz);
     bz = xrow_allsum(quad_allsum(bz));
-    uint32_t t[3][2];
-    split_fp8x3(x, block_scale_bits(eb), t);
+    uint32_t t[TERMS][2];
+    split_fp8(x, block_scale_bits<kTop>(eb), t);
     // (two head blocks: the second one goes through the other exchange region, so that one hand-over serves both)
     put_terms(nb == 0 ? lr.ex_qk : lr.ex_pv, lr.wq, t);
     if (NB == 1) {
@@ -315,7 +329,7 @@ __device__ __forceinline__ void qk_phase(const KeyRegs<BITS>& g, int valid, cons
       A[nb] = get_operand(lr.ex_qk, lr.rd);
       lds_order();
     }
-    scale_a[nb] = (int)eb - 7 - 4 * lr.ua;
+    scale_a[nb] = (int)eb - (int)kTop - 4 * lr.ua;
     // the head's zero-point term, from a lane that holds head hd in the operand role (lane 4 hd)
     off[nb] = __builtin_bit_cast(float, __builtin_amdgcn_ds_bpermute(16 * lr.hd, __builtin_bit_cast(int, bz)));
   }
@@ -338,7 +352,7 @@ __device__ __forceinline__ void qk_phase(const KeyRegs<BITS>& g, int valid, cons
       for (int hf = 0; hf < 2; ++hf) dq[2 * m + hf] = mfma_codes(A[0], w[2 * hf], w[2 * hf + 1], zero, scale_a[0], lr.pick);
     }
 #pragma unroll
-    for (int n = 0; n < 8; ++n) sc[0][n] = (dq[n][0] + dq[n][1]) + dq[n][2];
+    for (int n = 0; n < 8; ++n) sc[0][n] = sum_of_terms<TERMS>(dq[n]);
   }
 #pragma unroll
   for (int m = 0; m < 4; ++m) {
@@ -350,7 +364,7 @@ __device__ __forceinline__ void qk_phase(const KeyRegs<BITS>& g, int valid, cons
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
           const float4_t d = mfma_codes(A[nb], w[2 * hf], w[2 * hf + 1], zero, scale_a[nb], lr.pick);
-          sc[nb][2 * m + hf] = (d[0] + d[1]) + d[2];
+          sc[nb][2 * m + hf] = sum_of_terms<TERMS>(d);
         }
     } else {
       const uint32_t wl[4] = {g.kw[4 + m].x, g.kw[4 + m].y, g.kw[4 + m].z, g.kw[4 + m].w};  // low plane
@@ -364,7 +378,7 @@ __device__ __forceinline__ void qk_phase(const KeyRegs<BITS>& g, int valid, cons
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
           d[hf][nb] = mfma_codes(A[nb], wl[2 * hf], wl[2 * hf + 1], d[hf][nb], scale_a[nb], lr.pick);
-          sc[nb][2 * m + hf] = (d[hf][nb][0] + d[hf][nb][1]) + d[hf][nb][2];
+          sc[nb][2 * m + hf] = sum_of_terms<TERMS>(d[hf][nb]);
         }
     }
   }
@@ -423,10 +437,11 @@ __device__ __forceinline__ void update_reference(float (&sc)[NB][8], const float
 }
 
 // p = 2^(x - m), its sums, and E V of one group (Alg. 1 lines 9-10).  MASKED: tokens from `fp16_from` on count in the
-// sums of p but not in E V: their values are taken from the fp16 window (pv_window_tail).
-template <int NB, int BITS, bool MASKED = false>
+// sums of p but not in E V: their values are taken from the fp16 window (pv_window_tail).  group_sum: NULL, or where this lane's sums of the group's p go.
+// QK_TERMS: those of qk_phase, the fourth of which lies where the weights' spare row has to be zero if two head blocks share the regions.
+template <int NB, int BITS, bool MASKED = false, int QK_TERMS = 3>
 __device__ __forceinline__ void pv_phase(const ValueRegs<BITS>& g, const float (&sc)[NB][8], const float (&base)[NB], const Roles& lr,
-                                         WaveState<NB>& st, int fp16_from = kGroup) {
+                                         WaveState<NB>& st, int fp16_from = kGroup, float* group_sum = nullptr) {
   const uint32_t SZ[8] = {g.sz[0].x, g.sz[0].y, g.sz[0].z, g.sz[0].w, g.sz[1].x, g.sz[1].y, g.sz[1].z, g.sz[1].w};
   v8i_t A[NB];
   int scale_a[NB];
@@ -436,22 +451,25 @@ __device__ __forceinline__ void pv_phase(const ValueRegs<BITS>& g, const float (
   for (int n = 0; n < 8; ++n) mid[n] = fmaf((float)as_h2(SZ[n])[0], Rec<BITS>::kCentre, (float)as_h2(SZ[n])[1]);
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
-    float y[8], mx = 0.0f;
+    float y[8], mx = 0.0f, sum = 0.0f;
 #pragma unroll
     for (int n = 0; n < 8; ++n) {
       const float p = __builtin_amdgcn_exp2f(exponent(sc[nb][n], base[nb]));
       const half2_t sz = as_h2(SZ[n]);
       st.l[nb] += p;
+      sum += p;
       const bool coded = !MASKED || 16 * n + lr.jd < fp16_from;
       y[n] = coded ? fmaf(p, (float)sz[0], 0.0f) : 0.0f;  // p * value scale: the weight of the token's codes
       st.pz[nb] = coded ? fmaf(p, mid[n], st.pz[nb]) : st.pz[nb];
       mx = fmaxf(mx, y[n]);
     }
+    if (group_sum != nullptr) group_sum[nb] = sum;
     const uint32_t eb = block_exponent(row_umax(as_bits(mx)));  // over the 128 tokens of the head
     uint32_t t[3][2];
-    split_fp8x3(y, block_scale_bits(eb), t);
+    split_fp8(y, block_scale_bits(eb), t);
     uint32_t* region = nb == 0 ? lr.ex_pv : lr.ex_qk;
     put_terms(region, lr.wp, t);
+    if constexpr (NB == 2 && QK_TERMS > 3) *reinterpret_cast<u32x2_t*>(region + lr.wp + 96) = u32x2_t{0u, 0u};
     region[kExHead * lr.hd + kExExp] = eb;  // the same value from the 16 lanes of the row
     if (NB == 1) {
       lds_order();

@@ -34,8 +34,10 @@ def rounding(y, dtype):
 # ---- accumulated attention weight ---------------------------------------------------------------------------------------------------
 # Tolerance of a slot's weight.  A score q K_t = sum_c q_c s_c (code_c - centre) + sum_c q_c (z_c + centre s_c), with A_t = sum_c |q_c| (levels s_c +
 # |z_c|) above either sum of its terms' magnitudes, is off by
-#   - the products q_c s_c, held in two binary16 numbers: 2^-22 of each;
-#   - two sums of 128 terms in binary32, a rounding (or truncation, 2^-23) each: 128 * 2^-23 A_t at most each;
+#   - the products q_c s_c, held in two binary16 numbers, 2^-22 of each, or in four FP8 numbers, 2^-16 of each: with |code - centre| at most half of the
+#     levels 2^-17 A_t;
+#   - two sums of 128 terms in binary32, a rounding (or truncation, 2^-23) each: 128 * 2^-23 at most, of A_t / 2 for the codes' (the four FP8 terms' sums
+#     come to that together), of A_t in 10 roundings for the common part's: less than 2^-17 A_t and 2^-19 A_t;
 # so by d = 2^-15 A_t / sqrt(128) at most.  Exponents are binary32 numbers of size E = log2(e) max |score| + 16 (the reference's head room), rounded a few
 # times on their way (score, reference, logarithm of a sum, the difference of two): 8 * 2^-24 E ln 2; the exponential and the logarithm themselves
 # 2^-22.  An error d of the scores moves a normalised weight by a factor of e^(2 d) at most.  Sums of n weights, none negative: n * 2^-24.
