@@ -302,6 +302,15 @@ class KVLincRotary:
 
 
 _NOTHING = contextlib.nullcontext()
+_ROW_TYPES = {}
+
+
+def _row_types():
+    """KVLINC_F16, _BF16 or _F32 of torch's types."""
+    if not _ROW_TYPES:
+        import torch
+        _ROW_TYPES.update({torch.float16: KVLINC_F16, torch.bfloat16: KVLINC_BF16, torch.float32: KVLINC_F32})
+    return _ROW_TYPES
 
 
 class KVLincCache:
@@ -539,51 +548,62 @@ class KVLincCache:
         bytes with contiguous rows (a projection's output [B, T, heads, 128] transposed, say).  n_new: [B] int32 or None (all T); rows beyond it
         are left as they are (zero in outputs made here).  Row i is at position first[b] + depth[b, i] (None: 0; i) and, if counted, the tokens in
         the cache."""
-        import torch
-        types = {torch.float16: KVLINC_F16, torch.bfloat16: KVLINC_BF16, torch.float32: KVLINC_F32}
+        types = _row_types()
         if not isinstance(plan, KVLincRotary):
             raise KVLincError("plan has to be a KVLincRotary")
-        if plan.freq.device != self._device:
-            raise KVLincError("the plan is on %s, the cache on %s" % (plan.freq.device, self._device))
-        heads, given = (self.H_q, self.H_kv, self.H_kv), (q, k, v)
-        some = next((t for t in given if t is not None), None)
-        if not torch.is_tensor(some) or some.dim() != 4 or some.dtype not in types:
+        dev, B = self._device, self.B
+        if plan.freq.device != dev:
+            raise KVLincError("the plan is on %s, the cache on %s" % (plan.freq.device, dev))
+        some = q if q is not None else k if k is not None else v
+        taken = getattr(some, "dtype", None)
+        if taken not in types or some.dim() != 4:
             raise KVLincError("q, k or v is needed, a tensor of shape [B, heads, T, 128] and type %s" % ", ".join(str(t) for t in types))
         T = some.shape[2]
         if T < 1:
             raise KVLincError("there are no rows")
-        outs = [q_out, k_out, v_out]
         if dtype is None:
-            dtype = next((t.dtype for t in outs if torch.is_tensor(t)), torch.float16)
+            given = q_out if q_out is not None else k_out if k_out is not None else v_out
+            dtype = next(iter(types)) if given is None else getattr(given, "dtype", None)
         if dtype not in types:
             raise KVLincError("dtype has to be one of %s" % ", ".join(str(t) for t in types))
-        for t, out, h, name in zip(given, outs, heads, "qkv"):
-            shape = (self.B, h, T, 128)
+        rows, missing = [None, None, None], False
+        for i, t, out, h in ((0, q, q_out, self.H_q), (1, k, k_out, self.H_kv), (2, v, v_out, self.H_kv)):
             if t is None:
                 if out is not None:
-                    raise KVLincError("%s_out without %s" % (name, name))
+                    raise KVLincError("%s_out without %s" % ("qkv"[i], "qkv"[i]))
                 continue
-            if not torch.is_tensor(t) or t.dtype != some.dtype or t.shape != shape:
-                raise KVLincError("%s has to be a %s tensor of shape %s" % (name, some.dtype, shape))
-            if t.device != self._device:
-                raise KVLincError("%s is on %s, the cache on %s" % (name, t.device, self._device))
-            if t.stride(3) != 1:
-                raise KVLincError("the rows of %s have to be contiguous" % name)
-            if out is not None:
-                self._tensor(out, name + "_out", shape, dtype)
-        for t, name, shape in ((n_new, "n_new", (self.B,)), (first, "first", (self.B,)), (depth, "depth", (self.B, T))):
-            if t is not None:
-                self._tensor(t, name, shape, torch.int32)
-        with self._on(stream, plan.freq, n_new, first, depth, *given, *outs):
-            make = torch.empty if n_new is None else torch.zeros
-            rows = [None, None, None]
-            for i, (t, h) in enumerate(zip(given, heads)):
-                if t is not None:
-                    if outs[i] is None:
-                        outs[i] = make((self.B, h, T, 128), dtype=dtype, device=self._device)
-                    strides = (s if n > 1 else 0 for s, n in zip(t.stride(), t.shape[:3]))
-                    rows[i] = RowsStruct(t.data_ptr(), outs[i].data_ptr(), *strides)
-            rc = kvlinc_rotary(self, plan.struct, *rows, T, n_new, first, depth, bool(counted), types[some.dtype], types[dtype], stream)
+            shape = (B, h, T, 128)
+            if getattr(t, "dtype", None) is not taken or t.shape != shape:
+                raise KVLincError("%s has to be a %s tensor of shape %s" % ("qkv"[i], taken, shape))
+            if t.device != dev:
+                raise KVLincError("%s is on %s, the cache on %s" % ("qkv"[i], t.device, dev))
+            of_sequence, of_head, of_token, of_channel = t.stride()
+            if of_channel != 1:
+                raise KVLincError("the rows of %s have to be contiguous" % "qkv"[i])
+            to = 0
+            if out is None:
+                missing = True
+            else:
+                self._tensor(out, "qkv"[i] + "_out", shape, dtype)
+                to = out.data_ptr()
+            rows[i] = RowsStruct(t.data_ptr(), to, of_sequence if B > 1 else 0, of_head if h > 1 else 0, of_token if T > 1 else 0)
+        if n_new is not None:
+            self._tensor(n_new, "n_new", (B,), self.n_quant.dtype)
+        if first is not None:
+            self._tensor(first, "first", (B,), self.n_quant.dtype)
+        if depth is not None:
+            self._tensor(depth, "depth", (B, T), self.n_quant.dtype)
+        outs = [q_out, k_out, v_out]
+        with self._on(stream, plan.freq, n_new, first, depth, q, k, v, q_out, k_out, v_out):
+            if missing:
+                import torch
+                make = torch.empty if n_new is None else torch.zeros
+                for i, h in enumerate((self.H_q, self.H_kv, self.H_kv)):
+                    if rows[i] is not None and outs[i] is None:
+                        outs[i] = make((B, h, T, 128), dtype=dtype, device=dev)
+                        rows[i].out = outs[i].data_ptr()
+            rc = lib.kvlinc_rotary(self.struct, plan.struct, rows[0], rows[1], rows[2], T, _ptr(n_new), _ptr(first), _ptr(depth), 1 if counted else 0,
+                                   types[taken], types[dtype], _stream(stream))
         if rc != KVLINC_OK:
             raise KVLincError("kvlinc_rotary: " + kvlinc_strerror(rc))
         return tuple(outs)

@@ -162,12 +162,12 @@ def test_more_rows_than_a_grid_holds_are_refused():
 def test_workspaces():
     c = plain(max_groups=64)
     need = kb.kvlinc_decode_mass_workspace_bytes(c)
-    assert need >= 2 * 2 * 68 * 128
+    assert need >= 2 * 2 * 68 * 64
     for over in (dict(ws=None), dict(ws=0x800008), dict(size=need - 1)):
         assert decode(c, **over) == kb.KVLINC_EWORKSPACE
     assert decode(c, out=0x200000, mass_out=0x400000, size=0) == kb.KVLINC_EWORKSPACE  # (both in place: allowed)
     # a bound makes it no smaller than what any sequence of the cache needs
-    assert kb.kvlinc_decode_mass_workspace_bytes(c, 1) >= 2 * 2 * 68 * 128
+    assert kb.kvlinc_decode_mass_workspace_bytes(c, 1) >= 2 * 2 * 68 * 64
     need = kb.kvlinc_attention_mass_workspace_bytes(c, 4)
     assert need == 4 * 2 * 2 * 16 * (65 + 1)  # rows of a KV head: 16; a number for each of them and slot, and one more
     for over in (dict(ws=None), dict(ws=0x800008), dict(size=need - 1)):
