@@ -129,7 +129,7 @@ size_t kvlinc_cache_evict_workspace_bytes(const kvlinc_cache* cache);
  *   from           the cache
  *   to             where the kept groups, the window and the counters go: from itself (in place; the same descriptor in all of its buffers), or a cache
  *                  of the same B, H_q, H_kv, R, bits and flags that shares no memory with it, and has room for `limit` groups, or as many
- *                  as from has room for.  Storage of it beyond its counters may be overwritten; status, split_done stay as they are.
+ *                  as from has room for.  Storage of it beyond its counters may be overwritten; status stays as it is, split_done, which may be counted in, zero.
  *   mass           [B, H_kv, from->max_groups + 1] binary32
  *   mass_out       [B, H_kv, to->max_groups + 1] binary32: the mass of what is kept, the window's behind it, and zeros to the end.  May be mass
  *                  where both have room for as many groups.

@@ -97,7 +97,7 @@ MassCall make_mass(const kvlinc_cache& c, const kvlinc_half* q, const float* mas
 }
 
 // ---- eviction ----
-size_t evict_words(const kvlinc_cache& c) { return (size_t)(pairs_of(c) * (c.max_groups + 2)); }
+size_t evict_words(const kvlinc_cache& c) { return evicts_in_one_launch(c) ? 4 : (size_t)(pairs_of(c) * (c.max_groups + 2)); }
 constexpr int kBuffers = 5;  // those of a cache that eviction writes
 void buffers_of(const kvlinc_cache& c, Span (&s)[kBuffers]) {
   const size_t pairs = (size_t)pairs_of(c), window = pairs * c.R * kHeadDim * 2;
@@ -262,10 +262,13 @@ int kvlinc_cache_evict(const kvlinc_cache* from, const kvlinc_cache* to, const f
   a.offset = offset;
   a.offset_out = offset_out;
   a.kept = kept;
-  a.stride = from->max_groups;
-  a.source = static_cast<int32_t*>(workspace);
-  a.count = a.source + pairs_of(*from) * a.stride;
   a.in_place = in_place;
+  a.counted = in_place || mass == mass_out;
+  if (!evicts_in_one_launch(*from)) {
+    a.stride = from->max_groups;
+    a.source = static_cast<int32_t*>(workspace);
+    a.count = a.source + pairs_of(*from) * a.stride;
+  }
   return launch_evict(a, static_cast<hipStream_t>(stream));
 }
 

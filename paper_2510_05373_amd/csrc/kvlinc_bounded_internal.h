@@ -48,6 +48,9 @@ int launch_decode_mass(const MassCall& a, hipStream_t stream);
 int launch_attention_mass(const MassCall& a, hipStream_t stream);
 
 // ---- eviction ----
+// Groups of a pair that one wave holds the keys of; and the pairs of a sequence are counted in half a word.
+constexpr int kEvictOneLaunch = 1024;
+inline bool evicts_in_one_launch(const kvlinc_cache& c) { return c.max_groups <= kEvictOneLaunch && c.H_kv < (1 << 15); }
 struct EvictCall {
   kvlinc_cache from, to;
   const float* mass;
@@ -56,10 +59,12 @@ struct EvictCall {
   const int32_t* offset;
   int32_t* offset_out;
   int32_t* kept;
+  // where a launch of its own selects:
   int32_t* source;  // [B H_kv][stride] slots of the kept groups
   int32_t* count;   // [B H_kv][2] how many, and the first that has another slot than before
   long long stride;
   bool in_place;
+  bool counted;     // something is written over what all workgroups of a pair read
 };
 int launch_evict(const EvictCall& a, hipStream_t stream);
 

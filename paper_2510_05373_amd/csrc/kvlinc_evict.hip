@@ -1,9 +1,11 @@
 // Eviction: which groups of a (sequence, KV head) stay, by their mass, and their records moved together.
 //
-// Two launches.  The first has a workgroup for each pair: the mass of the m-th largest group is found by four counts of its bits, 8 at a time from the
-// top (as an unsigned number that orders like the mass), so that any number of groups takes five reads of their mass; those above it stay, and of those
-// equal to it the first ones.  It writes the list of what stays, in order, and the mass that goes with it.  The second moves records.  Into another
-// cache: a workgroup a record.  In place: a lane has 16 bytes of every record of a pair, and moves them from slot to slot in order.  A slot's
+// A group's key is an unsigned number that orders like its mass.  Caches of up to 1024 groups: one launch.  Every workgroup selects for itself, in one wave
+// that holds all keys of the pair: the largest threshold that enough keys reach is found bit by bit from the top, a comparison and a count of lanes for
+// every 64 keys, no memory and no barrier; those above it stay, and of those equal to it the first ones.  Nothing that it reads (mass, counters) is
+// written before all workgroups of the pair, or the sequence, have read it: whoever is the last to say so writes.  Larger caches: a launch before has
+// a workgroup for each pair that finds the threshold by four counts of the keys' bits, 8 at a time, five reads of the mass, and leaves the list of what stays.
+// Into another cache: a wave a record.  In place: a lane has 16 bytes of every record of a pair, and moves them from slot to slot in order.  A slot's
 // source is never below it, so what the lane reads has not been written yet, whatever other lanes have done: no workgroup waits for another.
 // Bound: bytes of the records that move, in and out.
 #include <hip/hip_runtime.h>
@@ -126,7 +128,99 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(EvictCall a) {
   }
 }
 
-// Counters of a sequence, by one thread of its first KV head: what the first launch has read may change now.
+// ---- selection by one wave ----
+constexpr int kMostKeys = kEvictOneLaunch, kKeyBlocks = kMostKeys / 64;
+struct Choice {
+  int n, cut, first_moved;  // groups, how many stay, the first slot with another group than before (cut: none)
+  float mass[kKeyBlocks + 1];  // of group 64 k + lane (n: the window's)
+  uint64_t stay[kKeyBlocks];
+};
+__device__ __forceinline__ void choose(Choice& c, const EvictCall& a, long long pair, int lane) {
+  const float* mass = a.mass + pair * (a.from.max_groups + 1);
+  const int most = (int)a.from.max_groups;
+#pragma unroll
+  for (int k = 0; k <= kKeyBlocks; ++k) c.mass[k] = 64 * k <= most ? mass[min(64 * k + lane, most)] : 0.0f;
+  c.n = lengths_of(a.from, (int)(pair / a.from.H_kv)).groups();
+  const int n = c.n, newest = n - a.last;
+  c.cut = n > a.limit ? a.keep : n;
+  c.first_moved = c.cut;
+  if (n <= a.limit) {
+#pragma unroll
+    for (int k = 0; k < kKeyBlocks; ++k) c.stay[k] = __builtin_amdgcn_ballot_w64(64 * k + lane < n);
+    return;
+  }
+  const auto of_choice = [&](int j) __attribute__((always_inline)) { return j >= a.first && j < newest; };
+  uint32_t key[kKeyBlocks];  // (0, which counts reach nowhere, for the first groups and the newest)
+#pragma unroll
+  for (int k = 0; k < kKeyBlocks; ++k) key[k] = of_choice(64 * k + lane) ? key_of(c.mass[k]) : 0u;
+  const auto reaching = [&](uint32_t t /* > 0 */) __attribute__((always_inline)) {
+    int count = 0;
+#pragma unroll
+    for (int k = 0; k < kKeyBlocks; ++k) {
+      if (64 * k >= n) break;
+      count += __popcll(__builtin_amdgcn_ballot_w64(key[k] >= t));
+    }
+    return count;
+  };
+  const int need = a.keep - a.first - a.last;
+  uint32_t t = 0;
+  bool exact = false;  // just as many keys as needed reach t
+  int bit = 31;
+  for (; bit >= 0 && need > 0 && !exact; --bit) {
+    const int count = reaching(t | 1u << bit);
+    if (count >= need) t |= 1u << bit;
+    exact = count == need;
+  }
+  // (t is the key of the last that stays, or between it and the next; keys equal to t: all stay, or the first ones)
+  int ties = exact ? n : need <= 0 ? 0 : need - (t == ~0u ? 0 : reaching(t + 1));
+  bool whole = true;
+#pragma unroll
+  for (int k = 0; k < kKeyBlocks; ++k) {
+    c.stay[k] = 0;
+    if (64 * k >= n) continue;
+    const int j = 64 * k + lane;
+    const bool tie = of_choice(j) && key[k] == t;
+    const uint64_t equal = __builtin_amdgcn_ballot_w64(tie);
+    const bool chosen = need > 0 && (key[k] > t || (tie && (int)__popcll(equal & ((1ull << lane) - 1)) < ties));
+    c.stay[k] = __builtin_amdgcn_ballot_w64(j < a.first || (j >= newest && j < n) || chosen);
+    ties -= (int)__popcll(equal);
+    if (whole && c.stay[k] != ~0ull) {
+      whole = false;
+      c.first_moved = min(c.cut, 64 * k + __builtin_ctzll(~c.stay[k]));
+    }
+  }
+}
+__device__ __forceinline__ void list_of(const Choice& c, int lane, uint16_t* list /* LDS */) {
+  int kept = 0;
+#pragma unroll
+  for (int k = 0; k < kKeyBlocks; ++k) {
+    if (64 * k >= c.n) break;
+    if ((c.stay[k] >> lane & 1) != 0) list[kept + __popcll(c.stay[k] & ((1ull << lane) - 1))] = (uint16_t)(64 * k + lane);
+    kept += __popcll(c.stay[k]);
+  }
+}
+// The mass that goes with what is kept, and the list for the caller.
+__device__ __forceinline__ void put_masses(const Choice& c, const EvictCall& a, long long pair, int lane) {
+  float* mass_out = a.mass_out + pair * (a.to.max_groups + 1);
+  int kept = 0;
+#pragma unroll
+  for (int k = 0; k <= kKeyBlocks; ++k) {
+    const int j = 64 * k + lane;
+    if (64 * k > c.n) break;
+    if (j == c.n) mass_out[c.cut] = c.mass[k];
+    if (k == kKeyBlocks) break;
+    const uint64_t stay = c.stay[k < kKeyBlocks ? k : 0];
+    if ((stay >> lane & 1) != 0) {
+      const int slot = kept + __popcll(stay & ((1ull << lane) - 1));
+      mass_out[slot] = c.mass[k];
+      if (a.kept != nullptr) a.kept[pair * a.to.max_groups + slot] = j;
+    }
+    kept += __popcll(stay);
+  }
+  for (long long j = c.cut + 1 + lane; j <= a.to.max_groups; j += 64) mass_out[j] = 0.0f;
+}
+
+// Counters of a sequence, by one thread, when everybody has read those of before.
 __device__ __forceinline__ void commit(const EvictCall& a, int b, int cut) {
   const Lengths len = lengths_of(a.from, b);
   const int dropped = (len.groups() - cut) * kGroup;
@@ -135,76 +229,154 @@ __device__ __forceinline__ void commit(const EvictCall& a, int b, int cut) {
   a.to.n_res[b] = len.nr;
 }
 
-// Into another cache.  Grid: pairs in x; in y, as many at a time as there are, the records, then the window: pieces of kPieceBytes of keys and of values.
-constexpr int kMoveThreads = 192, kPieceBytes = 8192;
-template <int BITS>
-__global__ __launch_bounds__(kMoveThreads) void move_kernel(EvictCall a, int records, int pieces) {
-  constexpr int kVectors = Rec<BITS>::kWords / 4;
-  const int tid = threadIdx.x;
+// What is written once: by a pair's workgroup `first`, or, where it is written over what the others read, by the last of the pair's `workgroups` to say that
+// they have read it, and of the sequence's last ones by the last.  The counters that tell are the cache's own, zero before and after: of a
+// pair, and in the upper half of the first pair's of the sequence, one for each of its pairs.
+__device__ __forceinline__ int arrive(const EvictCall& a, long long pair, int lane) {
+  int before = 0;
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");  // (mass and counters have been read)
+  if (lane == 0 && a.counted) before = __hip_atomic_fetch_add(a.to.split_done + pair, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
+  return before;
+}
+__device__ __forceinline__ void write_once(const Choice& c, const EvictCall& a, long long pair, int lane, bool first, int before, int workgroups) {
+  if (a.counted ? (__builtin_amdgcn_readfirstlane(before) & 0xffff) != workgroups - 1 : !first) return;
+  put_masses(c, a, pair, lane);
+  const int heads = a.from.H_kv;
+  const long long sequence = pair / heads;
+  if (lane != 0) return;
+  if (!a.counted) {
+    if (pair % heads == 0) commit(a, (int)sequence, c.cut);
+    return;
+  }
+  __hip_atomic_fetch_add(a.to.split_done + pair, -workgroups, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
+  const int others = __hip_atomic_fetch_add(a.to.split_done + sequence * heads, 1 << 16, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM) >> 16;
+  if (others != heads - 1) return;
+  __hip_atomic_fetch_add(a.to.split_done + sequence * heads, -(heads << 16), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
+  commit(a, (int)sequence, c.cut);
+}
+
+// Into another cache.  Grid: pairs in x, workgroups of a pair in y; a wave takes records, and, with the same number of 16-byte runs at a time, the window.
+// SELECTED: a launch before has left the list.
+constexpr int kMoveWaves = 4;
+template <int BITS, bool SELECTED>
+__global__ __launch_bounds__(64 * kMoveWaves) void move_kernel(EvictCall a) {
+  constexpr int kRuns = Rec<BITS>::kWords / 4 / 64;
+  static_assert(Rec<BITS>::kWords % 256 == 0, "whole runs of every lane");
+  __shared__ uint16_t sList[SELECTED ? 1 : kMostKeys];
+  __shared__ int sCut;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const long long pair = blockIdx.x;
-  const int cut = a.count[2 * pair];
-  for (int y = blockIdx.y; y < records + 2 * pieces; y += gridDim.y) {
-    const u32x4_t* src;
-    u32x4_t* dst;
-    int vectors = kVectors;
-    if (y < records) {
-      if (y >= cut) continue;
-      const int from = a.source[pair * a.stride + y];
-      src = reinterpret_cast<const u32x4_t*>(a.from.groups + (pair * a.from.max_groups + from) * Rec<BITS>::kWords);
-      dst = reinterpret_cast<u32x4_t*>(a.to.groups + (pair * a.to.max_groups + y) * Rec<BITS>::kWords);
-    } else {
-      const int bytes = a.from.R * kHeadDim * 2, part = y - records, piece = part < pieces ? part : part - pieces;
-      const long long at = pair * (bytes / 16) + piece * (kPieceBytes / 16);
-      src = reinterpret_cast<const u32x4_t*>(part < pieces ? a.from.k_res : a.from.v_res) + at;
-      dst = reinterpret_cast<u32x4_t*>(part < pieces ? a.to.k_res : a.to.v_res) + at;
-      vectors = min(kPieceBytes, bytes - piece * kPieceBytes) / 16;
-      if (part == 0 && tid == 0 && pair % a.from.H_kv == 0) commit(a, (int)(pair / a.from.H_kv), cut);
+  const int runs = a.from.R * (kHeadDim * 2 / 16), pieces = (runs + 64 * kRuns - 1) / (64 * kRuns);  // of the window's keys, and of its values
+  int cut = 0;
+  const auto units = [&]() __attribute__((always_inline)) {
+    for (int u = blockIdx.y * kMoveWaves + wave; u < 2 * pieces + cut; u += gridDim.y * kMoveWaves) {
+      const u32x4_t* src;
+      u32x4_t* dst;
+      int left = 64 * kRuns;
+      if (u >= 2 * pieces) {
+        const int slot = u - 2 * pieces;
+        const int from = SELECTED ? a.source[pair * a.stride + slot] : (int)sList[slot];
+        src = reinterpret_cast<const u32x4_t*>(a.from.groups + (pair * a.from.max_groups + from) * Rec<BITS>::kWords);
+        dst = reinterpret_cast<u32x4_t*>(a.to.groups + (pair * a.to.max_groups + slot) * Rec<BITS>::kWords);
+      } else {
+        const bool keys = u < pieces;
+        const int at = (keys ? u : u - pieces) * 64 * kRuns;
+        src = reinterpret_cast<const u32x4_t*>(keys ? a.from.k_res : a.from.v_res) + pair * runs + at;
+        dst = reinterpret_cast<u32x4_t*>(keys ? a.to.k_res : a.to.v_res) + pair * runs + at;
+        left = min(left, runs - at);
+      }
+      u32x4_t v[kRuns];
+#pragma unroll
+      for (int i = 0; i < kRuns; ++i)
+        if (64 * i + lane < left) v[i] = __builtin_nontemporal_load(src + 64 * i + lane);
+#pragma unroll
+      for (int i = 0; i < kRuns; ++i)
+        if (64 * i + lane < left) dst[64 * i + lane] = v[i];
     }
-    for (int i = tid; i < vectors; i += kMoveThreads) dst[i] = __builtin_nontemporal_load(src + i);
+  };
+  if constexpr (SELECTED) {
+    cut = a.count[2 * pair];
+    if (tid == 0 && blockIdx.y == 0 && pair % a.from.H_kv == 0) commit(a, (int)(pair / a.from.H_kv), cut);
+    units();
+  } else {
+    if (wave == 0) {
+      Choice c;
+      choose(c, a, pair, lane);
+      const int before = arrive(a, pair, lane);
+      list_of(c, lane, sList);
+      if (lane == 0) sCut = c.cut;
+      write_once(c, a, pair, lane, blockIdx.y == 0, before, gridDim.y);
+    }
+    __syncthreads();
+    cut = __builtin_amdgcn_readfirstlane(sCut);
+    units();
   }
 }
 
 // In place.  Grid: pairs in x, waves of 64 runs of 16 bytes of a record in y.
 constexpr int kAhead = 16;  // loads of a lane under way
-template <int BITS>
+template <int BITS, bool SELECTED>
 __global__ __launch_bounds__(64) void close_up_kernel(EvictCall a) {
   constexpr int kVectors = Rec<BITS>::kWords / 4;
-  const int at = blockIdx.y * 64 + threadIdx.x;
+  static_assert(kVectors % 64 == 0, "grid");
+  __shared__ uint16_t sList[SELECTED ? 1 : kMostKeys];
+  const int lane = threadIdx.x, at = blockIdx.y * 64 + lane;
   const long long pair = blockIdx.x;
-  const int cut = a.count[2 * pair];
-  if (at == 0 && pair % a.from.H_kv == 0) commit(a, (int)(pair / a.from.H_kv), cut);
-  if (at >= kVectors) return;
-  const int32_t* source = a.source + pair * a.stride;
   u32x4_t* base = reinterpret_cast<u32x4_t*>(a.to.groups + pair * a.to.max_groups * Rec<BITS>::kWords) + at;
-  for (int j0 = a.count[2 * pair + 1]; j0 < cut; j0 += kAhead) {
-    u32x4_t v[kAhead];
+  const auto move = [&](int first, int cut) __attribute__((always_inline)) {
+    const int32_t* source = a.source + pair * a.stride;
+    for (int j0 = first; j0 < cut; j0 += kAhead) {
+      u32x4_t v[kAhead];
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) v[i] = base[(long long)source[min(j0 + i, cut - 1)] * kVectors];
+      for (int i = 0; i < kAhead; ++i) {
+        const int slot = min(j0 + i, cut - 1);
+        v[i] = base[(long long)(SELECTED ? source[slot] : (int)sList[slot]) * kVectors];
+      }
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i)
-      if (j0 + i < cut) base[(long long)(j0 + i) * kVectors] = v[i];
+      for (int i = 0; i < kAhead; ++i)
+        if (j0 + i < cut) base[(long long)(j0 + i) * kVectors] = v[i];
+    }
+  };
+  if constexpr (SELECTED) {
+    const int cut = a.count[2 * pair];
+    if (at == 0 && pair % a.from.H_kv == 0) commit(a, (int)(pair / a.from.H_kv), cut);
+    move(a.count[2 * pair + 1], cut);
+  } else {
+    Choice c;
+    choose(c, a, pair, lane);
+    const int before = arrive(a, pair, lane);
+    if (c.first_moved < c.cut) {
+      list_of(c, lane, sList);
+      __syncthreads();
+      move(c.first_moved, c.cut);
+    }
+    write_once(c, a, pair, lane, blockIdx.y == 0, before, gridDim.y);
   }
 }
 
-template <int BITS>
+template <int BITS, bool SELECTED>
 void launch_moves(const EvictCall& a, hipStream_t stream) {
   const unsigned pairs = (unsigned)(a.from.B * a.from.H_kv);
   if (a.in_place) {
-    hipLaunchKernelGGL((close_up_kernel<BITS>), dim3(pairs, (Rec<BITS>::kWords / 4 + 63) / 64), dim3(64), 0, stream, a);
+    hipLaunchKernelGGL((close_up_kernel<BITS, SELECTED>), dim3(pairs, Rec<BITS>::kWords / 4 / 64), dim3(64), 0, stream, a);
   } else {
     const long long records = a.limit < a.from.max_groups ? a.limit : a.from.max_groups;
-    const int pieces = (a.from.R * kHeadDim * 2 + kPieceBytes - 1) / kPieceBytes;
-    const long long all = records + 2 * pieces, most = 32768 < (1 << 24) / pairs ? 32768 : (1 << 24) / pairs;
-    hipLaunchKernelGGL((move_kernel<BITS>), dim3(pairs, (unsigned)(all < most ? all : most < 1 ? 1 : most)), dim3(kMoveThreads), 0, stream, a, (int)records, pieces);
+    const long long units = records + 2 * ((a.from.R * kHeadDim * 2 + Rec<BITS>::kWords * 4 - 1) / (Rec<BITS>::kWords * 4));
+    const long long all = (units + kMoveWaves - 1) / kMoveWaves, most = 16384 / pairs;
+    hipLaunchKernelGGL((move_kernel<BITS, SELECTED>), dim3(pairs, (unsigned)(all < most ? all : most < 1 ? 1 : most)), dim3(64 * kMoveWaves), 0, stream, a);
   }
 }
 
 }  // namespace
 
 int launch_evict(const EvictCall& a, hipStream_t stream) {
+  if (evicts_in_one_launch(a.from)) {
+    a.from.bits == 2 ? launch_moves<2, false>(a, stream) : launch_moves<4, false>(a, stream);
+    return hipGetLastError() == hipSuccess ? KVLINC_OK : KVLINC_EHIP;
+  }
   hipLaunchKernelGGL(select_kernel, dim3((unsigned)(a.from.B * a.from.H_kv)), dim3(kSelectThreads), 0, stream, a);
   if (hipGetLastError() != hipSuccess) return KVLINC_EHIP;
-  a.from.bits == 2 ? launch_moves<2>(a, stream) : launch_moves<4>(a, stream);
+  a.from.bits == 2 ? launch_moves<2, true>(a, stream) : launch_moves<4, true>(a, stream);
   return hipGetLastError() == hipSuccess ? KVLINC_OK : KVLINC_EHIP;
 }
 

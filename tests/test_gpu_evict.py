@@ -101,6 +101,35 @@ def test_sizes(groups, keep, first, last, bits):
     run_case(2, 3, [128 * groups], [1, 128], groups + 1, keep, first=first, last=last, bits=bits, seed=groups)
 
 
+@pytest.mark.parametrize("room", [63, 64, 65, 127, 1023, 1024, 1025])
+def test_as_many_groups_as_a_wave_or_a_launch_selects_from_and_one_more_or_less(room):
+    for n, keep, first, last in ((room, room - 1, 0, 1), (room - 1, room // 2, 1, 2), (room, 2, 1, 1)):
+        c = run_case(1, 2, [128 * n], [7], room, keep, first=first, last=last, seed=room)
+        assert (c.split_done == 0).all()
+
+
+@pytest.mark.parametrize("B, H_kv", [(1, 1), (1, 40), (70, 3), (3, 33)])
+def test_counters_that_tell_who_writes_last_are_zero_again(B, H_kv):
+    c = cache_of(B, H_kv, H_kv, [128 * n for n in (30, 11, 10, 3)], [9, 1], 30)
+    before, mass = copy_of(c), mass_of(c)
+    offset = torch.zeros(B, dtype=torch.int32, device="cuda")
+    for i in range(3):  # (the second and third time there is nothing to drop)
+        moved = mass.clone() if i == 0 else moved
+        c.evict(moved, 8, limit=10, first=1, last=2, offset=offset)
+        assert (c.split_done == 0).all()
+        check(before, mass, c, moved, None, offset, 8, 10, 1, 2)
+
+
+def test_into_another_cache_with_the_mass_in_place():
+    c = cache_of(3, 2, 2, [128 * n for n in (30, 11, 12)], [9, 1], 30)
+    mass, before = mass_of(c), copy_of(c)
+    to = cache_of(3, 2, 2, 0, 0, 30, seed=1)
+    moved, offset = mass.clone(), torch.zeros(3, dtype=torch.int32, device="cuda")
+    assert c.evict(moved, 8, limit=11, first=1, last=2, to=to, mass_out=moved, offset=offset) is to
+    check(before, mass, to, moved, None, offset, 8, 11, 1, 2)
+    assert (to.split_done == 0).all() and torch.equal(c.n_quant, before.n_quant) and torch.equal(c.groups, before.groups)
+
+
 def test_ragged_lengths_and_a_limit_above_what_is_kept():
     run_case(8, 2, [0, 128, 512, 640, 768, 1024, 2048, 0], [0, 5, 1, 128, 128, 30, 77, 9], 20, 5, limit=6, last=2)
     run_case(5, 1, [128 * n for n in (30, 29, 28, 2, 12)], [64], 30, 12, limit=28, first=0, last=3, small=40)
