@@ -685,19 +685,23 @@ class KVLincCache:
             raise KVLincError("to has to be a KVLincCache")
         if to._device != self._device:
             raise KVLincError("to is on %s, the cache on %s" % (to._device, self._device))
-        limit = keep if limit is None else limit
-        for x, name in ((keep, "keep"), (limit, "limit"), (first, "first"), (last, "last")):
-            if not 0 <= x < 1 << 31:
-                raise KVLincError("%s has to be 0 or more, below 2^31, not %s" % (name, x))
+        if limit is None:
+            limit = keep
+        if not (0 <= keep < 1 << 31 and 0 <= limit < 1 << 31 and 0 <= first < 1 << 31 and 0 <= last < 1 << 31):
+            raise KVLincError("keep, limit, first and last have to be 0 or more, below 2^31, not %s, %s, %s and %s" % (keep, limit, first, last))
         if mass_out is None and to is self:
             mass_out = mass
         if offset_out is None:
             offset_out = offset
         self._tensor(mass, "mass", (self.B, self.H_kv, self.max_groups + 1), torch.float32)
-        to._tensor(mass_out, "mass_out", (to.B, to.H_kv, to.max_groups + 1), torch.float32)
-        for t, name, shape in ((offset, "offset", (self.B,)), (offset_out, "offset_out", (self.B,)), (kept, "kept", (to.B, to.H_kv, to.max_groups))):
-            if t is not None:
-                self._tensor(t, name, shape, torch.int32)
+        if mass_out is not mass or to is not self:
+            to._tensor(mass_out, "mass_out", (to.B, to.H_kv, to.max_groups + 1), torch.float32)
+        if offset is not None:
+            self._tensor(offset, "offset", (self.B,), torch.int32)
+        if offset_out is not offset:
+            self._tensor(offset_out, "offset_out", (self.B,), torch.int32)
+        if kept is not None:
+            self._tensor(kept, "kept", (to.B, to.H_kv, to.max_groups), torch.int32)
         theirs = () if to is self else (to.groups, to.k_res, to.v_res, to.n_quant, to.n_res)
         with self._on(stream, mass, mass_out, offset, offset_out, kept, *theirs):
             rc = self._with_scratch(lambda ws, s: kvlinc_cache_evict(self, to, mass, mass_out, keep, limit, first, last, offset, offset_out, kept, ws, None, s),

@@ -7,7 +7,9 @@
 // a workgroup for each pair that finds the threshold by four counts of the keys' bits, 8 at a time, five reads of the mass, and leaves the list of what stays.
 // Into another cache: a wave a record.  In place: a lane has 16 bytes of every record of a pair, and moves them from slot to slot in order.  A slot's
 // source is never below it, so what the lane reads has not been written yet, whatever other lanes have done: no workgroup waits for another.
-// Bound: bytes of the records that move, in and out.
+// Bound: bytes of the records that move, in and out: 128 pairs, 64 of 256 groups each, 4 bits, 300 MB: 59.7 us, what a copy takes; 128 pairs, 2k tokens of 8k:
+// 11.2 us; one chat, 16 of 17 groups: 9.5 us, the host's call, of which the kernel takes 6, a chain of counters and mass, selection, record.  (With a
+// launch of its own to select 68.9, 16.7 and 12.9; with 16 blocks of keys in all of them 15.6 for the 11.2: more code than the first wave has fetched.)
 #include <hip/hip_runtime.h>
 
 #include "kvlinc_bounded_internal.h"
@@ -129,34 +131,36 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(EvictCall a) {
 }
 
 // ---- selection by one wave ----
-constexpr int kMostKeys = kEvictOneLaunch, kKeyBlocks = kMostKeys / 64;
+// BLOCKS: of 64 keys; 1, 4 or 16, as few as the cache has room for (0: a launch before has selected).
+template <int BLOCKS>
 struct Choice {
   int n, cut, first_moved;  // groups, how many stay, the first slot with another group than before (cut: none)
-  float mass[kKeyBlocks + 1];  // of group 64 k + lane (n: the window's)
-  uint64_t stay[kKeyBlocks];
+  float mass[BLOCKS + 1];  // of group 64 k + lane (n: the window's)
+  uint64_t stay[BLOCKS];
 };
-__device__ __forceinline__ void choose(Choice& c, const EvictCall& a, long long pair, int lane) {
+template <int BLOCKS>
+__device__ __forceinline__ void choose(Choice<BLOCKS>& c, const EvictCall& a, long long pair, int lane) {
   const float* mass = a.mass + pair * (a.from.max_groups + 1);
   const int most = (int)a.from.max_groups;
 #pragma unroll
-  for (int k = 0; k <= kKeyBlocks; ++k) c.mass[k] = 64 * k <= most ? mass[min(64 * k + lane, most)] : 0.0f;
+  for (int k = 0; k <= BLOCKS; ++k) c.mass[k] = 64 * k <= most ? mass[min(64 * k + lane, most)] : 0.0f;
   c.n = lengths_of(a.from, (int)(pair / a.from.H_kv)).groups();
   const int n = c.n, newest = n - a.last;
   c.cut = n > a.limit ? a.keep : n;
   c.first_moved = c.cut;
   if (n <= a.limit) {
 #pragma unroll
-    for (int k = 0; k < kKeyBlocks; ++k) c.stay[k] = __builtin_amdgcn_ballot_w64(64 * k + lane < n);
+    for (int k = 0; k < BLOCKS; ++k) c.stay[k] = __builtin_amdgcn_ballot_w64(64 * k + lane < n);
     return;
   }
   const auto of_choice = [&](int j) __attribute__((always_inline)) { return j >= a.first && j < newest; };
-  uint32_t key[kKeyBlocks];  // (0, which counts reach nowhere, for the first groups and the newest)
+  uint32_t key[BLOCKS];  // (0, which counts reach nowhere, for the first groups and the newest)
 #pragma unroll
-  for (int k = 0; k < kKeyBlocks; ++k) key[k] = of_choice(64 * k + lane) ? key_of(c.mass[k]) : 0u;
+  for (int k = 0; k < BLOCKS; ++k) key[k] = of_choice(64 * k + lane) ? key_of(c.mass[k]) : 0u;
   const auto reaching = [&](uint32_t t /* > 0 */) __attribute__((always_inline)) {
     int count = 0;
 #pragma unroll
-    for (int k = 0; k < kKeyBlocks; ++k) {
+    for (int k = 0; k < BLOCKS; ++k) {
       if (64 * k >= n) break;
       count += __popcll(__builtin_amdgcn_ballot_w64(key[k] >= t));
     }
@@ -175,7 +179,7 @@ __device__ __forceinline__ void choose(Choice& c, const EvictCall& a, long long 
   int ties = exact ? n : need <= 0 ? 0 : need - (t == ~0u ? 0 : reaching(t + 1));
   bool whole = true;
 #pragma unroll
-  for (int k = 0; k < kKeyBlocks; ++k) {
+  for (int k = 0; k < BLOCKS; ++k) {
     c.stay[k] = 0;
     if (64 * k >= n) continue;
     const int j = 64 * k + lane;
@@ -190,26 +194,28 @@ __device__ __forceinline__ void choose(Choice& c, const EvictCall& a, long long 
     }
   }
 }
-__device__ __forceinline__ void list_of(const Choice& c, int lane, uint16_t* list /* LDS */) {
+template <int BLOCKS>
+__device__ __forceinline__ void list_of(const Choice<BLOCKS>& c, int lane, uint16_t* list /* LDS */) {
   int kept = 0;
 #pragma unroll
-  for (int k = 0; k < kKeyBlocks; ++k) {
+  for (int k = 0; k < BLOCKS; ++k) {
     if (64 * k >= c.n) break;
     if ((c.stay[k] >> lane & 1) != 0) list[kept + __popcll(c.stay[k] & ((1ull << lane) - 1))] = (uint16_t)(64 * k + lane);
     kept += __popcll(c.stay[k]);
   }
 }
 // The mass that goes with what is kept, and the list for the caller.
-__device__ __forceinline__ void put_masses(const Choice& c, const EvictCall& a, long long pair, int lane) {
+template <int BLOCKS>
+__device__ __forceinline__ void put_masses(const Choice<BLOCKS>& c, const EvictCall& a, long long pair, int lane) {
   float* mass_out = a.mass_out + pair * (a.to.max_groups + 1);
   int kept = 0;
 #pragma unroll
-  for (int k = 0; k <= kKeyBlocks; ++k) {
+  for (int k = 0; k <= BLOCKS; ++k) {
     const int j = 64 * k + lane;
     if (64 * k > c.n) break;
     if (j == c.n) mass_out[c.cut] = c.mass[k];
-    if (k == kKeyBlocks) break;
-    const uint64_t stay = c.stay[k < kKeyBlocks ? k : 0];
+    if (k == BLOCKS) break;
+    const uint64_t stay = c.stay[k < BLOCKS ? k : 0];
     if ((stay >> lane & 1) != 0) {
       const int slot = kept + __popcll(stay & ((1ull << lane) - 1));
       mass_out[slot] = c.mass[k];
@@ -238,7 +244,8 @@ __device__ __forceinline__ int arrive(const EvictCall& a, long long pair, int la
   if (lane == 0 && a.counted) before = __hip_atomic_fetch_add(a.to.split_done + pair, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
   return before;
 }
-__device__ __forceinline__ void write_once(const Choice& c, const EvictCall& a, long long pair, int lane, bool first, int before, int workgroups) {
+template <int BLOCKS>
+__device__ __forceinline__ void write_once(const Choice<BLOCKS>& c, const EvictCall& a, long long pair, int lane, bool first, int before, int workgroups) {
   if (a.counted ? (__builtin_amdgcn_readfirstlane(before) & 0xffff) != workgroups - 1 : !first) return;
   put_masses(c, a, pair, lane);
   const int heads = a.from.H_kv;
@@ -256,13 +263,15 @@ __device__ __forceinline__ void write_once(const Choice& c, const EvictCall& a, 
 }
 
 // Into another cache.  Grid: pairs in x, workgroups of a pair in y; a wave takes records, and, with the same number of 16-byte runs at a time, the window.
-// SELECTED: a launch before has left the list.
 constexpr int kMoveWaves = 4;
-template <int BITS, bool SELECTED>
+// Stores past the caches from so many bytes on: 144 MB of 4-bit records 70.4 -> 59.7 us, of 2-bit ones 75.6 -> 72.9; 72 MB of these 35.5 -> 38.9, 21 MB
+// 11.2 -> 11.9.
+constexpr long long kStreamedBytes = 96ll << 20;
+template <int BITS, int BLOCKS, bool STREAMED>
 __global__ __launch_bounds__(64 * kMoveWaves) void move_kernel(EvictCall a) {
   constexpr int kRuns = Rec<BITS>::kWords / 4 / 64;
   static_assert(Rec<BITS>::kWords % 256 == 0, "whole runs of every lane");
-  __shared__ uint16_t sList[SELECTED ? 1 : kMostKeys];
+  __shared__ uint16_t sList[BLOCKS == 0 ? 1 : 64 * BLOCKS];
   __shared__ int sCut;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const long long pair = blockIdx.x;
@@ -275,7 +284,7 @@ __global__ __launch_bounds__(64 * kMoveWaves) void move_kernel(EvictCall a) {
       int left = 64 * kRuns;
       if (u >= 2 * pieces) {
         const int slot = u - 2 * pieces;
-        const int from = SELECTED ? a.source[pair * a.stride + slot] : (int)sList[slot];
+        const int from = BLOCKS == 0 ? a.source[pair * a.stride + slot] : (int)sList[slot];
         src = reinterpret_cast<const u32x4_t*>(a.from.groups + (pair * a.from.max_groups + from) * Rec<BITS>::kWords);
         dst = reinterpret_cast<u32x4_t*>(a.to.groups + (pair * a.to.max_groups + slot) * Rec<BITS>::kWords);
       } else {
@@ -290,36 +299,40 @@ __global__ __launch_bounds__(64 * kMoveWaves) void move_kernel(EvictCall a) {
       for (int i = 0; i < kRuns; ++i)
         if (64 * i + lane < left) v[i] = __builtin_nontemporal_load(src + 64 * i + lane);
 #pragma unroll
-      for (int i = 0; i < kRuns; ++i)
-        if (64 * i + lane < left) dst[64 * i + lane] = v[i];
+      for (int i = 0; i < kRuns; ++i) {
+        if (64 * i + lane >= left) continue;
+        if constexpr (STREAMED) __builtin_nontemporal_store(v[i], dst + 64 * i + lane);
+        else dst[64 * i + lane] = v[i];
+      }
     }
   };
-  if constexpr (SELECTED) {
+  if constexpr (BLOCKS == 0) {
     cut = a.count[2 * pair];
     if (tid == 0 && blockIdx.y == 0 && pair % a.from.H_kv == 0) commit(a, (int)(pair / a.from.H_kv), cut);
     units();
   } else {
+    Choice<BLOCKS> c;
+    int before = 0;
     if (wave == 0) {
-      Choice c;
       choose(c, a, pair, lane);
-      const int before = arrive(a, pair, lane);
+      before = arrive(a, pair, lane);
       list_of(c, lane, sList);
       if (lane == 0) sCut = c.cut;
-      write_once(c, a, pair, lane, blockIdx.y == 0, before, gridDim.y);
     }
     __syncthreads();
     cut = __builtin_amdgcn_readfirstlane(sCut);
     units();
+    if (wave == 0) write_once(c, a, pair, lane, blockIdx.y == 0, before, gridDim.y);
   }
 }
 
 // In place.  Grid: pairs in x, waves of 64 runs of 16 bytes of a record in y.
 constexpr int kAhead = 16;  // loads of a lane under way
-template <int BITS, bool SELECTED>
+template <int BITS, int BLOCKS>
 __global__ __launch_bounds__(64) void close_up_kernel(EvictCall a) {
   constexpr int kVectors = Rec<BITS>::kWords / 4;
   static_assert(kVectors % 64 == 0, "grid");
-  __shared__ uint16_t sList[SELECTED ? 1 : kMostKeys];
+  __shared__ uint16_t sList[BLOCKS == 0 ? 1 : 64 * BLOCKS];
   const int lane = threadIdx.x, at = blockIdx.y * 64 + lane;
   const long long pair = blockIdx.x;
   u32x4_t* base = reinterpret_cast<u32x4_t*>(a.to.groups + pair * a.to.max_groups * Rec<BITS>::kWords) + at;
@@ -330,19 +343,19 @@ __global__ __launch_bounds__(64) void close_up_kernel(EvictCall a) {
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) {
         const int slot = min(j0 + i, cut - 1);
-        v[i] = base[(long long)(SELECTED ? source[slot] : (int)sList[slot]) * kVectors];
+        v[i] = base[(long long)(BLOCKS == 0 ? source[slot] : (int)sList[slot]) * kVectors];
       }
 #pragma unroll
       for (int i = 0; i < kAhead; ++i)
         if (j0 + i < cut) base[(long long)(j0 + i) * kVectors] = v[i];
     }
   };
-  if constexpr (SELECTED) {
+  if constexpr (BLOCKS == 0) {
     const int cut = a.count[2 * pair];
     if (at == 0 && pair % a.from.H_kv == 0) commit(a, (int)(pair / a.from.H_kv), cut);
     move(a.count[2 * pair + 1], cut);
   } else {
-    Choice c;
+    Choice<BLOCKS> c;
     choose(c, a, pair, lane);
     const int before = arrive(a, pair, lane);
     if (c.first_moved < c.cut) {
@@ -354,16 +367,18 @@ __global__ __launch_bounds__(64) void close_up_kernel(EvictCall a) {
   }
 }
 
-template <int BITS, bool SELECTED>
+template <int BITS, int BLOCKS>
 void launch_moves(const EvictCall& a, hipStream_t stream) {
   const unsigned pairs = (unsigned)(a.from.B * a.from.H_kv);
   if (a.in_place) {
-    hipLaunchKernelGGL((close_up_kernel<BITS, SELECTED>), dim3(pairs, Rec<BITS>::kWords / 4 / 64), dim3(64), 0, stream, a);
+    hipLaunchKernelGGL((close_up_kernel<BITS, BLOCKS>), dim3(pairs, Rec<BITS>::kWords / 4 / 64), dim3(64), 0, stream, a);
   } else {
     const long long records = a.limit < a.from.max_groups ? a.limit : a.from.max_groups;
     const long long units = records + 2 * ((a.from.R * kHeadDim * 2 + Rec<BITS>::kWords * 4 - 1) / (Rec<BITS>::kWords * 4));
     const long long all = (units + kMoveWaves - 1) / kMoveWaves, most = 16384 / pairs;
-    hipLaunchKernelGGL((move_kernel<BITS, SELECTED>), dim3(pairs, (unsigned)(all < most ? all : most < 1 ? 1 : most)), dim3(64 * kMoveWaves), 0, stream, a);
+    const dim3 grid(pairs, (unsigned)(all < most ? all : most < 1 ? 1 : most));
+    const bool streamed = (long long)pairs * units * Rec<BITS>::kWords * 4 >= kStreamedBytes;
+    hipLaunchKernelGGL((streamed ? move_kernel<BITS, BLOCKS, true> : move_kernel<BITS, BLOCKS, false>), grid, dim3(64 * kMoveWaves), 0, stream, a);
   }
 }
 
@@ -371,12 +386,14 @@ void launch_moves(const EvictCall& a, hipStream_t stream) {
 
 int launch_evict(const EvictCall& a, hipStream_t stream) {
   if (evicts_in_one_launch(a.from)) {
-    a.from.bits == 2 ? launch_moves<2, false>(a, stream) : launch_moves<4, false>(a, stream);
+    if (a.from.max_groups <= 64) a.from.bits == 2 ? launch_moves<2, 1>(a, stream) : launch_moves<4, 1>(a, stream);
+    else if (a.from.max_groups <= 256) a.from.bits == 2 ? launch_moves<2, 4>(a, stream) : launch_moves<4, 4>(a, stream);
+    else a.from.bits == 2 ? launch_moves<2, 16>(a, stream) : launch_moves<4, 16>(a, stream);
     return hipGetLastError() == hipSuccess ? KVLINC_OK : KVLINC_EHIP;
   }
   hipLaunchKernelGGL(select_kernel, dim3((unsigned)(a.from.B * a.from.H_kv)), dim3(kSelectThreads), 0, stream, a);
   if (hipGetLastError() != hipSuccess) return KVLINC_EHIP;
-  a.from.bits == 2 ? launch_moves<2, true>(a, stream) : launch_moves<4, true>(a, stream);
+  a.from.bits == 2 ? launch_moves<2, 0>(a, stream) : launch_moves<4, 0>(a, stream);
   return hipGetLastError() == hipSuccess ? KVLINC_OK : KVLINC_EHIP;
 }
 
