@@ -45,25 +45,22 @@ long long groups_of_bound(const kvlinc_cache& c, int max_context) {
   return groups < c.max_groups ? groups : c.max_groups;
 }
 
-// Decode: as windowed decode has its splits (plan_windowed in kvlinc_context_api.hip).
+// Decode: two workgroups of four waves a compute unit, as many as have a group for each wave, which the sequences share (part_of in kvlinc_decode_mass.hip).
 struct DecodePlan {
-  int splits;
-  long long slots;
+  long long units, slots;
   size_t part_floats, sums;
   size_t bytes() const { return part_floats * sizeof(float) + sums * sizeof(unsigned long long); }
 };
 DecodePlan plan_decode(const kvlinc_cache& c, int max_context) {
-  const long long pairs = pairs_of(c), groups = groups_of_bound(c, max_context);
+  const long long groups = groups_of_bound(c, max_context), splits = (groups + 3) / 4;
   DecodePlan p{};
-  long long s = 512 / pairs;
-  const long long most = (groups + 3) / 4;
-  if (s > most) s = most;
-  if (s > kMaxContextSplits) s = kMaxContextSplits;
-  if (s < 1) s = 1;
-  p.splits = (int)s;
+  const long long most = c.B * (splits < kMaxContextSplits ? splits : kMaxContextSplits);
+  p.units = 512 / c.H_kv;
+  if (p.units > most) p.units = most;
+  if (p.units < c.B) p.units = c.B;
   p.slots = c.max_groups + 4;  // (the window's 128 tokens in runs of 32; whatever max_context says, so that no sequence is too long for it)
-  p.part_floats = s > 1 ? (size_t)(c.B * (long long)c.H_q * s) * kPartStride : 0;
-  p.sums = (size_t)(pairs * p.slots) * 8;
+  p.part_floats = p.units > c.B ? (size_t)(p.units * c.H_q) * kPartStride : 0;
+  p.sums = (size_t)(pairs_of(c) * p.slots) * 8;
   return p;
 }
 
@@ -190,7 +187,7 @@ int kvlinc_decode_attention_mass(const kvlinc_cache* cache, const kvlinc_half* q
   MassCall a = make_mass(*cache, q, mass, decay, mass_out);
   a.T = 1;
   a.out = reinterpret_cast<_Float16*>(out);
-  a.splits = p.splits;
+  a.units = (int)p.units;
   a.slots = p.slots;
   a.sums = static_cast<unsigned long long*>(workspace);
   a.part = p.part_floats != 0 ? reinterpret_cast<float*>(a.sums + p.sums) : nullptr;  // (sums: a multiple of 64 bytes)

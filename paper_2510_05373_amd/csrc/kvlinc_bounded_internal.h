@@ -35,7 +35,8 @@ struct MassCall {
   const float* mass;  // NULL: zeros
   float* mass_out;
   float decay;
-  int T, gq, splits;
+  int T, gq;
+  int units;          // decode: workgroups of a KV head, B or more
   _Float16* out;
   float* part;        // decode: partial results of the splits as in kvlinc_context_internal.h; splits > 1 only
   unsigned long long* sums;  // decode: [B H_kv][slots][8] pairs {reference, sum of weights} of a head, see kvlinc_decode_mass.hip

@@ -7,10 +7,10 @@
 // bytes a group beside the 9216 or 17408 it reads; and who joins the splits of a pair, and so knows the maximum M and the sum L of every head, makes
 //     mass[j] = decay mass[j] + sum over heads of 2^(reference - M) sum / L,
 // always in the same order.  No second pass over keys, no second launch.
-// Bound: bytes of the groups.  32 sequences of 32k tokens, 7 heads, 4 bits: 119.0 us, 4.9 TB/s; with half of the tokens missing from the shortest 106.5
-// (the splits are made for the longest); 16 of 8k, 2 bits: 22.3 us, 3.6 TB/s, of which the chain of counters, first record, arrival, join and mass takes
-// 6; one of 300 tokens: 8.4 us, the host's calls.  (The walk of few-row attention, which unpacks the codes for binary16 products: 119.5 for the 106.5,
-// 28 for the 22.3.  Two workgroups a compute unit, 512 in all; with 1024 110 and 26, three a unit at 2 bits spill.)
+// Bound: bytes of the groups.  32 sequences of 32k tokens, 7 heads, 4 bits: 117.8 us, 4.9 TB/s; of 16k to 32k 95, 4.7; 16 of 8k, 2 bits: 22.3 us, 3.6 TB/s,
+// of which the chain of counters, first record, arrival, join and mass takes 6; one of 300 tokens: 8.4 us, the host's calls.  (The walk of few-row
+// attention, which unpacks the codes for binary16 products: 119.5 for the 95, 28 for the 22.3.  Two workgroups a compute unit, 512 in all; with 1024
+// 16 of 8k take 26, and three a unit at 2 bits spill.)
 #include <hip/hip_runtime.h>
 
 #include "kvlinc_bounded_internal.h"
@@ -28,7 +28,69 @@ constexpr int kSlotsAhead = 8;  // slots of a lane requested together
 // {reference, sum} of a head: a store past the caches that are not coherent across the chip.
 __device__ __forceinline__ void put_sum(unsigned long long* at, float reference, float sum) { st_coherent2(reinterpret_cast<float*>(at), reference, sum); }
 
-// Grid, one-dimensional: (sequence, KV head) fastest, then the split.
+// ---- which sequence and split a workgroup has ----
+__device__ __forceinline__ int wave_sum(int v) {
+  uint32_t u = (uint32_t)v;
+  u += dpp_u<kRowRor1>(u);
+  u += dpp_u<kRowRor2>(u);
+  u += dpp_u<kRowRor4>(u);
+  u += dpp_u<kRowRor8>(u);
+  auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  u = a[0] + a[1];
+  auto b = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return __builtin_amdgcn_readfirstlane((int)(b[0] + b[1]));
+}
+__device__ __forceinline__ int quotient_up(int n, int d) { return (int)((float)(n + d - 1) / (float)d); }  // (exact below 2^24)
+struct Part {
+  int b, split, splits;
+  int before;  // splits of the sequences ahead, with room for those that a pair does not use
+  int room;    // of the pair
+};
+// The sequences are cut into splits of the same number of groups a wave, the smallest with which the workgroups suffice: `units`, B at least, a KV head.  A
+// lane a sequence; more than 64 of them are cut into as many splits each.  False: this workgroup has none.  (32 sequences of 16k to 32k tokens 108 us
+// with four splits each, 96.8 so.)
+__device__ __forceinline__ bool part_of(const kvlinc_cache& c, int units, int unit, int lane, Part& p) {
+  const int most = units / c.B;
+  if (units == c.B || c.B == 1 || c.B > 64) {
+    p.b = unit / most;
+    p.split = unit - p.b * most;
+    p.before = p.b * most;
+    p.room = most;
+    if (p.b >= c.B) return false;
+    p.splits = max(1, min(most, (lengths_of(c, p.b).groups() + kWaves - 1) / kWaves));
+    return p.split < p.splits;
+  }
+  const int groups = lane < c.B ? (c.n_quant[min(lane, c.B - 1)] + kGroup - 1) / kGroup : 0;
+  const uint32_t in_row = row_umax((uint32_t)groups);
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) top = max(top, (uint32_t)__builtin_amdgcn_readlane((int)in_row, 16 * i));
+  const auto splits_at = [&](int rounds) __attribute__((always_inline)) {
+    return lane < c.B ? max(1, min(kMaxContextSplits, quotient_up(groups, kWaves * rounds))) : 0;
+  };
+  int low = max(1, quotient_up(wave_sum(groups), kWaves * units)), high = max(low, quotient_up((int)top, kWaves * most));
+  while (low < high) {
+    const int mid = (low + high) / 2;
+    if (wave_sum(splits_at(mid)) <= units) high = mid;
+    else low = mid + 1;
+  }
+  const int splits = splits_at(high);
+  int upto = splits;  // summed over the lanes up to this one
+  upto += __builtin_amdgcn_update_dpp(0, upto, 0x111, 0xf, 0xf, true);  // (the lane 1, 2, 4, 8 before it in its row of 16)
+  upto += __builtin_amdgcn_update_dpp(0, upto, 0x112, 0xf, 0xf, true);
+  upto += __builtin_amdgcn_update_dpp(0, upto, 0x114, 0xf, 0xf, true);
+  upto += __builtin_amdgcn_update_dpp(0, upto, 0x118, 0xf, 0xf, true);
+  const int row = lane >> 4, r0 = __builtin_amdgcn_readlane(upto, 15), r1 = __builtin_amdgcn_readlane(upto, 31), r2 = __builtin_amdgcn_readlane(upto, 47);
+  upto += (row > 0 ? r0 : 0) + (row > 1 ? r1 : 0) + (row > 2 ? r2 : 0);
+  p.b = __popcll(__builtin_amdgcn_ballot_w64(upto <= unit));
+  if (p.b >= c.B) return false;
+  p.splits = p.room = __builtin_amdgcn_readlane(splits, p.b);
+  p.before = __builtin_amdgcn_readlane(upto, p.b) - p.splits;
+  p.split = unit - p.before;
+  return true;
+}
+
+// Grid, one-dimensional: KV heads fastest, then what part_of shares out.
 template <int NB, bool SLIDING, int BITS>
 __global__ __launch_bounds__(kThreads, 2) void decode_mass_kernel(MassCall a) {
   constexpr int kCombine = 2 * kWaves * NB * 4 + kWaves * NB * 4 * kHeadDim, kRecordWords = Rec<BITS>::kWords, kTerms = 4;
@@ -39,12 +101,12 @@ __global__ __launch_bounds__(kThreads, 2) void decode_mass_kernel(MassCall a) {
   static_assert(kWaves * 2 * kExWords >= kThreads / 16 * kMaxContextSplits, "weights of the join");
   const kvlinc_cache& c = a.cache;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int pairs = c.B * c.H_kv, split = blockIdx.x / pairs, bh = blockIdx.x - split * pairs, b = bh / c.H_kv, gq = a.gq;
-  const Lengths len = lengths_of(c, b);
+  const int unit = blockIdx.x / c.H_kv, head_kv = blockIdx.x - unit * c.H_kv, gq = a.gq;
+  Part mine;
+  if (!part_of(c, a.units, unit, lane, mine)) return;
+  const int split = mine.split, n_splits = mine.splits, bh = mine.b * c.H_kv + head_kv;
+  const Lengths len = lengths_of(c, mine.b);
   const int G = len.groups();
-  // every workgroup of the pair comes to the same number: a split has a group for each wave
-  const int n_splits = max(1, min(a.splits, (G + kWaves - 1) / kWaves));
-  if (split >= n_splits) return;
   const long long row0 = (long long)bh * gq;  // (one token a sequence: rows are heads)
   unsigned long long* const sums = a.sums + bh * a.slots * kSumHeads;
 
@@ -127,7 +189,8 @@ __global__ __launch_bounds__(kThreads, 2) void decode_mass_kernel(MassCall a) {
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wave's sums are where everybody sees them
   __syncthreads();
   const bool direct = n_splits == 1;
-  const __amdgpu_buffer_rsrc_t part = buffer_of(a.part + (direct ? 0 : row0 * a.splits * kPartStride), direct ? 0 : (long long)gq * a.splits * kPartBytes);
+  const long long part0 = ((long long)mine.before * c.H_kv + (long long)head_kv * mine.room) * gq;
+  const __amdgpu_buffer_rsrc_t part = buffer_of(a.part + (direct ? 0 : part0 * kPartStride), direct ? 0 : (long long)gq * n_splits * kPartBytes);
   const int h = tid >> 4, ch = 8 * (lane & 15);  // 16 lanes a head
   if (h < gq) {
     float M = -INFINITY, L = 0.0f, o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
@@ -150,7 +213,7 @@ __global__ __launch_bounds__(kThreads, 2) void decode_mass_kernel(MassCall a) {
       finish_row(o, L, lane, a.out + (row0 + h) * kHeadDim);
       if ((lane & 15) == 0) { sRowM[h] = M; sRowL[h] = L; }
     } else {
-      const int place = (h * a.splits + split) * kPartBytes;
+      const int place = (h * n_splits + split) * kPartBytes;
       if ((lane & 15) == 0) store2(part, place, M, L);
       store4(part, place + 16 + 4 * ch, o[0], o[1], o[2], o[3]);
       store4(part, place + 32 + 4 * ch, o[4], o[5], o[6], o[7]);
@@ -185,7 +248,7 @@ __global__ __launch_bounds__(kThreads, 2) void decode_mass_kernel(MassCall a) {
   if (!direct) {
     if (h < gq) {
       float o[8], L, M;
-      join_row(part, h * a.splits * kPartBytes, n_splits, reinterpret_cast<float*>(&ex[0][0]) + kMaxContextSplits * h, lane, o, L, M);
+      join_row(part, h * n_splits * kPartBytes, n_splits, reinterpret_cast<float*>(&ex[0][0]) + kMaxContextSplits * h, lane, o, L, M);
       finish_row(o, L, lane, a.out + (row0 + h) * kHeadDim);
       if ((lane & 15) == 0) { sRowM[h] = M; sRowL[h] = L; }
     }
@@ -225,7 +288,7 @@ __global__ __launch_bounds__(kThreads, 2) void decode_mass_kernel(MassCall a) {
 }  // namespace
 
 int launch_decode_mass(const MassCall& a, hipStream_t stream) {
-  const dim3 grid((unsigned)((long long)a.cache.B * a.cache.H_kv * a.splits));
+  const dim3 grid((unsigned)((long long)a.units * a.cache.H_kv));
   const bool sliding = (a.cache.flags & KVLINC_FLAG_SLIDING_VALUES) != 0;
   void (*kernel)(MassCall) = a.cache.bits == 4 ? (a.gq > 4 ? (sliding ? decode_mass_kernel<2, true, 4> : decode_mass_kernel<2, false, 4>)
                                                            : (sliding ? decode_mass_kernel<1, true, 4> : decode_mass_kernel<1, false, 4>))

@@ -106,6 +106,13 @@ def test_decode_head_layouts(H_q, H_kv, bits):
     run_decode(1200 + H_q, H_q, H_kv, [500, 131, 0, 64], bits, decay=0.5)
 
 
+@pytest.mark.parametrize("lengths, H_q, H_kv", [([6000, 40, 900, 0, 2300], 4, 1), ([130, 8300, 131], 10, 2), ([5000] * 7 + [4871], 3, 3), ([0, 0, 1500, 0], 2, 2),
+                                                ([600 - 7 * i for i in range(64)], 2, 1), ([(37 * i) % 800 for i in range(70)], 1, 1)])
+def test_decode_of_uneven_batches(lengths, H_q, H_kv):
+    for bound in (0, max(lengths), 500):
+        run_decode(1230 + len(lengths), H_q, H_kv, lengths, 2, decay=0.5, bound=bound)
+
+
 @pytest.mark.parametrize("bits", [2, 4])
 @pytest.mark.parametrize("bound", [0, 1, 700, 1 << 30])
 def test_decode_bounds_size_the_launch_only(bound, bits):
