@@ -442,6 +442,7 @@ __device__ __forceinline__ void update_reference(float (&sc)[NB][8], const float
 template <int NB, int BITS, bool MASKED = false, int QK_TERMS = 3>
 __device__ __forceinline__ void pv_phase(const ValueRegs<BITS>& g, const float (&sc)[NB][8], const float (&base)[NB], const Roles& lr,
                                          WaveState<NB>& st, int fp16_from = kGroup, float* group_sum = nullptr) {
+  constexpr uint32_t kTop = QK_TERMS == 3 ? 7u : 2u;  // (see qk_phase)
   const uint32_t SZ[8] = {g.sz[0].x, g.sz[0].y, g.sz[0].z, g.sz[0].w, g.sz[1].x, g.sz[1].y, g.sz[1].z, g.sz[1].w};
   v8i_t A[NB];
   int scale_a[NB];
@@ -466,7 +467,7 @@ __device__ __forceinline__ void pv_phase(const ValueRegs<BITS>& g, const float (
     if (group_sum != nullptr) group_sum[nb] = sum;
     const uint32_t eb = block_exponent(row_umax(as_bits(mx)));  // over the 128 tokens of the head
     uint32_t t[3][2];
-    split_fp8(y, block_scale_bits(eb), t);
+    split_fp8(y, block_scale_bits<kTop>(eb), t);
     uint32_t* region = nb == 0 ? lr.ex_pv : lr.ex_qk;
     put_terms(region, lr.wp, t);
     if constexpr (NB == 2 && QK_TERMS > 3) *reinterpret_cast<u32x2_t*>(region + lr.wp + 96) = u32x2_t{0u, 0u};
@@ -474,7 +475,7 @@ __device__ __forceinline__ void pv_phase(const ValueRegs<BITS>& g, const float (
     if (NB == 1) {
       lds_order();
       A[nb] = get_operand(lr.ex_pv, lr.rd);
-      scale_a[nb] = (int)lr.ex_pv[kExHead * lr.ha + kExExp] - 7 - 4 * lr.ua;
+      scale_a[nb] = (int)lr.ex_pv[kExHead * lr.ha + kExExp] - (int)kTop - 4 * lr.ua;
       lds_order();
     }
   }
@@ -484,7 +485,7 @@ __device__ __forceinline__ void pv_phase(const ValueRegs<BITS>& g, const float (
     for (int nb = 0; nb < NB; ++nb) {
       const uint32_t* region = nb == 0 ? lr.ex_pv : lr.ex_qk;
       A[nb] = get_operand(region, lr.rd);
-      scale_a[nb] = (int)region[kExHead * lr.ha + kExExp] - 7 - 4 * lr.ua;
+      scale_a[nb] = (int)region[kExHead * lr.ha + kExExp] - (int)kTop - 4 * lr.ua;
     }
     lds_order();
   }
