@@ -1,8 +1,11 @@
 // What query rows add to the accumulated attention weight of the groups, without their output rows.
 //
-// Three launches.  scores_kernel leaves, for every row and slot (a group, or the window), log2 of the row's sum of weights over the slot's tokens;
+// Three steps.  scores_kernel leaves, for every row and slot (a group, or the window), log2 of the row's sum of weights over the slot's tokens;
 // rows_kernel makes of them the same over all tokens that the row sees; and columns_kernel sums 2^(the first - the second) over the rows of a slot.
-// So the weights are formed once, groups do not wait for one another, and what goes through memory is 4 bytes a row and group.
+// So the weights are formed once, groups do not wait for one another, and what goes through memory is 4 bytes a row and group.  Where a pair's numbers fit into
+// LDS one workgroup takes the last two steps (masses_of_pair), in a launch of its own or in the first one.
+// Bound: matrix work with vector work beside it, see below: 2048 rows of 8 pairs of 4 heads over 32768 tokens 790 us (two products: 1.4 PFLOP/s), of which the
+// last two steps take 27; 32 rows of 128 pairs over up to 8192 tokens 69 us, the longest sequence's 4 groups a wave and 8 blocks of rows.
 //
 // scores_kernel.  S^T = K Q^T on v_mfma_f32_16x16x32_f16: codes as binary16 numbers, query times key scales in two binary16 terms (exactness as in
 // kvlinc_rows.hip).  A wave unpacks a group's key tile into 128 registers and goes over blocks of 16 rows with it: 64 products, 32 exponentials a lane.
@@ -17,6 +20,7 @@
 #include <type_traits>
 
 #include "kvlinc_bounded_internal.h"
+#include "kvlinc_join.h"
 #include "kvlinc_row_parts.h"
 
 namespace kvlinc {
@@ -97,10 +101,84 @@ __device__ __forceinline__ void hide_from(float4_t (&x)[8], int end, int g) {
     for (int r = 0; r < 4; ++r) x[n][r] = 16 * n + token_order(4 * g + r) >= end ? -INFINITY : x[n][r];
 }
 
+// The mass of a pair from log2 of its rows' sums, by a workgroup: the numbers in LDS, [slots][rows], the sums of the rows over their slots, a thread four
+// rows and a part of the slots, and those of the slots over their rows, 16 threads a slot.  COHERENT: other workgroups of the launch have left them.
+template <int THREADS, bool COHERENT>
+__device__ __forceinline__ void masses_of_pair(const MassCall& a, const Place& at, int bh, float* sLse, float* sRow /* LDS, 4 THREADS */) {
+  const int tid = threadIdx.x, G = at.len.groups(), rows = a.rows;
+  // unlike scores_kernel's, numbers of slots that a row does not see are read here, and left
+  const auto first_of = [&](int slot) { return slot < G ? slot * kGroup : at.len.nq; };
+  float* lse = a.lse + (long long)bh * a.slots * rows;
+  const int slots = at.rows == 0 ? 0 : G + (at.len.nr > 0 ? 1 : 0);
+  const __amdgpu_buffer_rsrc_t from_others = buffer_of(lse, COHERENT ? slots * rows * 4 : 0);
+#pragma unroll 8
+  for (int i = 4 * tid; i < slots * rows; i += 4 * THREADS)
+    *reinterpret_cast<float4_t*>(sLse + i) = COHERENT ? load4(from_others, 4 * i) : *reinterpret_cast<const float4_t*>(lse + i);
+  __syncthreads();
+  const int quads = rows / 4, parts = min(THREADS / quads, slots), quad = tid % quads, part = tid / quads;
+  if (part < parts) {
+    int p[4];
+    float m[4], l[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      p[i] = at.position(min(4 * quad + i, at.rows - 1), a.gq);
+      m[i] = -INFINITY;
+      l[i] = 0.0f;
+    }
+#pragma unroll 4
+    for (int s = part; s < slots; s += parts) {
+      const float4_t v = *reinterpret_cast<const float4_t*>(sLse + s * rows + 4 * quad);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) m[i] = fmaxf(m[i], first_of(s) <= p[i] ? v[i] : -INFINITY);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m[i] = finite_reference(m[i]);
+#pragma unroll 4
+    for (int s = part; s < slots; s += parts) {
+      const float4_t v = *reinterpret_cast<const float4_t*>(sLse + s * rows + 4 * quad);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) l[i] += __builtin_amdgcn_exp2f(first_of(s) <= p[i] ? v[i] - m[i] : -INFINITY);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sRow[part * rows + 4 * quad + i] = m[i] + __builtin_amdgcn_logf(l[i]);  // (-inf: it sees none of them)
+  }
+  __syncthreads();
+  for (int row = tid; row < rows && slots > 0; row += THREADS) {
+    float M = -INFINITY, L = 0.0f;
+    for (int i = 0; i < parts; ++i) M = fmaxf(M, sRow[i * rows + row]);
+    M = finite_reference(M);
+    for (int i = 0; i < parts; ++i) L += __builtin_amdgcn_exp2f(sRow[i * rows + row] - M);
+    sRow[row] = M + __builtin_amdgcn_logf(L);  // (nobody else reads this row's)
+  }
+  __syncthreads();
+  const int of_slot = tid & 15;
+  for (int slot = tid >> 4; slot <= G; slot += THREADS / 16) {
+    const int from = max(first_of(slot) - (at.len.total() - at.T), 0) * a.gq;  // rows before that of the first token do not see it
+    float w = 0.0f;
+    for (int r = 4 * of_slot; slot < slots && r < at.rows; r += 64) {
+      const float4_t v = *reinterpret_cast<const float4_t*>(sLse + slot * rows + r), to = *reinterpret_cast<const float4_t*>(sRow + r);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w += __builtin_amdgcn_exp2f(r + i >= from && r + i < at.rows ? v[i] - to[i] : -INFINITY);
+    }
+    w += dpp_f<kRowRor1>(w);
+    w += dpp_f<kRowRor2>(w);
+    w += dpp_f<kRowRor4>(w);
+    w += dpp_f<kRowRor8>(w);
+    const long long column = (long long)bh * (a.cache.max_groups + 1) + slot;
+    if (of_slot == 0) a.mass_out[column] = a.mass != nullptr ? fmaf(a.decay, a.mass[column], w) : w;
+  }
+  if (G >= a.slots && bh % a.cache.H_kv == 0 && tid == 0) atomicOr(a.cache.status, KVLINC_ST_BOUND);
+}
+
 // Grid, one-dimensional: pairs fastest, then runs of kScoreWaves splits of the slots, then sets of a.blocks blocks of rows.
-template <int BITS>
+// WHOLE: a pair's numbers, kWholeNumbers at most of kWholeRows, fit into the LDS that the queries leave: its workgroup that arrives last at the pair's
+// counter (zero before and after) forms the mass of them.
+constexpr int kWholeNumbers = kMostBlocks * 16 * kQueryStride / 2, kWholeRows = 64 * kScoreWaves;
+template <int BITS, bool WHOLE>
 __global__ __launch_bounds__(64 * kScoreWaves, 2) void scores_kernel(MassCall a, int blocks, int runs) {
-  __shared__ __align__(16) half_t sQuery[kMostBlocks * 16][kQueryStride];
+  __shared__ __align__(16) float sNumbers[kWholeNumbers];
+  half_t (*sQuery)[kQueryStride] = reinterpret_cast<half_t (*)[kQueryStride]>(sNumbers);
+  __shared__ __align__(16) float sRow[WHOLE ? 4 * 64 * kScoreWaves : 1];
   __shared__ __align__(16) u32x4_t sMeta[kScoreWaves][33];  // key scales, zero-points, zeros
   __shared__ float sUnit[kMostBlocks * 16], sRef[kScoreWaves][kMostBlocks * 16];
   __shared__ int sPosition[kMostBlocks * 16], sLossy;
@@ -109,7 +187,12 @@ __global__ __launch_bounds__(64 * kScoreWaves, 2) void scores_kernel(MassCall a,
   const int pairs = c.B * c.H_kv, unit_id = blockIdx.x / pairs, bh = blockIdx.x - unit_id * pairs, set = unit_id / runs, split = (unit_id - set * runs) * kScoreWaves + wave;
   const int b = bh / c.H_kv, gq = a.gq, row0 = 16 * blocks * set;
   const Place at = place_of(a, b);
-  if (row0 >= at.rows) return;
+  if (row0 >= at.rows) {
+    if constexpr (WHOLE) {
+      if (at.rows == 0 && unit_id == 0) masses_of_pair<64 * kScoreWaves, true>(a, at, bh, sNumbers, sRow);
+    }
+    return;
+  }
   const int G = at.len.groups(), splits = runs * kScoreWaves, n_blocks = min(blocks, (at.rows - row0 + 15) / 16);
   const long long head0 = (long long)bh * gq;
   auto query_of = [&](int row) {  // (rows beyond the last take its query)
@@ -158,7 +241,11 @@ __global__ __launch_bounds__(64 * kScoreWaves, 2) void scores_kernel(MassCall a,
   };
   auto leave = [&](int slot, int k, const Column& col, float sum) __attribute__((always_inline)) {
     sRef[wave][16 * k + j] = col.m;  // (the same in the four lanes of a column: each reads what it has written)
-    if (g == 0) lse[(long long)slot * a.rows + 16 * k + j] = finite_reference(col.m) + __builtin_amdgcn_logf(sum);
+    if (g != 0) return;
+    float* to = lse + (long long)slot * a.rows + 16 * k + j;
+    const float of_slot = finite_reference(col.m) + __builtin_amdgcn_logf(sum);
+    if constexpr (WHOLE) __hip_atomic_store(to, of_slot, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
+    else *to = of_slot;
   };
   // What the zero-points and the centring add to a score is a product, too: of rows that are the zero-points (in every quarter's first row of the
   // product) and the scales (in the second), so that every lane finds both sums of its column.
@@ -272,6 +359,16 @@ __global__ __launch_bounds__(64 * kScoreWaves, 2) void scores_kernel(MassCall a,
       leave(G, k, col, sum);
     }
   }
+  if constexpr (WHOLE) {
+    const int workgroups = (at.rows + 16 * blocks - 1) / (16 * blocks) * runs;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wave's numbers are where everybody sees them
+    __syncthreads();
+    if (tid == 0) sLossy = __hip_atomic_fetch_add(c.split_done + bh, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM) == workgroups - 1;
+    __syncthreads();
+    if (__builtin_amdgcn_readfirstlane(sLossy) == 0) return;
+    if (tid == 0) c.split_done[bh] = 0;
+    masses_of_pair<64 * kScoreWaves, true>(a, at, bh, sNumbers, sRow);
+  }
 }
 
 // Slots whose first token a row at position p sees: groups 0 .. n - 1, and the window.
@@ -329,50 +426,10 @@ __global__ __launch_bounds__(64 * kRowWaves) void rows_kernel(MassCall a) {
 // Both of what follows scores_kernel in one launch, a workgroup a pair, where its numbers fit into LDS.
 constexpr int kPairThreads = 1024, kPairNumbers = 32768;
 __global__ __launch_bounds__(kPairThreads) void pair_kernel(MassCall a) {
-  extern __shared__ float sLse[];  // [slots][rows]
-  __shared__ float sM[kPairThreads], sL[kPairThreads];
-  const int tid = threadIdx.x, lane = tid & 63, bh = blockIdx.x, b = bh / a.cache.H_kv;
-  const Place at = place_of(a, b);
-  const int G = at.len.groups(), rows = a.rows;
-  // unlike scores_kernel's, numbers of slots that a row does not see are read here, and left
-  const auto first_of = [&](int slot) { return slot < G ? slot * kGroup : at.len.nq; };
-  const float* lse = a.lse + (long long)bh * a.slots * rows;
-  const int slots = at.rows == 0 ? 0 : G + (at.len.nr > 0 ? 1 : 0);
-  for (int i = 4 * tid; i < slots * rows; i += 4 * kPairThreads) *reinterpret_cast<float4_t*>(sLse + i) = *reinterpret_cast<const float4_t*>(lse + i);
-  __syncthreads();
-  // a row's sum: its slots shared by `parts` threads
-  const int parts = kPairThreads / rows, row = tid % rows, part = tid / rows;
-  float m = -INFINITY, l = 0.0f;
-  if (part < parts && row < at.rows) {
-    const int p = at.position(row, a.gq);
-    for (int s = part; s < slots; s += parts)
-      if (first_of(s) <= p) m = fmaxf(m, sLse[s * rows + row]);
-    const float to = finite_reference(m);
-    for (int s = part; s < slots; s += parts)
-      if (first_of(s) <= p) l += __builtin_amdgcn_exp2f(sLse[s * rows + row] - to);
-  }
-  sM[tid] = l == 0.0f ? -INFINITY : finite_reference(m);
-  sL[tid] = l;
-  __syncthreads();
-  float M = -INFINITY, L = 0.0f;
-  if (tid < rows) {
-    for (int i = 0; i < parts; ++i) M = fmaxf(M, sM[i * rows + tid]);
-    M = finite_reference(M);
-    for (int i = 0; i < parts; ++i) L = fmaf(__builtin_amdgcn_exp2f(sM[i * rows + tid] - M), sL[i * rows + tid], L);
-  }
-  __syncthreads();
-  if (tid < rows) sM[tid] = M + __builtin_amdgcn_logf(L);
-  __syncthreads();
-  for (int slot = tid >> 6; slot <= G; slot += kPairThreads / 64) {
-    const int from = max(first_of(slot) - (at.len.total() - at.T), 0) * a.gq;  // rows before that of the first token do not see it
-    float w = 0.0f;
-    if (slot < slots)
-      for (int r = from + lane; r < at.rows; r += 64) w += __builtin_amdgcn_exp2f(sLse[slot * rows + r] - sM[r]);
-    w = wave_allsum(w);
-    const long long column = (long long)bh * (a.cache.max_groups + 1) + slot;
-    if (lane == 0) a.mass_out[column] = a.mass != nullptr ? fmaf(a.decay, a.mass[column], w) : w;
-  }
-  if (G >= a.slots && bh % a.cache.H_kv == 0 && tid == 0) atomicOr(a.cache.status, KVLINC_ST_BOUND);
+  extern __shared__ __align__(16) float sLse[];  // [slots][rows]
+  __shared__ __align__(16) float sRow[4 * kPairThreads];
+  const Place at = place_of(a, blockIdx.x / a.cache.H_kv);
+  masses_of_pair<kPairThreads, false>(a, at, blockIdx.x, sLse, sRow);
 }
 
 // The mass.  Grid: a wave a slot, those of a pair one after the other.
@@ -423,9 +480,13 @@ int launch_attention_mass(const MassCall& a, hipStream_t stream) {
   if (splits < 1) splits = 1;
   const long long runs = (splits + kScoreWaves - 1) / kScoreWaves;
   const dim3 grid((unsigned)(pairs * sets * runs)), block(64 * kScoreWaves);
-  if (a.cache.bits == 2) hipLaunchKernelGGL((scores_kernel<2>), grid, block, 0, stream, a, (int)blocks, (int)runs);
-  else hipLaunchKernelGGL((scores_kernel<4>), grid, block, 0, stream, a, (int)blocks, (int)runs);
+  // One launch with few numbers (8 pairs of 128 rows: 700 tokens 8.6 us for 11.2) or many pairs (64 sequences of 2048 tokens 71 us for 76.6); few pairs of many
+  // numbers have more threads in a launch of their own (one sequence of 4096 tokens 13.1 us for 15.2).
+  const bool whole = a.rows <= kWholeRows && a.slots * a.rows <= (pairs < 32 ? kWholeNumbers / 4 : kWholeNumbers);
+  void (*scores)(MassCall, int, int) = a.cache.bits == 2 ? (whole ? scores_kernel<2, true> : scores_kernel<2, false>) : (whole ? scores_kernel<4, true> : scores_kernel<4, false>);
+  hipLaunchKernelGGL(scores, grid, block, 0, stream, a, (int)blocks, (int)runs);
   if (hipGetLastError() != hipSuccess) return KVLINC_EHIP;
+  if (whole) return KVLINC_OK;
   if (a.rows <= kPairThreads && a.slots * a.rows <= kPairNumbers) {
     hipLaunchKernelGGL(pair_kernel, dim3((unsigned)pairs), dim3(kPairThreads), (size_t)(a.slots * a.rows) * sizeof(float), stream, a);
     return hipGetLastError() == hipSuccess ? KVLINC_OK : KVLINC_EHIP;

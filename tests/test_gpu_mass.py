@@ -131,7 +131,7 @@ def test_decode_static_caches_with_a_partial_group(keep, R, n):
 
 
 def test_decode_of_many_pairs_and_splits():
-    run_decode(1330, 4, 2, [int(n) for n in np.random.default_rng(4).integers(0, 700, size=70)])  # more than 64 pairs: four waves
+    run_decode(1330, 4, 2, [int(n) for n in np.random.default_rng(4).integers(0, 700, size=70)])  # more than 64 sequences
     run_decode(1331, 2, 1, [20000])                                                                # 32 splits
 
 
@@ -230,6 +230,11 @@ def test_rows_sliding_values():
 @pytest.mark.parametrize("H_q, H_kv, lengths, T", [(8, 1, [9000], 64), (4, 2, [3000, 2000, 10, 600], 300), (2, 1, [700] * 40, 9)])
 def test_rows_of_larger_calls(H_q, H_kv, lengths, T):
     run_rows(1540, H_q, H_kv, lengths, [min(T, n) for n in lengths])
+
+
+@pytest.mark.parametrize("lengths, T, bits", [([4000], 20, 2), ([3000, 4100, 77], 13, 4), ([1500 - 40 * i for i in range(33)] + [0], 20, 2), ([2500, 2300], 200, 2)])
+def test_rows_where_their_sums_fit_and_where_not(lengths, T, bits):
+    run_rows(1590 + T, 8, 1, lengths, [min(T, n) if i % 5 != 3 else 0 for i, n in enumerate(lengths)], bits, bound=max(lengths))
 
 
 def test_a_bound_that_is_true():
