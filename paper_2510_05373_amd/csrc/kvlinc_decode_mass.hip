@@ -7,9 +7,9 @@
 // bytes a group beside the 9216 or 17408 it reads; and who joins the splits of a pair, and so knows the maximum M and the sum L of every head, makes
 //     mass[j] = decay mass[j] + sum over heads of 2^(reference - M) sum / L,
 // always in the same order.  No second pass over keys, no second launch.
-// Bound: bytes of the groups.  32 sequences of 32k tokens, 7 heads, 4 bits: 117.8 us, 4.9 TB/s; of 16k to 32k 95, 4.7; 16 of 8k, 2 bits: 22.3 us, 3.6 TB/s,
+// Bound: bytes of the groups.  32 sequences of 32k tokens, 7 heads, 4 bits: 117.8 us, 4.9 TB/s; of 16k to 32k 97 to 99, 4.5; 16 of 8k, 2 bits: 22.3 us, 3.6 TB/s,
 // of which the chain of counters, first record, arrival, join and mass takes 6; one of 300 tokens: 8.4 us, the host's calls.  (The walk of few-row
-// attention, which unpacks the codes for binary16 products: 119.5 for the 95, 28 for the 22.3.  Two workgroups a compute unit, 512 in all; with 1024
+// attention, which unpacks the codes for binary16 products: 119.5 for the 97, 28 for the 22.3.  Two workgroups a compute unit, 512 in all; with 1024
 // 16 of 8k take 26, and three a unit at 2 bits spill.)
 #include <hip/hip_runtime.h>
 
@@ -48,7 +48,7 @@ struct Part {
 };
 // The sequences are cut into splits of the same number of groups a wave, the smallest with which the workgroups suffice: `units`, B at least, a KV head.  A
 // lane a sequence; more than 64 of them are cut into as many splits each.  False: this workgroup has none.  (32 sequences of 16k to 32k tokens 108 us
-// with four splits each, 96.8 so.)
+// with four splits each, 96.8 so; of equal lengths nothing is lost.)
 __device__ __forceinline__ bool part_of(const kvlinc_cache& c, int units, int unit, int lane, Part& p) {
   const int most = units / c.B;
   if (units == c.B || c.B == 1 || c.B > 64) {
