@@ -702,7 +702,7 @@ class KVLincCache:
             self._tensor(offset_out, "offset_out", (self.B,), torch.int32)
         if kept is not None:
             self._tensor(kept, "kept", (to.B, to.H_kv, to.max_groups), torch.int32)
-        theirs = () if to is self else (to.groups, to.k_res, to.v_res, to.n_quant, to.n_res)
+        theirs = () if to is self else (to.groups, to.k_res, to.v_res, to.n_quant, to.n_res, to.split_done)
         with self._on(stream, mass, mass_out, offset, offset_out, kept, *theirs):
             rc = self._with_scratch(lambda ws, s: kvlinc_cache_evict(self, to, mass, mass_out, keep, limit, first, last, offset, offset_out, kept, ws, None, s),
                                     lambda: kvlinc_cache_evict_workspace_bytes(self))

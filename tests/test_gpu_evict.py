@@ -130,6 +130,11 @@ def test_into_another_cache_with_the_mass_in_place():
     assert (to.split_done == 0).all() and torch.equal(c.n_quant, before.n_quant) and torch.equal(c.groups, before.groups)
 
 
+@pytest.mark.parametrize("bits, groups, keep", [(2, 800, 700), (4, 420, 370), (2, 1100, 900)])
+def test_many_bytes(bits, groups, keep):
+    run_case(2, 8, [128 * groups, 128 * groups - 128], [5, 128], groups, keep, first=2, last=3, bits=bits)
+
+
 def test_ragged_lengths_and_a_limit_above_what_is_kept():
     run_case(8, 2, [0, 128, 512, 640, 768, 1024, 2048, 0], [0, 5, 1, 128, 128, 30, 77, 9], 20, 5, limit=6, last=2)
     run_case(5, 1, [128 * n for n in (30, 29, 28, 2, 12)], [64], 30, 12, limit=28, first=0, last=3, small=40)

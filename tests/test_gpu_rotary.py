@@ -86,6 +86,24 @@ def test_many_tokens(B, T):
     run_case(B=B, T=T, H_q=6, H_kv=2, din="bf16", held=(0,))
 
 
+@pytest.mark.parametrize("channels, interleaved", [(128, False), (96, False), (128, True), (36, False)])
+@pytest.mark.parametrize("din, dout", [("f16", "f16"), ("f32", "f16"), ("bf16", "f32"), ("f32", "f32")])
+def test_a_large_call_gives_what_smaller_ones_give(channels, interleaved, din, dout):
+    plan, T = kv.KVLincRotary(kv.rotary_frequencies(channels), interleaved=interleaved, magnitude=0.75), 6002  # 74 MB of 2-byte results
+    cache = kv.KVLincCache(1, 32, 8, 128)
+    q, k, v = inputs(1, 32, 8, T, din, True)
+    large = cache.rotary(plan, q, k, v, dtype=ref.TYPES[dout])
+    for t0 in range(0, T, 1500):
+        part = [t[:, :, t0:t0 + 1500] for t in (q, k, v)]
+        small = cache.rotary(plan, *part, first=torch.tensor([t0], dtype=torch.int32, device="cuda"), dtype=ref.TYPES[dout])
+        for a, b in zip(large, small):
+            assert torch.equal(a[:, :, t0:t0 + 1500], b)
+    if din == dout:
+        mine = [t.contiguous() for t in (q, k, v)]
+        cache.rotary(plan, *mine, q_out=mine[0], k_out=mine[1], v_out=mine[2])
+        assert all(torch.equal(a, b) for a, b in zip(mine, large))
+
+
 @pytest.mark.parametrize("interleaved, channels", [(False, 128), (True, 96), (False, 20)])
 def test_ragged_rows(interleaved, channels):
     run_case(B=4, T=11, rows=[11, 0, 1, 6], interleaved=interleaved, channels=channels, held=(0, 129))
