@@ -116,6 +116,14 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
+def _current_device():
+    import torch
+    try:
+        return torch._C._cuda_getDevice()
+    except AttributeError:
+        return torch.cuda.current_device()
+
+
 def _stream(stream):
     if stream is None:
         import torch
@@ -415,7 +423,7 @@ class KVLincCache:
         dev = self._device
         if dev.type != "cuda":
             raise KVLincError("the cache is on %s: the kernels need a GPU" % dev)
-        here = torch.cuda.current_device() == dev.index
+        here = _current_device() == dev.index
         if stream is None:
             return _NOTHING if here else torch.cuda.device(dev)
         if not hasattr(stream, "cuda_stream"):
@@ -584,7 +592,8 @@ class KVLincCache:
             if out is None:
                 missing = True
             else:
-                self._tensor(out, "qkv"[i] + "_out", shape, dtype)
+                if getattr(out, "dtype", None) is not dtype or out.shape != shape or out.device != dev or not out.is_contiguous():
+                    self._tensor(out, "qkv"[i] + "_out", shape, dtype)  # (says what is wrong)
                 to = out.data_ptr()
             rows[i] = RowsStruct(t.data_ptr(), to, of_sequence if B > 1 else 0, of_head if h > 1 else 0, of_token if T > 1 else 0)
         if n_new is not None:
