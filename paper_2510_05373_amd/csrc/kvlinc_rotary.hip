@@ -23,7 +23,7 @@ constexpr long long kStreamedBytes = 64ll << 20;
 // Which numbers of a row a lane has: 16 / RUN runs of RUN, so that the 8 lanes of a row have 128 bytes side by side of the wider type: RUN = 8, or 4 with
 // binary32.  (With binary32 in runs of 8, and with pairs of neighbours in runs of 8 beside each other, a store left every second 16 bytes to the next one:
 // 384 MB of binary32 185 us for 132, 192 MB of neighbours 91 for 72.)
-// kApart, kNeighbours: pairs within the lane.  kAny: pairs `channels` / 2 apart where that is not a multiple of 8; the partners come through LDS.
+// kApart, kNeighbours: pairs within the lane.  kAny: pairs `channels` / 2 apart, the partners come through LDS.
 enum Layout { kApart, kNeighbours, kAny };
 
 struct Turn {
@@ -83,7 +83,7 @@ __global__ __launch_bounds__(64 * kRotaryWaves) void rotary_kernel(RotaryCall a)
   for (int r = 0; r < RUNS; ++r) {
     const int j = l + 8 * (r / 2), beyond = RUN * j - half, second = r % 2;
     if (second == 0) turned[r / 2] = L != kApart || beyond < 0;
-    at[r] = L != kApart ? RUN * (l + 8 * r) : beyond < 0 ? RUN * j + second * half : a.channels + 2 * beyond + second * RUN;
+    at[r] = L != kApart ? RUN * (l + 8 * r) : beyond < 0 ? RUN * j + second * half : a.channels + beyond + second * (kHeadDim / 2 - half);
   }
   Turn turn[kAngles];
 #pragma unroll
@@ -91,6 +91,7 @@ __global__ __launch_bounds__(64 * kRotaryWaves) void rotary_kernel(RotaryCall a)
     const int c = L == kApart ? at[2 * (i / RUN)] + i % RUN : L == kNeighbours ? at[2 * i / RUN] + 2 * i % RUN : at[i / RUN] + i % RUN;
     const int pair = L == kNeighbours ? c / 2 : L == kAny && c >= half ? c - half : c;
     turn[i] = turn_of(position, a.freq[min(pair, half - 1)], a.magnitude);
+    if (L == kAny) turn[i] = c < half ? Turn{turn[i].cos, -turn[i].sin} : Turn{turn[i].sin, turn[i].cos};  // of the pair's first number, and its second
   }
 
   for (int step = 0; step < a.steps; ++step) {
@@ -128,8 +129,8 @@ __global__ __launch_bounds__(64 * kRotaryWaves) void rotary_kernel(RotaryCall a)
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const int c = at[i / RUN] + i % RUN;
-        const float part = mine[c < half ? c + half : c < a.channels ? c - half : c] * turn[i].sin;
-        y[i] = c >= a.channels ? x[i] : fmaf(x[i], turn[i].cos, c < half ? -part : part);
+        const float other = mine[c < half ? c + half : c < a.channels ? c - half : c], u = c < half ? x[i] : other, v = c < half ? other : x[i];
+        y[i] = c >= a.channels ? x[i] : fmaf(u, turn[i].cos, v * turn[i].sin);
       }
       wave_order();
     }
@@ -154,9 +155,8 @@ void launch_from(const RotaryCall& a, int dtype_in, int dtype_out, dim3 grid, hi
   else launch_to<L, STREAMED, float>(a, dtype_out, grid, stream);
 }
 template <Layout L>
-void launch_layout(const RotaryCall& a, int dtype_in, int dtype_out, dim3 grid, hipStream_t stream) {
-  const long long numbers = (long long)a.B * a.T * a.heads * kHeadDim;
-  if (numbers * (dtype_out == KVLINC_F32 ? 4 : 2) >= kStreamedBytes && (dtype_in == KVLINC_F32 || dtype_out != KVLINC_F32)) launch_from<L, true>(a, dtype_in, dtype_out, grid, stream);
+void launch_layout(const RotaryCall& a, int dtype_in, int dtype_out, bool streamed, dim3 grid, hipStream_t stream) {
+  if (streamed) launch_from<L, true>(a, dtype_in, dtype_out, grid, stream);
   else launch_from<L, false>(a, dtype_in, dtype_out, grid, stream);
 }
 
@@ -172,9 +172,14 @@ int launch_rotary(const RotaryCall& call, bool interleaved, int dtype_in, int dt
   if (shares < 1) shares = 1;
   a.steps = (int)((runs + shares - 1) / shares);
   const dim3 grid((unsigned)((tokens + kRotaryWaves - 1) / kRotaryWaves), (unsigned)((runs + a.steps - 1) / a.steps));
-  if (interleaved) launch_layout<kNeighbours>(a, dtype_in, dtype_out, grid, stream);
-  else if (a.channels % 16 == 0) launch_layout<kApart>(a, dtype_in, dtype_out, grid, stream);
-  else launch_layout<kAny>(a, dtype_in, dtype_out, grid, stream);
+  const bool streamed = tokens * a.heads * kHeadDim * (dtype_out == KVLINC_F32 ? 4 : 2) >= kStreamedBytes && (dtype_in == KVLINC_F32 || dtype_out != KVLINC_F32);
+  // Where a part of the channels turns, a lane with the two halves of its pairs leaves less than 128 bytes side by side: 8 x 2048 tokens of 48 heads, 32, 64
+  // and 96 channels 84, 83 and 85 us, past the caches 109, 90 and 109; with runs side by side, the partners by LDS, and past the caches 75, 76 and 79, but
+  // 2 x 1024 tokens 15.8 for 11.9 (twice the angles).
+  const bool apart = a.channels == kHeadDim || (a.channels % 16 == 0 && !streamed);
+  if (interleaved) launch_layout<kNeighbours>(a, dtype_in, dtype_out, streamed, grid, stream);
+  else if (apart) launch_layout<kApart>(a, dtype_in, dtype_out, streamed, grid, stream);
+  else launch_layout<kAny>(a, dtype_in, dtype_out, streamed, grid, stream);
   return hipGetLastError() == hipSuccess ? KVLINC_OK : KVLINC_EHIP;
 }
 
