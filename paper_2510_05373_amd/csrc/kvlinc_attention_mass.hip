@@ -194,6 +194,7 @@ __global__ __launch_bounds__(64 * kScoreWaves, 2) void scores_kernel(MassCall a,
     return;
   }
   const int G = at.len.groups(), splits = runs * kScoreWaves, n_blocks = min(blocks, (at.rows - row0 + 15) / 16);
+  if (!WHOLE && at.position(min(row0 + 16 * n_blocks, at.rows) - 1, gq) < 0) return;  // (rows ahead of the first token)
   const long long head0 = (long long)bh * gq;
   auto query_of = [&](int row) {  // (rows beyond the last take its query)
     const RowPlace p = row_place(min(row, at.rows - 1), gq);
@@ -385,7 +386,7 @@ __global__ __launch_bounds__(64 * kRowWaves) void rows_kernel(MassCall a) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, pairs = a.cache.B * a.cache.H_kv, run = blockIdx.x / pairs, bh = blockIdx.x - run * pairs;
   const int row = 64 * run + lane;
   const Place at = place_of(a, bh / a.cache.H_kv);
-  if (64 * run >= at.rows) return;
+  if (64 * run >= at.rows || at.position(min(64 * run + 63, at.rows - 1), a.gq) < 0) return;
   const Seen see = seen_by(at.len, row < at.rows ? at.position(row, a.gq) : -1);
   const int G = at.len.groups(), slots = see.groups;
   const float* lse = a.lse + bh * a.slots * a.rows + min(row, at.rows - 1);
