@@ -9,8 +9,9 @@
 // always in the same order.  No second pass over keys, no second launch.
 // Bound: bytes of the groups.  32 sequences of 32k tokens, 7 heads, 4 bits: 117.8 us, 4.9 TB/s; of 16k to 32k 97 to 99, 4.5; 16 of 8k, 2 bits: 22.3 us, 3.6 TB/s,
 // of which the chain of counters, first record, arrival, join and mass takes 6; one of 300 tokens: 8.4 us, the host's calls.  (The walk of few-row
-// attention, which unpacks the codes for binary16 products: 119.5 for the 97, 28 for the 22.3.  Two workgroups a compute unit, 512 in all; with 1024
-// 16 of 8k take 26, and three a unit at 2 bits spill.)
+// attention, which unpacks the codes for binary16 products: 119.5 for the 97, 28 for the 22.3.  Some 512 workgroups, two a compute unit; with 768 or
+// 1024 16 of 8k take 22.1 and 26.  At 2 bits and up to 4 heads a unit has room for three, which serves batches of more pairs than 512: 736 of up to 900 tokens
+// 17.3 us for 23.1, 800 of 1500 29 for 31.7.)
 #include <hip/hip_runtime.h>
 
 #include "kvlinc_bounded_internal.h"
@@ -23,7 +24,7 @@ namespace {
 constexpr int kHalfMirror = 0x141;  // row_half_mirror: lane 7 - i of every 8
 constexpr int kSumHeads = 8;    // pairs {reference, sum} of a slot
 constexpr int kShare = 32;     // tokens of the window a wave takes, with a slot of their own
-constexpr int kSlotsAhead = 8;  // slots of a lane requested together
+constexpr int kSlotsAhead = 4;  // slots of a lane requested together
 
 // {reference, sum} of a head: a store past the caches that are not coherent across the chip.
 __device__ __forceinline__ void put_sum(unsigned long long* at, float reference, float sum) { st_coherent2(reinterpret_cast<float*>(at), reference, sum); }
@@ -92,7 +93,7 @@ __device__ __forceinline__ bool part_of(const kvlinc_cache& c, int units, int un
 
 // Grid, one-dimensional: KV heads fastest, then what part_of shares out.
 template <int NB, bool SLIDING, int BITS>
-__global__ __launch_bounds__(kThreads, 2) void decode_mass_kernel(MassCall a) {
+__global__ __launch_bounds__(kThreads, NB == 1 && BITS == 2 ? 3 : 2) void decode_mass_kernel(MassCall a) {
   constexpr int kCombine = 2 * kWaves * NB * 4 + kWaves * NB * 4 * kHeadDim, kRecordWords = Rec<BITS>::kWords, kTerms = 4;
   __shared__ __align__(16) float lds[kCombine + kWaves * 2 * kExWords];
   uint32_t (*ex)[2 * kExWords] = reinterpret_cast<uint32_t (*)[2 * kExWords]>(lds + kCombine);
