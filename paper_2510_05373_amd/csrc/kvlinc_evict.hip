@@ -265,7 +265,7 @@ __device__ __forceinline__ void write_once(const Choice<BLOCKS>& c, const EvictC
 // Into another cache.  Grid: pairs in x, workgroups of a pair in y; a wave takes records, and, with the same number of 16-byte runs at a time, the window.
 constexpr int kMoveWaves = 4;
 // Stores past the caches from so many bytes on: 144 MB of 4-bit records 70.4 -> 59.7 us, of 2-bit ones 75.6 -> 72.9; 72 MB of these 35.5 -> 38.9, 21 MB
-// 11.2 -> 11.9.
+// 11.2 -> 11.9.  In place 136 MB 69.9 -> 64.2.
 constexpr long long kStreamedBytes = 96ll << 20;
 template <int BITS, int BLOCKS, bool STREAMED>
 __global__ __launch_bounds__(64 * kMoveWaves) void move_kernel(EvictCall a) {
@@ -328,7 +328,7 @@ __global__ __launch_bounds__(64 * kMoveWaves) void move_kernel(EvictCall a) {
 
 // In place.  Grid: pairs in x, waves of 64 runs of 16 bytes of a record in y.
 constexpr int kAhead = 16;  // loads of a lane under way
-template <int BITS, int BLOCKS>
+template <int BITS, int BLOCKS, bool STREAMED>
 __global__ __launch_bounds__(64) void close_up_kernel(EvictCall a) {
   constexpr int kVectors = Rec<BITS>::kWords / 4;
   static_assert(kVectors % 64 == 0, "grid");
@@ -343,11 +343,15 @@ __global__ __launch_bounds__(64) void close_up_kernel(EvictCall a) {
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) {
         const int slot = min(j0 + i, cut - 1);
-        v[i] = base[(long long)(BLOCKS == 0 ? source[slot] : (int)sList[slot]) * kVectors];
+        const u32x4_t* from = base + (long long)(BLOCKS == 0 ? source[slot] : (int)sList[slot]) * kVectors;
+        v[i] = STREAMED ? __builtin_nontemporal_load(from) : *from;
       }
 #pragma unroll
-      for (int i = 0; i < kAhead; ++i)
-        if (j0 + i < cut) base[(long long)(j0 + i) * kVectors] = v[i];
+      for (int i = 0; i < kAhead; ++i) {
+        if (j0 + i >= cut) continue;
+        if constexpr (STREAMED) __builtin_nontemporal_store(v[i], base + (long long)(j0 + i) * kVectors);
+        else base[(long long)(j0 + i) * kVectors] = v[i];
+      }
     }
   };
   if constexpr (BLOCKS == 0) {
@@ -371,7 +375,9 @@ template <int BITS, int BLOCKS>
 void launch_moves(const EvictCall& a, hipStream_t stream) {
   const unsigned pairs = (unsigned)(a.from.B * a.from.H_kv);
   if (a.in_place) {
-    hipLaunchKernelGGL((close_up_kernel<BITS, BLOCKS>), dim3(pairs, Rec<BITS>::kWords / 4 / 64), dim3(64), 0, stream, a);
+    const long long records = a.keep < a.from.max_groups ? a.keep : a.from.max_groups;
+    const bool streamed = (long long)pairs * records * Rec<BITS>::kWords * 4 >= kStreamedBytes;
+    hipLaunchKernelGGL((streamed ? close_up_kernel<BITS, BLOCKS, true> : close_up_kernel<BITS, BLOCKS, false>), dim3(pairs, Rec<BITS>::kWords / 4 / 64), dim3(64), 0, stream, a);
   } else {
     const long long records = a.limit < a.from.max_groups ? a.limit : a.from.max_groups;
     const long long units = records + 2 * ((a.from.R * kHeadDim * 2 + Rec<BITS>::kWords * 4 - 1) / (Rec<BITS>::kWords * 4));
