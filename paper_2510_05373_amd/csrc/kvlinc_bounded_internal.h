@@ -49,9 +49,10 @@ int launch_decode_mass(const MassCall& a, hipStream_t stream);
 int launch_attention_mass(const MassCall& a, hipStream_t stream);
 
 // ---- eviction ----
-// Groups of a pair that one wave holds the keys of; and the pairs of a sequence are counted in half a word.
-constexpr int kEvictOneLaunch = 1024;
-inline bool evicts_in_one_launch(const kvlinc_cache& c) { return c.max_groups <= kEvictOneLaunch && c.H_kv < (1 << 15); }
+// Caches of few groups, whose keys every workgroup's wave holds (and a sequence's pairs are counted in half a word): 256 pairs of 300 groups at 2 bits, 32 kept,
+// 38.2 us for 42.1 with a launch of its own to select, of 500 40.8 for 42.3, of 1000 49.2 for 45.2; 128 pairs at 4 bits, 64 kept of 256 59.7 for 68.9,
+// of 500 72.7 for 66.3.
+inline bool evicts_in_one_launch(const kvlinc_cache& c) { return c.max_groups <= (c.bits == 2 ? 512 : 256) && c.H_kv < (1 << 15); }
 struct EvictCall {
   kvlinc_cache from, to;
   const float* mass;

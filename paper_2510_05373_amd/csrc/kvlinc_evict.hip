@@ -1,6 +1,6 @@
 // Eviction: which groups of a (sequence, KV head) stay, by their mass, and their records moved together.
 //
-// A group's key is an unsigned number that orders like its mass.  Caches of up to 1024 groups: one launch.  Every workgroup selects for itself, in one wave
+// A group's key is an unsigned number that orders like its mass.  Caches of up to 512 or 256 groups: one launch.  Every workgroup selects for itself, in one wave
 // that holds all keys of the pair: the largest threshold that enough keys reach is found bit by bit from the top, a comparison and a count of lanes for
 // every 64 keys, no memory and no barrier; those above it stay, and of those equal to it the first ones.  Nothing that it reads (mass, counters) is
 // written before all workgroups of the pair, or the sequence, have read it: whoever is the last to say so writes.  Larger caches: a launch before has
@@ -9,7 +9,7 @@
 // source is never below it, so what the lane reads has not been written yet, whatever other lanes have done: no workgroup waits for another.
 // Bound: bytes of the records that move, in and out: 128 pairs, 64 of 256 groups each, 4 bits, 300 MB: 59.7 us, what a copy takes; 128 pairs, 2k tokens of 8k:
 // 11.2 us; one chat, 16 of 17 groups: 9.5 us, the host's call, of which the kernel takes 6, a chain of counters and mass, selection, record.  (With a
-// launch of its own to select 68.9, 16.7 and 12.9; with 16 blocks of keys in all of them 15.6 for the 11.2: more code than the first wave has fetched.)
+// launch of its own to select 68.9, 16.7 and 12.9; with what is written once ahead of the moves 15.0 for the 11.2.)
 #include <hip/hip_runtime.h>
 
 #include "kvlinc_bounded_internal.h"
@@ -131,7 +131,7 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(EvictCall a) {
 }
 
 // ---- selection by one wave ----
-// BLOCKS: of 64 keys; 1, 4 or 16, as few as the cache has room for (0: a launch before has selected).
+// BLOCKS: of 64 keys; 1, 4 or 8, as few as the cache has room for (0: a launch before has selected).
 template <int BLOCKS>
 struct Choice {
   int n, cut, first_moved;  // groups, how many stay, the first slot with another group than before (cut: none)
@@ -394,7 +394,7 @@ int launch_evict(const EvictCall& a, hipStream_t stream) {
   if (evicts_in_one_launch(a.from)) {
     if (a.from.max_groups <= 64) a.from.bits == 2 ? launch_moves<2, 1>(a, stream) : launch_moves<4, 1>(a, stream);
     else if (a.from.max_groups <= 256) a.from.bits == 2 ? launch_moves<2, 4>(a, stream) : launch_moves<4, 4>(a, stream);
-    else a.from.bits == 2 ? launch_moves<2, 16>(a, stream) : launch_moves<4, 16>(a, stream);
+    else launch_moves<2, 8>(a, stream);  // (at 4 bits there are no more)
     return hipGetLastError() == hipSuccess ? KVLINC_OK : KVLINC_EHIP;
   }
   hipLaunchKernelGGL(select_kernel, dim3((unsigned)(a.from.B * a.from.H_kv)), dim3(kSelectThreads), 0, stream, a);

@@ -101,10 +101,11 @@ def test_sizes(groups, keep, first, last, bits):
     run_case(2, 3, [128 * groups], [1, 128], groups + 1, keep, first=first, last=last, bits=bits, seed=groups)
 
 
-@pytest.mark.parametrize("room", [63, 64, 65, 127, 1023, 1024, 1025])
-def test_as_many_groups_as_a_wave_or_a_launch_selects_from_and_one_more_or_less(room):
+@pytest.mark.parametrize("bits", [2, 4])
+@pytest.mark.parametrize("room", [63, 64, 65, 127, 255, 256, 257, 511, 512, 513, 1024])
+def test_as_many_groups_as_a_wave_or_a_launch_selects_from_and_one_more_or_less(room, bits):
     for n, keep, first, last in ((room, room - 1, 0, 1), (room - 1, room // 2, 1, 2), (room, 2, 1, 1)):
-        c = run_case(1, 2, [128 * n], [7], room, keep, first=first, last=last, seed=room)
+        c = run_case(1, 2, [128 * n], [7], room, keep, first=first, last=last, bits=bits, seed=room)
         assert (c.split_done == 0).all()
 
 
