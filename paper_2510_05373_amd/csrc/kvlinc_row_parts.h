@@ -319,9 +319,8 @@ __device__ __forceinline__ void group_scores(Rows& st, const Record<BITS>& rec, 
 }
 
 // Scores become weights; O^T += V^T P^T of the group.  e: value_exponent of put_meta.  SLIDING: tokens from fp16_from on take their values from the window.
-// Returns this lane's sum of the group's weights.
 template <int BITS, int S, bool SLIDING>
-__device__ __forceinline__ float group_values(Rows& st, const Record<BITS>& rec, const u32x4_t* meta, int e, float (&x)[8 / S][4], float unit, float base, int fp16_from,
+__device__ __forceinline__ void group_values(Rows& st, const Record<BITS>& rec, const u32x4_t* meta, int e, float (&x)[8 / S][4], float unit, float base, int fp16_from,
                                              const half_t* v_win, int quads, int lane) {
   constexpr int kBlocks = 8 / S;
   const float scale = bits_f32((uint32_t)(127 + e) << 23);
@@ -396,7 +395,6 @@ __device__ __forceinline__ float group_values(Rows& st, const Record<BITS>& rec,
         p[n][r] = (S == 1 || n / kBlocks == st.subset) && 16 * n + token_order(4 * (lane >> 4) + r) >= fp16_from ? x[n % kBlocks][r] : 0.0f;
     window_values<8>(st, v_win, quads, 0, p, lane);
   }
-  return l * scale;
 }
 
 // Weights of up to 32 raw key rows of 128 halves, `count` of them there (all in subset 0).  Rows beyond count take the last one's keys.  Returns
