@@ -109,8 +109,8 @@ size_t kvlinc_attention_mass_workspace_bytes(const kvlinc_cache* cache, int32_t 
  *   mass, decay, mass_out   as above
  *   workspace      at least kvlinc_attention_mass_workspace_bytes(cache, T, max_context) bytes, 16-byte aligned: 4 bytes for every row of a query head
  *                  and group
- *   max_context    host-side upper bound on n_quant + n_res (<= 0: capacity).  It sizes the workspace: the rows of a sequence that holds more add
- *                  nothing, and KVLINC_ST_BOUND is set in *status.
+ *   max_context    host-side upper bound on n_quant + n_res (<= 0: capacity).  It sizes the workspace: the rows of a sequence that holds more tokens
+ *                  (max_context + 1 or more) add nothing, and KVLINC_ST_BOUND is set in *status.
  */
 int kvlinc_attention_mass(const kvlinc_cache* cache, const kvlinc_half* q, const int32_t* n_rows, int32_t T, const float* mass, float decay,
                           float* mass_out, void* workspace, size_t workspace_bytes, int32_t max_context, void* stream);

@@ -32,7 +32,8 @@ enum {
 
 /* Bit of *status, beside those of kvlinc.h. */
 enum {
-  KVLINC_ST_BOUND = 16 /* kvlinc_prompt_attention: a sequence held more tokens than max_context said; its output rows are zeros */
+  KVLINC_ST_BOUND = 16 /* kvlinc_prompt_attention: a sequence held more tokens than max_context said; its output rows are zeros.
+                             kvlinc_attention_mass: likewise; its rows have added nothing */
 };
 
 /* Bytes of device scratch kvlinc_prompt_attention needs for T rows a sequence when no sequence holds more than max_context

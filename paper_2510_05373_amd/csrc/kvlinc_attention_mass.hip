@@ -34,13 +34,14 @@ constexpr float kMostSum = 0x1p14f;
 struct Place {
   Lengths len;
   int rows, T;  // rows of a KV head, rows of a query head
+  bool beyond;  // more tokens than the caller's bound: no rows
   __device__ __forceinline__ int position(int row, int gq) const { return len.total() - T + row / gq; }
 };
 __device__ __forceinline__ Place place_of(const MassCall& a, int b) {
   const Lengths len = lengths_of(a.cache, b);
   const int T = a.n_rows != nullptr ? min(max(a.n_rows[b], 0), a.T) : a.T;
-  const bool fits = len.groups() < a.slots;
-  return Place{len, fits ? T * a.gq : 0, T};
+  const bool beyond = len.total() > a.bound || len.groups() >= a.slots;  // (the latter in no cache whose counters hold)
+  return Place{len, beyond ? 0 : T * a.gq, T, beyond};
 }
 
 template <int BITS>
@@ -167,7 +168,7 @@ __device__ __forceinline__ void masses_of_pair(const MassCall& a, const Place& a
     const long long column = (long long)bh * (a.cache.max_groups + 1) + slot;
     if (of_slot == 0) a.mass_out[column] = a.mass != nullptr ? fmaf(a.decay, a.mass[column], w) : w;
   }
-  if (G >= a.slots && bh % a.cache.H_kv == 0 && tid == 0) atomicOr(a.cache.status, KVLINC_ST_BOUND);
+  if (at.beyond && bh % a.cache.H_kv == 0 && tid == 0) atomicOr(a.cache.status, KVLINC_ST_BOUND);
 }
 
 // Grid, one-dimensional: pairs fastest, then runs of kScoreWaves splits of the slots, then sets of a.blocks blocks of rows.
@@ -444,7 +445,7 @@ __global__ __launch_bounds__(64 * kColumnWaves) void columns_kernel(MassCall a, 
   const Place at = place_of(a, b);
   const int G = at.len.groups();
   if (slot > G) return;
-  if (slot == G && G >= a.slots && bh % a.cache.H_kv == 0 && lane == 0) atomicOr(a.cache.status, KVLINC_ST_BOUND);
+  if (slot == G && at.beyond && bh % a.cache.H_kv == 0 && lane == 0) atomicOr(a.cache.status, KVLINC_ST_BOUND);
   const int first = slot < G ? slot * kGroup : at.len.nq;  // rows before that of the first token do not see it
   const int from = at.rows == 0 ? 0 : max(first - (at.len.total() - at.T), 0) * a.gq;
   const float* lse = a.lse + (bh * a.slots + slot) * a.rows;

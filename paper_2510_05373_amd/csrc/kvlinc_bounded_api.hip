@@ -39,9 +39,12 @@ bool bad_mass(const kvlinc_cache& c, const float* mass, float decay, const float
 }
 bool bad_workspace(const void* workspace, size_t bytes, size_t need) { return bad_address(workspace, 16) || bytes < need; }
 
+long long tokens_of_bound(const kvlinc_cache& c, int max_context) {
+  const long long cap = c.max_groups * kGroup + c.R;
+  return max_context > 0 && max_context < cap ? max_context : cap;
+}
 long long groups_of_bound(const kvlinc_cache& c, int max_context) {
-  const long long cap = c.max_groups * kGroup + c.R, ctx = max_context > 0 && max_context < cap ? max_context : cap;
-  const long long groups = (ctx + kGroup - 1) / kGroup;
+  const long long groups = (tokens_of_bound(c, max_context) + kGroup - 1) / kGroup;
   return groups < c.max_groups ? groups : c.max_groups;
 }
 
@@ -210,6 +213,7 @@ int kvlinc_attention_mass(const kvlinc_cache* cache, const kvlinc_half* q, const
   a.n_rows = n_rows;
   a.T = T;
   a.slots = p.slots;
+  a.bound = (int)tokens_of_bound(*cache, max_context);
   a.rows = (int)p.rows;
   a.lse = static_cast<float*>(workspace);
   a.row_lse = a.lse + p.lse;

@@ -43,6 +43,7 @@ struct MassCall {
   float* lse;         // rows: [B H_kv][slots][rows] log2 of a row's sum of weights over the slot's tokens
   float* row_lse;     // rows: [B H_kv][rows] the same over all tokens it sees
   long long slots;
+  int bound;          // rows: a sequence of more tokens is not taken; one of so many needs no more than `slots`
   int rows;           // of a (sequence, KV head), up to a multiple of 16
 };
 int launch_decode_mass(const MassCall& a, hipStream_t stream);
