@@ -53,7 +53,7 @@ typedef struct kvlinc_rows {
  *
  *   cache      B, H_q, H_kv and, where counted is 1, the counters n_quant and n_res
  *   q, k, v    rows of H_q, H_kv, H_kv heads; each may be NULL, not all three
- *   T          rows per sequence, 1 .. 2^24; B * T below 2^26
+ *   T          rows per sequence, 1 .. 2^24; B * T at most 2^26 - 4
  *   n_new      [B] int32 on the device: sequence b has its first n_new[b] (0..T) rows; NULL = T for all.  (A value below 0 is read as 0, one
  *              above T as T.)  Rows from n_new[b] on are not read, and not written.
  *   first      [B] int32 on the device, NULL = 0 for all

@@ -130,7 +130,8 @@ int kvlinc_rotary(const kvlinc_cache* cache, const kvlinc_rotation* rotation, co
   if (rc != KVLINC_OK) return rc;
   if (rotation == nullptr || rotation->channels < 2 || rotation->channels > kHeadDim || rotation->channels % 2 != 0) return KVLINC_EINVAL;
   if (rotation->interleaved < 0 || rotation->interleaved > 1 || !std::isfinite(rotation->magnitude) || bad_address(rotation->freq, 16)) return KVLINC_EINVAL;
-  if (T < 1 || T > (1 << 24) || (long long)cache->B * T >= (1ll << 26) || counted < 0 || counted > 1) return KVLINC_EINVAL;
+  // (2^26 tokens, four to a workgroup of 256, would be 2^32 threads)
+  if (T < 1 || T > (1 << 24) || (long long)cache->B * T > (1ll << 26) - 4 || counted < 0 || counted > 1) return KVLINC_EINVAL;
   if (misaligned(n_new, 4) || misaligned(first, 4) || misaligned(depth, 4)) return KVLINC_EINVAL;
   if (dtype_in < KVLINC_F16 || dtype_in > KVLINC_F32 || dtype_out < KVLINC_F16 || dtype_out > KVLINC_F32) return KVLINC_EINVAL;
   RotaryCall a{};
