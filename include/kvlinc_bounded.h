@@ -14,7 +14,7 @@
  * Slots beyond c are not touched by the calls that add; new groups start from what is there: zero them once, kvlinc_cache_evict keeps them zero.
  *
  * None of the calls that take weights or evict works with the adapters of the correction (KVLINC_EINVAL): its states stand for all tokens
- * ever quantized.
+ * ever quantized.  They take caches with B * H_kv below 2^24, B * H_kv * (max_groups + 1) below 2^26 and room for less than 2^31 - 256 tokens a sequence.
  */
 #ifndef KVLINC_BOUNDED_H
 #define KVLINC_BOUNDED_H
@@ -105,7 +105,7 @@ size_t kvlinc_attention_mass_workspace_bytes(const kvlinc_cache* cache, int32_t 
  *   q              [B, H_q, T, 128] fp16
  *   n_rows         [B] int32 on the device: sequence b has its first n_rows[b] (0..T) rows; NULL = T for all.  (A value below 0 is read as 0, one
  *                  above T as T.)  Rows from n_rows[b] on are not read.
- *   T              rows per (sequence, head), 1 .. 2^20; B * H_kv * ceil(T * H_q / H_kv / 64) below 2^22, B * H_kv * max_groups below 2^26
+ *   T              rows per (sequence, head), 1 .. 2^20; B * H_kv * ceil(T * H_q / H_kv / 64) below 2^22
  *   mass, decay, mass_out   as above
  *   workspace      at least kvlinc_attention_mass_workspace_bytes(cache, T, max_context) bytes, 16-byte aligned: 4 bytes for every row of a query head
  *                  and group

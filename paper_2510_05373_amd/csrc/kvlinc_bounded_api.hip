@@ -24,7 +24,7 @@ bool overlap(const Span& p, const Span& q) {
 long long pairs_of(const kvlinc_cache& c) { return (long long)c.B * c.H_kv; }
 // Positions below 2^31, the grids' threads below 2^32.
 bool too_large(const kvlinc_cache& c) {
-  return pairs_of(c) >= (1ll << 24) || c.max_groups * kGroup + c.R > INT32_MAX - 2 * kGroup || pairs_of(c) * (c.max_groups + 1) > (1ll << 26);
+  return pairs_of(c) >= (1ll << 24) || c.max_groups * kGroup + c.R > INT32_MAX - 2 * kGroup || pairs_of(c) * (c.max_groups + 1) >= (1ll << 26);
 }
 int check_mass_cache(const kvlinc_cache* c) {
   const int rc = kvlinc_cache_validate(c);
