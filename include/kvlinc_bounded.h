@@ -62,7 +62,7 @@ typedef struct kvlinc_rows {
  *              the cache any more, see kvlinc_cache_evict);  0: first[b] + depth[b][i]
  *   dtype_in, dtype_out   KVLINC_F16, KVLINC_BF16 or KVLINC_F32, of all three tensors
  *
- * Angles are formed and reduced in binary64 (exact to 2^-53 of p freq), sines, cosines and products in binary32; a number is rounded to dtype_out
+ * Angles are formed and reduced in binary64 (exact to 2^-51 of p freq), sines, cosines and products in binary32; a number is rounded to dtype_out
  * once.  (A finite number beyond the range of dtype_out becomes infinite, which the append reports.)
  */
 int kvlinc_rotary(const kvlinc_cache* cache, const kvlinc_rotation* rotation, const kvlinc_rows* q, const kvlinc_rows* k, const kvlinc_rows* v,

@@ -1,9 +1,9 @@
 // Rotary positions of new rows: queries and keys turned, values taken along, from any strides to the layout of the cache's calls.
 //
 // A wave has one token; 8 lanes have a row of 128 numbers, so that it takes 8 heads at a time, `steps` times.  A lane has the same pairs in every
-// row: it forms its 8 sines and cosines once.  The angle in turns, p freq / 2 pi, is formed in binary64 and reduced there to a quarter of a turn around
-// its nearest one (exact), so that binary32 has nothing to lose at far positions; sine and cosine of |x| <= pi / 4 are their Taylor series up to
-// x^9 and x^10 (the next terms are below 2^-29).
+// row: it forms its 8 sines and cosines once.  The angle in turns, p freq / 2 pi, is formed in binary64 (the constant and two products: 2.56 * 2^-53 of it at
+// most) and reduced there to a quarter of a turn around its nearest one (exact), so that binary32 has nothing to lose at far positions; sine and cosine of
+// |x| <= pi / 4 are their Taylor series up to x^9 and x^10 (the next terms are below 2^-29).
 // Bound: bytes, a row in and out once: 16 sequences of up to 2048 tokens, 48 heads, binary16 from bfloat16: 109.7 us, 5.4 TB/s; single tokens and drafts: the
 // host's call, 9.7 us, of which the kernel takes 3.6 and 5.
 #include <hip/hip_runtime.h>
