@@ -108,7 +108,8 @@ size_t kvlinc_attention_mass_workspace_bytes(const kvlinc_cache* cache, int32_t 
  *   T              rows per (sequence, head), 1 .. 2^20; B * H_kv * ceil(T * H_q / H_kv / 64) below 2^22
  *   mass, decay, mass_out   as above
  *   workspace      at least kvlinc_attention_mass_workspace_bytes(cache, T, max_context) bytes, 16-byte aligned: 4 bytes for every row of a query head
- *                  and group
+ *                  and group that max_context tokens can have (all rows of a prompt of 32768 tokens, 32 query heads: 1.1 GB, of 131072: 17.2 GB;
+ *                  a prompt that is appended in chunks, with a call behind each of them, needs that of a chunk)
  *   max_context    host-side upper bound on n_quant + n_res (<= 0: capacity).  It sizes the workspace: the rows of a sequence that holds more tokens
  *                  (max_context + 1 or more) add nothing, and KVLINC_ST_BOUND is set in *status.
  */

@@ -658,7 +658,8 @@ class KVLincCache:
         """The attention weight that the groups receive from T query rows of every sequence, its newest tokens, which the cache already holds: mass_out =
         decay mass + their weights (mass_out None: in mass itself, or a new one; mass None: zeros).  q: [B, H_q, T, 128] fp16; n_rows: [B] int32 or None
         (all T).  max_context: the most tokens that any sequence holds (0: whatever the cache has room for); one that holds more adds
-        nothing, and KVLINC_ST_BOUND is set in `status`.  Returns mass_out."""
+        nothing, and KVLINC_ST_BOUND is set in `status`.  The scratch, kept with the cache, is 4 bytes for every row of a query head and group of max_context
+        (all rows of 32768 tokens, 32 heads: 1.1 GB): a long prompt chunk by chunk, a call behind each append, needs that of a chunk.  Returns mass_out."""
         import torch
         if not torch.is_tensor(q) or q.dim() != 4:
             raise KVLincError("q has to be a tensor of shape [B, H_q, T, 128]")

@@ -5,7 +5,11 @@
 // So the weights are formed once, groups do not wait for one another, and what goes through memory is 4 bytes a row and group.  Where a pair's numbers fit into
 // LDS one workgroup takes the last two steps (masses_of_pair), in a launch of its own or in the first one.
 // Bound: matrix work with vector work beside it, see below: 2048 rows of 8 pairs of 4 heads over 32768 tokens 790 us (two products: 1.4 PFLOP/s), of which the
-// last two steps take 27; 32 rows of 128 pairs over up to 8192 tokens 69 us, the longest sequence's 4 groups a wave and 8 blocks of rows.
+// last two steps take 27; 32 rows of 128 pairs over up to 8192 tokens 69 us, the longest sequence's 4 groups a wave and 8 blocks of rows (1.75 us each; launch,
+// the rows' way to LDS, first record, arrival and the last two steps the rest, some 16).  At 4 bits 874 and 76: keys take more to unpack, and <4, false> and
+// <4, true> spill 5 and 10 registers.  Waves of a workgroup share slots, not blocks of rows: where a sequence has fewer slots than four, some have nothing to do.
+// 64 prompts with all of their rows, 8 pairs of 4 heads each: of 100 tokens 56 us (a copy of the rows 11), 250 157 (27), 500 398 (54); one of 8192 511 (one
+// product 227).
 //
 // scores_kernel.  S^T = K Q^T on v_mfma_f32_16x16x32_f16: codes as binary16 numbers, query times key scales in two binary16 terms (exactness as in
 // kvlinc_rows.hip).  A wave unpacks a group's key tile into 128 registers and goes over blocks of 16 rows with it: 64 products, 32 exponentials a lane.

@@ -49,6 +49,9 @@ long long groups_of_bound(const kvlinc_cache& c, int max_context) {
 }
 
 // Decode: two workgroups of four waves a compute unit, as many as have a group for each wave, which the sequences share (part_of in kvlinc_decode_mass.hip).
+// Not more than that: from B H_kv = 512 on every pair has one, whatever its length (64 sequences of 8 KV heads: equal lengths of 9216 tokens 65 us, 2k to 16k,
+// 1.1 times as many in all, 89; one of 32768 among 500s 110, where 31 of these leave room to share 21); and a pair has kMaxContextSplits at most (one
+// sequence of 131072 tokens: 2 KV heads 36 us, 8 of them 33).
 struct DecodePlan {
   long long units, slots;
   size_t part_floats, sums;

@@ -11,7 +11,8 @@
 // of which the chain of counters, first record, arrival, join and mass takes 6; one of 300 tokens: 8.4 us, the host's calls.  (The walk of few-row
 // attention, which unpacks the codes for binary16 products: 119.5 for the 97, 28 for the 22.3.  Some 512 workgroups, two a compute unit; with 768 or
 // 1024 16 of 8k take 22.1 and 26.  At 2 bits and up to 4 heads a unit has room for three, which serves batches of more pairs than 512: 736 of up to 900 tokens
-// 17.3 us for 23.1, 800 of 1500 29 for 31.7.)
+// 17.3 us for 23.1, 800 of 1500 29 for 31.7.)  That room costs <1, *, 2> two registers' spills outside its loop (12 bytes a lane); <2, false, 4> and
+// <2, true, 4> spill 11 and 18 in it (48 and 68 bytes a lane, 6 MB of the 4-bit call's writes).
 #include <hip/hip_runtime.h>
 
 #include "kvlinc_bounded_internal.h"
@@ -48,8 +49,8 @@ struct Part {
   int room;    // of the pair
 };
 // The sequences are cut into splits of the same number of groups a wave, the smallest with which the workgroups suffice: `units`, B at least, a KV head.  A
-// lane a sequence; more than 64 of them are cut into as many splits each.  False: this workgroup has none.  (32 sequences of 16k to 32k tokens 108 us
-// with four splits each, 96.8 so; of equal lengths nothing is lost.)
+// lane a sequence; more than 64 of them are cut into as many splits each, and with no more workgroups than sequences every pair has one.  False: this
+// workgroup has none.  (32 sequences of 16k to 32k tokens 108 us with four splits each, 96.8 so; of equal lengths nothing is lost.)
 __device__ __forceinline__ bool part_of(const kvlinc_cache& c, int units, int unit, int lane, Part& p) {
   const int most = units / c.B;
   if (units == c.B || c.B == 1 || c.B > 64) {

@@ -8,8 +8,11 @@
 // Into another cache: a wave a record.  In place: a lane has 16 bytes of every record of a pair, and moves them from slot to slot in order.  A slot's
 // source is never below it, so what the lane reads has not been written yet, whatever other lanes have done: no workgroup waits for another.
 // Bound: bytes of the records that move, in and out: 128 pairs, 64 of 256 groups each, 4 bits, 300 MB: 59.7 us, what a copy takes; 128 pairs, 2k tokens of 8k:
-// 11.2 us; one chat, 16 of 17 groups: 9.5 us, the host's call, of which the kernel takes 6, a chain of counters and mass, selection, record.  (With a
-// launch of its own to select 68.9, 16.7 and 12.9; with what is written once ahead of the moves 15.0 for the 11.2.)
+// 11.2 us; one chat, 16 of 17 groups: 9.4 us, the host's call, of which the kernel takes 5.3, a chain of counters and mass, selection, record.  (With a
+// launch of its own to select 68.9, 16.7 and 12.9; with what is written once ahead of the moves 15.0 for the 11.2.)  Caches of more groups pay for the
+// launch that selects: 256 pairs of 1000 groups, 32 kept, 45 us, a copy 30.  In place few pairs have few waves, 9 or 17 each, every one a chain of
+// loads and stores, 16 slots at a time: 8 pairs that all close up behind their second group, from a graph, 16 slots 5.0 us, 64 8.5, 511 40 (into another
+// cache 17.9, a copy 14.8), 2 pairs of 511 38 (9.5, 3.7); 128 pairs, 64 of 256 groups at 4 bits 66 (60.6, 55.9).
 #include <hip/hip_runtime.h>
 
 #include "kvlinc_bounded_internal.h"
