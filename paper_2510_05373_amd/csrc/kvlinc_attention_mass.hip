@@ -44,7 +44,7 @@ struct Place {
 __device__ __forceinline__ Place place_of(const MassCall& a, int b) {
   const Lengths len = lengths_of(a.cache, b);
   const int T = a.n_rows != nullptr ? min(max(a.n_rows[b], 0), a.T) : a.T;
-  const bool beyond = len.total() > a.bound || len.groups() >= a.slots;  // (the latter in no cache whose counters hold)
+  const bool beyond = len.total() > a.bound;
   return Place{len, beyond ? 0 : T * a.gq, T, beyond};
 }
 
